@@ -10,9 +10,9 @@ from .zo import (ZO_ERR_ALIGN, ZO_ERR_ARG, ZO_ERR_CUDA, ZO_ERR_DTYPE, ZO_ERR_NON
                  perturb2, perturb_pair, perturb_quadratic_loss, perturb_quadratic_loss_workspace_size, precondition,
                  probe_bytes, probe_signs, quadratic_loss, quadratic_loss_static, quadratic_loss_workspace_size,
                  set_packing, status_string, update, update_sequential, version)
-from . import replicas
+from . import forward, replicas
 
-__all__ = ["replicas", "ParamList", "QuadraticLoss", "QuadraticPass", "QuadraticPoints", "ZoError", "perturb_quadratic_loss",
+__all__ = ["forward", "replicas", "ParamList", "QuadraticLoss", "QuadraticPass", "QuadraticPoints", "ZoError", "perturb_quadratic_loss",
            "perturb_quadratic_loss_workspace_size", "set_packing", "get_packing", "packing", "perturb", "perturb2", "perturb_pair",
            "precondition", "update", "update_sequential", "probe_bytes", "probe_signs", "quadratic_loss",
            "quadratic_loss_static", "quadratic_loss_workspace_size", "status_string", "version", "ZO_OK",

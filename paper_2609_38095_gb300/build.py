@@ -20,8 +20,10 @@ LIB = os.path.join(HERE, "libzo.so")
 STAMP = LIB + ".arch"   # architecture the library was linked for
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["zo_api.cu", "zo_stream_kernels.cu", "zo_update_lut8.cu", "zo_small_kernels.cu",
-           "zo_quad_step.cu", "zo_update_items.cu", "zo_update_blocks.cu"]
-HEADERS = ["zo_blocks.cuh", "zo_device.cuh", "zo_items.h", "zo_launch.h", "zo_precond.cuh"]
+           "zo_quad_step.cu", "zo_update_items.cu", "zo_update_blocks.cu",
+           "zo_forward_api.cu", "zo_rotate.cu", "zo_attention.cu", "zo_decode_scalar.cu", "zo_token_loss.cu"]
+HEADERS = ["zo_blocks.cuh", "zo_decode.cuh", "zo_device.cuh", "zo_forward.cuh", "zo_items.h", "zo_launch.h",
+           "zo_precond.cuh"]
 
 
 def nvcc() -> str:
@@ -47,7 +49,7 @@ def _stale(target, deps):
 
 def build(force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    hdrs = [os.path.join(CSRC, h) for h in HEADERS] + [os.path.join(INCLUDE, "zo.h")]
+    hdrs = [os.path.join(CSRC, h) for h in HEADERS] + [os.path.join(INCLUDE, h) for h in ("zo.h", "zo_forward.h")]
     jobs = []
     objs = []
     for s in SOURCES:

@@ -324,6 +324,19 @@ thread_local zo::UpdateItemsParams<zo::kItemsMany> tl_update_many;
 
 }  // namespace
 
+namespace zo {
+
+int report_cuda_error(cudaError_t e, const char* where) { return cuda_fail(e, where); }
+
+int device_sms(int* sms) {
+  DeviceInfo* d = nullptr;
+  const int rc = device_info(&d);
+  if (rc == ZO_OK) *sms = d->sms;
+  return rc;
+}
+
+}  // namespace zo
+
 extern "C" {
 
 const char* zo_status_string(int status) {

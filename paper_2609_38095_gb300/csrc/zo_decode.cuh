@@ -1,0 +1,136 @@
+// zo_decode.cuh -- what the kernels of one-token attention share: how a
+// cluster's CTAs and their warps split a sequence, and how they join.
+//
+// A cluster of CTAs takes one sequence and key-value head. The keys go in tiles
+// of 16 to the cluster's warps in turn, so that warps differ by one tile at
+// most; a warp keeps a running maximum, sum and output for each of its query
+// heads and shares nothing with the others until its last key. Then a CTA joins
+// its warps in shared memory and the cluster its CTAs over distributed shared
+// memory, each CTA a part of the output: one launch, no workspace, and an order
+// of additions that depends on the launch's shape alone.
+#pragma once
+
+#include "zo_forward.cuh"
+
+namespace zo {
+
+constexpr int kDecodeKeys = 16;  // keys of a warp's tile
+
+template <int HB>
+struct DecodeJoin {  // a CTA's statistics, read by its peers
+  float top[HB], total[HB];
+  int bad;
+};
+
+struct DecodePlace {
+  int b, g, head0, heads;  // sequence, key-value head, first query head, query heads here
+  int64_t len;
+  int bad;  // a length beyond the page table
+};
+
+template <int HB>
+__device__ __forceinline__ DecodePlace decode_place(const DecodeParams& p, uint32_t cluster) {
+  const int blocks = p.head_blocks;
+  DecodePlace w;
+  w.b = cluster / (p.kv_heads * blocks);
+  const int rest = cluster - w.b * (p.kv_heads * blocks);
+  w.g = rest / blocks;
+  const int first = (rest - w.g * blocks) * HB;
+  w.head0 = w.g * p.group + first;
+  w.heads = min(HB, p.group - first);
+  w.len = max(p.lengths[w.b], 0);
+  w.bad = w.len > p.max_pages * p.page_size;
+  if (w.bad) w.len = 0;
+  return w;
+}
+
+// Key j's page and row in it; page -1 where j is beyond the length, and where
+// the table names no page of the cache (bad).
+__device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePlace& w, int64_t j, int& bad) {
+  if (j >= w.len) return make_int2(-1, 0);
+  const uint32_t at = static_cast<uint32_t>(j), page = at / static_cast<uint32_t>(p.page_size);
+  const int id = p.pages[w.b * p.pages_stride + page];
+  if (id < 0 || id >= p.n_pages) {
+    bad = 1;
+    return make_int2(-1, 0);
+  }
+  return make_int2(id, static_cast<int>(at - page * p.page_size));
+}
+
+// Every thread of the cluster. outs: [kWarps][HB][DP] unscaled outputs, tops and
+// totals: [kWarps][HB] (log2 units), all in shared memory.
+template <typename T, int HB, int DP, int kWarps>
+__device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodePlace& w, float* outs, const float* tops,
+                                            const float* totals, DecodeJoin<HB>& join) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < HB) {
+    float top = -kInf, total = 0.0f;
+    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[i * HB + tid]);
+    for (int i = 0; i < kWarps; ++i)
+      if (top > -kInf || totals[i * HB + tid] != 0.0f) total += totals[i * HB + tid] * exp2_approx(tops[i * HB + tid] - top);
+    join.top[tid] = top;
+    join.total[tid] = total;
+  }
+  for (int i = tid; i < w.heads * DP; i += kWarps * 32) {
+    const int h = i / DP;
+    float top = -kInf, x = 0.0f;
+    for (int n = 0; n < kWarps; ++n) top = fmaxf(top, tops[n * HB + h]);
+    if (top > -kInf)
+      for (int n = 0; n < kWarps; ++n) x = fmaf(outs[n * HB * DP + i], exp2_approx(tops[n * HB + h] - top), x);
+    outs[i] = x;
+  }
+  const uint32_t ranks = cluster_size(), rank = cluster_rank();
+  cluster_sync();
+  T* out = static_cast<T*>(p.out) + w.b * p.out_token;
+  for (int i = rank * (kWarps * 32) + tid; i < w.heads * DP; i += ranks * (kWarps * 32)) {
+    const int h = i / DP, d = i - h * DP;
+    float top = -kInf, x = 0.0f, total = 0.0f;
+    bool bad = false;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      top = fmaxf(top, peer_load(peer_address(&join.top[h], r)));
+      bad = bad || __float_as_int(peer_load(peer_address(&join.bad, r))) != 0;
+    }
+    for (uint32_t r = 0; r < ranks; ++r) {
+      const float part = peer_load(peer_address(&join.top[h], r));
+      const float scale = top == -kInf ? 0.0f : exp2_approx(part - top);
+      total = fmaf(peer_load(peer_address(&join.total[h], r)), scale, total);
+      x = fmaf(peer_load(peer_address(outs + i, r)), scale, x);
+    }
+    const int head = w.head0 + h;
+    if (d < p.dim) out[head * p.out_head + d] = narrow<T>(bad ? NAN : total == 0.0f ? 0.0f : x / total);
+    if (d == 0 && p.lse != nullptr)
+      p.lse[static_cast<int64_t>(w.b) * p.heads + head] = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+  }
+  cluster_sync();  // no CTA leaves before its part is read
+}
+
+// CTAs of a cluster: enough that `per_sm` CTAs per SM have work, none with less
+// than `least` keys of the longest sequence that the page table can hold.
+inline int decode_cluster(int64_t items, int64_t longest, int sms, int per_sm, int64_t least) {
+  int c = 1;
+  while (c < 16 && items * c < static_cast<int64_t>(sms) * per_sm && longest >= 2 * c * least) c *= 2;
+  return c;
+}
+
+template <typename K>
+cudaError_t launch_decode(K kernel, const DecodeParams& p, int64_t items, int cluster, int threads, int bytes,
+                          cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(static_cast<unsigned>(items * cluster));
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = bytes;
+  c.stream = stream;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, p);
+}
+
+}  // namespace zo

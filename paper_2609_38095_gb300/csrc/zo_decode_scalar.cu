@@ -1,0 +1,214 @@
+// zo_decode_scalar.cu -- one-token attention over a paged cache on the fp32
+// units: every type, head size, stride and alignment (zo_attention_decode).
+#include "zo_decode.cuh"
+
+namespace zo {
+
+namespace {
+
+constexpr int kBlockHeads = 8;  // query heads of a cluster
+
+template <int DP>
+struct Scalar {
+  static constexpr int kWarps = DP == 256 ? 2 : 4;
+  static constexpr int kStages = 2;
+  static constexpr int kPitch = DP + 4;  // floats from one key to the next: 16 keys' vectors on distinct banks
+  static constexpr int kStage = kDecodeKeys * (kPitch + DP);
+  static constexpr int kWarp = kStages * kStage + kDecodeKeys * kBlockHeads;  // and the keys' weights
+  static constexpr int kBytes = 4 * (kWarps * kWarp + kBlockHeads * DP + 2 * kWarps * kBlockHeads);
+  static_assert(kBlockHeads * DP * kWarps <= kWarps * kWarp, "a warp's output takes its tiles' place");
+};
+
+// A warp's tile of 16 keys lies in its own shared memory as fp32, the next one
+// on its way (fp32 caches by cp.async; others are widened on the way and stored
+// before the products start). Scores: a lane has half of a key's dot product
+// with every head; outputs: a lane has DP / 32 elements of every head.
+template <typename T, int DP, bool kAsync>
+__global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
+    decode_scalar_kernel(const __grid_constant__ DecodeParams p) {
+  using S = Scalar<DP>;
+  constexpr int HB = kBlockHeads;
+  extern __shared__ __align__(16) float smem[];
+  __shared__ DecodeJoin<HB> join;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float* qs = smem;  // [HB][DP]
+  float* tops = qs + HB * DP;
+  float* totals = tops + S::kWarps * HB;
+  float* tiles = totals + S::kWarps * HB;
+  float* mine = tiles + warp * S::kWarp;
+  float* weights = mine + S::kStages * S::kStage;  // [16][HB]
+  const uint32_t ranks = cluster_size();
+  const DecodePlace w = decode_place<HB>(p, blockIdx.x / ranks);
+  if (threadIdx.x == 0) join.bad = w.bad;
+  const T* q = static_cast<const T*>(p.q) + w.b * p.q_token;
+  for (int i = threadIdx.x; i < HB * DP; i += S::kWarps * 32) {
+    const int h = i / DP, d = i - h * DP;
+    qs[i] = h < w.heads && d < p.dim ? widen(q[(w.head0 + h) * p.q_head + d]) : 0.0f;
+  }
+  __syncthreads();
+
+  const T* kc = static_cast<const T*>(p.k) + w.g * p.k_head;
+  const T* vc = static_cast<const T*>(p.v) + w.g * p.v_head;
+  const int64_t tiles_in = (w.len + kDecodeKeys - 1) / kDecodeKeys;
+  const int64_t step = static_cast<int64_t>(ranks) * S::kWarps;
+  int bad = 0;
+
+  auto fetch = [&](int64_t tile, int stage) {
+    float* ks = mine + stage * S::kStage;
+    float* vs = ks + kDecodeKeys * S::kPitch;
+    const int2 key = decode_key(p, w, tile * kDecodeKeys + (lane & 15), bad);
+    for (int r = 0; r < kDecodeKeys; ++r) {
+      const int page = __shfl_sync(0xFFFFFFFFu, key.x, r), row = __shfl_sync(0xFFFFFFFFu, key.y, r);
+      const T* k = kc + page * p.k_page + row * p.k_token;
+      const T* v = vc + page * p.v_page + row * p.v_token;
+      if constexpr (kAsync) {
+#pragma unroll
+        for (int c = lane; c < DP / 4; c += 32) {
+          const int n = page >= 0 && c * 4 < p.dim ? 16 : 0;  // the rest is filled with zeros
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           static_cast<uint32_t>(__cvta_generic_to_shared(ks + r * S::kPitch + c * 4))),
+                       "l"(n ? static_cast<const void*>(k + c * 4) : p.k), "r"(n)
+                       : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           static_cast<uint32_t>(__cvta_generic_to_shared(vs + r * DP + c * 4))),
+                       "l"(n ? static_cast<const void*>(v + c * 4) : p.v), "r"(n)
+                       : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int d = lane; d < DP; d += 32) {
+          const bool in = page >= 0 && d < p.dim;
+          ks[r * S::kPitch + d] = in ? widen(k[d]) : 0.0f;
+          vs[r * DP + d] = in ? widen(v[d]) : 0.0f;
+        }
+      }
+    }
+    if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  const float scale2 = p.softcap > 0.0f ? p.scale / p.softcap : p.scale * kLog2e, cap2 = p.softcap * kLog2e;
+  float slope2[HB], top[HB], total[HB], acc[HB][DP / 32];
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    slope2[h] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] * kLog2e : 0.0f;
+    top[h] = -kInf;
+    total[h] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) acc[h][c] = 0.0f;
+  }
+  int64_t tile = static_cast<int64_t>(cluster_rank()) * S::kWarps + warp;
+  int stage = 0;
+  if (tile < tiles_in) fetch(tile, 0);
+  for (; tile < tiles_in; tile += step, stage ^= 1) {
+    if (tile + step < tiles_in) {
+      fetch(tile + step, stage ^ 1);
+      if constexpr (kAsync) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    } else {
+      if constexpr (kAsync) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    const float* ks = mine + stage * S::kStage;
+    const float* vs = ks + kDecodeKeys * S::kPitch;
+    const int key = lane & 15, half = lane >> 4;
+    const int64_t j = tile * kDecodeKeys + key;
+    float s[HB] = {};
+#pragma unroll 4
+    for (int c = half * (DP / 8); c < (half + 1) * (DP / 8); ++c) {
+      const float4 x = *reinterpret_cast<const float4*>(ks + key * S::kPitch + c * 4);
+#pragma unroll
+      for (int h = 0; h < HB; ++h) {
+        const float4 y = *reinterpret_cast<const float4*>(qs + h * DP + c * 4);
+        s[h] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[h]))));
+      }
+    }
+    const float away = static_cast<float>(w.len - 1 - j);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      float x = s[h] + __shfl_xor_sync(0xFFFFFFFFu, s[h], 16);
+      x = p.softcap > 0.0f ? cap2 * tanhf(x * scale2) : x * scale2;
+      x = j < w.len ? x - slope2[h] * away : -kInf;
+      float most = x;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+      const float next = fmaxf(top[h], most), base = next == -kInf ? 0.0f : next;
+      if (next > top[h]) {  // the same for the whole warp
+        const float back = exp2_approx(top[h] - base);
+        total[h] *= back;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) acc[h][c] *= back;
+        top[h] = next;
+      }
+      s[h] = exp2_approx(x - base);
+      total[h] += half == 0 ? s[h] : 0.0f;
+    }
+    if (half == 0) {
+      *reinterpret_cast<float4*>(weights + key * HB) = make_float4(s[0], s[1], s[2], s[3]);
+      *reinterpret_cast<float4*>(weights + key * HB + 4) = make_float4(s[4], s[5], s[6], s[7]);
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int r = 0; r < kDecodeKeys; ++r) {
+      const float4 wa = *reinterpret_cast<const float4*>(weights + r * HB);
+      const float4 wb = *reinterpret_cast<const float4*>(weights + r * HB + 4);
+      const float wr[HB] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+#pragma unroll
+      for (int c = 0; c < DP / 32; ++c) {
+        const float x = vs[r * DP + c * 32 + lane];
+#pragma unroll
+        for (int h = 0; h < HB; ++h) acc[h][c] = fmaf(wr[h], x, acc[h][c]);
+      }
+    }
+    __syncwarp();  // the tile and the weights may be overwritten
+  }
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    float sum = total[h];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) {
+      tops[warp * HB + h] = top[h];
+      totals[warp * HB + h] = sum;
+    }
+  }
+  if (bad) join.bad = 1;
+  __syncthreads();  // every warp is done with its tiles: the outputs take their place
+#pragma unroll
+  for (int h = 0; h < HB; ++h)
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) tiles[(warp * HB + h) * DP + c * 32 + lane] = acc[h][c];
+  decode_join<T, HB, DP, S::kWarps>(p, w, tiles, tops, totals, join);
+}
+
+template <typename T, int DP, bool kAsync>
+cudaError_t launch_size(DecodeParams p, int64_t batch, int sms, cudaStream_t stream) {
+  using S = Scalar<DP>;
+  p.head_blocks = (p.group + kBlockHeads - 1) / kBlockHeads;
+  const int64_t items = batch * p.kv_heads * p.head_blocks;
+  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 2, 128);
+  return launch_decode(decode_scalar_kernel<T, DP, kAsync>, p, items, c, S::kWarps * 32, S::kBytes, stream);
+}
+
+template <typename T>
+cudaError_t launch_type(const DecodeParams& p, int64_t batch, int sms, cudaStream_t stream) {
+  if constexpr (sizeof(T) == 4) {
+    if (p.dim % 4 == 0 && p.k_page % 4 == 0 && p.k_token % 4 == 0 && p.k_head % 4 == 0 && p.v_page % 4 == 0 &&
+        p.v_token % 4 == 0 && p.v_head % 4 == 0 && aligned_to(p.k, 16) && aligned_to(p.v, 16)) {
+      if (p.dim <= 64) return launch_size<T, 64, true>(p, batch, sms, stream);
+      if (p.dim <= 128) return launch_size<T, 128, true>(p, batch, sms, stream);
+      return launch_size<T, 256, true>(p, batch, sms, stream);
+    }
+  }
+  if (p.dim <= 64) return launch_size<T, 64, false>(p, batch, sms, stream);
+  if (p.dim <= 128) return launch_size<T, 128, false>(p, batch, sms, stream);
+  return launch_size<T, 256, false>(p, batch, sms, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream) {
+  if (dtype == 0) return launch_type<float>(p, batch, sms, stream);
+  if (dtype == 1) return launch_type<__nv_bfloat16>(p, batch, sms, stream);
+  return launch_type<__half>(p, batch, sms, stream);
+}
+
+}  // namespace zo

@@ -1,0 +1,219 @@
+// zo_forward_api.cu -- the extern "C" entry points declared in
+// include/zo_forward.h: argument validation and the choice of kernel.
+// Everything here runs on the host and only enqueues kernels.
+#include <cmath>
+
+#include "zo_forward.cuh"
+#include "zo_forward.h"
+#include "zo_launch.h"
+
+namespace {
+
+constexpr int64_t kMaxIndex = INT64_C(0x7FFFFFFF);  // rows, keys and launch grids count in 32 bits
+
+int element_size(int32_t dtype) { return dtype == ZO_F32 ? 4 : 2; }
+
+bool known(int32_t dtype) { return dtype == ZO_F32 || dtype == ZO_BF16 || dtype == ZO_F16; }
+
+bool misaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+bool bad_strides(int64_t a, int64_t b, int64_t c = 0) { return a < 0 || b < 0 || c < 0; }
+
+int check_heads(int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype) {
+  if (head_dim < 1 || head_dim > ZO_MAX_HEAD_DIM || heads < 1 || heads > ZO_MAX_HEADS || kv_heads < 1 ||
+      heads % kv_heads != 0)
+    return ZO_ERR_ARG;
+  return known(dtype) ? ZO_OK : ZO_ERR_DTYPE;
+}
+
+int check_scores(float scale, float softcap) {
+  return std::isfinite(scale) && std::isfinite(softcap) && softcap >= 0.0f ? ZO_OK : ZO_ERR_ARG;
+}
+
+int finish(cudaError_t e, const char* what) { return e == cudaSuccess ? ZO_OK : zo::report_cuda_error(e, what); }
+
+}  // namespace
+
+extern "C" {
+
+int zo_rotary_table(float* table, int64_t rows, int32_t rotary_dim, double base, double scale, int64_t original,
+                    double low, double high, double magnitude, void* stream) {
+  if (rows < 0 || rotary_dim < 2 || rotary_dim > ZO_MAX_HEAD_DIM || rotary_dim % 2 != 0) return ZO_ERR_ARG;
+  if (!(std::isfinite(base) && base > 0.0 && std::isfinite(scale) && scale > 0.0 && original >= 0)) return ZO_ERR_ARG;
+  if (!(std::isfinite(low) && std::isfinite(high) && low <= high && std::isfinite(magnitude))) return ZO_ERR_ARG;
+  if (rows == 0) return ZO_OK;
+  if (table == nullptr) return ZO_ERR_ARG;
+  if (misaligned(table, 4)) return ZO_ERR_ALIGN;
+  return finish(zo::launch_rotary_table(table, rows, rotary_dim, base, scale, original, low, high, magnitude,
+                                        static_cast<cudaStream_t>(stream)),
+                "rotary_table_kernel");
+}
+
+int zo_document_spans(const int32_t* q_starts, const int32_t* k_starts, const int32_t* prefix, int32_t docs,
+                      int32_t* spans, int64_t tokens, void* stream) {
+  if (docs < 0 || tokens < 0 || tokens > kMaxIndex) return ZO_ERR_ARG;
+  if (tokens == 0) return ZO_OK;
+  if (spans == nullptr || (docs > 0 && (q_starts == nullptr || k_starts == nullptr))) return ZO_ERR_ARG;
+  if (misaligned(q_starts, 4) || misaligned(k_starts, 4) || misaligned(prefix, 4) || misaligned(spans, 4))
+    return ZO_ERR_ALIGN;
+  return finish(zo::launch_document_spans(q_starts, k_starts, prefix, docs, spans, tokens,
+                                          static_cast<cudaStream_t>(stream)),
+                "document_spans_kernel");
+}
+
+int zo_rotate_heads(const zo_head_part* parts, int32_t n_parts, int64_t tokens, int32_t head_dim, int32_t dtype,
+                    const float* table, int64_t table_rows, int32_t rotary_dim, int32_t layout, const void* positions,
+                    const void* slots, int32_t index_bytes, int64_t n_slots, int64_t page_size, float eps,
+                    void* stream) {
+  if (n_parts < 0 || n_parts > 3 || (n_parts > 0 && parts == nullptr)) return ZO_ERR_ARG;
+  if (tokens < 0 || tokens > kMaxIndex || head_dim < 1 || head_dim > ZO_MAX_HEAD_DIM) return ZO_ERR_ARG;
+  if (!known(dtype)) return ZO_ERR_DTYPE;
+  if (!(std::isfinite(eps) && eps >= 0.0f) || (index_bytes != 4 && index_bytes != 8)) return ZO_ERR_ARG;
+  zo::RotateParams r = {};
+  bool rotate = false, slotted = false;
+  const size_t size = element_size(dtype);
+  for (int i = 0; i < n_parts; ++i) {
+    const zo_head_part& in = parts[i];
+    if (in.heads < 1 || in.heads > ZO_MAX_HEADS || (in.flags & ~(ZO_HEADS_ROTATE | ZO_HEADS_SLOTTED)) != 0 ||
+        in.reserved != 0 || bad_strides(in.in.token, in.in.head) || bad_strides(in.out.token, in.out.head, in.out.page))
+      return ZO_ERR_ARG;
+    if (in.weight != nullptr && !known(in.weight_dtype)) return ZO_ERR_DTYPE;
+    if (tokens > 0 && (in.in.ptr == nullptr || in.out.ptr == nullptr)) return ZO_ERR_ARG;
+    if (misaligned(in.in.ptr, size) || misaligned(in.out.ptr, size) ||
+        (in.weight != nullptr && misaligned(in.weight, element_size(in.weight_dtype))))
+      return ZO_ERR_ALIGN;
+    zo::RotatePart& out = r.part[i];
+    out = {in.in.ptr,    in.out.ptr,  in.weight,       in.in.token,
+           in.in.head,   in.out.page, in.out.token,    in.out.head,
+           in.weight_dtype, in.heads, (in.flags & ZO_HEADS_ROTATE) != 0, (in.flags & ZO_HEADS_SLOTTED) != 0, 0};
+    rotate = rotate || out.rotate;
+    slotted = slotted || out.slotted;
+  }
+  if (rotate) {
+    if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > head_dim || table_rows < 0 ||
+        (layout != ZO_ROTARY_HALF && layout != ZO_ROTARY_INTERLEAVED))
+      return ZO_ERR_ARG;
+    if (tokens > 0 && (positions == nullptr || (table == nullptr && table_rows > 0))) return ZO_ERR_ARG;
+    if (misaligned(table, 4) || misaligned(positions, index_bytes)) return ZO_ERR_ALIGN;
+  }
+  if (slotted) {
+    if (n_slots < 0 || page_size < 1 || (tokens > 0 && slots == nullptr)) return ZO_ERR_ARG;
+    if (misaligned(slots, index_bytes)) return ZO_ERR_ALIGN;
+  }
+  if (n_parts == 0 || tokens == 0) return ZO_OK;
+  r.n_parts = n_parts;
+  r.dim = head_dim;
+  r.rotary = rotate ? rotary_dim : 0;
+  r.interleaved = layout == ZO_ROTARY_INTERLEAVED;
+  r.index64 = index_bytes == 8;
+  r.tokens = tokens;
+  r.table = table;
+  r.table_rows = table_rows;
+  r.positions = positions;
+  r.slots = slots;
+  r.n_slots = n_slots;
+  r.page_size = page_size;
+  r.eps = eps;
+  return finish(zo::launch_rotate_heads(r, dtype, static_cast<cudaStream_t>(stream)), "rotate_heads_kernel");
+}
+
+int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_rows* out, int64_t q_tokens,
+                 int64_t k_tokens, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                 const int32_t* spans, float scale, float softcap, const float* slopes, float* lse, void* stream) {
+  if (q == nullptr || k == nullptr || v == nullptr || out == nullptr) return ZO_ERR_ARG;
+  if (q_tokens < 0 || q_tokens > kMaxIndex || k_tokens < 0 || k_tokens > kMaxIndex) return ZO_ERR_ARG;
+  int rc = check_heads(heads, kv_heads, head_dim, dtype);
+  if (rc == ZO_OK) rc = check_scores(scale, softcap);
+  if (rc != ZO_OK) return rc;
+  if (bad_strides(q->token, q->head, k->token) || bad_strides(k->head, v->token, v->head) ||
+      bad_strides(out->token, out->head))
+    return ZO_ERR_ARG;
+  if (q_tokens == 0) return ZO_OK;
+  if (q->ptr == nullptr || out->ptr == nullptr || spans == nullptr) return ZO_ERR_ARG;
+  if (k_tokens > 0 && (k->ptr == nullptr || v->ptr == nullptr)) return ZO_ERR_ARG;
+  const size_t size = element_size(dtype);
+  if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
+      misaligned(spans, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
+    return ZO_ERR_ALIGN;
+  zo::AttentionParams p = {};
+  p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
+  p.q_token = q->token, p.q_head = q->head, p.k_token = k->token, p.k_head = k->head;
+  p.v_token = v->token, p.v_head = v->head, p.out_token = out->token, p.out_head = out->head;
+  p.q_tokens = q_tokens, p.k_tokens = k_tokens;
+  p.heads = heads, p.group = heads / kv_heads, p.dim = head_dim;
+  p.spans = spans;
+  p.scale = scale, p.softcap = softcap;
+  p.slopes = slopes;
+  p.lse = lse;
+  return finish(zo::launch_attention_tiles(p, dtype, static_cast<cudaStream_t>(stream)), "attention_tiles_kernel");
+}
+
+int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, const zo_rows* out, int64_t batch,
+                        int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype, const int32_t* pages,
+                        int64_t pages_stride, int64_t max_pages, int64_t n_pages, int32_t page_size,
+                        const int32_t* lengths, float scale, float softcap, const float* slopes, float* lse,
+                        void* stream) {
+  if (q == nullptr || k == nullptr || v == nullptr || out == nullptr) return ZO_ERR_ARG;
+  int rc = check_heads(heads, kv_heads, head_dim, dtype);
+  if (rc == ZO_OK) rc = check_scores(scale, softcap);
+  if (rc != ZO_OK) return rc;
+  // a launch has at most 16 CTAs per sequence and query head
+  if (batch < 0 || batch > kMaxIndex / 16 / heads || max_pages < 0 || n_pages < 0 || n_pages > kMaxIndex ||
+      page_size < 1 || pages_stride < 0 || max_pages > (INT64_C(1) << 40))
+    return ZO_ERR_ARG;
+  if (bad_strides(q->token, q->head, out->token) || bad_strides(out->head, k->page, k->token) ||
+      bad_strides(k->head, v->page, v->token) || bad_strides(v->head, 0))
+    return ZO_ERR_ARG;
+  if (batch == 0) return ZO_OK;
+  if (q->ptr == nullptr || out->ptr == nullptr || lengths == nullptr) return ZO_ERR_ARG;
+  if ((max_pages > 0 && pages == nullptr) || (n_pages > 0 && (k->ptr == nullptr || v->ptr == nullptr))) return ZO_ERR_ARG;
+  const size_t size = element_size(dtype);
+  if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
+      misaligned(pages, 4) || misaligned(lengths, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
+    return ZO_ERR_ALIGN;
+  int sms = 0;
+  rc = zo::device_sms(&sms);
+  if (rc != ZO_OK) return rc;
+  zo::DecodeParams p = {};
+  p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
+  p.q_token = q->token, p.q_head = q->head, p.out_token = out->token, p.out_head = out->head;
+  p.k_page = k->page, p.k_token = k->token, p.k_head = k->head;
+  p.v_page = v->page, p.v_token = v->token, p.v_head = v->head;
+  p.pages_stride = pages_stride, p.max_pages = max_pages, p.n_pages = n_pages;
+  p.pages = pages, p.lengths = lengths;
+  p.heads = heads, p.kv_heads = kv_heads, p.group = heads / kv_heads, p.dim = head_dim, p.page_size = page_size;
+  p.scale = scale, p.softcap = softcap;
+  p.slopes = slopes;
+  p.lse = lse;
+  return finish(zo::launch_decode_scalar(p, batch, dtype, sms, static_cast<cudaStream_t>(stream)),
+                "decode_scalar_kernel");
+}
+
+int64_t zo_token_loss_workspace_size(int64_t tokens) { return 8 * (tokens > 0 ? tokens : 1); }
+
+int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
+                  int32_t target_bytes, int32_t flags, void* loss, float* nll, void* workspace,
+                  int64_t workspace_bytes, void* stream) {
+  if (tokens < 0 || tokens > kMaxIndex / 8 || vocab < 1 || vocab > kMaxIndex || row < 0 ||
+      (target_bytes != 4 && target_bytes != 8) || (flags & ~(ZO_LOSS_MEAN | ZO_LOSS_ADD | ZO_LOSS_F32)) != 0)
+    return ZO_ERR_ARG;
+  if (!known(dtype)) return ZO_ERR_DTYPE;
+  if (loss == nullptr || (tokens > 0 && (logits == nullptr || targets == nullptr))) return ZO_ERR_ARG;
+  if (misaligned(logits, element_size(dtype)) || misaligned(targets, target_bytes) ||
+      misaligned(loss, flags & ZO_LOSS_F32 ? 4 : 8) || misaligned(nll, 4) || misaligned(workspace, 8))
+    return ZO_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < zo_token_loss_workspace_size(tokens)) return ZO_ERR_WORKSPACE;
+  int sms = 0;
+  const int rc = zo::device_sms(&sms);
+  if (rc != ZO_OK) return rc;
+  zo::TokenLossParams p = {};
+  p.logits = logits;
+  p.row = row, p.tokens = tokens, p.vocab = vocab;
+  p.targets = targets;
+  p.target64 = target_bytes == 8, p.flags = flags;
+  p.loss = loss, p.nll = nll;
+  p.rows = static_cast<double*>(workspace);
+  return finish(zo::launch_token_loss(p, dtype, sms, static_cast<cudaStream_t>(stream)), "token_loss_kernel");
+}
+
+}  // extern "C"

@@ -8,6 +8,11 @@
 
 namespace zo {
 
+// What the ABI layers share: a CUDA error noted for zo_last_cuda_error
+// (returns ZO_ERR_CUDA), and the current device's SMs (returns a zo_status).
+int report_cuda_error(cudaError_t e, const char* where);
+int device_sms(int* sms);
+
 constexpr int kStatusNonFinite = -4;  // ZO_ERR_NONFINITE
 constexpr int kPrecondOneSided = 1;   // ZO_PRECOND_ONE_SIDED
 constexpr int kPrecondRelative = 2;   // ZO_PRECOND_RELATIVE_CURVATURE

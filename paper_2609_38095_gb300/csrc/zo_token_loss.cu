@@ -1,0 +1,208 @@
+// zo_token_loss.cu -- a token's -log p of its target from its logits, and the
+// sum over the tokens (zo_token_loss).
+#include "zo_forward.cuh"
+
+namespace zo {
+
+namespace {
+
+constexpr int kLossThreads = 512;
+constexpr int kLossVectors = 4;  // 16-byte loads in flight per thread
+constexpr int kSumThreads = 1024;
+
+struct Tail {  // max and sum of exp(x - max)
+  float top;
+  double sum;
+};
+
+__device__ __forceinline__ Tail join(Tail a, Tail b) {
+  // (-FLT_MAX, 0) is the empty one; exp(x - top) in fp64 only where sums meet
+  const float top = fmaxf(a.top, b.top);
+  return {top, a.sum * exp2_approx((a.top - top) * kLog2e) + b.sum * exp2_approx((b.top - top) * kLog2e)};
+}
+
+__device__ __forceinline__ Tail warp_join(Tail t) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    t = join(t, {__shfl_xor_sync(0xFFFFFFFFu, t.top, o), __shfl_xor_sync(0xFFFFFFFFu, t.sum, o)});
+  return t;
+}
+
+// x joins a thread's running maximum and sum; n values at once. x - top, then
+// times log2(e): the difference is formed before its rounding, so logits far
+// from 0 (or all at the type's lowest value) lose nothing.
+template <int N>
+__device__ __forceinline__ void take(const float* x, float& top, float& sum) {
+  float most = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+  if (most > top) {
+    sum *= exp2_approx((top - most) * kLog2e);
+    top = most;
+  }
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += exp2_approx((x[i] - top) * kLog2e);
+  sum += s;
+}
+
+// A token per CTA, or per cluster of CTAs that split the vocabulary where there
+// are fewer tokens than the SMs hold CTAs. One pass with the running maximum
+// and sum in registers; bound by HBM: each counted row is read once.
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) token_loss_kernel(const __grid_constant__ TokenLossParams p,
+                                                                  int parts) {
+  constexpr int E = Vec<T>::kN;
+  __shared__ float tops[kLossThreads / 32];
+  __shared__ double sums[kLossThreads / 32];
+  __shared__ float part_top;
+  __shared__ float part_sum[2];  // high and low part
+  const int64_t t = blockIdx.x / parts;
+  const int rank = blockIdx.x % parts, tid = threadIdx.x;
+  const int64_t target = load_index(p.targets, t, p.target64);
+  if (target < 0 || target >= p.vocab) {
+    if (rank == 0 && tid == 0) {
+      p.rows[t] = target < 0 ? 0.0 : NAN;
+      if (p.nll != nullptr) p.nll[t] = target < 0 ? 0.0f : NAN;
+    }
+    return;
+  }
+  const T* x = static_cast<const T*>(p.logits) + t * p.row;
+  const int64_t from = p.vocab * rank / parts, to = p.vocab * (rank + 1) / parts;
+  const int64_t off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(x + from) % 16) / sizeof(T);
+  const int64_t head = min(from + (off ? E - off : 0), to), vectors = (to - head) / E;
+  float top = -3.402823466e38f, sum = 0.0f;
+  if (tid < head - from) {
+    const float one = widen(x[from + tid]);
+    take<1>(&one, top, sum);
+  }
+  if (tid < to - head - vectors * E) {
+    const float one = widen(x[head + vectors * E + tid]);
+    take<1>(&one, top, sum);
+  }
+  const uint4* v = reinterpret_cast<const uint4*>(x + head);
+  int64_t i = tid;
+  for (; i + (kLossVectors - 1) * kLossThreads < vectors; i += kLossVectors * kLossThreads) {
+    uint4 raw[kLossVectors];
+#pragma unroll
+    for (int n = 0; n < kLossVectors; ++n) raw[n] = __ldcs(v + i + n * kLossThreads);
+    float f[kLossVectors * E];
+#pragma unroll
+    for (int n = 0; n < kLossVectors; ++n) Vec<T>::widen_all(raw[n], f + n * E);
+    take<kLossVectors * E>(f, top, sum);
+  }
+  for (; i < vectors; i += kLossThreads) {
+    float f[E];
+    Vec<T>::widen_all(__ldcs(v + i), f);
+    take<E>(f, top, sum);
+  }
+  Tail mine = warp_join({top, sum});
+  if ((tid & 31) == 0) {
+    tops[tid >> 5] = mine.top;
+    sums[tid >> 5] = mine.sum;
+  }
+  __syncthreads();
+  if (tid < 32) {
+    constexpr int kWarps = kLossThreads / 32;
+    mine = warp_join(tid < kWarps ? Tail{tops[tid], sums[tid]} : Tail{-3.402823466e38f, 0.0});
+    if (tid == 0 && parts > 1) {
+      part_top = mine.top;
+      part_sum[0] = static_cast<float>(mine.sum);
+      part_sum[1] = static_cast<float>(mine.sum - part_sum[0]);
+    }
+  }
+  if (parts > 1) {
+    cluster_sync();
+    if (rank == 0 && tid < 32) {
+      mine = {-3.402823466e38f, 0.0};
+      if (tid < parts)
+        mine = {peer_load(peer_address(&part_top, tid)),
+                static_cast<double>(peer_load(peer_address(&part_sum[0], tid))) +
+                    peer_load(peer_address(&part_sum[1], tid))};
+      mine = warp_join(mine);
+    }
+    cluster_sync();  // no CTA leaves before its part is read
+  }
+  if (rank == 0 && tid == 0) {
+    const double nll = log(mine.sum) + (static_cast<double>(mine.top) - widen(x[target]));
+    p.rows[t] = nll;
+    if (p.nll != nullptr) p.nll[t] = static_cast<float>(nll);
+  }
+}
+
+// The tokens' sum in one CTA, in an order of their number alone. Launched so
+// that it may be resident before the tokens' kernel has ended.
+__global__ void __launch_bounds__(kSumThreads) token_loss_sum_kernel(const __grid_constant__ TokenLossParams p) {
+  __shared__ double sums[kSumThreads / 32];
+  __shared__ double counts[kSumThreads / 32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  double sum = 0.0, count = 0.0;
+  for (int64_t t = threadIdx.x; t < p.tokens; t += kSumThreads) {
+    sum += p.rows[t];
+    if (p.flags & 1) count += load_index(p.targets, t, p.target64) >= 0 ? 1.0 : 0.0;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    sums[threadIdx.x >> 5] = sum;
+    counts[threadIdx.x >> 5] = count;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  sum = count = 0.0;
+  for (int i = 0; i < kSumThreads / 32; ++i) {
+    sum += sums[i];
+    count += counts[i];
+  }
+  if (p.flags & 1) sum = count > 0.0 ? sum / count : NAN;
+  if (p.flags & 4) {
+    float* out = static_cast<float*>(p.loss);
+    *out = static_cast<float>(p.flags & 2 ? *out + sum : sum);
+  } else {
+    double* out = static_cast<double*>(p.loss);
+    *out = p.flags & 2 ? *out + sum : sum;
+  }
+}
+
+template <typename F, typename... A>
+cudaError_t launch_with(F f, unsigned grid, unsigned threads, cudaLaunchAttribute attr, cudaStream_t stream, A... a) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3(threads);
+  c.stream = stream;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, f, a...);
+}
+
+template <typename T>
+cudaError_t launch_rows(const TokenLossParams& p, int sms, cudaStream_t stream) {
+  int parts = 1;
+  while (parts < 8 && p.tokens * parts * 2 <= 4 * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = parts;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  return launch_with(token_loss_kernel<T>, static_cast<unsigned>(p.tokens * parts), kLossThreads, attr, stream, p,
+                     parts);
+}
+
+}  // namespace
+
+cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream) {
+  if (p.tokens > 0) {
+    const cudaError_t e = dtype == 0   ? launch_rows<float>(p, sms, stream)
+                          : dtype == 1 ? launch_rows<__nv_bfloat16>(p, sms, stream)
+                                       : launch_rows<__half>(p, sms, stream);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  return launch_with(token_loss_sum_kernel, 1, kSumThreads, attr, stream, p);
+}
+
+}  // namespace zo
