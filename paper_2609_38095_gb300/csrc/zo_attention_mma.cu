@@ -1,0 +1,455 @@
+// zo_attention_mma.cu -- attention of packed documents on the tensor cores:
+// 16-bit types, heads of up to 128 elements, vectors aligned to 16 bytes
+// (zo_attention).
+#include "zo_forward.cuh"
+#include "zo_tcgen05.cuh"
+
+namespace zo {
+
+bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
+                   int64_t token_stride) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (encode == nullptr) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+  // a dimension of one element has no stride of its own
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? head_stride * 2 : 16),
+                                 static_cast<cuuint64_t>(tokens > 1 ? token_stride * 2 : 16)};
+  const cuuint32_t box[3] = {64, 1, 128}, steps[3] = {1, 1, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims,
+                strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
+constexpr int kRows = 128;     // query rows of a slot, keys of a tile
+constexpr int kMmaThreads = 384;
+// Registers of a softmax thread (a row's 128 scores and the rest) and of the others: 2 x 128 threads and 128, no more in
+// all than the 168 each that 384 threads are launched with.
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "the shares exceed the launch's registers");
+constexpr int kChunk = kRows * 128;  // bytes of 64 elements of 128 rows
+constexpr float kSlack = 8.0f;       // log2: how far scores may pass the reference before the output is rescaled
+
+template <int D>
+struct Plan {
+  static constexpr int kTile = D / 64 * kChunk;            // bytes of a tile of queries, keys or values
+  static constexpr int kStages = D == 128 ? 5 : 8;         // tiles of keys and values in turn
+  static constexpr int kBytes = (2 + kStages) * kTile + 1024;
+};
+
+struct MmaShared {
+  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2], p_full[2], o_full[2], drain;
+  int lo[2], hi[2];
+  uint32_t tmem;
+  int dead;
+};
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  return static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a);
+}
+__device__ __forceinline__ float low2(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float high2(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+  uint32_t r;
+  if constexpr (__is_same(T, __nv_bfloat16)) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+// A CTA has two slots of 128 query rows: two heads that share their keys (the
+// same rows, the same spans) where a group has an even number of them, else two
+// tiles of rows of one head. Keys and values go by in tiles of 128; while one
+// slot's scores pass through the softmax, the tensor cores work for the other.
+//
+//   warps 0-3, 4-7   softmax of slot 0, 1: a thread has a row
+//   warp 8           the matrix products, one thread
+//   warp 9           TMA loads, one thread (warps 10 and 11 complete their warpgroup)
+//
+// Tensor memory (512 columns): scores of slots 0 and 1, 128 each, the weights in
+// 16 bits over the first half of their scores' columns; outputs from column 256
+// on. S = Q K^T has both operands in shared memory; O += P V takes P from tensor
+// memory and V as TMA left it, along N. A slot's next scores are issued behind
+// the product that reads its weights, so they may take their place.
+//
+// The output is rescaled only when a row's maximum has passed the reference that
+// its weights are relative to by 2^8, which seldom happens after the first tiles:
+// weights up to 256 lose nothing in 16 bits and their sum is fp32. At that point
+// the last product is done, because the scores were issued after it.
+template <typename T, int D, bool kCap, bool kBias>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+    attention_mma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                         const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttentionParams p,
+                         int by_heads) {
+  using L = Plan<D>;
+  constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+  extern __shared__ uint8_t raw[];
+  __shared__ MmaShared sh;
+  uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // queries of both slots, then the stages
+  uint8_t* stages = tiles + 2 * L::kTile;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int per = by_heads ? p.heads / 2 : p.heads;  // CTAs per tile of rows; the longest causal rows come first
+  const int item = blockIdx.x % per, block = gridDim.x / per - 1 - blockIdx.x / per;
+  const int head0 = by_heads ? item * 2 : item, kv_head = head0 / p.group;
+  volatile int* dead = &sh.dead;
+
+  if (tid == 0) {
+    mbar_init(&sh.q_full, 1);
+    for (int i = 0; i < L::kStages; ++i) {
+      mbar_init(&sh.kv_full[i], 1);
+      mbar_init(&sh.kv_empty[i], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sh.s_full[s], 1);
+      mbar_init(&sh.p_full[s], 4);
+      mbar_init(&sh.o_full[s], 1);
+      sh.lo[s] = 0x7FFFFFFF;
+      sh.hi[s] = 0;
+    }
+    mbar_init(&sh.drain, 1);
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) tmem_alloc(&sh.tmem, 512);
+  __syncthreads();
+  int64_t row = 0;
+  int lo = 0, hi = 0, self = 0;
+  const int slot = warp >> 2;
+  if (warp < 8) {
+    row = (by_heads ? block : 2 * static_cast<int64_t>(block) + slot) * kRows + (tid & 127);
+    if (row < p.q_tokens) {
+      lo = max(p.spans[row], 0);
+      hi = min(p.spans[p.q_tokens + row], static_cast<int>(p.k_tokens));
+      if (kBias) self = p.spans[2 * p.q_tokens + row];
+    }
+    if (hi <= lo) lo = hi = 0;
+    const int least = __reduce_min_sync(0xFFFFFFFFu, hi > lo ? lo : 0x7FFFFFFF);
+    const int most = __reduce_max_sync(0xFFFFFFFFu, hi);
+    if (lane == 0 && most > 0) {
+      atomicMin(&sh.lo[slot], least);
+      atomicMax(&sh.hi[slot], most);
+    }
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = sh.tmem;
+  const int begin = min(sh.lo[0], sh.lo[1]), stop = max(sh.hi[0], sh.hi[1]);
+  const int n = stop > begin ? (stop - begin + kRows - 1) / kRows : 0;  // tiles of keys
+  int from[2], to[2];                                                   // those that a slot sees
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    from[s] = to[s] = 0;
+    if (sh.hi[s] > sh.lo[s]) {
+      from[s] = (sh.lo[s] - begin) / kRows;
+      to[s] = (sh.hi[s] - begin + kRows - 1) / kRows;
+    }
+  }
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 9 && lane == 0 && n > 0) {
+      mbar_expect(&sh.q_full, 2 * L::kTile);
+      for (int s = 0; s < 2; ++s)
+        for (int c = 0; c < D / 64; ++c)
+          tma_load_3d(tiles + s * L::kTile + c * kChunk, &q_map, c * 64, by_heads ? head0 + s : head0,
+                      (by_heads ? block : 2 * block + s) * kRows, &sh.q_full);
+      int issued = 0;
+      for (int i = 0; i < 2 * n; ++i) {
+        const int stage = i % L::kStages;
+        if (i >= L::kStages && !mbar_wait(&sh.kv_empty[stage], (i / L::kStages - 1) & 1, dead)) break;
+        mbar_expect(&sh.kv_full[stage], L::kTile);
+        for (int c = 0; c < D / 64; ++c)
+          tma_load_3d(stages + stage * L::kTile + c * kChunk, i % 2 == 0 ? &k_map : &v_map, c * 64, kv_head,
+                      begin + (i / 2) * kRows, &sh.kv_full[stage]);
+        ++issued;
+      }
+      if (*dead) {  // nothing may land in shared memory after the CTA is gone
+        const long long start = clock64();
+        for (int i = max(0, issued - L::kStages); i < issued; ++i)
+          while (!mbar_try(&sh.kv_full[i % L::kStages], (i / L::kStages) & 1) && clock64() - start < kWaitCycles) {}
+        while (!mbar_try(&sh.q_full, 0) && clock64() - start < kWaitCycles) {}
+      }
+    }
+    if (warp == 8) {
+      const uint32_t q0 = smem_address(tiles), kv0 = smem_address(stages);
+      constexpr uint32_t kScores = mma_desc(kBf16, kRows, false), kOutput = mma_desc(kBf16, D, true);
+      int waits[2] = {0, 0};  // of a slot's weights
+      bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
+      for (int j = 0; j <= n && n > 0 && alive; ++j) {
+        const int vi = 2 * j - 1, ki = 2 * j;  // places in the order of loads
+        if (j > 0) {
+          alive = mbar_wait_warp(&sh.kv_full[vi % L::kStages], (vi / L::kStages) & 1, dead);
+          if (!alive) break;
+          const int rest = stop - (begin + (j - 1) * kRows);
+          if (rest < kRows) {  // keys that no row sees: their weight is 0, and 0 times what is there has to be 0
+            uint8_t* v = stages + (vi % L::kStages) * L::kTile;
+            for (int i = lane; i < (kRows - rest) * 8 * (D / 64); i += 32) {
+              const int c = i / ((kRows - rest) * 8), at = i - c * (kRows - rest) * 8;
+              *reinterpret_cast<uint4*>(v + c * kChunk + (rest + at / 8) * 128 + at % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+        }
+        bool k_here = false;
+  #pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t scores = tmem + s * 128, out = tmem + 256 + s * D;
+          if (j > from[s] && j <= to[s]) {
+            alive = mbar_wait_warp(&sh.p_full[s], waits[s]++ & 1, dead);
+            if (!alive) break;
+            tmem_fence_after();
+            if (lane == 0) {
+              const uint32_t v = kv0 + (vi % L::kStages) * L::kTile;
+  #pragma unroll
+              for (int k = 0; k < kRows / 16; ++k)
+                mma_ts(out, scores + k * 8, operand_desc(v + k * 2048, kChunk, 1024), kOutput, j - 1 > from[s] || k > 0);
+              if (j == to[s]) mma_commit(&sh.o_full[s]);
+            }
+          }
+          if (j >= from[s] && j < to[s]) {
+            if (!k_here) {
+              alive = mbar_wait_warp(&sh.kv_full[ki % L::kStages], (ki / L::kStages) & 1, dead);
+              if (!alive) break;
+              k_here = true;
+            }
+            tmem_fence_after();
+            if (lane == 0) {
+              const uint32_t q = q0 + s * L::kTile, k = kv0 + (ki % L::kStages) * L::kTile;
+  #pragma unroll
+              for (int d = 0; d < D / 16; ++d)
+                mma_ss(scores, operand_desc(q + d / 4 * kChunk + d % 4 * 32, 16, 1024),
+                       operand_desc(k + d / 4 * kChunk + d % 4 * 32, 16, 1024), kScores, d > 0);
+              mma_commit(&sh.s_full[s]);
+            }
+          }
+        }
+        if (!alive) break;
+        if (j < n && !k_here) {  // no row of this tile's keys: pass it by
+          alive = mbar_wait_warp(&sh.kv_full[ki % L::kStages], (ki / L::kStages) & 1, dead);
+          if (!alive) break;
+        }
+        if (lane == 0) {
+          if (j > 0) mma_commit(&sh.kv_empty[vi % L::kStages]);
+          if (j < n) mma_commit(&sh.kv_empty[ki % L::kStages]);
+        }
+        __syncwarp();
+      }
+      if (*dead && lane == 0) {
+        mma_commit(&sh.drain);
+        const long long start = clock64();
+        while (!mbar_try(&sh.drain, 0) && clock64() - start < kWaitCycles) {}
+      }
+      __syncwarp();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int h = by_heads ? head0 + slot : head0;
+    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t scores = at + slot * 128, out = at + 256 + slot * D;
+    const float scale2 = kCap ? p.scale / p.softcap : p.scale * kLog2e;
+    const float cap2 = p.softcap * kLog2e, slope2 = kBias ? p.slopes[h] * kLog2e : 0.0f;
+    float base = -kInf, total = 0.0f;  // log2 of what the weights are relative to, and their sum
+    bool alive = true;
+    for (int j = from[slot]; j < to[slot]; ++j) {
+      alive = mbar_wait_warp(&sh.s_full[slot], (j - from[slot]) & 1, dead);
+      if (!alive) break;
+      tmem_fence_after();
+      uint32_t x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_load32(x[c], scores + c * 32);
+      tmem_wait_ld(x[0]);
+#pragma unroll
+      for (int c = 1; c < 4; ++c) tie32(x[c]);
+      const int key0 = begin + j * kRows;
+      if (kCap || kBias) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float s = __uint_as_float(x[c][i]);
+            s = kCap ? capped(s, scale2, cap2) : s * scale2;
+            if (kBias) s -= slope2 * fabsf(static_cast<float>(self - (key0 + c * 32 + i)));
+            x[c][i] = __float_as_uint(s);
+          }
+      }
+      if (!__all_sync(0xFFFFFFFFu, lo <= key0 && hi >= key0 + kRows)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int key = key0 + c * 32 + i;
+            if (key < lo || key >= hi) x[c][i] = __float_as_uint(-kInf);
+          }
+      }
+      float most[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        most[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+        for (int i = 1; i < 32; ++i) most[c] = fmaxf(most[c], __uint_as_float(x[c][i]));
+      }
+      float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+      if (!kCap && !kBias) top *= scale2;
+      const bool moved = top > base + kSlack || (base == -kInf && top > -kInf);
+      if (__any_sync(0xFFFFFFFFu, moved)) {
+        const float back = moved ? (base == -kInf ? 0.0f : exp2_approx(base - top)) : 1.0f;
+        if (moved) base = top;
+        total *= back;
+        if (j > from[slot]) {
+          const bool fresh = total == 0.0f;  // no weight yet: what is there may be anything times 0
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_load32(o, out + c * 32);
+            tmem_wait_ld(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = fresh && moved ? 0u : __float_as_uint(__uint_as_float(o[i]) * back);
+            tmem_store32(out + c * 32, o);
+          }
+        }
+      }
+      const float shift = base == -kInf ? 0.0f : -base;
+      const float times = kCap || kBias ? 1.0f : scale2;
+      const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
+      uint64_t sums[2] = {0, 0};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int c = half * 2 + i / 16, e = i % 16 * 2;
+          const uint64_t t = fma2(pack2(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])), times2, shift2);
+          const float a = exp2_approx(low2(t)), b = exp2_approx(high2(t));
+          sums[i & 1] = add2(sums[i & 1], pack2(a, b));
+          w[i] = narrow2<T>(a, b);
+        }
+        tmem_store32(scores + half * 32, w);
+      }
+      const uint64_t sum = add2(sums[0], sums[1]);
+      total += low2(sum) + high2(sum);
+      tmem_wait_st();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.p_full[slot]);
+    }
+    const bool any = to[slot] > from[slot];
+    if (alive && any) alive = mbar_wait_warp(&sh.o_full[slot], 0, dead);
+    tmem_fence_after();
+    const bool seen = alive && any && total != 0.0f;
+    const float over = seen ? 1.0f / total : 0.0f;
+    bool finite = !seen || total < kInf;
+    T* to_row = static_cast<T*>(p.out) + row * p.out_token + h * p.out_head;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      if (alive && any) {
+        tmem_load32(o, out + c * 32);
+        tmem_wait_ld(o);
+      }
+      if (row < p.q_tokens) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          if (c * 32 + e >= p.dim) continue;
+          float f[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            f[i] = !alive ? NAN : seen ? __uint_as_float(o[e + i]) * over : 0.0f;
+            finite = finite && fabsf(f[i]) < kInf;
+          }
+          *reinterpret_cast<uint4*>(to_row + c * 32 + e) = Vec<T>::narrow_all(f);
+        }
+      }
+    }
+    if (row < p.q_tokens && p.lse != nullptr)
+      p.lse[h * p.q_tokens + row] = !alive ? NAN : seen ? (base + log2f(total)) * kLn2 : -kInf;
+    __syncwarp();  // the row's first values are written before its second
+    for (uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite); left != 0; left &= left - 1) {
+      const int r = __ffs(left) - 1;
+      attention_row<T>(p, row - lane + r, h, lane);
+    }
+  }
+  tmem_fence_before();
+  __syncthreads();
+  if (warp == 8) {
+    tmem_fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+template <typename T, int D, bool kCap, bool kBias>
+cudaError_t launch_kind(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
+                        cudaStream_t stream) {
+  using L = Plan<D>;
+  const auto kernel = attention_mma_kernel<T, D, kCap, kBias>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  if (e != cudaSuccess) return e;
+  const int by_heads = p.group % 2 == 0;
+  const int64_t rows = by_heads ? kRows : 2 * kRows;
+  const int64_t grid = (p.q_tokens + rows - 1) / rows * (by_heads ? p.heads / 2 : p.heads);
+  kernel<<<static_cast<unsigned>(grid), kMmaThreads, L::kBytes, stream>>>(q, k, v, p, by_heads);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_head(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
+                        cudaStream_t stream) {
+  if (p.softcap > 0.0f)
+    return p.slopes != nullptr ? launch_kind<T, D, true, true>(q, k, v, p, stream)
+                               : launch_kind<T, D, true, false>(q, k, v, p, stream);
+  return p.slopes != nullptr ? launch_kind<T, D, false, true>(q, k, v, p, stream)
+                             : launch_kind<T, D, false, false>(q, k, v, p, stream);
+}
+
+}  // namespace
+
+bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stream, cudaError_t* e) {
+  const auto vectors = [](const void* x, int64_t token, int64_t head, int64_t tokens, int64_t heads) {
+    return aligned_to(x, 16) && token % 8 == 0 && head % 8 == 0 && (token > 0 || tokens <= 1) && (head > 0 || heads <= 1);
+  };
+  const int kv_heads = p.heads / p.group;
+  constexpr int64_t kMost = 0x7FFFFFFF - 4 * kRows;  // rows, keys and CTAs, a last tile's end among them, in 32 bits
+  // The scores' maximum is taken before the scale, and -inf times it has to stay -inf: it is positive
+  if (dtype == 0 || p.dim > 128 || p.dim % 8 != 0 || p.k_tokens == 0 || !(p.scale > 0.0f)) return false;
+  if (p.q_tokens > kMost || p.k_tokens > kMost || (p.q_tokens / kRows + 1) * p.heads > kMost) return false;
+  if (!vectors(p.q, p.q_token, p.q_head, p.q_tokens, p.heads) || !vectors(p.k, p.k_token, p.k_head, p.k_tokens, kv_heads) ||
+      !vectors(p.v, p.v_token, p.v_head, p.k_tokens, kv_heads) ||
+      !vectors(p.out, p.out_token, p.out_head, p.q_tokens, p.heads))
+    return false;
+  CUtensorMap q, k, v;
+  const bool bf16 = dtype == 1;
+  if (!make_head_map(&q, bf16, p.q, p.dim, p.heads, p.q_tokens, p.q_head, p.q_token) ||
+      !make_head_map(&k, bf16, p.k, p.dim, kv_heads, p.k_tokens, p.k_head, p.k_token) ||
+      !make_head_map(&v, bf16, p.v, p.dim, kv_heads, p.k_tokens, p.v_head, p.v_token))
+    return false;
+  if (bf16)
+    *e = p.dim <= 64 ? launch_head<__nv_bfloat16, 64>(q, k, v, p, stream) : launch_head<__nv_bfloat16, 128>(q, k, v, p, stream);
+  else
+    *e = p.dim <= 64 ? launch_head<__half, 64>(q, k, v, p, stream) : launch_head<__half, 128>(q, k, v, p, stream);
+  return true;
+}
+
+}  // namespace zo

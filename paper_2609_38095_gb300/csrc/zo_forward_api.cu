@@ -145,6 +145,8 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
   p.scale = scale, p.softcap = softcap;
   p.slopes = slopes;
   p.lse = lse;
+  cudaError_t e = cudaSuccess;
+  if (zo::launch_attention_mma(p, dtype, static_cast<cudaStream_t>(stream), &e)) return finish(e, "attention_mma_kernel");
   return finish(zo::launch_attention_tiles(p, dtype, static_cast<cudaStream_t>(stream)), "attention_tiles_kernel");
 }
 
