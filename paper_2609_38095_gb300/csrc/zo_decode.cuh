@@ -25,7 +25,7 @@ struct DecodeJoin {  // a CTA's statistics, read by its peers
 struct DecodePlace {
   int b, g, head0, heads;  // sequence, key-value head, first query head, query heads here
   int64_t len;
-  int bad;  // a length beyond the page table
+  int bad;  // a length beyond the page table, or no cache
 };
 
 template <int HB>
@@ -39,7 +39,7 @@ __device__ __forceinline__ DecodePlace decode_place(const DecodeParams& p, uint3
   w.head0 = w.g * p.group + first;
   w.heads = min(HB, p.group - first);
   w.len = max(p.lengths[w.b], 0);
-  w.bad = w.len > p.max_pages * p.page_size;
+  w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0);
   if (w.bad) w.len = 0;
   return w;
 }

@@ -81,6 +81,7 @@ cudaError_t launch_attention_tiles(const AttentionParams& p, int dtype, cudaStre
 // admit it (false: nothing was launched).
 bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream);
+bool launch_decode_mma(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream);
 
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -187,6 +187,9 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
   p.scale = scale, p.softcap = softcap;
   p.slopes = slopes;
   p.lse = lse;
+  cudaError_t e = cudaSuccess;
+  if (zo::launch_decode_mma(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
+    return finish(e, "decode_mma_kernel");
   return finish(zo::launch_decode_scalar(p, batch, dtype, sms, static_cast<cudaStream_t>(stream)),
                 "decode_scalar_kernel");
 }
