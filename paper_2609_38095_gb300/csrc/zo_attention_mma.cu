@@ -55,30 +55,6 @@ struct MmaShared {
   int dead;
 };
 
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  return static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a);
-}
-__device__ __forceinline__ float low2(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); }
-__device__ __forceinline__ float high2(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
-
-template <typename T>
-__device__ __forceinline__ uint32_t narrow2(float a, float b) {
-  uint32_t r;
-  if constexpr (__is_same(T, __nv_bfloat16)) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-
 // A CTA has two slots of 128 query rows: two heads that share their keys (the
 // same rows, the same spans) where a group has an even number of them, else two
 // tiles of rows of one head. Keys and values go by in tiles of 128; while one

@@ -45,14 +45,6 @@ __device__ __forceinline__ void mma16816(float& c0, float& c1, float& c2, float&
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pair16(float a, float b) {
-  uint32_t r;
-  if constexpr (__is_same(T, __nv_bfloat16)) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-
 // A warp's tiles of 16 keys come by cp.async, two ahead of the one in use, into
 // its own shared memory, 16-byte vectors swizzled by row. Scores: m16n8k16 with
 // the query heads as the 16 rows (8 of them zeros where HB is 8, and their
@@ -207,7 +199,7 @@ __global__ void __launch_bounds__(kWarps * 32) decode_mma_kernel(const __grid_co
       for (int n = 0; n < 2; ++n) {
         const float a = exp2_approx(s[n][2 * r] - shift), b = exp2_approx(s[n][2 * r + 1] - shift);
         total[r] += a + b;
-        weight[n][r] = pair16<T>(a, b);
+        weight[n][r] = narrow2<T>(a, b);
       }
     }
     {

@@ -2,6 +2,7 @@
 // include/zo_forward.h: argument validation and the choice of kernel.
 // Everything here runs on the host and only enqueues kernels.
 #include <cmath>
+#include <cstring>
 
 #include "zo_forward.cuh"
 #include "zo_forward.h"
@@ -83,8 +84,9 @@ int zo_rotate_heads(const zo_head_part* parts, int32_t n_parts, int64_t tokens, 
         (in.weight != nullptr && misaligned(in.weight, element_size(in.weight_dtype))))
       return ZO_ERR_ALIGN;
     zo::RotatePart& out = r.part[i];
-    out = {in.in.ptr,    in.out.ptr,  in.weight,       in.in.token,
-           in.in.head,   in.out.page, in.out.token,    in.out.head,
+    const int64_t one = in.heads > 1;  // one head has no stride, nor has one token
+    out = {in.in.ptr,         in.out.ptr,  in.weight,    tokens > 1 ? in.in.token : 0,
+           in.in.head * one,  in.out.page, in.out.token, in.out.head * one,
            in.weight_dtype, in.heads, (in.flags & ZO_HEADS_ROTATE) != 0, (in.flags & ZO_HEADS_SLOTTED) != 0, 0};
     rotate = rotate || out.rotate;
     slotted = slotted || out.slotted;
@@ -135,10 +137,13 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
   if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
       misaligned(spans, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
     return ZO_ERR_ALIGN;
+  const auto lone = [](int64_t stride, int64_t n) { return n > 1 ? stride : 0; };  // one element has no stride
   zo::AttentionParams p = {};
   p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
-  p.q_token = q->token, p.q_head = q->head, p.k_token = k->token, p.k_head = k->head;
-  p.v_token = v->token, p.v_head = v->head, p.out_token = out->token, p.out_head = out->head;
+  p.q_token = lone(q->token, q_tokens), p.q_head = lone(q->head, heads);
+  p.k_token = lone(k->token, k_tokens), p.k_head = lone(k->head, kv_heads);
+  p.v_token = lone(v->token, k_tokens), p.v_head = lone(v->head, kv_heads);
+  p.out_token = lone(out->token, q_tokens), p.out_head = lone(out->head, heads);
   p.q_tokens = q_tokens, p.k_tokens = k_tokens;
   p.heads = heads, p.group = heads / kv_heads, p.dim = head_dim;
   p.spans = spans;
@@ -179,8 +184,9 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
   zo::DecodeParams p = {};
   p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
   p.q_token = q->token, p.q_head = q->head, p.out_token = out->token, p.out_head = out->head;
-  p.k_page = k->page, p.k_token = k->token, p.k_head = k->head;
-  p.v_page = v->page, p.v_token = v->token, p.v_head = v->head;
+  const auto lone = [](int64_t stride, int64_t n) { return n > 1 ? stride : 0; };  // one element has no stride
+  p.k_page = lone(k->page, n_pages), p.k_token = lone(k->token, page_size), p.k_head = lone(k->head, kv_heads);
+  p.v_page = lone(v->page, n_pages), p.v_token = lone(v->token, page_size), p.v_head = lone(v->head, kv_heads);
   p.pages_stride = pages_stride, p.max_pages = max_pages, p.n_pages = n_pages;
   p.pages = pages, p.lengths = lengths;
   p.heads = heads, p.kv_heads = kv_heads, p.group = heads / kv_heads, p.dim = head_dim, p.page_size = page_size;
@@ -219,6 +225,47 @@ int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab
   p.loss = loss, p.nll = nll;
   p.rows = static_cast<double*>(workspace);
   return finish(zo::launch_token_loss(p, dtype, sms, static_cast<cudaStream_t>(stream)), "token_loss_kernel");
+}
+
+// The entry points above with their arguments in one block, as the Python binding
+// lays them out (a ctypes call costs by its arguments; not part of the public
+// interface).
+int zo_internal_rotate_heads(const int64_t* a, void* stream) {
+  float eps;
+  std::memcpy(&eps, a + 13, sizeof(eps));
+  return zo_rotate_heads(reinterpret_cast<const zo_head_part*>(a + 14), static_cast<int32_t>(a[0]), a[1],
+                         static_cast<int32_t>(a[2]), static_cast<int32_t>(a[3]), reinterpret_cast<const float*>(a[4]), a[5],
+                         static_cast<int32_t>(a[6]), static_cast<int32_t>(a[7]), reinterpret_cast<const void*>(a[8]),
+                         reinterpret_cast<const void*>(a[9]), static_cast<int32_t>(a[10]), a[11], a[12], eps, stream);
+}
+
+int zo_internal_attention(const int64_t* a, void* stream) {
+  float f[2];  // scale, softcap
+  std::memcpy(f, a + 21, sizeof(f));
+  const zo_rows* rows = reinterpret_cast<const zo_rows*>(a);
+  return zo_attention(rows, rows + 1, rows + 2, rows + 3, a[12], a[13], static_cast<int32_t>(a[14]),
+                      static_cast<int32_t>(a[15]), static_cast<int32_t>(a[16]), static_cast<int32_t>(a[17]),
+                      reinterpret_cast<const int32_t*>(a[18]), f[0], f[1], reinterpret_cast<const float*>(a[19]),
+                      reinterpret_cast<float*>(a[20]), stream);
+}
+
+int zo_internal_attention_decode(const int64_t* a, void* stream) {
+  float f[2];  // scale, softcap
+  std::memcpy(f, a + 27, sizeof(f));
+  const zo_rows *q = reinterpret_cast<const zo_rows*>(a), *out = reinterpret_cast<const zo_rows*>(a + 3);
+  const zo_pages *k = reinterpret_cast<const zo_pages*>(a + 6), *v = reinterpret_cast<const zo_pages*>(a + 10);
+  return zo_attention_decode(q, k, v, out, a[14], static_cast<int32_t>(a[15]), static_cast<int32_t>(a[16]),
+                             static_cast<int32_t>(a[17]), static_cast<int32_t>(a[18]),
+                             reinterpret_cast<const int32_t*>(a[19]), a[20], a[21], a[22], static_cast<int32_t>(a[23]),
+                             reinterpret_cast<const int32_t*>(a[24]), f[0], f[1], reinterpret_cast<const float*>(a[25]),
+                             reinterpret_cast<float*>(a[26]), stream);
+}
+
+int zo_internal_token_loss(const int64_t* a, void* stream) {
+  return zo_token_loss(reinterpret_cast<const void*>(a[0]), a[1], a[2], a[3], static_cast<int32_t>(a[4]),
+                       reinterpret_cast<const void*>(a[5]), static_cast<int32_t>(a[6]), static_cast<int32_t>(a[7]),
+                       reinterpret_cast<void*>(a[8]), reinterpret_cast<float*>(a[9]), reinterpret_cast<void*>(a[10]), a[11],
+                       stream);
 }
 
 }  // extern "C"

@@ -7,7 +7,8 @@ namespace zo {
 namespace {
 
 constexpr int kRotateThreads = 256;
-constexpr int kHeadsPerGroup = 4;  // heads that a group of lanes takes, their loads issued together
+constexpr int kHeadsPerGroup = 2;  // heads that a group of lanes takes, their loads issued together
+constexpr int kRotateCtas = 4;     // per SM, by registers: with two heads per group 64 KB in flight
 
 // Position t's row of the table; a position outside it: NULL.
 __device__ __forceinline__ const float* table_row(const RotateParams& p, int64_t t) {
@@ -30,6 +31,15 @@ __device__ __forceinline__ const RotatePart& part_of(const RotateParams& p, int 
   return p.part[i];
 }
 
+__device__ __forceinline__ float weight_at(const RotatePart& part, int i) {
+  if (part.weight_dtype == 0) return static_cast<const float*>(part.weight)[i];
+  if (part.weight_dtype == 1) return widen(static_cast<const __nv_bfloat16*>(part.weight)[i]);
+  return widen(static_cast<const __half*>(part.weight)[i]);
+}
+
+template <typename T>
+constexpr int kCode = sizeof(T) == 4 ? 0 : __is_same(T, __nv_bfloat16) ? 1 : 2;  // zo_dtype
+
 // A head lies on kLanes lanes, each with a unit of two 16-byte vectors: the two
 // halves of its pairs (layout half), or neighbours (interleaved, and what is not
 // rotated), so that a lane has both elements of a pair and reads E cosines and
@@ -37,7 +47,7 @@ __device__ __forceinline__ const RotatePart& part_of(const RotateParams& p, int 
 // kHeadsPerGroup * 32 / kLanes heads; angles and weight are loaded once for them.
 // Bound by HBM: 2 bytes in and 2 out per 16-bit element.
 template <typename T, int kLanes>
-__global__ void __launch_bounds__(kRotateThreads) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
   constexpr int E = Vec<T>::kN;
   constexpr int kGroups = 32 / kLanes;
   const int lane = threadIdx.x & 31;
@@ -65,7 +75,7 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_heads_kernel(const __gr
       raw[n][1] = *reinterpret_cast<const uint4*>(in + h * part.in_head + b);
     }
   }
-  float cs[E], sn[E], w[2 * E];
+  float cs[E], sn[E];
   if (turned) {
     const float* angles = table_row(p, t);
 #pragma unroll
@@ -79,20 +89,10 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_heads_kernel(const __gr
     }
   }
   const bool norm = part.weight != nullptr;
+  uint4 w[2];  // packed: as floats, a quarter of the registers would be weights
   if (norm && here) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (part.weight_dtype == 0) {
-        w[e] = static_cast<const float*>(part.weight)[a + e];
-        w[E + e] = static_cast<const float*>(part.weight)[b + e];
-      } else if (part.weight_dtype == 1) {
-        w[e] = widen(static_cast<const __nv_bfloat16*>(part.weight)[a + e]);
-        w[E + e] = widen(static_cast<const __nv_bfloat16*>(part.weight)[b + e]);
-      } else {
-        w[e] = widen(static_cast<const __half*>(part.weight)[a + e]);
-        w[E + e] = widen(static_cast<const __half*>(part.weight)[b + e]);
-      }
-    }
+    w[0] = *reinterpret_cast<const uint4*>(static_cast<const T*>(part.weight) + a);
+    w[1] = *reinterpret_cast<const uint4*>(static_cast<const T*>(part.weight) + b);
   }
 #pragma unroll
   for (int n = 0; n < kHeadsPerGroup; ++n) {
@@ -108,8 +108,13 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_heads_kernel(const __gr
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       const float r = rsqrtf(sum / p.dim + p.eps);
+      float f[E];
+      Vec<T>::widen_all(w[0], f);
 #pragma unroll
-      for (int e = 0; e < 2 * E; ++e) x[e] = here ? x[e] * r * w[e] : 0.0f;
+      for (int e = 0; e < E; ++e) x[e] = x[e] * r * f[e];
+      Vec<T>::widen_all(w[1], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[E + e] = x[E + e] * r * f[e];
     }
     if (turned) {
       if (p.interleaved) {
@@ -173,9 +178,7 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_heads_any_kernel(const 
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         if (at[c][s] < p.dim) {
-          const float w = part.weight_dtype == 0   ? static_cast<const float*>(part.weight)[at[c][s]]
-                          : part.weight_dtype == 1 ? widen(static_cast<const __nv_bfloat16*>(part.weight)[at[c][s]])
-                                                   : widen(static_cast<const __half*>(part.weight)[at[c][s]]);
+          const float w = weight_at(part, at[c][s]);
           x[c][s] = x[c][s] * r * w;
         }
   }
@@ -246,11 +249,12 @@ __global__ void document_spans_kernel(const int32_t* q_starts, const int32_t* k_
   }
 }
 
-// Whether every vector of a part starts on 16 bytes.
+// Whether every vector of a part, its weight's among them, starts on 16 bytes and is of the data's type.
 template <typename T>
 bool part_aligned(const RotatePart& r) {
   constexpr int64_t E = Vec<T>::kN;
-  return aligned_to(r.in, 16) && aligned_to(r.out, 16) && r.in_token % E == 0 && r.in_head % E == 0 &&
+  return (r.weight == nullptr || (r.weight_dtype == kCode<T> && aligned_to(r.weight, 16))) && aligned_to(r.in, 16) &&
+         aligned_to(r.out, 16) && r.in_token % E == 0 && r.in_head % E == 0 &&
          r.out_token % E == 0 && r.out_head % E == 0 && (!r.slotted || r.out_page % E == 0);
 }
 

@@ -6,7 +6,8 @@ namespace zo {
 
 namespace {
 
-constexpr int kLossThreads = 512;
+constexpr int kLossThreads = 256;
+constexpr int kLossCtas = 5;     // per SM, by registers: with kLossVectors 80 KB in flight
 constexpr int kLossVectors = 4;  // 16-byte loads in flight per thread
 constexpr int kSumThreads = 1024;
 
@@ -40,18 +41,26 @@ __device__ __forceinline__ void take(const float* x, float& top, float& sum) {
     sum *= exp2_approx((top - most) * kLog2e);
     top = most;
   }
-  float s = 0.0f;
+  if constexpr (N == 1) {
+    sum += exp2_approx((x[0] - top) * kLog2e);
+  } else {
+    const uint64_t away = pack2(-top, -top), unit = pack2(kLog2e, kLog2e);
+    uint64_t s = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) s += exp2_approx((x[i] - top) * kLog2e);
-  sum += s;
+    for (int i = 0; i < N; i += 2) {
+      const uint64_t d = mul2(add2(pack2(x[i], x[i + 1]), away), unit);
+      s = add2(s, pack2(exp2_approx(low2(d)), exp2_approx(high2(d))));
+    }
+    sum += low2(s) + high2(s);
+  }
 }
 
 // A token per CTA, or per cluster of CTAs that split the vocabulary where there
 // are fewer tokens than the SMs hold CTAs. One pass with the running maximum
 // and sum in registers; bound by HBM: each counted row is read once.
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads) token_loss_kernel(const __grid_constant__ TokenLossParams p,
-                                                                  int parts) {
+__global__ void __launch_bounds__(kLossThreads, kLossCtas)
+    token_loss_kernel(const __grid_constant__ TokenLossParams p, int parts) {
   constexpr int E = Vec<T>::kN;
   __shared__ float tops[kLossThreads / 32];
   __shared__ double sums[kLossThreads / 32];
@@ -81,20 +90,19 @@ __global__ void __launch_bounds__(kLossThreads) token_loss_kernel(const __grid_c
     take<1>(&one, top, sum);
   }
   const uint4* v = reinterpret_cast<const uint4*>(x + head);
-  int64_t i = tid;
-  for (; i + (kLossVectors - 1) * kLossThreads < vectors; i += kLossVectors * kLossThreads) {
+  const int n = static_cast<int>(vectors);
+  const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
+  for (int i = tid; i < n; i += kLossVectors * kLossThreads) {
     uint4 raw[kLossVectors];
 #pragma unroll
-    for (int n = 0; n < kLossVectors; ++n) raw[n] = __ldcs(v + i + n * kLossThreads);
+    for (int k = 0; k < kLossVectors; ++k) {
+      raw[k] = make_uint4(none, none, none, none);
+      if (i + k * kLossThreads < n) raw[k] = __ldcs(v + i + k * kLossThreads);
+    }
     float f[kLossVectors * E];
 #pragma unroll
-    for (int n = 0; n < kLossVectors; ++n) Vec<T>::widen_all(raw[n], f + n * E);
+    for (int k = 0; k < kLossVectors; ++k) Vec<T>::widen_all(raw[k], f + k * E);
     take<kLossVectors * E>(f, top, sum);
-  }
-  for (; i < vectors; i += kLossThreads) {
-    float f[E];
-    Vec<T>::widen_all(__ldcs(v + i), f);
-    take<E>(f, top, sum);
   }
   Tail mine = warp_join({top, sum});
   if ((tid & 31) == 0) {
@@ -151,12 +159,15 @@ __global__ void __launch_bounds__(kSumThreads) token_loss_sum_kernel(const __gri
     counts[threadIdx.x >> 5] = count;
   }
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  sum = count = 0.0;
-  for (int i = 0; i < kSumThreads / 32; ++i) {
-    sum += sums[i];
-    count += counts[i];
+  if (threadIdx.x >= 32) return;
+  sum = sums[threadIdx.x];
+  count = counts[threadIdx.x];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
   }
+  if (threadIdx.x != 0) return;
   if (p.flags & 1) sum = count > 0.0 ? sum / count : NAN;
   if (p.flags & 4) {
     float* out = static_cast<float*>(p.loss);
@@ -181,7 +192,7 @@ cudaError_t launch_with(F f, unsigned grid, unsigned threads, cudaLaunchAttribut
 template <typename T>
 cudaError_t launch_rows(const TokenLossParams& p, int sms, cudaStream_t stream) {
   int parts = 1;
-  while (parts < 8 && p.tokens * parts * 2 <= 4 * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
+  while (parts < 8 && p.tokens * parts * 2 <= kLossCtas * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = parts;

@@ -22,6 +22,7 @@ The method has no backward pass: a tensor that asks for a gradient is refused
 where torch would record one.
 """
 import ctypes
+from struct import Struct
 
 import torch
 
@@ -54,11 +55,26 @@ def _lib():
             "zo_token_loss_workspace_size": ([i64], i64),
             "zo_token_loss": ([vp, i64, i64, i64, i32, vp, i32, i32, vp, vp, vp, i64, vp], ctypes.c_int),
         }
+        for name in ("rotate_heads", "attention", "attention_decode", "token_loss"):
+            sig["zo_internal_" + name] = ([ctypes.c_char_p, vp], ctypes.c_int)
         for name, (args, res) in sig.items():
             f = getattr(L, name)
             f.argtypes, f.restype = args, res
         _signed = True
     return L
+
+
+# A call's arguments travel in one block; the checks of the calls below are one
+# expression each, and the functions named _refuse_* say what was wrong. (On the
+# GB300's host cores an attribute of a tensor costs 0.1 us and a Python call 0.3,
+# of 10 to 15 us that a call takes in all.)
+_ROTATE = [None] + [Struct(f"13qfxxxx{10 * n}q") for n in (1, 2, 3)]
+_ATTENTION = Struct("21qff")
+_DECODE = Struct("27qff")
+_LOSS = Struct("12q")
+_grad = torch.is_grad_enabled
+_empty = torch.empty
+
 
 
 def _rows(t, what, dim, like=None):
@@ -76,13 +92,13 @@ def _rows(t, what, dim, like=None):
         raise ValueError(f"{what} is on {t.device}, expected {like.device}")
     if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{what}: the elements of a head must be contiguous")
-    if t.requires_grad and torch.is_grad_enabled():
+    if t.requires_grad and _grad():
         raise RuntimeError(f"{what} asks for a gradient, which this operator does not have")
     return t
 
 
-def _flat(t, what, dtypes, device, dim=1):
-    """Checks a contiguous tensor of numbers beside the heads."""
+def _flat(t, what, dtypes, device, dim=1, n=None):
+    """Checks a contiguous tensor of numbers beside the heads, of n elements."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor")
     if t.dtype not in dtypes:
@@ -91,12 +107,11 @@ def _flat(t, what, dtypes, device, dim=1):
         raise ValueError(f"{what} is on {t.device}, expected {device}")
     if t.dim() != dim or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous, with {dim} dimension{'s' if dim > 1 else ''}")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{what} must have {n} elements, got {t.numel()}")
+    if t.requires_grad and _grad():
+        raise RuntimeError(f"{what} asks for a gradient, which this operator does not have")
     return t
-
-
-def _stride(t, i):
-    """The stride of dimension i; 0 where only its first element exists."""
-    return t.stride(i) if t.shape[i] > 1 else 0
 
 
 def rotary_table(rows, rotary_dim, base=10000.0, scale=1.0, original=0, low=1.0, high=32.0, magnitude=1.0, device=None):
@@ -119,13 +134,48 @@ def document_spans(q_starts, k_starts=None, prefix=None, *, tokens):
     dev, docs = q_starts.device, q_starts.numel() - 1
     if docs < 0:
         raise ValueError("q_starts must have one element more than there are documents")
-    k_starts = q_starts if k_starts is None else _flat(k_starts, "k_starts", (torch.int32,), dev)
-    if k_starts.numel() != docs + 1 or (prefix is not None and _flat(prefix, "prefix", (torch.int32,), dev).numel() != docs):
-        raise ValueError("k_starts must have as many elements as q_starts, prefix one less")
+    k_starts = q_starts if k_starts is None else _flat(k_starts, "k_starts", (torch.int32,), dev, n=docs + 1)
+    if prefix is not None:
+        _flat(prefix, "prefix", (torch.int32,), dev, n=docs)
     spans = torch.empty(3, tokens, dtype=torch.int32, device=dev)
     _zo._launch("zo_document_spans", _zo._index(dev), _lib().zo_document_spans, q_starts.data_ptr(), k_starts.data_ptr(),
                 prefix.data_ptr() if prefix is not None else None, docs, spans.data_ptr(), tokens)
     return spans
+
+
+def _refuse_part(what, q, x, weight, out, by_slot):
+    _rows(x, what, 3, None if what == "q" else q)
+    if x.shape[0] != q.shape[0] or x.shape[2] != q.shape[2]:
+        raise ValueError(f"{what} must have q's tokens and head size")
+    if weight is not None:
+        _flat(weight, f"{what}_weight", DTYPE_CODE, q.device, n=q.shape[2])
+    _rows(out, f"{what}_out", 4 if by_slot and out.dim() == 4 else 3, q)
+    raise ValueError(f"{what}_out must have {what}'s heads and, without slots, tokens")
+
+
+def _part(what, q, idx, dtype, tokens, dim, x, weight, out, flags):
+    """The output of one of rotate_heads's tensors, its words of the argument block, and its rows and rows per page."""
+    shape = x.shape
+    if out is None:
+        out = _empty(shape, dtype=dtype, device=x.device)
+    made, steps, by_slot = out.shape, out.stride(), flags & 2
+    strides = x.stride()
+    if not (len(shape) == 3 and x.dtype == dtype == out.dtype and x.get_device() == idx == out.get_device()
+            and shape[0] == tokens and shape[2] == dim and (strides[2] == 1 or dim == 1) and (steps[-1] == 1 or dim == 1)
+            and made[-2:] == shape[1:] and (len(made) == 3 or (by_slot and len(made) == 4)) and (by_slot or made[0] == tokens)
+            and (weight is None or (weight.numel() == dim and weight.dtype in DTYPE_CODE and weight.get_device() == idx
+                                    and weight.dim() == 1 and weight.is_contiguous()))
+            and not (_grad() and (x.requires_grad or out.requires_grad or (weight is not None and weight.requires_grad)))):
+        _refuse_part(what, q, x, weight, out, by_slot)
+    if len(made) == 4:
+        page, rows, per_page = steps[0], made[0] * made[1], made[1]
+    else:
+        page, rows, per_page = 0, made[0], made[0]
+    kind = shape[1] << 32
+    if weight is not None:
+        kind |= DTYPE_CODE[weight.dtype]
+    return out, (x.data_ptr(), strides[0], strides[1], out.data_ptr(), page, steps[-3], steps[-2],
+                 0 if weight is None else weight.data_ptr(), kind, flags), rows, per_page
 
 
 def rotate_heads(q, k=None, v=None, *, table, positions, q_weight=None, k_weight=None, eps=1e-6, layout="half",
@@ -134,80 +184,64 @@ def rotate_heads(q, k=None, v=None, *, table, positions, q_weight=None, k_weight
     v is copied (zo_rotate_heads). Returns what was written, one tensor per tensor given: q alone, (q, k) or (q, k, v);
     new tensors where no *_out is given. With slots (one per token) k and v go to rows of a cache, k_out and v_out:
     (rows, kv_heads, head_dim) or (pages, page_size, kv_heads, head_dim). q_out may be q, and k_out k."""
-    _rows(q, "q", 3)
-    dev, dtype, (tokens, _, dim) = q.device, q.dtype, q.shape
+    shape, idx, index = q.shape, q.get_device(), positions.dtype
+    if not (idx >= 0 and len(shape) == 3 and q.dtype in DTYPE_CODE):
+        _rows(q, "q", 3)
+    tokens, _, dim = shape
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(LAYOUTS)}")
-    _flat(table, "table", (torch.float32,), dev, 2)
-    _flat(positions, "positions", INDEX_BYTES, dev)
-    if positions.numel() != tokens:
-        raise ValueError("positions must have one element per token")
-    if v is not None and k is None:
-        raise ValueError("v needs k")
+    size = table.shape
+    if not (len(size) == 2 and table.dtype is torch.float32 and table.is_contiguous() and table.get_device() == idx
+            and index in INDEX_BYTES and positions.get_device() == idx and positions.shape == shape[:1]
+            and positions.is_contiguous()):
+        _flat(table, "table", (torch.float32,), q.device, 2)
+        _flat(positions, "positions", INDEX_BYTES, q.device, n=tokens)
+    by_slot, rows, per_page = 0, 1, 1
     if slots is not None:
         if k is None or k_out is None or (v is None) != (v_out is None):
             raise ValueError("slots need k and the cache that it goes to, and v both or neither")
-        _flat(slots, "slots", (positions.dtype,), dev)
-        if slots.numel() != tokens:
-            raise ValueError("slots must have one element per token")
-    words, made = [], []
-    n_slots = page_size = 1
-    for what, x, weight, out, rotate in (("q", q, q_weight, q_out, 1), ("k", k, k_weight, k_out, 1), ("v", v, None, v_out, 0)):
-        if x is None:
-            if out is not None or weight is not None:
-                raise ValueError(f"an output or weight is given for {what}, but not {what}")
-            continue
-        if what != "q":
-            _rows(x, what, 3, q)
-            if x.shape[0] != tokens or x.shape[2] != dim:
-                raise ValueError(f"{what} must have q's tokens and head size")
-        if weight is not None:
-            _flat(weight, f"{what}_weight", DTYPE_CODE, dev)
-            if weight.numel() != dim:
-                raise ValueError(f"{what}_weight must have one element per element of a head")
-            if weight.requires_grad and torch.is_grad_enabled():
-                raise RuntimeError(f"{what}_weight asks for a gradient, which this operator does not have")
-        by_slot = slots is not None and what != "q"
-        if out is None:
-            out = torch.empty(x.shape, dtype=dtype, device=dev)
-        paged = by_slot and out.dim() == 4
-        _rows(out, f"{what}_out", 4 if paged else 3, q)
-        if out.shape[-2:] != x.shape[-2:] or (not by_slot and out.shape[0] != tokens):
-            raise ValueError(f"{what}_out must have {what}'s heads and, without slots, tokens")
-        if by_slot:
-            size = (out.shape[0] * out.shape[1], out.shape[1]) if paged else (out.shape[0], max(out.shape[0], 1))
-            if what == "k":
-                n_slots, page_size = size
-            elif size != (n_slots, page_size):
-                raise ValueError("k_out and v_out must have the same rows")
-        words += [x.data_ptr(), _stride(x, 0), _stride(x, 1), out.data_ptr(), _stride(out, 0) if paged else 0,
-                  _stride(out, -3), _stride(out, -2), weight.data_ptr() if weight is not None else 0,
-                  (DTYPE_CODE[weight.dtype] if weight is not None else 0) | x.shape[1] << 32,
-                  rotate | (2 if by_slot else 0)]
-        made.append(out)
-    arr = (ctypes.c_int64 * len(words))(*words)
-    _zo._launch("zo_rotate_heads", _zo._index(dev), _lib().zo_rotate_heads, ctypes.addressof(arr), len(made), tokens, dim,
-                DTYPE_CODE[dtype], table.data_ptr(), table.shape[0], table.shape[1], LAYOUTS[layout], positions.data_ptr(),
-                slots.data_ptr() if slots is not None else None, INDEX_BYTES[positions.dtype], n_slots, max(page_size, 1),
-                eps)
-    return made[0] if len(made) == 1 else tuple(made)
+        _flat(slots, "slots", (index,), q.device, n=tokens)
+        by_slot = 2
+    if (k is None and (v is not None or k_out is not None or k_weight is not None)) or (v is None and v_out is not None):
+        raise ValueError("an output, weight or v is given for a tensor that is not")
+    out, words, _, _ = _part("q", q, idx, q.dtype, tokens, dim, q, q_weight, q_out, 1)
+    made = (out,)
+    if k is not None:
+        out, more, rows, per_page = _part("k", q, idx, q.dtype, tokens, dim, k, k_weight, k_out, 1 | by_slot)
+        made, words = made + (out,), words + more
+    if v is not None:
+        out, more, *same = _part("v", q, idx, q.dtype, tokens, dim, v, None, v_out, by_slot)
+        made, words = made + (out,), words + more
+        if by_slot and same != [rows, per_page]:
+            raise ValueError("k_out and v_out must have the same rows")
+    block = _ROTATE[len(made)].pack(len(made), tokens, dim, DTYPE_CODE[q.dtype], table.data_ptr(), size[0], size[1],
+                                    LAYOUTS[layout], positions.data_ptr(), 0 if slots is None else slots.data_ptr(),
+                                    INDEX_BYTES[index], rows, per_page or 1, eps, *words)
+    _zo._launch("zo_rotate_heads", idx, _lib().zo_internal_rotate_heads, block)
+    return made[0] if len(made) == 1 else made
 
 
-def _shared(q, k, v, out, scale, slopes, dim):
-    """Checks that attention and decode_attention share; returns (out, scale)."""
+def _refuse_attention(q, k, v, out, slopes, dim):
+    """Says why attention's or decode_attention's tensors of heads are none that it takes."""
+    _rows(q, "q", 3)
     _rows(k, "k", dim, q)
     _rows(v, "v", dim, q)
     if k.shape != v.shape or k.shape[-1] != q.shape[2]:
         raise ValueError("k and v must have the same shape and q's head size")
     if k.shape[-2] == 0 or q.shape[1] % k.shape[-2]:
         raise ValueError("the key-value heads must divide the query heads")
-    if slopes is not None and _flat(slopes, "slopes", (torch.float32,), q.device).numel() != q.shape[1]:
-        raise ValueError("slopes must have one element per query head")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif _rows(out, "out", 3, q).shape != q.shape:
+    if slopes is not None:
+        _flat(slopes, "slopes", (torch.float32,), q.device, n=q.shape[1])
+    if out is not None and _rows(out, "out", 3, q).shape != q.shape:
         raise ValueError("out must have q's shape")
-    return out, q.shape[2] ** -0.5 if scale is None else scale
+
+
+def _beside(shape, dtype, idx, slopes, out):
+    """Whether slopes and out, where given, fit queries of that shape."""
+    return (slopes is None or (slopes.dtype is torch.float32 and slopes.get_device() == idx and slopes.shape == shape[1:2]
+                               and slopes.is_contiguous() and not (_grad() and slopes.requires_grad))) and (
+        out is None or (out.shape == shape and out.dtype == dtype and out.get_device() == idx
+                        and (out.stride(2) == 1 or shape[2] == 1) and not (_grad() and out.requires_grad)))
 
 
 def attention(q, k, v, spans, *, scale=None, softcap=0.0, slopes=None, out=None, with_lse=False):
@@ -215,18 +249,26 @@ def attention(q, k, v, spans, *, scale=None, softcap=0.0, slopes=None, out=None,
     span (zo_attention). spans: document_spans, or any int32 (3, tokens) of first key, end and own key. softcap: scores
     are softcap * tanh(score / softcap); slopes: float32 (heads), a bias of -slope * distance. Returns out, or (out,
     lse) with lse float32 (heads, tokens)."""
-    _rows(q, "q", 3)
-    out, scale = _shared(q, k, v, out, scale, slopes, 3)
-    tokens, heads, dim = q.shape
-    if _flat(spans, "spans", (torch.int32,), q.device, 2).shape != (3, tokens):
+    shape, size, dtype, idx = q.shape, k.shape, q.dtype, q.get_device()
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if not (idx >= 0 and len(shape) == 3 == len(size) and v.shape == size and size[2] == shape[2] and dtype in DTYPE_CODE
+            and k.dtype == dtype == v.dtype and k.get_device() == idx == v.get_device() and size[1] > 0
+            and shape[1] % size[1] == 0 and (qs[2] == 1 == ks[2] == vs[2] or shape[2] == 1) and _beside(shape, dtype, idx, slopes, out)
+            and not (_grad() and (q.requires_grad or k.requires_grad or v.requires_grad))):
+        _refuse_attention(q, k, v, out, slopes, 3)
+    tokens, heads, dim = shape
+    if not (spans.dtype is torch.int32 and spans.get_device() == idx and spans.shape == (3, tokens) and spans.is_contiguous()):
+        _flat(spans, "spans", (torch.int32,), q.device, 2)
         raise ValueError("spans must have shape (3, tokens)")
-    lse = torch.empty(heads, tokens, dtype=torch.float32, device=q.device) if with_lse else None
-    arr = (ctypes.c_int64 * 12)(q.data_ptr(), _stride(q, 0), _stride(q, 1), k.data_ptr(), _stride(k, 0), _stride(k, 1),
-                                v.data_ptr(), _stride(v, 0), _stride(v, 1), out.data_ptr(), _stride(out, 0), _stride(out, 1))
-    at = ctypes.addressof(arr)
-    _zo._launch("zo_attention", _zo._index(q.device), _lib().zo_attention, at, at + 24, at + 48, at + 72, tokens,
-                k.shape[0], heads, k.shape[1], dim, DTYPE_CODE[q.dtype], spans.data_ptr(), scale, softcap,
-                slopes.data_ptr() if slopes is not None else None, lse.data_ptr() if with_lse else None)
+    if out is None:
+        out = _empty(shape, dtype=dtype, device=q.device)
+    os = out.stride()
+    lse = _empty((heads, tokens), dtype=torch.float32, device=q.device) if with_lse else None
+    block = _ATTENTION.pack(q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], out.data_ptr(),
+                            os[0], os[1], tokens, size[0], heads, size[1], dim, DTYPE_CODE[dtype], spans.data_ptr(),
+                            0 if slopes is None else slopes.data_ptr(), lse.data_ptr() if with_lse else 0,
+                            dim ** -0.5 if scale is None else scale, softcap)
+    _zo._launch("zo_attention", idx, _lib().zo_internal_attention, block)
     return (out, lse) if with_lse else out
 
 
@@ -235,28 +277,35 @@ def decode_attention(q, k_cache, v_cache, pages, lengths, *, scale=None, softcap
     sequence, its own the last (zo_attention_decode). k_cache, v_cache: (pages, page_size, kv_heads, head_dim); pages:
     int32 (batch, pages of the longest); lengths: int32 (batch). Returns out, or (out, lse) with lse float32 (batch,
     heads)."""
-    _rows(q, "q", 3)
-    out, scale = _shared(q, k_cache, v_cache, out, scale, slopes, 4)
-    batch, heads, dim = q.shape
-    if not isinstance(pages, torch.Tensor) or pages.dtype != torch.int32 or pages.device != q.device:
-        raise TypeError("pages must be an int32 tensor on q's device")
-    if pages.dim() != 2 or pages.shape[0] != batch or (pages.shape[1] > 1 and pages.stride(1) != 1):
-        raise ValueError("pages must have one row per sequence, contiguous")
-    if _flat(lengths, "lengths", (torch.int32,), q.device).numel() != batch:
-        raise ValueError("lengths must have one element per sequence")
-    n_pages, page_size, kv_heads = k_cache.shape[:3]
+    shape, size, dtype, idx = q.shape, k_cache.shape, q.dtype, q.get_device()
+    qs, ks, vs = q.stride(), k_cache.stride(), v_cache.stride()
+    if not (idx >= 0 and len(shape) == 3 and len(size) == 4 and v_cache.shape == size and size[3] == shape[2]
+            and dtype in DTYPE_CODE and k_cache.dtype == dtype == v_cache.dtype
+            and k_cache.get_device() == idx == v_cache.get_device() and size[2] > 0 and shape[1] % size[2] == 0
+            and (qs[2] == 1 == ks[3] == vs[3] or shape[2] == 1) and _beside(shape, dtype, idx, slopes, out)
+            and not (_grad() and (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad))):
+        _refuse_attention(q, k_cache, v_cache, out, slopes, 4)
+    batch, heads, dim = shape
+    table, steps = pages.shape, pages.stride()
+    if not (pages.dtype is torch.int32 and pages.get_device() == idx and len(table) == 2 and table[0] == batch
+            and (steps[1] == 1 or table[1] <= 1)):
+        raise ValueError("pages must be an int32 tensor on q's device with a contiguous row per sequence")
+    if not (lengths.dtype is torch.int32 and lengths.get_device() == idx and lengths.shape == shape[:1]
+            and lengths.is_contiguous()):
+        _flat(lengths, "lengths", (torch.int32,), q.device, n=batch)
+    n_pages, page_size, kv_heads, _ = size
     if page_size < 1:
         raise ValueError("a page must hold at least one row")
-    lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device) if with_lse else None
-    k, v = k_cache, v_cache
-    arr = (ctypes.c_int64 * 14)(q.data_ptr(), _stride(q, 0), _stride(q, 1), k.data_ptr(), _stride(k, 0), _stride(k, 1),
-                                _stride(k, 2), v.data_ptr(), _stride(v, 0), _stride(v, 1), _stride(v, 2), out.data_ptr(),
-                                _stride(out, 0), _stride(out, 1))
-    at = ctypes.addressof(arr)
-    _zo._launch("zo_attention_decode", _zo._index(q.device), _lib().zo_attention_decode, at, at + 24, at + 56, at + 88, batch,
-                heads, kv_heads, dim, DTYPE_CODE[q.dtype], pages.data_ptr(), _stride(pages, 0), pages.shape[1], n_pages,
-                page_size, lengths.data_ptr(), scale, softcap, slopes.data_ptr() if slopes is not None else None,
-                lse.data_ptr() if with_lse else None)
+    if out is None:
+        out = _empty(shape, dtype=dtype, device=q.device)
+    os = out.stride()
+    lse = _empty((batch, heads), dtype=torch.float32, device=q.device) if with_lse else None
+    block = _DECODE.pack(q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], k_cache.data_ptr(), ks[0], ks[1], ks[2],
+                         v_cache.data_ptr(), vs[0], vs[1], vs[2], batch, heads, kv_heads, dim, DTYPE_CODE[dtype],
+                         pages.data_ptr(), steps[0], table[1], n_pages, page_size, lengths.data_ptr(),
+                         0 if slopes is None else slopes.data_ptr(), lse.data_ptr() if with_lse else 0,
+                         dim ** -0.5 if scale is None else scale, softcap)
+    _zo._launch("zo_attention_decode", idx, _lib().zo_internal_attention_decode, block)
     return (out, lse) if with_lse else out
 
 
@@ -264,21 +313,25 @@ def token_loss(logits, targets, *, mean=False, add=False, out=None, dtype=torch.
     """-log p of the targets under logits (tokens, vocab), summed over the tokens whose target is not negative, or their
     mean (zo_token_loss). Returns a one-element tensor: `out` (for instance losses[k, 0:1] of a step's loss table; added
     to what is there with add), or a new one of `dtype` (float64 or float32). with_nll: also each token's, float32."""
-    _rows(logits, "logits", 2)
-    dev, (tokens, vocab) = logits.device, logits.shape
-    _flat(targets, "targets", INDEX_BYTES, dev)
-    if targets.numel() != tokens:
-        raise ValueError("targets must have one element per token")
+    shape, idx, kind, strides = logits.shape, logits.get_device(), targets.dtype, logits.stride()
+    if not (idx >= 0 and len(shape) == 2 and logits.dtype in DTYPE_CODE and (strides[1] == 1 or shape[1] == 1)
+            and not (logits.requires_grad and _grad())):
+        _rows(logits, "logits", 2)
+    tokens, vocab = shape
+    if not (kind in INDEX_BYTES and targets.get_device() == idx and targets.shape == shape[:1] and targets.is_contiguous()):
+        _flat(targets, "targets", INDEX_BYTES, logits.device, n=tokens)
     if out is None:
         if add:
             raise ValueError("add needs out")
-        out = torch.empty(1, dtype=dtype, device=dev)
-    if _flat(out, "out", (torch.float64, torch.float32), dev).numel() != 1:
-        raise ValueError("out must have one element")
-    nll = torch.empty(tokens, dtype=torch.float32, device=dev) if with_nll else None
-    work = torch.empty(max(tokens, 1), dtype=torch.float64, device=dev)
-    flags = (LOSS_MEAN if mean else 0) | (LOSS_ADD if add else 0) | (LOSS_F32 if out.dtype == torch.float32 else 0)
-    _zo._launch("zo_token_loss", _zo._index(dev), _lib().zo_token_loss, logits.data_ptr(), _stride(logits, 0), tokens, vocab,
-                DTYPE_CODE[logits.dtype], targets.data_ptr(), INDEX_BYTES[targets.dtype], flags, out.data_ptr(),
-                nll.data_ptr() if with_nll else None, work.data_ptr(), work.numel() * 8)
+        out = _empty(1, dtype=dtype, device=logits.device)
+    single = out.dtype is torch.float32
+    if not ((single or out.dtype is torch.float64) and out.get_device() == idx and out.shape == (1,)):
+        _flat(out, "out", (torch.float64, torch.float32), logits.device, n=1)
+    nll = _empty(tokens, dtype=torch.float32, device=logits.device) if with_nll else None
+    work = _empty(tokens or 1, dtype=torch.float64, device=logits.device)
+    flags = (LOSS_MEAN if mean else 0) | (LOSS_ADD if add else 0) | (LOSS_F32 if single else 0)
+    block = _LOSS.pack(logits.data_ptr(), strides[0] if tokens > 1 else 0, tokens, vocab, DTYPE_CODE[logits.dtype],
+                       targets.data_ptr(), INDEX_BYTES[kind], flags, out.data_ptr(), nll.data_ptr() if with_nll else 0,
+                       work.data_ptr(), 8 * (tokens or 1))
+    _zo._launch("zo_token_loss", idx, _lib().zo_internal_token_loss, block)
     return (out, nll) if with_nll else out
