@@ -2,7 +2,7 @@
 // cluster's CTAs and their warps split a sequence, and how they join.
 //
 // A cluster of CTAs takes one sequence and key-value head. The keys go in tiles
-// of 16 to the cluster's warps in turn, so that warps differ by one tile at
+// of 16 or 32 to the cluster's warps in turn, so that warps differ by one tile at
 // most; a warp keeps a running maximum, sum and output for each of its query
 // heads and shares nothing with the others until its last key. Then a CTA joins
 // its warps in shared memory and the cluster its CTAs over distributed shared
@@ -14,12 +14,13 @@
 
 namespace zo {
 
-constexpr int kDecodeKeys = 16;  // keys of a warp's tile
+constexpr int kMaxCluster = 16;
 
 template <int HB>
-struct DecodeJoin {  // a CTA's statistics, read by its peers
+struct DecodeJoin {  // a CTA's statistics, read by its peers; and what it makes of theirs
   float top[HB], total[HB];
   int bad;
+  float scale[kMaxCluster][HB], over[HB], lse[HB];
 };
 
 struct DecodePlace {
@@ -48,7 +49,8 @@ __device__ __forceinline__ DecodePlace decode_place(const DecodeParams& p, uint3
 // the table names no page of the cache (bad).
 __device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePlace& w, int64_t j, int& bad) {
   if (j >= w.len) return make_int2(-1, 0);
-  const uint32_t at = static_cast<uint32_t>(j), page = at / static_cast<uint32_t>(p.page_size);
+  const uint32_t at = static_cast<uint32_t>(j);
+  const uint32_t page = p.page_shift >= 0 ? at >> p.page_shift : at / static_cast<uint32_t>(p.page_size);
   const int id = p.pages[w.b * p.pages_stride + page];
   if (id < 0 || id >= p.n_pages) {
     bad = 1;
@@ -82,25 +84,40 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
   }
   const uint32_t ranks = cluster_size(), rank = cluster_rank();
   cluster_sync();
+  // a thread per head and CTA of the cluster: 16 lanes hold a head's CTAs
+  for (int i = tid; i < HB * kMaxCluster; i += kWarps * 32) {
+    const int h = i / kMaxCluster, r = i % kMaxCluster;
+    const bool in = r < static_cast<int>(ranks);
+    const float mine = in ? peer_load(peer_address(&join.top[h], r)) : -kInf;
+    const float part = in ? peer_load(peer_address(&join.total[h], r)) : 0.0f;
+    bool bad = in && __float_as_int(peer_load(peer_address(&join.bad, r))) != 0;
+    float top = mine;
+#pragma unroll
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float scale = top == -kInf ? 0.0f : exp2_approx(mine - top);
+    float total = part * scale;
+    if (part != part) total = part;  // a NaN where every score is one
+#pragma unroll
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad);
+    bad = (bads >> (tid & 16) & 0xFFFFu) != 0;
+    join.scale[r][h] = scale;
+    if (r == 0) {
+      join.over[h] = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
+      join.lse[h] = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+    }
+  }
+  __syncthreads();
   T* out = static_cast<T*>(p.out) + w.b * p.out_token;
   for (int i = rank * (kWarps * 32) + tid; i < w.heads * DP; i += ranks * (kWarps * 32)) {
     const int h = i / DP, d = i - h * DP;
-    float top = -kInf, x = 0.0f, total = 0.0f;
-    bool bad = false;
-    for (uint32_t r = 0; r < ranks; ++r) {
-      top = fmaxf(top, peer_load(peer_address(&join.top[h], r)));
-      bad = bad || __float_as_int(peer_load(peer_address(&join.bad, r))) != 0;
-    }
-    for (uint32_t r = 0; r < ranks; ++r) {
-      const float part = peer_load(peer_address(&join.top[h], r));
-      const float scale = top == -kInf ? 0.0f : exp2_approx(part - top);
-      total = fmaf(peer_load(peer_address(&join.total[h], r)), scale, total);
-      x = fmaf(peer_load(peer_address(outs + i, r)), scale, x);
-    }
+    float x = 0.0f;
+#pragma unroll 4
+    for (uint32_t r = 0; r < ranks; ++r) x = fmaf(peer_load(peer_address(outs + i, r)), join.scale[r][h], x);
     const int head = w.head0 + h;
-    if (d < p.dim) out[head * p.out_head + d] = narrow<T>(bad ? NAN : total == 0.0f ? 0.0f : x / total);
-    if (d == 0 && p.lse != nullptr)
-      p.lse[static_cast<int64_t>(w.b) * p.heads + head] = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+    const float over = join.over[h];
+    if (d < p.dim) out[head * p.out_head + d] = narrow<T>(over == 0.0f ? 0.0f : x * over);
+    if (d == 0 && p.lse != nullptr) p.lse[static_cast<int64_t>(w.b) * p.heads + head] = join.lse[h];
   }
   cluster_sync();  // no CTA leaves before its part is read
 }
@@ -109,7 +126,7 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
 // than `least` keys of the longest sequence that the page table can hold.
 inline int decode_cluster(int64_t items, int64_t longest, int sms, int per_sm, int64_t least) {
   int c = 1;
-  while (c < 16 && items * c < static_cast<int64_t>(sms) * per_sm && longest >= 2 * c * least) c *= 2;
+  while (c < kMaxCluster && items * c < static_cast<int64_t>(sms) * per_sm && longest >= 2 * c * least) c *= 2;
   return c;
 }
 

@@ -11,9 +11,11 @@ constexpr float kSlack = 8.0f;  // log2: how far scores may pass the reference b
 
 template <int DP, int HB>
 struct Tiles {
-  static constexpr int kStages = 3;
+  static constexpr int kBlocksOfKeys = DP == 64 ? 2 : 1;  // of 16, in a tile
+  static constexpr int kKeys = 16 * kBlocksOfKeys;
+  static constexpr int kStages = 2;
   static constexpr int kRow = DP * 2;                      // bytes of a key
-  static constexpr int kStage = 2 * kDecodeKeys * kRow;    // keys, then values
+  static constexpr int kStage = 2 * kKeys * kRow;      // keys, then values
   static constexpr int kWarp = kStages * kStage;
   static constexpr int kBytes = kWarps * kWarp + 2 * kWarps * HB * 4;
   static_assert(HB * DP * 4 <= kWarp, "a warp's output takes its tiles' place");
@@ -33,29 +35,35 @@ __device__ __forceinline__ void load4_transposed(uint32_t (&r)[4], uint32_t at) 
 }
 
 template <typename T>
-__device__ __forceinline__ void mma16816(float& c0, float& c1, float& c2, float& c3, uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (__is_same(T, __nv_bfloat16))
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c0), "+f"(c1), "+f"(c2), "+f"(c3)
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c0), "+f"(c1), "+f"(c2), "+f"(c3)
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A warp's tiles of 16 keys come by cp.async, two ahead of the one in use, into
-// its own shared memory, 16-byte vectors swizzled by row. Scores: m16n8k16 with
-// the query heads as the 16 rows (8 of them zeros where HB is 8, and their
-// halves of the accumulators are not kept), which leaves the weights in the
-// layout of the next product's left operand. The 16 x 16 products are far from
-// what bounds this: the cache is read once, from HBM. (A 128-row tcgen05 tile
-// would be empty but for `group` rows.)
+// An 8 x 8 matrix of 16-bit values, a row's pair per thread, transposed within the warp.
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// A warp's tiles of 16 keys come by cp.async into its own shared memory, the
+// next one on its way, 16-byte vectors swizzled by row. The keys are the 16 rows
+// of m16n8k16 and 8 query heads its columns (with the heads as rows, half the
+// products would be of zeros for groups of up to 8): S^T = K Q^T, then
+// O^T += V^T P^T, for which the weights are transposed by movmatrix. (A 128-row
+// tcgen05 tile would be empty but for the group's columns.) Bound by HBM's
+// latency and the chain of a tile, so many warps: three CTAs per SM.
 template <typename T, int DP, int HB>
-__global__ void __launch_bounds__(kWarps * 32) decode_mma_kernel(const __grid_constant__ DecodeParams p) {
+__global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) decode_mma_kernel(const __grid_constant__ DecodeParams p) {
   using L = Tiles<DP, HB>;
-  constexpr int kVectors = DP / 8, kHalves = HB / 8;  // 16-byte vectors of a key; rows of a thread
+  constexpr int kVectors = DP / 8, kBlocks = HB / 8, kDeep = L::kBlocksOfKeys;  // a key's 16-byte vectors; blocks of 8 heads
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ DecodeJoin<HB> join;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -68,154 +76,176 @@ __global__ void __launch_bounds__(kWarps * 32) decode_mma_kernel(const __grid_co
 
   const T* kc = static_cast<const T*>(p.k) + w.g * p.k_head;
   const T* vc = static_cast<const T*>(p.v) + w.g * p.v_head;
-  const int64_t tiles_in = (w.len + kDecodeKeys - 1) / kDecodeKeys;
+  const int64_t tiles_in = (w.len + L::kKeys - 1) / L::kKeys;
   const int64_t step = static_cast<int64_t>(ranks) * kWarps;
   const int64_t first = static_cast<int64_t>(cluster_rank()) * kWarps + warp;
+  const int len = static_cast<int>(w.len);
   int bad = 0;
-  const auto find = [&](int64_t tile) { return decode_key(p, w, tile * kDecodeKeys + (lane & 15), bad); };
-  const auto fetch = [&](int2 key, int stage) {
+  // A lane finds the place of one of a tile's keys, in bytes from where its vectors start (-1: no key), long before it is
+  // needed; the caches mostly have the same strides.
+  const bool same = p.k_page == p.v_page && p.k_token == p.v_token;
+  struct Place {
+    int64_t k, v;
+  };
+  const auto find = [&](int64_t tile) {
+    const int2 key = decode_key(p, w, tile * L::kKeys + lane % L::kKeys, bad);
+    Place at = {-1, -1};
+    if (key.x >= 0) {
+      at.k = (key.x * p.k_page + key.y * p.k_token) * 2;
+      at.v = same ? at.k : (key.x * p.v_page + key.y * p.v_token) * 2;
+    }
+    return at;
+  };
+  const int vector = lane % kVectors;
+  const char* kl = reinterpret_cast<const char*>(kc + (vector * 8 < p.dim ? vector * 8 : 0));
+  const char* vl = reinterpret_cast<const char*>(vc + (vector * 8 < p.dim ? vector * 8 : 0));
+  const int bytes = vector * 8 < p.dim ? 16 : 0;  // of a vector; the rest is filled with zeros
+  const auto fetch = [&](const Place& place, int stage) {
     constexpr int kRowsAtOnce = 32 / kVectors > 0 ? 32 / kVectors : 1;
-    const uint32_t ks = tiles + stage * L::kStage, vs = ks + kDecodeKeys * L::kRow;
-    const int c = lane % kVectors;
+    const uint32_t ks = tiles + stage * L::kStage, vs = ks + L::kKeys * L::kRow;
 #pragma unroll
-    for (int i = 0; i < kDecodeKeys / kRowsAtOnce; ++i) {
+    for (int i = 0; i < L::kKeys / kRowsAtOnce; ++i) {
       const int r = i * kRowsAtOnce + lane / kVectors;
-      const int page = __shfl_sync(0xFFFFFFFFu, key.x, r), row = __shfl_sync(0xFFFFFFFFu, key.y, r);
-      const int n = page >= 0 && c * 8 < p.dim ? 16 : 0;  // the rest is filled with zeros
-      const uint32_t at = r * L::kRow + ((c ^ (r & 7)) << 4);
-      const void* k = n ? static_cast<const void*>(kc + page * p.k_page + row * p.k_token + c * 8) : p.k;
-      const void* v = n ? static_cast<const void*>(vc + page * p.v_page + row * p.v_token + c * 8) : p.v;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + at), "l"(k), "r"(n) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + at), "l"(v), "r"(n) : "memory");
+      const int64_t k = __shfl_sync(0xFFFFFFFFu, place.k, r);
+      const int64_t v = same ? k : __shfl_sync(0xFFFFFFFFu, place.v, r);
+      const uint32_t at = r * L::kRow + ((vector ^ (r & 7)) << 4);
+      const int n = k >= 0 ? bytes : 0;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + at), "l"(kl + (k >= 0 ? k : 0)), "r"(n)
+                   : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + at), "l"(vl + (k >= 0 ? v : 0)), "r"(n)
+                   : "memory");
     }
   };
 
-  int2 ahead = find(first);
+  Place ahead = find(first);
 #pragma unroll
   for (int s = 0; s < L::kStages - 1; ++s) {
-    const int2 key = ahead;
+    const Place place = ahead;
     ahead = find(first + (s + 1) * step);
-    if (first + s * step < tiles_in) fetch(key, s);
+    if (first + s * step < tiles_in) fetch(place, s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  // the queries as left operands: rows lane / 4 and lane / 4 + 8, columns 2 (lane mod 4) and 8 more
-  uint32_t qa[DP / 16][2 * kHalves];
+  // the queries as right operands: head lane / 4 (and 8 more), elements 2 (lane mod 4) and 8 more
+  uint32_t qb[kBlocks][DP / 16][2];
 #pragma unroll
-  for (int s = 0; s < DP / 16; ++s)
+  for (int m = 0; m < kBlocks; ++m)
 #pragma unroll
-    for (int r = 0; r < kHalves; ++r)
+    for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int h = lane / 4 + 8 * r, d = s * 16 + c * 8 + lane % 4 * 2;
-        qa[s][c * kHalves + r] = 0;
+        const int h = lane / 4 + 8 * m, d = s * 16 + c * 8 + lane % 4 * 2;
+        qb[m][s][c] = 0;
         if (h < w.heads && d < p.dim) {
-          const T* q = static_cast<const T*>(p.q) + w.b * p.q_token + (w.head0 + h) * p.q_head + d;
-          uint16_t e[2];
-          e[0] = *reinterpret_cast<const uint16_t*>(q);
-          e[1] = *reinterpret_cast<const uint16_t*>(q + 1);
-          qa[s][c * kHalves + r] = e[0] | static_cast<uint32_t>(e[1]) << 16;
+          const uint16_t* q = reinterpret_cast<const uint16_t*>(static_cast<const T*>(p.q) + w.b * p.q_token +
+                                                                (w.head0 + h) * p.q_head + d);
+          qb[m][s][c] = q[0] | static_cast<uint32_t>(q[1]) << 16;
         }
       }
   const float scale2 = p.softcap > 0.0f ? p.scale / p.softcap : p.scale * kLog2e, cap2 = p.softcap * kLog2e;
-  float slope2[kHalves], base[kHalves], total[kHalves], acc[DP / 8][2 * kHalves];
+  // a thread's two heads of each block of 8: 2 (lane mod 4) and the next
+  float slope2[kBlocks][2], base[kBlocks][2], total[kBlocks][2], acc[kBlocks][DP / 16][4];
 #pragma unroll
-  for (int r = 0; r < kHalves; ++r) {
-    const int h = lane / 4 + 8 * r;
-    slope2[r] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] * kLog2e : 0.0f;
-    base[r] = -kInf;
-    total[r] = 0.0f;
-  }
+  for (int m = 0; m < kBlocks; ++m)
 #pragma unroll
-  for (int n = 0; n < DP / 8; ++n)
+    for (int c = 0; c < 2; ++c) {
+      const int h = lane % 4 * 2 + c + 8 * m;
+      slope2[m][c] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] * kLog2e : 0.0f;
+      base[m][c] = -kInf;
+      total[m][c] = 0.0f;
 #pragma unroll
-    for (int c = 0; c < 2 * kHalves; ++c) acc[n][c] = 0.0f;
+      for (int n = 0; n < DP / 16; ++n) acc[m][n][2 * c] = acc[m][n][2 * c + 1] = 0.0f;
+    }
 
   int stage = 0;
   for (int64_t tile = first; tile < tiles_in; tile += step) {
     {
-      const int2 key = ahead;
+      const Place place = ahead;
       const int64_t next = tile + (L::kStages - 1) * step;
       ahead = find(next + step);
-      if (next < tiles_in) fetch(key, stage == 0 ? L::kStages - 1 : stage - 1);
+      if (next < tiles_in) fetch(place, stage == 0 ? L::kStages - 1 : stage - 1);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 1) : "memory");
     __syncwarp();
-    const uint32_t ks = tiles + stage * L::kStage, vs = ks + kDecodeKeys * L::kRow;
-    float s[2][4] = {};  // keys 0-7 and 8-15; a thread's two of each row
-    {
-      const int row = (lane & 7) + (lane >> 4 << 3);
+    const uint32_t ks = tiles + stage * L::kStage, vs = ks + L::kKeys * L::kRow;
+    // scores: keys lane / 4 and 8 more of each block of 16, the thread's heads; even and odd steps apart
+    float s[kBlocks][kDeep][2][4] = {};
+#pragma unroll
+    for (int b = 0; b < kDeep; ++b) {
+      const int row = b * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d) {
-        uint32_t b[4];
-        load4(b, ks + row * L::kRow + (((2 * d + (lane >> 3 & 1)) ^ (row & 7)) << 4));
+        uint32_t a[4];
+        load4(a, ks + row * L::kRow + (((2 * d + (lane >> 4)) ^ (row & 7)) << 4));
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-          mma16816<T>(s[n][0], s[n][1], s[n][2], s[n][3], qa[d][0], kHalves == 2 ? qa[d][1] : 0u, qa[d][kHalves],
-                      kHalves == 2 ? qa[d][3] : 0u, b[2 * n], b[2 * n + 1]);
+        for (int m = 0; m < kBlocks; ++m) mma16816<T>(s[m][b][d & 1], a, qb[m][d][0], qb[m][d][1]);
       }
     }
-    const int64_t j0 = tile * kDecodeKeys + lane % 4 * 2;
-    float back[kHalves];
+    const int j = static_cast<int>(tile) * L::kKeys + lane / 4;
+    const float away = static_cast<float>(len - 1 - j);
+    const bool part = tile == tiles_in - 1;  // a tile that may pass the length
+    float back[kBlocks][2];
     bool moved = false;
+    uint32_t weight[kBlocks][kDeep][2];
 #pragma unroll
-    for (int r = 0; r < kHalves; ++r) {
-      float most = -kInf;
+    for (int m = 0; m < kBlocks; ++m) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int c = 0; c < 2; ++c) {
+        float x[kDeep][2];
+        float most = -kInf;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int64_t j = j0 + n * 8 + c;
-          float x = s[n][2 * r + c];
-          x = p.softcap > 0.0f ? capped(x, scale2, cap2) : x * scale2;
-          x = j < w.len ? x - slope2[r] * static_cast<float>(w.len - 1 - j) : -kInf;
-          s[n][2 * r + c] = x;
-          most = fmaxf(most, x);
+        for (int b = 0; b < kDeep; ++b)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int key = j + b * 16 + r * 8;
+            float y = s[m][b][0][2 * r + c] + s[m][b][1][2 * r + c];
+            y = p.softcap > 0.0f ? capped(y, scale2, cap2) : y * scale2;
+            if (p.slopes != nullptr) y -= slope2[m][c] * (away - (b * 16 + r * 8));
+            if (part && key >= len) y = -kInf;
+            x[b][r] = y;
+            most = fmaxf(most, y);
+          }
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 4));
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 8));
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 16));
+        back[m][c] = 1.0f;
+        if (most > base[m][c] + kSlack || (base[m][c] == -kInf && most > -kInf)) {
+          back[m][c] = exp2_approx(base[m][c] - most);
+          base[m][c] = most;
+          moved = true;
         }
-      most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-      back[r] = 1.0f;
-      if (most > base[r] + kSlack || (base[r] == -kInf && most > -kInf)) {
-        back[r] = exp2_approx(base[r] - most);
-        base[r] = most;
-        moved = true;
+        const float shift = base[m][c] == -kInf ? 0.0f : base[m][c];
+        total[m][c] *= back[m][c];
+#pragma unroll
+        for (int b = 0; b < kDeep; ++b)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            s[m][b][r][c] = exp2_approx(x[b][r] - shift);
+            total[m][c] += s[m][b][r][c];
+          }
       }
-      total[r] *= back[r];
+#pragma unroll
+      for (int b = 0; b < kDeep; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) weight[m][b][r] = transposed(narrow2<T>(s[m][b][r][0], s[m][b][r][1]));
     }
     if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
-      for (int n = 0; n < DP / 8; ++n)
+      for (int m = 0; m < kBlocks; ++m)
 #pragma unroll
-        for (int r = 0; r < kHalves; ++r) {
-          acc[n][2 * r] *= back[r];
-          acc[n][2 * r + 1] *= back[r];
-        }
+        for (int n = 0; n < DP / 16; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[m][n][c] *= back[m][c & 1];
     }
-    uint32_t weight[2][kHalves];
 #pragma unroll
-    for (int r = 0; r < kHalves; ++r) {
-      const float shift = base[r] == -kInf ? 0.0f : base[r];
+    for (int b = 0; b < kDeep; ++b) {
+      const int row = b * 16 + (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const float a = exp2_approx(s[n][2 * r] - shift), b = exp2_approx(s[n][2 * r + 1] - shift);
-        total[r] += a + b;
-        weight[n][r] = narrow2<T>(a, b);
-      }
-    }
-    {
-      const int row = (lane & 7) + (lane >> 3 & 1) * 8;
+      for (int n = 0; n < DP / 16; ++n) {
+        uint32_t a[4];
+        load4_transposed(a, vs + row * L::kRow + (((2 * n + (lane >> 3 & 1)) ^ (row & 7)) << 4));
 #pragma unroll
-      for (int d = 0; d < DP / 16; ++d) {
-        uint32_t b[4];
-        load4_transposed(b, vs + row * L::kRow + (((2 * d + (lane >> 4)) ^ (row & 7)) << 4));
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          float none0 = 0.0f, none1 = 0.0f;
-          float* a = acc[2 * d + n];
-          mma16816<T>(a[0], a[1], kHalves == 2 ? a[2 * (kHalves - 1)] : none0, kHalves == 2 ? a[2 * kHalves - 1] : none1,
-                      weight[0][0], kHalves == 2 ? weight[0][kHalves - 1] : 0u, weight[1][0],
-                      kHalves == 2 ? weight[1][kHalves - 1] : 0u, b[2 * n], b[2 * n + 1]);
-        }
+        for (int m = 0; m < kBlocks; ++m) mma16816<T>(acc[m][n], a, weight[m][b][0], weight[m][b][1]);
       }
     }
     __syncwarp();  // the stage may be filled again
@@ -223,24 +253,28 @@ __global__ void __launch_bounds__(kWarps * 32) decode_mma_kernel(const __grid_co
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
-  for (int r = 0; r < kHalves; ++r) {
-    float sum = total[r];
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-    if (lane % 4 == 0) {
-      tops[warp * HB + lane / 4 + 8 * r] = base[r];
-      totals[warp * HB + lane / 4 + 8 * r] = sum;
+  for (int m = 0; m < kBlocks; ++m)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float sum = total[m][c];
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 4);
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+      if (lane < 4) {
+        tops[warp * HB + lane * 2 + c + 8 * m] = base[m][c];
+        totals[warp * HB + lane * 2 + c + 8 * m] = sum;
+      }
     }
-  }
   __syncthreads();  // join.bad is set, and every warp is done with its tiles: the outputs take their place
   if (bad) join.bad = 1;
   float* outs = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int n = 0; n < DP / 8; ++n)
+  for (int m = 0; m < kBlocks; ++m)
 #pragma unroll
-    for (int r = 0; r < kHalves; ++r)
-      *reinterpret_cast<float2*>(outs + (warp * HB + lane / 4 + 8 * r) * DP + n * 8 + lane % 4 * 2) =
-          make_float2(acc[n][2 * r], acc[n][2 * r + 1]);
+    for (int n = 0; n < DP / 16; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        outs[(warp * HB + lane % 4 * 2 + (c & 1) + 8 * m) * DP + n * 16 + lane / 4 + c / 2 * 8] = acc[m][n][c];
   decode_join<T, HB, DP, kWarps>(p, w, outs, tops, totals, join);
 }
 
@@ -248,7 +282,9 @@ template <typename T, int DP, int HB>
 cudaError_t launch_size(DecodeParams p, int64_t batch, int sms, cudaStream_t stream) {
   p.head_blocks = (p.group + HB - 1) / HB;
   const int64_t items = batch * p.kv_heads * p.head_blocks;
-  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 4, 128);
+  // CTAs per SM: 4 leave long sequences in too few (48 of up to 16384 keys 293 us, with 6 or 8 248); 8 split short ones
+  // for their joins' sake (16 of up to 4001 keys, 32 heads: 67 us, with 4 or 6 57)
+  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6, 128);
   return launch_decode(decode_mma_kernel<T, DP, HB>, p, items, c, kWarps * 32, Tiles<DP, HB>::kBytes, stream);
 }
 

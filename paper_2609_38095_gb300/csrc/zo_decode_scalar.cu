@@ -6,7 +6,8 @@ namespace zo {
 
 namespace {
 
-constexpr int kBlockHeads = 8;  // query heads of a cluster
+constexpr int kBlockHeads = 8;   // query heads of a cluster
+constexpr int kDecodeKeys = 16;  // keys of a warp's tile
 
 template <int DP>
 struct Scalar {

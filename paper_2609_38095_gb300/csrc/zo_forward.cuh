@@ -55,6 +55,7 @@ struct DecodeParams {
   int64_t pages_stride, max_pages, n_pages;
   const int32_t *pages, *lengths;
   int32_t heads, kv_heads, group, dim, page_size;
+  int32_t page_shift;   // log2 of page_size, -1 where it is no power of two
   int32_t head_blocks;  // CTAs (or clusters) per key-value head, by blocks of query heads
   float scale, softcap;
   const float* slopes;

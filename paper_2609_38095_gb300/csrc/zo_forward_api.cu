@@ -190,6 +190,7 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
   p.pages_stride = pages_stride, p.max_pages = max_pages, p.n_pages = n_pages;
   p.pages = pages, p.lengths = lengths;
   p.heads = heads, p.kv_heads = kv_heads, p.group = heads / kv_heads, p.dim = head_dim, p.page_size = page_size;
+  p.page_shift = (page_size & (page_size - 1)) == 0 ? __builtin_ctz(page_size) : -1;
   p.scale = scale, p.softcap = softcap;
   p.slopes = slopes;
   p.lse = lse;
