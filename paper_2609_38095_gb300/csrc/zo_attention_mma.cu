@@ -32,24 +32,22 @@ bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int head
 
 namespace {
 
-constexpr int kRows = 128;     // query rows of a slot, keys of a tile
+constexpr int kRows = 128;           // query rows of a slot, keys of a load
+constexpr int kKeys = 64;            // keys of a step
 constexpr int kMmaThreads = 384;
-// Registers of a softmax thread (a row's 128 scores and the rest) and of the others: 2 x 128 threads and 128, no more in
-// all than the 168 each that 384 threads are launched with.
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
-static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "the shares exceed the launch's registers");
+constexpr int kSoftmaxWarps = 8;
 constexpr int kChunk = kRows * 128;  // bytes of 64 elements of 128 rows
 constexpr float kSlack = 8.0f;       // log2: how far scores may pass the reference before the output is rescaled
 
 template <int D>
 struct Plan {
-  static constexpr int kTile = D / 64 * kChunk;            // bytes of a tile of queries, keys or values
-  static constexpr int kStages = D == 128 ? 5 : 8;         // tiles of keys and values in turn
+  static constexpr int kTile = D / 64 * kChunk;     // bytes of a tile of queries, keys or values
+  static constexpr int kStages = D == 128 ? 5 : 8;  // tiles of keys and values in turn
   static constexpr int kBytes = (2 + kStages) * kTile + 1024;
 };
 
 struct MmaShared {
-  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2], p_full[2], o_full[2], drain;
+  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2][2], p_full[2][2], o_done[2], drain;
   int lo[2], hi[2];
   uint32_t tmem;
   int dead;
@@ -57,23 +55,29 @@ struct MmaShared {
 
 // A CTA has two slots of 128 query rows: two heads that share their keys (the
 // same rows, the same spans) where a group has an even number of them, else two
-// tiles of rows of one head. Keys and values go by in tiles of 128; while one
-// slot's scores pass through the softmax, the tensor cores work for the other.
+// tiles of rows of one head. Keys and values come in tiles of 128 and go through
+// the products in steps of 64.
 //
 //   warps 0-3, 4-7   softmax of slot 0, 1: a thread has a row
 //   warp 8           the matrix products, one thread
-//   warp 9           TMA loads, one thread (warps 10 and 11 complete their warpgroup)
+//   warp 9           TMA loads, one thread (10 and 11 have nothing to do)
 //
-// Tensor memory (512 columns): scores of slots 0 and 1, 128 each, the weights in
-// 16 bits over the first half of their scores' columns; outputs from column 256
-// on. S = Q K^T has both operands in shared memory; O += P V takes P from tensor
-// memory and V as TMA left it, along N. A slot's next scores are issued behind
-// the product that reads its weights, so they may take their place.
+// Tensor memory (512 columns): a slot's scores of two steps, 64 columns each, the
+// weights of a step in 16 bits over the first half of its scores; outputs from
+// column 256 on. S = Q K^T has both operands in shared memory; O += P V takes P
+// from tensor memory and V as TMA left it, along N. Step j's scores are issued
+// before step j - 1's O, so a softmax has its next scores when it is done; they
+// take the place of step j - 2's weights, whose product was issued before them.
+//
+// What bounds it: the products with 64 columns read 6 KB of shared memory in the
+// 32 cycles that they would take, so a step is 384 + 256 cycles per slot, 2560 for
+// 128 keys and both slots (with 128 columns 2048, but then there is no tensor
+// memory for a second step, and a slot's softmax, 1600 cycles and two waits of
+// 400, is in series with its own products: 8192 tokens of 32 heads took 460 us).
 //
 // The output is rescaled only when a row's maximum has passed the reference that
-// its weights are relative to by 2^8, which seldom happens after the first tiles:
-// weights up to 256 lose nothing in 16 bits and their sum is fp32. At that point
-// the last product is done, because the scores were issued after it.
+// its weights are relative to by 2^8, which seldom happens after the first steps:
+// weights up to 256 lose nothing in 16 bits and their sum is fp32.
 template <typename T, int D, bool kCap, bool kBias>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_mma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -85,7 +89,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __shared__ MmaShared sh;
   uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // queries of both slots, then the stages
   uint8_t* stages = tiles + 2 * L::kTile;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = static_cast<int>(uniform(tid >> 5)), lane = tid & 31;
   const int per = by_heads ? p.heads / 2 : p.heads;  // CTAs per tile of rows; the longest causal rows come first
   const int item = blockIdx.x % per, block = gridDim.x / per - 1 - blockIdx.x / per;
   const int head0 = by_heads ? item * 2 : item, kv_head = head0 / p.group;
@@ -98,9 +102,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       mbar_init(&sh.kv_empty[i], 1);
     }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&sh.s_full[s], 1);
-      mbar_init(&sh.p_full[s], 4);
-      mbar_init(&sh.o_full[s], 1);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&sh.s_full[s][b], 1);
+        mbar_init(&sh.p_full[s][b], 4);
+      }
+      mbar_init(&sh.o_done[s], 1);
       sh.lo[s] = 0x7FFFFFFF;
       sh.hi[s] = 0;
     }
@@ -108,12 +114,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) tmem_alloc(&sh.tmem, 512);
+  if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, 512);
   __syncthreads();
   int64_t row = 0;
   int lo = 0, hi = 0, self = 0;
   const int slot = warp >> 2;
-  if (warp < 8) {
+  if (warp < kSoftmaxWarps) {
     row = (by_heads ? block : 2 * static_cast<int64_t>(block) + slot) * kRows + (tid & 127);
     if (row < p.q_tokens) {
       lo = max(p.spans[row], 0);
@@ -131,29 +137,29 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const uint32_t tmem = sh.tmem;
-  const int begin = min(sh.lo[0], sh.lo[1]), stop = max(sh.hi[0], sh.hi[1]);
-  const int n = stop > begin ? (stop - begin + kRows - 1) / kRows : 0;  // tiles of keys
+  const uint32_t tmem = uniform(sh.tmem);
+  const int begin = static_cast<int>(uniform(min(sh.lo[0], sh.lo[1])));
+  const int stop = static_cast<int>(uniform(max(sh.hi[0], sh.hi[1])));
+  const int n = stop > begin ? (stop - begin + kKeys - 1) / kKeys : 0;  // steps
   int from[2], to[2];                                                   // those that a slot sees
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     from[s] = to[s] = 0;
     if (sh.hi[s] > sh.lo[s]) {
-      from[s] = (sh.lo[s] - begin) / kRows;
-      to[s] = (sh.hi[s] - begin + kRows - 1) / kRows;
+      from[s] = static_cast<int>(uniform((sh.lo[s] - begin) / kKeys));
+      to[s] = static_cast<int>(uniform((sh.hi[s] - begin + kKeys - 1) / kKeys));
     }
   }
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 9 && lane == 0 && n > 0) {
+  if (warp == kSoftmaxWarps + 1) {
+    if (lane == 0 && n > 0) {
       mbar_expect(&sh.q_full, 2 * L::kTile);
       for (int s = 0; s < 2; ++s)
         for (int c = 0; c < D / 64; ++c)
           tma_load_3d(tiles + s * L::kTile + c * kChunk, &q_map, c * 64, by_heads ? head0 + s : head0,
                       (by_heads ? block : 2 * block + s) * kRows, &sh.q_full);
       int issued = 0;
-      for (int i = 0; i < 2 * n; ++i) {
+      for (int i = 0; i < (n + 1) / 2 * 2; ++i) {  // keys 0, values 0, keys 1, ...
         const int stage = i % L::kStages;
         if (i >= L::kStages && !mbar_wait(&sh.kv_empty[stage], (i / L::kStages - 1) & 1, dead)) break;
         mbar_expect(&sh.kv_full[stage], L::kTile);
@@ -169,142 +175,146 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         while (!mbar_try(&sh.q_full, 0) && clock64() - start < kWaitCycles) {}
       }
     }
-    if (warp == 8) {
-      const uint32_t q0 = smem_address(tiles), kv0 = smem_address(stages);
-      constexpr uint32_t kScores = mma_desc(kBf16, kRows, false), kOutput = mma_desc(kBf16, D, true);
-      int waits[2] = {0, 0};  // of a slot's weights
-      bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
-      for (int j = 0; j <= n && n > 0 && alive; ++j) {
-        const int vi = 2 * j - 1, ki = 2 * j;  // places in the order of loads
-        if (j > 0) {
-          alive = mbar_wait_warp(&sh.kv_full[vi % L::kStages], (vi / L::kStages) & 1, dead);
+  } else if (warp == kSoftmaxWarps) {
+    const uint32_t at = uniform(smem_address(stages));
+    const uint64_t queries = operand_desc(uniform(smem_address(tiles)), 16, 1024);
+    const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, kChunk, 1024);
+    constexpr uint32_t kScores = mma_desc(kBf16, kKeys, false), kOutput = mma_desc(kBf16, D, true);
+    constexpr uint32_t kHalf = kKeys * 128;  // bytes from a tile's first 64 rows to its last
+    const auto after = [](int stage) { return stage + 1 == L::kStages ? 0 : stage + 1; };
+    // the stages in use of keys (0, 2, 4, ... in the order of loads) and of values (1, 3, 5, ...)
+    int k_stage = 0, v_stage = 1;
+    uint32_t k_parity = 0, v_parity = 0;
+    bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
+    for (int j = 0; j <= n && n > 0 && alive; ++j) {
+      if (j < n) {
+        if (j % 2 == 0) {
+          if (j > 0)
+            for (int i = 0; i < 2; ++i) k_parity ^= (k_stage = after(k_stage)) == 0;
+          alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
           if (!alive) break;
-          const int rest = stop - (begin + (j - 1) * kRows);
-          if (rest < kRows) {  // keys that no row sees: their weight is 0, and 0 times what is there has to be 0
-            uint8_t* v = stages + (vi % L::kStages) * L::kTile;
-            for (int i = lane; i < (kRows - rest) * 8 * (D / 64); i += 32) {
-              const int c = i / ((kRows - rest) * 8), at = i - c * (kRows - rest) * 8;
-              *reinterpret_cast<uint4*>(v + c * kChunk + (rest + at / 8) * 128 + at % 8 * 16) = make_uint4(0, 0, 0, 0);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-          }
         }
-        bool k_here = false;
-  #pragma unroll
+        const uint64_t k = keys + (static_cast<uint32_t>(k_stage) * L::kTile + j % 2 * kHalf) / 16;
+        tmem_fence_after();
+#pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const uint32_t scores = tmem + s * 128, out = tmem + 256 + s * D;
-          if (j > from[s] && j <= to[s]) {
-            alive = mbar_wait_warp(&sh.p_full[s], waits[s]++ & 1, dead);
-            if (!alive) break;
-            tmem_fence_after();
-            if (lane == 0) {
-              const uint32_t v = kv0 + (vi % L::kStages) * L::kTile;
-  #pragma unroll
-              for (int k = 0; k < kRows / 16; ++k)
-                mma_ts(out, scores + k * 8, operand_desc(v + k * 2048, kChunk, 1024), kOutput, j - 1 > from[s] || k > 0);
-              if (j == to[s]) mma_commit(&sh.o_full[s]);
-            }
-          }
-          if (j >= from[s] && j < to[s]) {
-            if (!k_here) {
-              alive = mbar_wait_warp(&sh.kv_full[ki % L::kStages], (ki / L::kStages) & 1, dead);
-              if (!alive) break;
-              k_here = true;
-            }
-            tmem_fence_after();
-            if (lane == 0) {
-              const uint32_t q = q0 + s * L::kTile, k = kv0 + (ki % L::kStages) * L::kTile;
-  #pragma unroll
-              for (int d = 0; d < D / 16; ++d)
-                mma_ss(scores, operand_desc(q + d / 4 * kChunk + d % 4 * 32, 16, 1024),
-                       operand_desc(k + d / 4 * kChunk + d % 4 * 32, 16, 1024), kScores, d > 0);
-              mma_commit(&sh.s_full[s]);
-            }
+          if (j < from[s] || j >= to[s]) continue;
+          const int b = (j - from[s]) & 1;
+          const uint32_t scores = tmem + s * 128 + b * kKeys;
+          const uint64_t q = queries + s * (L::kTile / 16);
+          if (elect_one()) {
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+              mma_ss(scores, q + (d / 4 * kChunk + d % 4 * 32) / 16, k + (d / 4 * kChunk + d % 4 * 32) / 16, kScores, d > 0);
+            mma_commit(&sh.s_full[s][b]);
           }
         }
+        if ((j % 2 == 1 || j == n - 1) && elect_one()) mma_commit(&sh.kv_empty[k_stage]);
+      }
+      const int i = j - 1;
+      if (i < 0) continue;
+      if (i % 2 == 0) {
+        if (i > 0)
+          for (int c = 0; c < 2; ++c) v_parity ^= (v_stage = after(v_stage)) == 0;
+        alive = mbar_wait_warp(&sh.kv_full[v_stage], v_parity, dead);
         if (!alive) break;
-        if (j < n && !k_here) {  // no row of this tile's keys: pass it by
-          alive = mbar_wait_warp(&sh.kv_full[ki % L::kStages], (ki / L::kStages) & 1, dead);
-          if (!alive) break;
+        const int rest = stop - (begin + i * kKeys);
+        if (rest < kRows) {  // keys that no row sees: their weight is 0, and 0 times what is there has to be 0
+          uint8_t* v = stages + v_stage * L::kTile;
+          for (int e = lane; e < (kRows - rest) * 8 * (D / 64); e += 32) {
+            const int c = e / ((kRows - rest) * 8), r = e - c * (kRows - rest) * 8;
+            *reinterpret_cast<uint4*>(v + c * kChunk + (rest + r / 8) * 128 + r % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
         }
-        if (lane == 0) {
-          if (j > 0) mma_commit(&sh.kv_empty[vi % L::kStages]);
-          if (j < n) mma_commit(&sh.kv_empty[ki % L::kStages]);
+      }
+      const uint64_t v = values + (static_cast<uint32_t>(v_stage) * L::kTile + i % 2 * kHalf) / 16;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (i < from[s] || i >= to[s]) continue;
+        const int c = i - from[s], b = c & 1;
+        alive = mbar_wait_warp(&sh.p_full[s][b], c >> 1 & 1, dead);
+        if (!alive) break;
+        tmem_fence_after();
+        const uint32_t weights = tmem + s * 128 + b * kKeys, out = tmem + 256 + s * D;
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k) mma_ts(out, weights + k * 8, v + k * (2048 / 16), kOutput, c > 0 || k > 0);
+          mma_commit(&sh.o_done[s]);
         }
-        __syncwarp();
       }
-      if (*dead && lane == 0) {
-        mma_commit(&sh.drain);
-        const long long start = clock64();
-        while (!mbar_try(&sh.drain, 0) && clock64() - start < kWaitCycles) {}
-      }
+      if (!alive) break;
+      if ((i % 2 == 1 || i == n - 1) && elect_one()) mma_commit(&sh.kv_empty[v_stage]);
       __syncwarp();
     }
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    if (*dead && elect_one()) {
+      mma_commit(&sh.drain);
+      const long long start = clock64();
+      while (!mbar_try(&sh.drain, 0) && clock64() - start < kWaitCycles) {}
+    }
+    __syncwarp();
+  } else if (warp < kSoftmaxWarps) {
     const int h = by_heads ? head0 + slot : head0;
-    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t scores = at + slot * 128, out = at + 256 + slot * D;
+    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + 256 + slot * D;
     const float scale2 = kCap ? p.scale / p.softcap : p.scale * kLog2e;
     const float cap2 = p.softcap * kLog2e, slope2 = kBias ? p.slopes[h] * kLog2e : 0.0f;
+    const int steps = to[slot] - from[slot];
     float base = -kInf, total = 0.0f;  // log2 of what the weights are relative to, and their sum
     bool alive = true;
-    for (int j = from[slot]; j < to[slot]; ++j) {
-      alive = mbar_wait_warp(&sh.s_full[slot], (j - from[slot]) & 1, dead);
+    for (int c = 0; c < steps; ++c) {
+      const int b = c & 1;
+      const uint32_t scores = at + slot * 128 + b * kKeys;
+      alive = mbar_wait_warp(&sh.s_full[slot][b], c >> 1 & 1, dead);
       if (!alive) break;
       tmem_fence_after();
-      uint32_t x[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_load32(x[c], scores + c * 32);
+      uint32_t x[2][32];
+      tmem_load32(x[0], scores);
+      tmem_load32(x[1], scores + 32);
       tmem_wait_ld(x[0]);
-#pragma unroll
-      for (int c = 1; c < 4; ++c) tie32(x[c]);
-      const int key0 = begin + j * kRows;
+      tie32(x[1]);
+      const int key0 = begin + (from[slot] + c) * kKeys;
       if (kCap || kBias) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float s = __uint_as_float(x[c][i]);
-            s = kCap ? capped(s, scale2, cap2) : s * scale2;
-            if (kBias) s -= slope2 * fabsf(static_cast<float>(self - (key0 + c * 32 + i)));
-            x[c][i] = __float_as_uint(s);
-          }
+        for (int e = 0; e < 64; ++e) {
+          float s = __uint_as_float(x[e / 32][e % 32]);
+          s = kCap ? capped(s, scale2, cap2) : s * scale2;
+          if (kBias) s -= slope2 * fabsf(static_cast<float>(self - (key0 + e)));
+          x[e / 32][e % 32] = __float_as_uint(s);
+        }
       }
-      if (!__all_sync(0xFFFFFFFFu, lo <= key0 && hi >= key0 + kRows)) {
+      if (!__all_sync(0xFFFFFFFFu, lo <= key0 && hi >= key0 + kKeys)) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int key = key0 + c * 32 + i;
-            if (key < lo || key >= hi) x[c][i] = __float_as_uint(-kInf);
-          }
+        for (int e = 0; e < 64; ++e)
+          if (key0 + e < lo || key0 + e >= hi) x[e / 32][e % 32] = __float_as_uint(-kInf);
       }
       float most[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        most[c] = __uint_as_float(x[c][0]);
+      for (int e = 0; e < 4; ++e) {
+        most[e] = __uint_as_float(x[e / 2][e % 2 * 16]);
 #pragma unroll
-        for (int i = 1; i < 32; ++i) most[c] = fmaxf(most[c], __uint_as_float(x[c][i]));
+        for (int i = 1; i < 16; ++i) most[e] = fmaxf(most[e], __uint_as_float(x[e / 2][e % 2 * 16 + i]));
       }
       float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
       if (!kCap && !kBias) top *= scale2;
       const bool moved = top > base + kSlack || (base == -kInf && top > -kInf);
       if (__any_sync(0xFFFFFFFFu, moved)) {
-        const float back = moved ? (base == -kInf ? 0.0f : exp2_approx(base - top)) : 1.0f;
+        const bool fresh = moved && base == -kInf;  // no weight yet: what is there may be anything times 0
+        const float back = !moved ? 1.0f : fresh ? 0.0f : exp2_approx(base - top);
         if (moved) base = top;
         total *= back;
-        if (j > from[slot]) {
-          const bool fresh = total == 0.0f;  // no weight yet: what is there may be anything times 0
+        if (c > 0) {
+          // the step before is in the output (the one before that is: these scores were issued behind it)
+          alive = mbar_wait_warp(&sh.o_done[slot], (c - 1) & 1, dead);
+          if (!alive) break;
+          tmem_fence_after();
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_load32(o, out + c * 32);
-            tmem_wait_ld(o);
+          for (int d = 0; d < D / 16; ++d) {
+            uint32_t o[16];
+            tmem_load16_wait(o, out + d * 16);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = fresh && moved ? 0u : __float_as_uint(__uint_as_float(o[i]) * back);
-            tmem_store32(out + c * 32, o);
+            for (int i = 0; i < 16; ++i) o[i] = fresh ? 0u : __float_as_uint(__uint_as_float(o[i]) * back);
+            tmem_store16(out + d * 16, o);
           }
         }
       }
@@ -314,26 +324,29 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       uint64_t sums[2] = {0, 0};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        uint32_t w[32];
+        uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int c = half * 2 + i / 16, e = i % 16 * 2;
-          const uint64_t t = fma2(pack2(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])), times2, shift2);
-          const float a = exp2_approx(low2(t)), b = exp2_approx(high2(t));
-          sums[i & 1] = add2(sums[i & 1], pack2(a, b));
-          w[i] = narrow2<T>(a, b);
+        for (int i = 0; i < 16; ++i) {
+          const uint64_t t =
+              fma2(pack2(__uint_as_float(x[half][2 * i]), __uint_as_float(x[half][2 * i + 1])), times2, shift2);
+          const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
+          sums[i & 1] = add2(sums[i & 1], pack2(u, v));
+          w[i] = narrow2<T>(u, v);
         }
-        tmem_store32(scores + half * 32, w);
+        tmem_store16(scores + half * 16, w);
       }
       const uint64_t sum = add2(sums[0], sums[1]);
       total += low2(sum) + high2(sum);
       tmem_wait_st();
       tmem_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.p_full[slot]);
+      if (lane == 0) mbar_arrive(&sh.p_full[slot][b]);
     }
-    const bool any = to[slot] > from[slot];
-    if (alive && any) alive = mbar_wait_warp(&sh.o_full[slot], 0, dead);
+    const bool any = steps > 0;
+    // The last scores were issued behind the output's step before the last but one: a wait by parity for the last alone
+    // could be met by that one.
+    if (alive && steps > 1) alive = mbar_wait_warp(&sh.o_done[slot], (steps - 2) & 1, dead);
+    if (alive && any) alive = mbar_wait_warp(&sh.o_done[slot], (steps - 1) & 1, dead);
     tmem_fence_after();
     const bool seen = alive && any && total != 0.0f;
     const float over = seen ? 1.0f / total : 0.0f;
@@ -370,7 +383,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   }
   tmem_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kSoftmaxWarps) {
     tmem_fence_after();
     tmem_free(tmem, 512);
   }
