@@ -47,7 +47,7 @@ struct Plan {
 };
 
 struct MmaShared {
-  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2][2], p_full[2][2], o_done[2], drain;
+  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2][2], p_full[2][2], o_done[2], drain[2];
   int lo[2], hi[2];
   uint32_t tmem;
   int dead;
@@ -59,15 +59,16 @@ struct MmaShared {
 // the products in steps of 64.
 //
 //   warps 0-3, 4-7   softmax of slot 0, 1: a thread has a row
-//   warp 8           the matrix products, one thread
-//   warp 9           TMA loads, one thread (10 and 11 have nothing to do)
+//   warps 8, 9       the matrix products of slot 0, 1, one thread each: a warp alone issues a step's in more time than
+//                    they take
+//   warp 10          TMA loads, one thread (11 has nothing to do)
 //
 // Tensor memory (512 columns): a slot's scores of two steps, 64 columns each, the
 // weights of a step in 16 bits over the first half of its scores; outputs from
 // column 256 on. S = Q K^T has both operands in shared memory; O += P V takes P
-// from tensor memory and V as TMA left it, along N. Step j's scores are issued
-// before step j - 1's O, so a softmax has its next scores when it is done; they
-// take the place of step j - 2's weights, whose product was issued before them.
+// from tensor memory and V as TMA left it, along N. Behind step i's output go
+// step i + 2's scores, into the place of the weights that it has read: a slot's
+// softmax always has its next scores, and its tensor-core warp one wait per step.
 //
 // What bounds it: the products with 64 columns read 6 KB of shared memory in the
 // 32 cycles that they would take, so a step is 384 + 256 cycles per slot, 2560 for
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     mbar_init(&sh.q_full, 1);
     for (int i = 0; i < L::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
-      mbar_init(&sh.kv_empty[i], 1);
+      mbar_init(&sh.kv_empty[i], 2);
     }
     for (int s = 0; s < 2; ++s) {
       for (int b = 0; b < 2; ++b) {
@@ -107,10 +108,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         mbar_init(&sh.p_full[s][b], 4);
       }
       mbar_init(&sh.o_done[s], 1);
+      mbar_init(&sh.drain[s], 1);
       sh.lo[s] = 0x7FFFFFFF;
       sh.hi[s] = 0;
     }
-    mbar_init(&sh.drain, 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
   }
 
-  if (warp == kSoftmaxWarps + 1) {
+  if (warp == kSoftmaxWarps + 2) {
     if (lane == 0 && n > 0) {
       mbar_expect(&sh.q_full, 2 * L::kTile);
       for (int s = 0; s < 2; ++s)
@@ -175,48 +176,47 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         while (!mbar_try(&sh.q_full, 0) && clock64() - start < kWaitCycles) {}
       }
     }
-  } else if (warp == kSoftmaxWarps) {
+  } else if (warp == kSoftmaxWarps || warp == kSoftmaxWarps + 1) {
+    const int s = warp - kSoftmaxWarps, first = s ? from[1] : from[0], last = s ? to[1] : to[0];
     const uint32_t at = uniform(smem_address(stages));
-    const uint64_t queries = operand_desc(uniform(smem_address(tiles)), 16, 1024);
+    const uint64_t queries = operand_desc(uniform(smem_address(tiles)) + s * L::kTile, 16, 1024);
     const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, kChunk, 1024);
     constexpr uint32_t kScores = mma_desc(kBf16, kKeys, false), kOutput = mma_desc(kBf16, D, true);
     constexpr uint32_t kHalf = kKeys * 128;  // bytes from a tile's first 64 rows to its last
-    const auto after = [](int stage) { return stage + 1 == L::kStages ? 0 : stage + 1; };
-    // the stages in use of keys (0, 2, 4, ... in the order of loads) and of values (1, 3, 5, ...)
-    int k_stage = 0, v_stage = 1;
-    uint32_t k_parity = 0, v_parity = 0;
-    bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
-    for (int j = 0; j <= n && n > 0 && alive; ++j) {
-      if (j < n) {
-        if (j % 2 == 0) {
-          if (j > 0)
-            for (int i = 0; i < 2; ++i) k_parity ^= (k_stage = after(k_stage)) == 0;
-          alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
-          if (!alive) break;
-        }
-        const uint64_t k = keys + (static_cast<uint32_t>(k_stage) * L::kTile + j % 2 * kHalf) / 16;
-        tmem_fence_after();
+    const uint32_t scores = tmem + s * 128, out = tmem + 256 + s * D;
+    const auto scores_of = [&](int j, uint64_t k) {  // of step j, its keys at k
+      const int b = (j - first) & 1;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (j < from[s] || j >= to[s]) continue;
-          const int b = (j - from[s]) & 1;
-          const uint32_t scores = tmem + s * 128 + b * kKeys;
-          const uint64_t q = queries + s * (L::kTile / 16);
-          if (elect_one()) {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-              mma_ss(scores, q + (d / 4 * kChunk + d % 4 * 32) / 16, k + (d / 4 * kChunk + d % 4 * 32) / 16, kScores, d > 0);
-            mma_commit(&sh.s_full[s][b]);
-          }
-        }
-        if ((j % 2 == 1 || j == n - 1) && elect_one()) mma_commit(&sh.kv_empty[k_stage]);
+      for (int d = 0; d < D / 16; ++d)
+        mma_ss(scores + b * kKeys, queries + (d / 4 * kChunk + d % 4 * 32) / 16, k + (d / 4 * kChunk + d % 4 * 32) / 16,
+               kScores, d > 0);
+      mma_commit(&sh.s_full[s][b]);
+    };
+    // Tile t's keys are the loads' 2 t, its values 2 t + 1. The stages and parities of tile t's values and tile t + 1's keys:
+    int v_stage = 1, k_stage = 2;
+    uint32_t v_parity = 0, k_parity = 0;
+    const auto advance = [](int& stage, uint32_t& parity) {
+      if ((stage += 2) >= L::kStages) {
+        stage -= L::kStages;
+        parity ^= 1;
       }
-      const int i = j - 1;
-      if (i < 0) continue;
+    };
+    bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
+    if (n > 0 && alive) alive = mbar_wait_warp(&sh.kv_full[0], 0, dead);
+    if (n > 0 && alive && elect_one()) {  // the first two steps' scores
+      if (first == 0 && last > 0) scores_of(0, keys);
+      if (first <= 1 && last > 1) scores_of(1, keys + kHalf / 16);
+      mma_commit(&sh.kv_empty[0]);
+    }
+    for (int i = 0; i < n && alive; ++i) {  // step i's output, and step i + 2's scores in the place of step i's
+      const bool more = i / 2 * 2 + 2 < n;  // there is another tile
       if (i % 2 == 0) {
-        if (i > 0)
-          for (int c = 0; c < 2; ++c) v_parity ^= (v_stage = after(v_stage)) == 0;
+        if (i > 0) {
+          advance(v_stage, v_parity);
+          advance(k_stage, k_parity);
+        }
         alive = mbar_wait_warp(&sh.kv_full[v_stage], v_parity, dead);
+        if (alive && more) alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
         if (!alive) break;
         const int rest = stop - (begin + i * kKeys);
         if (rest < kRows) {  // keys that no row sees: their weight is 0, and 0 times what is there has to be 0
@@ -229,29 +229,34 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           __syncwarp();
         }
       }
-      const uint64_t v = values + (static_cast<uint32_t>(v_stage) * L::kTile + i % 2 * kHalf) / 16;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (i < from[s] || i >= to[s]) continue;
-        const int c = i - from[s], b = c & 1;
+      const int c = i - first, b = c & 1;
+      const bool mine = i >= first && i < last;
+      if (mine) {
         alive = mbar_wait_warp(&sh.p_full[s][b], c >> 1 & 1, dead);
         if (!alive) break;
-        tmem_fence_after();
-        const uint32_t weights = tmem + s * 128 + b * kKeys, out = tmem + 256 + s * D;
-        if (elect_one()) {
+      }
+      tmem_fence_after();
+      const uint64_t v = values + (static_cast<uint32_t>(v_stage) * L::kTile + i % 2 * kHalf) / 16;
+      const uint64_t k = keys + (static_cast<uint32_t>(k_stage) * L::kTile + i % 2 * kHalf) / 16;
+      if (elect_one()) {
+        if (mine) {
+          mma_ts(out, scores + b * kKeys, v, kOutput, c > 0);
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k) mma_ts(out, weights + k * 8, v + k * (2048 / 16), kOutput, c > 0 || k > 0);
+          for (int d = 1; d < kKeys / 16; ++d) mma_ts(out, scores + b * kKeys + d * 8, v + d * (2048 / 16), kOutput, true);
           mma_commit(&sh.o_done[s]);
         }
+        if (i + 2 >= first && i + 2 < last) scores_of(i + 2, k);
+        if (i % 2 == 1 || i == n - 1) {
+          mma_commit(&sh.kv_empty[v_stage]);
+          if (more) mma_commit(&sh.kv_empty[k_stage]);
+        }
       }
-      if (!alive) break;
-      if ((i % 2 == 1 || i == n - 1) && elect_one()) mma_commit(&sh.kv_empty[v_stage]);
-      __syncwarp();
     }
+    __syncwarp();
     if (*dead && elect_one()) {
-      mma_commit(&sh.drain);
+      mma_commit(&sh.drain[s]);
       const long long start = clock64();
-      while (!mbar_try(&sh.drain, 0) && clock64() - start < kWaitCycles) {}
+      while (!mbar_try(&sh.drain[s], 0) && clock64() - start < kWaitCycles) {}
     }
     __syncwarp();
   } else if (warp < kSoftmaxWarps) {
