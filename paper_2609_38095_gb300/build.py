@@ -1,15 +1,19 @@
 """Build libzo.so (the C-ABI library) in-tree for sm_103a.
 
 Each .cu file is compiled by its own nvcc process (in parallel), then linked
-into one shared library with the CUDA runtime linked statically.
+into one shared library with the CUDA runtime linked statically; beside it the
+Python module _binding.so (csrc/zo_binding.cpp) by the host compiler.
 Set ZO_PTXAS_VERBOSE=1 to print register / shared-memory usage.
 """
 import concurrent.futures as cf
+import importlib.metadata
+import importlib.util
 import os
 import platform
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -17,6 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build", platform.machine())   # objects of this host architecture
 LIB = os.path.join(HERE, "libzo.so")
+BINDING = os.path.join(HERE, "_binding.so")   # the Python module of csrc/zo_binding.cpp
 STAMP = LIB + ".arch"   # architecture the library was linked for
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["zo_api.cu", "zo_stream_kernels.cu", "zo_update_lut8.cu", "zo_small_kernels.cu",
@@ -41,6 +46,22 @@ def _flags():
     return f
 
 
+def _binding_command(out):
+    """One compiler call for the Python module, against the installed torch's headers and libraries."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        raise RuntimeError("g++ not found: a C++ compiler is required to build the Python module")
+    return [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", os.path.join(CSRC, "zo_binding.cpp"), "-o", out, "-I", INCLUDE,
+            "-isystem", os.path.join(torch, "include"), "-isystem", sysconfig.get_path("include"), "-isystem",
+            os.path.join(cuda, "include"), "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
+def _torch_version():
+    return importlib.metadata.version("torch")
+
+
 def _stale(target, deps):
     if not os.path.exists(target):
         return True
@@ -53,6 +74,12 @@ def build(force: bool = False) -> str:
     hdrs = [os.path.join(CSRC, h) for h in HEADERS] + [os.path.join(INCLUDE, h) for h in ("zo.h", "zo_forward.h")]
     jobs = []
     objs = []
+    made = f"{platform.machine()} {_torch_version()}"   # what the Python module was built for
+    binding_ok = os.path.exists(BINDING + ".arch") and open(BINDING + ".arch").read().strip() == made
+    binding_tmp = BINDING + f".tmp{os.getpid()}"
+    bind = force or not binding_ok or _stale(BINDING, [os.path.join(CSRC, "zo_binding.cpp"), hdrs[-1], __file__])
+    if bind:
+        jobs.append(_binding_command(binding_tmp))
     for s in SOURCES:
         src = os.path.join(CSRC, s)
         obj = os.path.join(BUILD, s.replace(".cu", ".o"))
@@ -70,7 +97,11 @@ def build(force: bool = False) -> str:
                 if r.stdout or r.stderr:
                     sys.stderr.write(r.stdout + r.stderr)
                 if r.returncode != 0:
-                    raise RuntimeError(f"nvcc failed: {' '.join(cmd)}")
+                    raise RuntimeError(f"compiler failed: {' '.join(cmd)}")
+    if bind:
+        os.replace(binding_tmp, BINDING)
+        with open(BINDING + ".arch", "w") as f:
+            f.write(made)
     arch_ok = os.path.exists(STAMP) and open(STAMP).read().strip() == platform.machine()
     if force or jobs or not arch_ok or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"

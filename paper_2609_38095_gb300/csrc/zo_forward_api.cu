@@ -2,7 +2,6 @@
 // include/zo_forward.h: argument validation and the choice of kernel.
 // Everything here runs on the host and only enqueues kernels.
 #include <cmath>
-#include <cstring>
 
 #include "zo_forward.cuh"
 #include "zo_forward.h"
@@ -226,47 +225,6 @@ int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab
   p.loss = loss, p.nll = nll;
   p.rows = static_cast<double*>(workspace);
   return finish(zo::launch_token_loss(p, dtype, sms, static_cast<cudaStream_t>(stream)), "token_loss_kernel");
-}
-
-// The entry points above with their arguments in one block, as the Python binding
-// lays them out (a ctypes call costs by its arguments; not part of the public
-// interface).
-int zo_internal_rotate_heads(const int64_t* a, void* stream) {
-  float eps;
-  std::memcpy(&eps, a + 13, sizeof(eps));
-  return zo_rotate_heads(reinterpret_cast<const zo_head_part*>(a + 14), static_cast<int32_t>(a[0]), a[1],
-                         static_cast<int32_t>(a[2]), static_cast<int32_t>(a[3]), reinterpret_cast<const float*>(a[4]), a[5],
-                         static_cast<int32_t>(a[6]), static_cast<int32_t>(a[7]), reinterpret_cast<const void*>(a[8]),
-                         reinterpret_cast<const void*>(a[9]), static_cast<int32_t>(a[10]), a[11], a[12], eps, stream);
-}
-
-int zo_internal_attention(const int64_t* a, void* stream) {
-  float f[2];  // scale, softcap
-  std::memcpy(f, a + 21, sizeof(f));
-  const zo_rows* rows = reinterpret_cast<const zo_rows*>(a);
-  return zo_attention(rows, rows + 1, rows + 2, rows + 3, a[12], a[13], static_cast<int32_t>(a[14]),
-                      static_cast<int32_t>(a[15]), static_cast<int32_t>(a[16]), static_cast<int32_t>(a[17]),
-                      reinterpret_cast<const int32_t*>(a[18]), f[0], f[1], reinterpret_cast<const float*>(a[19]),
-                      reinterpret_cast<float*>(a[20]), stream);
-}
-
-int zo_internal_attention_decode(const int64_t* a, void* stream) {
-  float f[2];  // scale, softcap
-  std::memcpy(f, a + 27, sizeof(f));
-  const zo_rows *q = reinterpret_cast<const zo_rows*>(a), *out = reinterpret_cast<const zo_rows*>(a + 3);
-  const zo_pages *k = reinterpret_cast<const zo_pages*>(a + 6), *v = reinterpret_cast<const zo_pages*>(a + 10);
-  return zo_attention_decode(q, k, v, out, a[14], static_cast<int32_t>(a[15]), static_cast<int32_t>(a[16]),
-                             static_cast<int32_t>(a[17]), static_cast<int32_t>(a[18]),
-                             reinterpret_cast<const int32_t*>(a[19]), a[20], a[21], a[22], static_cast<int32_t>(a[23]),
-                             reinterpret_cast<const int32_t*>(a[24]), f[0], f[1], reinterpret_cast<const float*>(a[25]),
-                             reinterpret_cast<float*>(a[26]), stream);
-}
-
-int zo_internal_token_loss(const int64_t* a, void* stream) {
-  return zo_token_loss(reinterpret_cast<const void*>(a[0]), a[1], a[2], a[3], static_cast<int32_t>(a[4]),
-                       reinterpret_cast<const void*>(a[5]), static_cast<int32_t>(a[6]), static_cast<int32_t>(a[7]),
-                       reinterpret_cast<void*>(a[8]), reinterpret_cast<float*>(a[9]), reinterpret_cast<void*>(a[10]), a[11],
-                       stream);
 }
 
 }  // extern "C"
