@@ -9,6 +9,7 @@ namespace {
 constexpr int kLossThreads = 256;
 constexpr int kLossCtas = 5;     // per SM, by registers: with kLossVectors 80 KB in flight
 constexpr int kLossVectors = 4;  // 16-byte loads in flight per thread
+constexpr int kMaxParts = 8;     // CTAs of a cluster, where tokens are few
 constexpr int kSumThreads = 1024;
 
 struct Tail {  // max and sum of exp(x - max)
@@ -16,18 +17,18 @@ struct Tail {  // max and sum of exp(x - max)
   double sum;
 };
 
-__device__ __forceinline__ Tail join(Tail a, Tail b) {
-  // (-FLT_MAX, 0) is the empty one; exp(x - top) in fp64 only where sums meet
-  const float top = fmaxf(a.top, b.top);
-  return {top, a.sum * exp2_approx((a.top - top) * kLog2e) + b.sum * exp2_approx((b.top - top) * kLog2e)};
-}
-
-__device__ __forceinline__ Tail warp_join(Tail t) {
+// The first kLanes lanes' tails as one, on each of them: the maxima first, so that a sum is scaled once; sums in fp64.
+template <int kLanes>
+__device__ __forceinline__ Tail lanes_join(Tail t) {
+  float top = t.top;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    t = join(t, {__shfl_xor_sync(0xFFFFFFFFu, t.top, o), __shfl_xor_sync(0xFFFFFFFFu, t.sum, o)});
-  return t;
+  for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  double sum = t.sum * exp2_approx((t.top - top) * kLog2e);
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  return {top, sum};
 }
+constexpr Tail kNone = {-3.402823466e38f, 0.0};
 
 // x joins a thread's running maximum and sum; n values at once. x - top, then
 // times log2(e): the difference is formed before its rounding, so logits far
@@ -66,6 +67,7 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   __shared__ double sums[kLossThreads / 32];
   __shared__ float part_top;
   __shared__ float part_sum[2];  // high and low part
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the sum's CTA may come once every CTA here has begun
   const int64_t t = blockIdx.x / parts;
   const int rank = blockIdx.x % parts, tid = threadIdx.x;
   const int64_t target = load_index(p.targets, t, p.target64);
@@ -104,7 +106,7 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
     for (int k = 0; k < kLossVectors; ++k) Vec<T>::widen_all(raw[k], f + k * E);
     take<kLossVectors * E>(f, top, sum);
   }
-  Tail mine = warp_join({top, sum});
+  Tail mine = lanes_join<32>({top, sum});
   if ((tid & 31) == 0) {
     tops[tid >> 5] = mine.top;
     sums[tid >> 5] = mine.sum;
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   __syncthreads();
   if (tid < 32) {
     constexpr int kWarps = kLossThreads / 32;
-    mine = warp_join(tid < kWarps ? Tail{tops[tid], sums[tid]} : Tail{-3.402823466e38f, 0.0});
+    mine = lanes_join<kWarps>(tid < kWarps ? Tail{tops[tid], sums[tid]} : kNone);
     if (tid == 0 && parts > 1) {
       part_top = mine.top;
       part_sum[0] = static_cast<float>(mine.sum);
@@ -122,12 +124,12 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   if (parts > 1) {
     cluster_sync();
     if (rank == 0 && tid < 32) {
-      mine = {-3.402823466e38f, 0.0};
+      mine = kNone;
       if (tid < parts)
         mine = {peer_load(peer_address(&part_top, tid)),
                 static_cast<double>(peer_load(peer_address(&part_sum[0], tid))) +
                     peer_load(peer_address(&part_sum[1], tid))};
-      mine = warp_join(mine);
+      mine = lanes_join<kMaxParts>(mine);
     }
     cluster_sync();  // no CTA leaves before its part is read
   }
@@ -145,7 +147,7 @@ __global__ void __launch_bounds__(kSumThreads) token_loss_sum_kernel(const __gri
   __shared__ double counts[kSumThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   double sum = 0.0, count = 0.0;
-  for (int64_t t = threadIdx.x; t < p.tokens; t += kSumThreads) {
+  for (int64_t t = threadIdx.x; t < p.tokens; t += blockDim.x) {
     sum += p.rows[t];
     if (p.flags & 1) count += load_index(p.targets, t, p.target64) >= 0 ? 1.0 : 0.0;
   }
@@ -160,8 +162,8 @@ __global__ void __launch_bounds__(kSumThreads) token_loss_sum_kernel(const __gri
   }
   __syncthreads();
   if (threadIdx.x >= 32) return;
-  sum = sums[threadIdx.x];
-  count = counts[threadIdx.x];
+  sum = threadIdx.x < blockDim.x / 32 ? sums[threadIdx.x] : 0.0;
+  count = threadIdx.x < blockDim.x / 32 ? counts[threadIdx.x] : 0.0;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -192,7 +194,7 @@ cudaError_t launch_with(F f, unsigned grid, unsigned threads, cudaLaunchAttribut
 template <typename T>
 cudaError_t launch_rows(const TokenLossParams& p, int sms, cudaStream_t stream) {
   int parts = 1;
-  while (parts < 8 && p.tokens * parts * 2 <= kLossCtas * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
+  while (parts < kMaxParts && p.tokens * parts * 2 <= kLossCtas * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = parts;
@@ -213,7 +215,8 @@ cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cuda
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
-  return launch_with(token_loss_sum_kernel, 1, kSumThreads, attr, stream, p);
+  const int64_t threads = p.tokens < kSumThreads ? (p.tokens + 31) / 32 * 32 : kSumThreads;
+  return launch_with(token_loss_sum_kernel, 1, static_cast<unsigned>(threads > 0 ? threads : 32), attr, stream, p);
 }
 
 }  // namespace zo
