@@ -7,7 +7,7 @@
 namespace zo {
 
 bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
-                   int64_t token_stride) {
+                   int64_t token_stride, int rows) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -24,7 +24,7 @@ bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int head
   // a dimension of one element has no stride of its own
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? head_stride * 2 : 16),
                                  static_cast<cuuint64_t>(tokens > 1 ? token_stride * 2 : 16)};
-  const cuuint32_t box[3] = {64, 1, 128}, steps[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)}, steps[3] = {1, 1, 1};
   return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims,
                 strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -53,6 +53,9 @@ struct MmaShared {
   int dead;
 };
 
+// Bits 0 to n - 1.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // A CTA has two slots of 128 query rows: two heads that share their keys (the
 // same rows, the same spans) where a group has an even number of them, else two
 // tiles of rows of one head. Keys and values come in tiles of 128 and go through
@@ -61,7 +64,7 @@ struct MmaShared {
 //   warps 0-3, 4-7   softmax of slot 0, 1: a thread has a row
 //   warps 8, 9       the matrix products of slot 0, 1, one thread each: a warp alone issues a step's in more time than
 //                    they take
-//   warp 10          TMA loads, one thread (11 has nothing to do)
+//   warp 10          TMA loads, one thread (11 only sets up the barriers)
 //
 // Tensor memory (512 columns): a slot's scores of two steps, 64 columns each, the
 // weights of a step in 16 bits over the first half of its scores; outputs from
@@ -82,8 +85,8 @@ struct MmaShared {
 template <typename T, int D, bool kCap, bool kBias>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_mma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-                         const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttentionParams p,
-                         int by_heads) {
+                         const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap o_map,
+                         const __grid_constant__ AttentionParams p, int by_heads) {
   using L = Plan<D>;
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
   extern __shared__ uint8_t raw[];
@@ -96,7 +99,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const int head0 = by_heads ? item * 2 : item, kv_head = head0 / p.group;
   volatile int* dead = &sh.dead;
 
-  if (tid == 0) {
+  int64_t row = 0;
+  int lo = 0, hi = 0, self = 0;
+  const int slot = warp >> 2;
+  if (warp < kSoftmaxWarps) {
+    row = (by_heads ? block : 2 * static_cast<int64_t>(block) + slot) * kRows + (tid & 127);
+    if (row < p.q_tokens) {
+      lo = max(p.spans[row], 0);
+      hi = min(p.spans[p.q_tokens + row], static_cast<int>(p.k_tokens));
+      if (kBias) self = p.spans[2 * p.q_tokens + row];
+    }
+    if (hi <= lo) lo = hi = 0;
+  }
+  if (tid == (kSoftmaxWarps + 3) * 32) {
     mbar_init(&sh.q_full, 1);
     for (int i = 0; i < L::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
@@ -116,18 +131,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, 512);
+  if (tid == (kSoftmaxWarps + 2) * 32) {
+    prefetch_map(&q_map);
+    prefetch_map(&k_map);
+    prefetch_map(&v_map);
+    prefetch_map(&o_map);
+  }
   __syncthreads();
-  int64_t row = 0;
-  int lo = 0, hi = 0, self = 0;
-  const int slot = warp >> 2;
+  if (tid == (kSoftmaxWarps + 2) * 32) {  // the queries, before the spans are known
+    mbar_expect(&sh.q_full, 2 * L::kTile);
+    for (int s = 0; s < 2; ++s)
+      for (int c = 0; c < D / 64; ++c)
+        tma_load_3d(tiles + s * L::kTile + c * kChunk, &q_map, c * 64, by_heads ? head0 + s : head0,
+                    (by_heads ? block : 2 * block + s) * kRows, &sh.q_full);
+  }
   if (warp < kSoftmaxWarps) {
-    row = (by_heads ? block : 2 * static_cast<int64_t>(block) + slot) * kRows + (tid & 127);
-    if (row < p.q_tokens) {
-      lo = max(p.spans[row], 0);
-      hi = min(p.spans[p.q_tokens + row], static_cast<int>(p.k_tokens));
-      if (kBias) self = p.spans[2 * p.q_tokens + row];
-    }
-    if (hi <= lo) lo = hi = 0;
     const int least = __reduce_min_sync(0xFFFFFFFFu, hi > lo ? lo : 0x7FFFFFFF);
     const int most = __reduce_max_sync(0xFFFFFFFFu, hi);
     if (lane == 0 && most > 0) {
@@ -153,12 +171,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   }
 
   if (warp == kSoftmaxWarps + 2) {
-    if (lane == 0 && n > 0) {
-      mbar_expect(&sh.q_full, 2 * L::kTile);
-      for (int s = 0; s < 2; ++s)
-        for (int c = 0; c < D / 64; ++c)
-          tma_load_3d(tiles + s * L::kTile + c * kChunk, &q_map, c * 64, by_heads ? head0 + s : head0,
-                      (by_heads ? block : 2 * block + s) * kRows, &sh.q_full);
+    if (lane == 0) {
       int issued = 0;
       for (int i = 0; i < (n + 1) / 2 * 2; ++i) {  // keys 0, values 0, keys 1, ...
         const int stage = i % L::kStages;
@@ -218,13 +231,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         alive = mbar_wait_warp(&sh.kv_full[v_stage], v_parity, dead);
         if (alive && more) alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
         if (!alive) break;
-        const int rest = stop - (begin + i * kKeys);
-        if (rest < kRows) {  // keys that no row sees: their weight is 0, and 0 times what is there has to be 0
-          uint8_t* v = stages + v_stage * L::kTile;
-          for (int e = lane; e < (kRows - rest) * 8 * (D / 64); e += 32) {
-            const int c = e / ((kRows - rest) * 8), r = e - c * (kRows - rest) * 8;
-            *reinterpret_cast<uint4*>(v + c * kChunk + (rest + r / 8) * 128 + r % 8 * 16) = make_uint4(0, 0, 0, 0);
-          }
+        const int rest = stop - (begin + i * kKeys), used = min(kRows, (n - i) * kKeys);
+        if (rest < used && stop < p.k_tokens) {
+          // keys that no row sees (TMA gives zeros only beyond the last of all): their weight is 0, and 0 times what is
+          // there has to be 0. A row's 16-byte vectors are swizzled among themselves.
+          uint8_t* v = stages + v_stage * L::kTile + lane % 8 * 16;
+          for (int r = rest + lane / 8; r < used; r += 4)
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(v + c * kChunk + r * 128) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
@@ -290,8 +304,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       }
       if (!__all_sync(0xFFFFFFFFu, lo <= key0 && hi >= key0 + kKeys)) {
 #pragma unroll
-        for (int e = 0; e < 64; ++e)
-          if (key0 + e < lo || key0 + e >= hi) x[e / 32][e % 32] = __float_as_uint(-kInf);
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t seen = bits_below(hi - key0 - 32 * c) & ~bits_below(lo - key0 - 32 * c);
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (!(seen >> e & 1)) x[c][e] = __float_as_uint(-kInf);
+        }
       }
       float most[4];
 #pragma unroll
@@ -302,27 +320,26 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       }
       float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
       if (!kCap && !kBias) top *= scale2;
-      const bool moved = top > base + kSlack || (base == -kInf && top > -kInf);
+      // A row's first score sets its reference: its output so far is a sum of zeros (or of 0 times NaN, which shows at the
+      // end), so there is nothing to rescale.
+      const bool moved = base > -kInf && top > base + kSlack;
       if (__any_sync(0xFFFFFFFFu, moved)) {
-        const bool fresh = moved && base == -kInf;  // no weight yet: what is there may be anything times 0
-        const float back = !moved ? 1.0f : fresh ? 0.0f : exp2_approx(base - top);
-        if (moved) base = top;
+        const float back = moved ? exp2_approx(base - top) : 1.0f;
         total *= back;
-        if (c > 0) {
-          // the step before is in the output (the one before that is: these scores were issued behind it)
-          alive = mbar_wait_warp(&sh.o_done[slot], (c - 1) & 1, dead);
-          if (!alive) break;
-          tmem_fence_after();
+        // the step before is in the output (the one before that is: these scores were issued behind it)
+        alive = mbar_wait_warp(&sh.o_done[slot], (c - 1) & 1, dead);
+        if (!alive) break;
+        tmem_fence_after();
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d) {
-            uint32_t o[16];
-            tmem_load16_wait(o, out + d * 16);
+        for (int d = 0; d < D / 16; ++d) {
+          uint32_t o[16];
+          tmem_load16_wait(o, out + d * 16);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = fresh ? 0u : __float_as_uint(__uint_as_float(o[i]) * back);
-            tmem_store16(out + d * 16, o);
-          }
+          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
+          tmem_store16(out + d * 16, o);
         }
       }
+      if (moved || base == -kInf) base = top;
       const float shift = base == -kInf ? 0.0f : -base;
       const float times = kCap || kBias ? 1.0f : scale2;
       const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
@@ -348,6 +365,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (lane == 0) mbar_arrive(&sh.p_full[slot][b]);
     }
     const bool any = steps > 0;
+    if (!any) alive = mbar_wait_warp(&sh.q_full, 0, dead);  // the queries' place is written below
     // The last scores were issued behind the output's step before the last but one: a wait by parity for the last alone
     // could be met by that one.
     if (alive && steps > 1) alive = mbar_wait_warp(&sh.o_done[slot], (steps - 2) & 1, dead);
@@ -356,7 +374,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     const bool seen = alive && any && total != 0.0f;
     const float over = seen ? 1.0f / total : 0.0f;
     bool finite = !seen || total < kInf;
-    T* to_row = static_cast<T*>(p.out) + row * p.out_token + h * p.out_head;
+    // Through shared memory, in the place of the slot's queries: a warp's rows of 64 elements as TMA stores them (rows
+    // apart in memory, a thread's own stores took 3 us).
+    const uint32_t mine = smem_address(tiles + slot * L::kTile) + (warp & 3) * 32 * 128;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[32];
@@ -364,24 +384,39 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_load32(o, out + c * 32);
         tmem_wait_ld(o);
       }
-      if (row < p.q_tokens) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          if (c * 32 + e >= p.dim) continue;
-          float f[8];
+      for (int e = 0; e < 32; e += 8) {
+        float f[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            f[i] = !alive ? NAN : seen ? __uint_as_float(o[e + i]) * over : 0.0f;
-            finite = finite && fabsf(f[i]) < kInf;
-          }
-          *reinterpret_cast<uint4*>(to_row + c * 32 + e) = Vec<T>::narrow_all(f);
+        for (int i = 0; i < 8; ++i) {
+          f[i] = !alive ? NAN : seen ? __uint_as_float(o[e + i]) * over : 0.0f;
+          finite = finite && fabsf(f[i]) < kInf;
         }
+        const uint4 w = Vec<T>::narrow_all(f);
+        const int vector = c % 2 * 4 + e / 8;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine + c / 2 * kChunk + lane * 128 +
+                                                                      ((vector ^ (lane & 7)) << 4)),
+                     "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
+                     : "memory");
       }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0 && row < p.q_tokens) {
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        if (c * 64 < p.dim) tma_store_3d(&o_map, c * 64, h, static_cast<int>(row), mine + c * kChunk);
+      tma_store_commit();
     }
     if (row < p.q_tokens && p.lse != nullptr)
       p.lse[h * p.q_tokens + row] = !alive ? NAN : seen ? (base + log2f(total)) * kLn2 : -kInf;
-    __syncwarp();  // the row's first values are written before its second
-    for (uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite); left != 0; left &= left - 1) {
+    uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite);
+    if (lane == 0) {
+      if (left != 0) tma_stored<false>();  // those rows are written again
+      else tma_stored<true>();
+    }
+    __syncwarp();
+    for (; left != 0; left &= left - 1) {
       const int r = __ffs(left) - 1;
       attention_row<T>(p, row - lane + r, h, lane);
     }
@@ -395,8 +430,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 }
 
 template <typename T, int D, bool kCap, bool kBias>
-cudaError_t launch_kind(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
-                        cudaStream_t stream) {
+cudaError_t launch_kind(const CUtensorMap (&m)[4], const AttentionParams& p, cudaStream_t stream) {
   using L = Plan<D>;
   const auto kernel = attention_mma_kernel<T, D, kCap, kBias>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
@@ -404,18 +438,17 @@ cudaError_t launch_kind(const CUtensorMap& q, const CUtensorMap& k, const CUtens
   const int by_heads = p.group % 2 == 0;
   const int64_t rows = by_heads ? kRows : 2 * kRows;
   const int64_t grid = (p.q_tokens + rows - 1) / rows * (by_heads ? p.heads / 2 : p.heads);
-  kernel<<<static_cast<unsigned>(grid), kMmaThreads, L::kBytes, stream>>>(q, k, v, p, by_heads);
+  kernel<<<static_cast<unsigned>(grid), kMmaThreads, L::kBytes, stream>>>(m[0], m[1], m[2], m[3], p, by_heads);
   return cudaGetLastError();
 }
 
 template <typename T, int D>
-cudaError_t launch_head(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
-                        cudaStream_t stream) {
+cudaError_t launch_head(const CUtensorMap (&m)[4], const AttentionParams& p, cudaStream_t stream) {
   if (p.softcap > 0.0f)
-    return p.slopes != nullptr ? launch_kind<T, D, true, true>(q, k, v, p, stream)
-                               : launch_kind<T, D, true, false>(q, k, v, p, stream);
-  return p.slopes != nullptr ? launch_kind<T, D, false, true>(q, k, v, p, stream)
-                             : launch_kind<T, D, false, false>(q, k, v, p, stream);
+    return p.slopes != nullptr ? launch_kind<T, D, true, true>(m, p, stream)
+                               : launch_kind<T, D, true, false>(m, p, stream);
+  return p.slopes != nullptr ? launch_kind<T, D, false, true>(m, p, stream)
+                             : launch_kind<T, D, false, false>(m, p, stream);
 }
 
 }  // namespace
@@ -433,16 +466,17 @@ bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stre
       !vectors(p.v, p.v_token, p.v_head, p.k_tokens, kv_heads) ||
       !vectors(p.out, p.out_token, p.out_head, p.q_tokens, p.heads))
     return false;
-  CUtensorMap q, k, v;
+  CUtensorMap m[4];
   const bool bf16 = dtype == 1;
-  if (!make_head_map(&q, bf16, p.q, p.dim, p.heads, p.q_tokens, p.q_head, p.q_token) ||
-      !make_head_map(&k, bf16, p.k, p.dim, kv_heads, p.k_tokens, p.k_head, p.k_token) ||
-      !make_head_map(&v, bf16, p.v, p.dim, kv_heads, p.k_tokens, p.v_head, p.v_token))
+  if (!make_head_map(&m[0], bf16, p.q, p.dim, p.heads, p.q_tokens, p.q_head, p.q_token, kRows) ||
+      !make_head_map(&m[1], bf16, p.k, p.dim, kv_heads, p.k_tokens, p.k_head, p.k_token, kRows) ||
+      !make_head_map(&m[2], bf16, p.v, p.dim, kv_heads, p.k_tokens, p.v_head, p.v_token, kRows) ||
+      !make_head_map(&m[3], bf16, p.out, p.dim, p.heads, p.q_tokens, p.out_head, p.out_token, 32))
     return false;
   if (bf16)
-    *e = p.dim <= 64 ? launch_head<__nv_bfloat16, 64>(q, k, v, p, stream) : launch_head<__nv_bfloat16, 128>(q, k, v, p, stream);
+    *e = p.dim <= 64 ? launch_head<__nv_bfloat16, 64>(m, p, stream) : launch_head<__nv_bfloat16, 128>(m, p, stream);
   else
-    *e = p.dim <= 64 ? launch_head<__half, 64>(q, k, v, p, stream) : launch_head<__half, 128>(q, k, v, p, stream);
+    *e = p.dim <= 64 ? launch_head<__half, 64>(m, p, stream) : launch_head<__half, 128>(m, p, stream);
   return true;
 }
 

@@ -81,6 +81,23 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+// From shared memory; what lies beyond the tensor is not written. tma_stored: the thread's stores have been read from
+// shared memory (kRead) or are done.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+               "r"(z), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <bool kRead>
+__device__ __forceinline__ void tma_stored() {
+  if constexpr (kRead) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
 // Shared-memory operand with the 128-byte swizzle; start, leading and stride offsets in bytes.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t start, uint32_t leading, uint32_t stride) {
   return static_cast<uint64_t>((start & 0x3FFFFu) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 |
@@ -171,10 +188,10 @@ __device__ __forceinline__ void tie32(uint32_t (&v)[32]) {
 
 #endif  // __CUDACC__
 
-// A tiled map of 16-bit heads, boxes of 64 elements x 1 head x 128 tokens with
+// A tiled map of 16-bit heads, boxes of 64 elements x 1 head x `rows` tokens with
 // the 128-byte swizzle; elements beyond a head's size and tokens beyond the
 // last are read as zeros. False if the strides admit none.
 bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
-                   int64_t token_stride);
+                   int64_t token_stride, int rows);
 
 }  // namespace zo
