@@ -77,7 +77,7 @@ cudaError_t launch_rotary_table(float* table, int64_t rows, int rotary, double b
 cudaError_t launch_document_spans(const int32_t* q_starts, const int32_t* k_starts, const int32_t* prefix, int docs,
                                   int32_t* spans, int64_t tokens, cudaStream_t stream);
 cudaError_t launch_rotate_heads(const RotateParams& p, int dtype, cudaStream_t stream);
-cudaError_t launch_attention_tiles(const AttentionParams& p, int dtype, cudaStream_t stream);
+cudaError_t launch_attention_tiles(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
 // The same on the tensor cores, where type, head size, strides and alignment
 // admit it (false: nothing was launched).
 bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stream, cudaError_t* e);

@@ -151,7 +151,10 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
   p.lse = lse;
   cudaError_t e = cudaSuccess;
   if (zo::launch_attention_mma(p, dtype, static_cast<cudaStream_t>(stream), &e)) return finish(e, "attention_mma_kernel");
-  return finish(zo::launch_attention_tiles(p, dtype, static_cast<cudaStream_t>(stream)), "attention_tiles_kernel");
+  int sms = 0;
+  rc = zo::device_sms(&sms);
+  if (rc != ZO_OK) return rc;
+  return finish(zo::launch_attention_tiles(p, dtype, sms, static_cast<cudaStream_t>(stream)), "attention_tiles_kernel");
 }
 
 int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, const zo_rows* out, int64_t batch,

@@ -194,3 +194,17 @@ def test_repeatable_streams_and_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
+@pytest.mark.parametrize("tokens,keys", [(1, 1000), (40, 5000), (130, 900)])
+def test_few_rows_many_keys(dtype, tokens, keys):
+    """Clusters that share a row's keys, tiles that no row sees among them, and rows that see nothing beside."""
+    g = gen(tokens)
+    q, k, v = (randn(g, n, 2, 96, dtype=dtype) for n in (tokens, keys, keys))
+    for spans in (F.document_spans(starts([tokens]), starts([keys]), tokens=tokens),
+                  torch.zeros(3, tokens, dtype=torch.int32, device="cuda")):
+        compare(q, k, v, spans)
+        if tokens > 40:
+            spans[1, 64:] = 0
+            compare(q, k, v, spans)
