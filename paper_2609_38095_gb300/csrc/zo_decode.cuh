@@ -45,18 +45,23 @@ __device__ __forceinline__ DecodePlace decode_place(const DecodeParams& p, uint3
   return w;
 }
 
+// The place of key j's page in a sequence's row of the page table.
+__device__ __forceinline__ uint32_t decode_page(const DecodeParams& p, int64_t j) {
+  const uint32_t at = static_cast<uint32_t>(j);
+  return p.page_shift >= 0 ? at >> p.page_shift : at / static_cast<uint32_t>(p.page_size);
+}
+
 // Key j's page and row in it; page -1 where j is beyond the length, and where
 // the table names no page of the cache (bad).
 __device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePlace& w, int64_t j, int& bad) {
   if (j >= w.len) return make_int2(-1, 0);
-  const uint32_t at = static_cast<uint32_t>(j);
-  const uint32_t page = p.page_shift >= 0 ? at >> p.page_shift : at / static_cast<uint32_t>(p.page_size);
+  const uint32_t page = decode_page(p, j);
   const int id = p.pages[w.b * p.pages_stride + page];
   if (id < 0 || id >= p.n_pages) {
     bad = 1;
     return make_int2(-1, 0);
   }
-  return make_int2(id, static_cast<int>(at - page * p.page_size));
+  return make_int2(id, static_cast<int>(static_cast<uint32_t>(j) - page * p.page_size));
 }
 
 // Every thread of the cluster. outs: [kWarps][HB][DP] unscaled outputs, tops and
@@ -122,11 +127,15 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
   cluster_sync();  // no CTA leaves before its part is read
 }
 
-// CTAs of a cluster: enough that `per_sm` CTAs per SM have work, none with less
-// than `least` keys of the longest sequence that the page table can hold.
-inline int decode_cluster(int64_t items, int64_t longest, int sms, int per_sm, int64_t least) {
+// CTAs of a cluster: a CTA per SM, none with less than 128 keys of the longest
+// sequence that the page table can hold; up to `per_sm` where each keeps 512,
+// because a CTA's start and its part in the join cost as much as some 200 keys
+// (128 sequences and heads of up to 4001 keys: 4 CTAs 33 us, 8 40 us).
+inline int decode_cluster(int64_t items, int64_t longest, int sms, int per_sm) {
   int c = 1;
-  while (c < kMaxCluster && items * c < static_cast<int64_t>(sms) * per_sm && longest >= 2 * c * least) c *= 2;
+  while (c < kMaxCluster && ((items * c < sms && longest >= 2 * c * 128) ||
+                             (items * c < static_cast<int64_t>(sms) * per_sm && longest >= 2 * c * 512)))
+    c *= 2;
   return c;
 }
 

@@ -81,19 +81,27 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
   const int64_t first = static_cast<int64_t>(cluster_rank()) * kWarps + warp;
   const int len = static_cast<int>(w.len);
   int bad = 0;
-  // A lane finds the place of one of a tile's keys, in bytes from where its vectors start (-1: no key), long before it is
-  // needed; the caches mostly have the same strides.
+  // A lane looks up the page of one of a tile's keys a whole tile before it needs it (a use any earlier would wait for the
+  // load), and then finds where the key's vectors start, in bytes (-1: no key). The caches mostly have the same strides.
   const bool same = p.k_page == p.v_page && p.k_token == p.v_token;
   struct Place {
     int64_t k, v;
   };
-  const auto find = [&](int64_t tile) {
-    const int2 key = decode_key(p, w, tile * L::kKeys + lane % L::kKeys, bad);
+  const auto look = [&](int64_t tile) {
+    const int64_t j = tile * L::kKeys + lane % L::kKeys;
+    return j < w.len ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+  };
+  const auto find = [&](int64_t tile, int id) {
+    const int64_t j = tile * L::kKeys + lane % L::kKeys;
     Place at = {-1, -1};
-    if (key.x >= 0) {
-      at.k = (key.x * p.k_page + key.y * p.k_token) * 2;
-      at.v = same ? at.k : (key.x * p.v_page + key.y * p.v_token) * 2;
+    if (j >= w.len) return at;
+    if (id < 0 || id >= p.n_pages) {
+      bad = 1;
+      return at;
     }
+    const int row = static_cast<int>(j - static_cast<int64_t>(decode_page(p, j)) * p.page_size);
+    at.k = (id * p.k_page + row * p.k_token) * 2;
+    at.v = same ? at.k : (id * p.v_page + row * p.v_token) * 2;
     return at;
   };
   const int vector = lane % kVectors;
@@ -117,12 +125,13 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
     }
   };
 
-  Place ahead = find(first);
+  int id = look(first);
 #pragma unroll
   for (int s = 0; s < L::kStages - 1; ++s) {
-    const Place place = ahead;
-    ahead = find(first + (s + 1) * step);
-    if (first + s * step < tiles_in) fetch(place, s);
+    const int64_t tile = first + s * step;
+    const int here = id;
+    id = look(tile + step);
+    if (tile < tiles_in) fetch(find(tile, here), s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   // the queries as right operands: head lane / 4 (and 8 more), elements 2 (lane mod 4) and 8 more
@@ -159,10 +168,10 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
   int stage = 0;
   for (int64_t tile = first; tile < tiles_in; tile += step) {
     {
-      const Place place = ahead;
       const int64_t next = tile + (L::kStages - 1) * step;
-      ahead = find(next + step);
-      if (next < tiles_in) fetch(place, stage == 0 ? L::kStages - 1 : stage - 1);
+      const int here = id;
+      id = look(next + step);
+      if (next < tiles_in) fetch(find(next, here), stage == 0 ? L::kStages - 1 : stage - 1);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 1) : "memory");
@@ -284,7 +293,7 @@ cudaError_t launch_size(DecodeParams p, int64_t batch, int sms, cudaStream_t str
   const int64_t items = batch * p.kv_heads * p.head_blocks;
   // CTAs per SM: 4 leave long sequences in too few (48 of up to 16384 keys 293 us, with 6 or 8 248); 8 split short ones
   // for their joins' sake (16 of up to 4001 keys, 32 heads: 67 us, with 4 or 6 57)
-  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6, 128);
+  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6);
   return launch_decode(decode_mma_kernel<T, DP, HB>, p, items, c, kWarps * 32, Tiles<DP, HB>::kBytes, stream);
 }
 

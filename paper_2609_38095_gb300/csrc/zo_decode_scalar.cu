@@ -185,7 +185,7 @@ cudaError_t launch_size(DecodeParams p, int64_t batch, int sms, cudaStream_t str
   using S = Scalar<DP>;
   p.head_blocks = (p.group + kBlockHeads - 1) / kBlockHeads;
   const int64_t items = batch * p.kv_heads * p.head_blocks;
-  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 2, 128);
+  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6);
   return launch_decode(decode_scalar_kernel<T, DP, kAsync>, p, items, c, S::kWarps * 32, S::kBytes, stream);
 }
 
