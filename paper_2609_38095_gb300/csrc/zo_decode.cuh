@@ -51,17 +51,15 @@ __device__ __forceinline__ uint32_t decode_page(const DecodeParams& p, int64_t j
   return p.page_shift >= 0 ? at >> p.page_shift : at / static_cast<uint32_t>(p.page_size);
 }
 
-// Key j's page and row in it; page -1 where j is beyond the length, and where
+// Key j's row in its page `id`; page -1 where j is beyond the length, and where
 // the table names no page of the cache (bad).
-__device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePlace& w, int64_t j, int& bad) {
+__device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePlace& w, int64_t j, int id, int& bad) {
   if (j >= w.len) return make_int2(-1, 0);
-  const uint32_t page = decode_page(p, j);
-  const int id = p.pages[w.b * p.pages_stride + page];
   if (id < 0 || id >= p.n_pages) {
     bad = 1;
     return make_int2(-1, 0);
   }
-  return make_int2(id, static_cast<int>(static_cast<uint32_t>(j) - page * p.page_size));
+  return make_int2(id, static_cast<int>(static_cast<uint32_t>(j) - decode_page(p, j) * static_cast<uint32_t>(p.page_size)));
 }
 
 // Every thread of the cluster. outs: [kWarps][HB][DP] unscaled outputs, tops and
@@ -89,10 +87,11 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
   }
   const uint32_t ranks = cluster_size(), rank = cluster_rank();
   cluster_sync();
-  // a thread per head and CTA of the cluster: 16 lanes hold a head's CTAs
-  for (int i = tid; i < HB * kMaxCluster; i += kWarps * 32) {
-    const int h = i / kMaxCluster, r = i % kMaxCluster;
-    const bool in = r < static_cast<int>(ranks);
+  // a thread per head and CTA of the cluster: 16 lanes hold a head's CTAs (every lane of a warp takes part, with heads or
+  // without)
+  for (int first = 0; first < HB * kMaxCluster; first += kWarps * 32) {
+    const int i = first + tid, h = min(i / kMaxCluster, HB - 1), r = i % kMaxCluster;
+    const bool in = i < HB * kMaxCluster && r < static_cast<int>(ranks);
     const float mine = in ? peer_load(peer_address(&join.top[h], r)) : -kInf;
     const float part = in ? peer_load(peer_address(&join.total[h], r)) : 0.0f;
     bool bad = in && __float_as_int(peer_load(peer_address(&join.bad, r))) != 0;
@@ -106,6 +105,7 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     for (int o = kMaxCluster / 2; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
     const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad);
     bad = (bads >> (tid & 16) & 0xFFFFu) != 0;
+    if (i >= HB * kMaxCluster) continue;
     join.scale[r][h] = scale;
     if (r == 0) {
       join.over[h] = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;

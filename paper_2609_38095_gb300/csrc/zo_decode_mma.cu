@@ -92,16 +92,12 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
     return j < w.len ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
   };
   const auto find = [&](int64_t tile, int id) {
-    const int64_t j = tile * L::kKeys + lane % L::kKeys;
+    const int2 key = decode_key(p, w, tile * L::kKeys + lane % L::kKeys, id, bad);
     Place at = {-1, -1};
-    if (j >= w.len) return at;
-    if (id < 0 || id >= p.n_pages) {
-      bad = 1;
-      return at;
+    if (key.x >= 0) {
+      at.k = (key.x * p.k_page + key.y * p.k_token) * 2;
+      at.v = same ? at.k : (key.x * p.v_page + key.y * p.v_token) * 2;
     }
-    const int row = static_cast<int>(j - static_cast<int64_t>(decode_page(p, j)) * p.page_size);
-    at.k = (id * p.k_page + row * p.k_token) * 2;
-    at.v = same ? at.k : (id * p.v_page + row * p.v_token) * 2;
     return at;
   };
   const int vector = lane % kVectors;

@@ -6,29 +6,27 @@ namespace zo {
 
 namespace {
 
-constexpr int kBlockHeads = 8;   // query heads of a cluster
 constexpr int kDecodeKeys = 16;  // keys of a warp's tile
 
-template <int DP>
+template <int DP, int HB>
 struct Scalar {
   static constexpr int kWarps = DP == 256 ? 2 : 4;
   static constexpr int kStages = 2;
   static constexpr int kPitch = DP + 4;  // floats from one key to the next: 16 keys' vectors on distinct banks
   static constexpr int kStage = kDecodeKeys * (kPitch + DP);
-  static constexpr int kWarp = kStages * kStage + kDecodeKeys * kBlockHeads;  // and the keys' weights
-  static constexpr int kBytes = 4 * (kWarps * kWarp + kBlockHeads * DP + 2 * kWarps * kBlockHeads);
-  static_assert(kBlockHeads * DP * kWarps <= kWarps * kWarp, "a warp's output takes its tiles' place");
+  static constexpr int kWarp = kStages * kStage + kDecodeKeys * HB;  // and the keys' weights
+  static constexpr int kBytes = 4 * (kWarps * kWarp + HB * DP + 2 * kWarps * HB);
+  static_assert(HB * DP * kWarps <= kWarps * kWarp, "a warp's output takes its tiles' place");
 };
 
 // A warp's tile of 16 keys lies in its own shared memory as fp32, the next one
 // on its way (fp32 caches by cp.async; others are widened on the way and stored
 // before the products start). Scores: a lane has half of a key's dot product
 // with every head; outputs: a lane has DP / 32 elements of every head.
-template <typename T, int DP, bool kAsync>
-__global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
+template <typename T, int DP, int HB, bool kAsync>
+__global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
     decode_scalar_kernel(const __grid_constant__ DecodeParams p) {
-  using S = Scalar<DP>;
-  constexpr int HB = kBlockHeads;
+  using S = Scalar<DP, HB>;
   extern __shared__ __align__(16) float smem[];
   __shared__ DecodeJoin<HB> join;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -54,10 +52,15 @@ __global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
   const int64_t step = static_cast<int64_t>(ranks) * S::kWarps;
   int bad = 0;
 
-  auto fetch = [&](int64_t tile, int stage) {
+  // a page is looked up a tile before its number is used, which would wait for the load
+  const auto look = [&](int64_t tile) {
+    const int64_t j = tile * kDecodeKeys + (lane & 15);
+    return j < w.len ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+  };
+  const auto fetch = [&](int64_t tile, int id, int stage) {
     float* ks = mine + stage * S::kStage;
     float* vs = ks + kDecodeKeys * S::kPitch;
-    const int2 key = decode_key(p, w, tile * kDecodeKeys + (lane & 15), bad);
+    const int2 key = decode_key(p, w, tile * kDecodeKeys + (lane & 15), id, bad);
     for (int r = 0; r < kDecodeKeys; ++r) {
       const int page = __shfl_sync(0xFFFFFFFFu, key.x, r), row = __shfl_sync(0xFFFFFFFFu, key.y, r);
       const T* k = kc + page * p.k_page + row * p.k_token;
@@ -99,10 +102,14 @@ __global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
   }
   int64_t tile = static_cast<int64_t>(cluster_rank()) * S::kWarps + warp;
   int stage = 0;
-  if (tile < tiles_in) fetch(tile, 0);
+  int id = look(tile);
+  if (tile < tiles_in) fetch(tile, id, 0);
+  id = look(tile + step);
   for (; tile < tiles_in; tile += step, stage ^= 1) {
+    const int here = id;
+    id = look(tile + 2 * step);
     if (tile + step < tiles_in) {
-      fetch(tile + step, stage ^ 1);
+      fetch(tile + step, here, stage ^ 1);
       if constexpr (kAsync) asm volatile("cp.async.wait_group 1;" ::: "memory");
     } else {
       if constexpr (kAsync) asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -143,15 +150,15 @@ __global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
       total[h] += half == 0 ? s[h] : 0.0f;
     }
     if (half == 0) {
-      *reinterpret_cast<float4*>(weights + key * HB) = make_float4(s[0], s[1], s[2], s[3]);
-      *reinterpret_cast<float4*>(weights + key * HB + 4) = make_float4(s[4], s[5], s[6], s[7]);
+#pragma unroll
+      for (int h = 0; h < HB; ++h) weights[key * HB + h] = s[h];
     }
     __syncwarp();
 #pragma unroll 4
     for (int r = 0; r < kDecodeKeys; ++r) {
-      const float4 wa = *reinterpret_cast<const float4*>(weights + r * HB);
-      const float4 wb = *reinterpret_cast<const float4*>(weights + r * HB + 4);
-      const float wr[HB] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+      float wr[HB];
+#pragma unroll
+      for (int h = 0; h < HB; ++h) wr[h] = weights[r * HB + h];
 #pragma unroll
       for (int c = 0; c < DP / 32; ++c) {
         const float x = vs[r * DP + c * 32 + lane];
@@ -180,13 +187,21 @@ __global__ void __launch_bounds__(Scalar<DP>::kWarps * 32)
   decode_join<T, HB, DP, S::kWarps>(p, w, tiles, tops, totals, join);
 }
 
-template <typename T, int DP, bool kAsync>
-cudaError_t launch_size(DecodeParams p, int64_t batch, int sms, cudaStream_t stream) {
-  using S = Scalar<DP>;
-  p.head_blocks = (p.group + kBlockHeads - 1) / kBlockHeads;
+template <typename T, int DP, int HB, bool kAsync>
+cudaError_t launch_heads(DecodeParams p, int64_t batch, int sms, cudaStream_t stream) {
+  using S = Scalar<DP, HB>;
+  p.head_blocks = (p.group + HB - 1) / HB;
   const int64_t items = batch * p.kv_heads * p.head_blocks;
   const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6);
-  return launch_decode(decode_scalar_kernel<T, DP, kAsync>, p, items, c, S::kWarps * 32, S::kBytes, stream);
+  return launch_decode(decode_scalar_kernel<T, DP, HB, kAsync>, p, items, c, S::kWarps * 32, S::kBytes, stream);
+}
+
+// A cluster's query heads: no more than the group has, whose products would be of zeros.
+template <typename T, int DP, bool kAsync>
+cudaError_t launch_size(const DecodeParams& p, int64_t batch, int sms, cudaStream_t stream) {
+  if (p.group == 1) return launch_heads<T, DP, 1, kAsync>(p, batch, sms, stream);
+  return p.group <= 4 ? launch_heads<T, DP, 4, kAsync>(p, batch, sms, stream)
+                      : launch_heads<T, DP, 8, kAsync>(p, batch, sms, stream);
 }
 
 template <typename T>
