@@ -61,14 +61,16 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
     float* ks = mine + stage * S::kStage;
     float* vs = ks + kDecodeKeys * S::kPitch;
     const int2 key = decode_key(p, w, tile * kDecodeKeys + (lane & 15), id, bad);
+    const int64_t k_at = key.x >= 0 ? key.x * p.k_page + key.y * p.k_token : -1;
+    const int64_t v_at = key.x >= 0 ? key.x * p.v_page + key.y * p.v_token : 0;
     for (int r = 0; r < kDecodeKeys; ++r) {
-      const int page = __shfl_sync(0xFFFFFFFFu, key.x, r), row = __shfl_sync(0xFFFFFFFFu, key.y, r);
-      const T* k = kc + page * p.k_page + row * p.k_token;
-      const T* v = vc + page * p.v_page + row * p.v_token;
+      const int64_t at = __shfl_sync(0xFFFFFFFFu, k_at, r);
+      const T* k = kc + at;
+      const T* v = vc + __shfl_sync(0xFFFFFFFFu, v_at, r);
       if constexpr (kAsync) {
 #pragma unroll
         for (int c = lane; c < DP / 4; c += 32) {
-          const int n = page >= 0 && c * 4 < p.dim ? 16 : 0;  // the rest is filled with zeros
+          const int n = at >= 0 && c * 4 < p.dim ? 16 : 0;  // the rest is filled with zeros
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                            static_cast<uint32_t>(__cvta_generic_to_shared(ks + r * S::kPitch + c * 4))),
                        "l"(n ? static_cast<const void*>(k + c * 4) : p.k), "r"(n)
@@ -81,7 +83,7 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
       } else {
 #pragma unroll
         for (int d = lane; d < DP; d += 32) {
-          const bool in = page >= 0 && d < p.dim;
+          const bool in = at >= 0 && d < p.dim;
           ks[r * S::kPitch + d] = in ? widen(k[d]) : 0.0f;
           vs[r * DP + d] = in ? widen(v[d]) : 0.0f;
         }

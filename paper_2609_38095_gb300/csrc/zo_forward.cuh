@@ -235,13 +235,16 @@ __device__ __noinline__ void attention_row(const AttentionParams& p, int64_t i, 
   const int64_t self = p.slopes != nullptr ? p.spans[2 * p.q_tokens + i] : 0;
   const float slope = p.slopes != nullptr ? p.slopes[h] : 0.0f;
   float qr[8], acc[8];
+  bool nan = false;
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
     qr[c] = lane + 32 * c < p.dim ? widen(q[lane + 32 * c]) : 0.0f;
     acc[c] = 0.0f;
+    nan = nan || qr[c] != qr[c];
   }
-  float top = -kInf, total = 0.0f;
-  for (int64_t j = first; j < end; ++j) {
+  nan = __any_sync(0xFFFFFFFFu, nan) && end > first;  // then every score is NaN (a forward that has diverged: all rows)
+  float top = -kInf, total = nan ? NAN : 0.0f;
+  for (int64_t j = first; j < end && total == total; ++j) {  // from the first NaN score on nothing changes
     float s = 0.0f;
 #pragma unroll
     for (int c = 0; c < 8; ++c)

@@ -7,8 +7,7 @@ namespace zo {
 namespace {
 
 constexpr int kRotateThreads = 256;
-constexpr int kHeadsPerGroup = 2;  // heads that a group of lanes takes, their loads issued together
-constexpr int kRotateCtas = 4;     // per SM, by registers: with two heads per group 64 KB in flight
+constexpr int kRotateCtas = 4;  // per SM, by registers
 
 // Position t's row of the table; a position outside it: NULL.
 __device__ __forceinline__ const float* table_row(const RotateParams& p, int64_t t) {
@@ -40,23 +39,69 @@ __device__ __forceinline__ float weight_at(const RotatePart& part, int i) {
 template <typename T>
 constexpr int kCode = sizeof(T) == 4 ? 0 : __is_same(T, __nv_bfloat16) ? 1 : 2;  // zo_dtype
 
-// A head lies on kLanes lanes, each with a unit of two 16-byte vectors: the two
-// halves of its pairs (layout half), or neighbours (interleaved, and what is not
-// rotated), so that a lane has both elements of a pair and reads E cosines and
-// sines at E times its number in both layouts. A warp takes one token's
-// kHeadsPerGroup * 32 / kLanes heads; angles and weight are loaded once for them.
-// Bound by HBM: 2 bytes in and 2 out per 16-bit element.
-template <typename T, int kLanes>
+// W words of 4 bytes in one load, W = 4 or 2.
+template <int W>
+struct Words {
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const void* p) {
+    if constexpr (W == 4) {
+      const uint4 u = *static_cast<const uint4*>(p);
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else {
+      const uint2 u = *static_cast<const uint2*>(p);
+      w[0] = u.x, w[1] = u.y;
+    }
+  }
+  __device__ __forceinline__ void store(void* p) const {
+    if constexpr (W == 4) *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  }
+  template <typename T>
+  __device__ __forceinline__ void widen_all(float* f) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        f[i] = __uint_as_float(w[i]);
+      } else if constexpr (__is_same(T, __nv_bfloat16)) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      } else {
+        const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        f[2 * i] = g.x;
+        f[2 * i + 1] = g.y;
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void narrow_all(const float* f) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+      else w[i] = narrow2<T>(f[2 * i], f[2 * i + 1]);
+    }
+  }
+};
+
+// A head lies on kLanes lanes, each with a unit of two vectors of W words: the
+// two halves of its pairs (layout half), or neighbours (interleaved, and what is
+// not rotated), so that a lane has both elements of a pair and reads E cosines
+// and sines at E times its number in both layouts. W is 4, or 2 where the size or
+// the rotated part leaves a half vector. A warp takes kHeads heads of each of its
+// groups of lanes; angles and weight are loaded once for them. Bound by HBM: 2
+// bytes in and 2 out per 16-bit element (50001 tokens of 80 heads of 128, fp16:
+// 361 us = 5.7 TB/s; two heads of 16-byte vectors per group of lanes 361, four on
+// fewer CTAs 365, one 521).
+template <typename T, int W, int kLanes>
 __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
-  constexpr int E = Vec<T>::kN;
-  constexpr int kGroups = 32 / kLanes;
+  constexpr int E = W * 4 / sizeof(T);
+  constexpr int kGroups = 32 / kLanes, kHeads = 8 / W;
   const int lane = threadIdx.x & 31;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kRotateThreads / 32) + (threadIdx.x >> 5);
   if (t >= p.tokens) return;
   const RotatePart& part = part_of(p, blockIdx.y);
   T* row = out_row<T>(p, part, t);
   if (row == nullptr) return;
-  const int unit = lane % kLanes, head0 = (blockIdx.y - part.slice) * kHeadsPerGroup * kGroups + lane / kLanes;
+  const int unit = lane % kLanes, head0 = (blockIdx.y - part.slice) * kHeads * kGroups + lane / kLanes;
   const bool here = unit * 2 * E < p.dim;
   const bool turned = part.rotate && unit * 2 * E < p.rotary;
   int a = unit * 2 * E, b = a + E;
@@ -65,42 +110,42 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
     b = p.rotary / 2 + a;
   }
   const T* in = static_cast<const T*>(part.in) + t * part.in_token;
-  uint4 raw[kHeadsPerGroup][2];
+  Words<W> raw[kHeads][2];
 #pragma unroll
-  for (int n = 0; n < kHeadsPerGroup; ++n) {
+  for (int n = 0; n < kHeads; ++n) {
     const int h = head0 + n * kGroups;
-    raw[n][0] = raw[n][1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < W; ++i) raw[n][0].w[i] = raw[n][1].w[i] = 0;
     if (here && h < part.heads) {
-      raw[n][0] = *reinterpret_cast<const uint4*>(in + h * part.in_head + a);
-      raw[n][1] = *reinterpret_cast<const uint4*>(in + h * part.in_head + b);
+      raw[n][0].load(in + h * part.in_head + a);
+      raw[n][1].load(in + h * part.in_head + b);
     }
   }
   float cs[E], sn[E];
   if (turned) {
     const float* angles = table_row(p, t);
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const float4 c = angles != nullptr ? *reinterpret_cast<const float4*>(angles + unit * E + e)
-                                         : make_float4(NAN, NAN, NAN, NAN);
-      const float4 s = angles != nullptr ? *reinterpret_cast<const float4*>(angles + p.rotary / 2 + unit * E + e)
-                                         : make_float4(NAN, NAN, NAN, NAN);
-      cs[e] = c.x, cs[e + 1] = c.y, cs[e + 2] = c.z, cs[e + 3] = c.w;
-      sn[e] = s.x, sn[e + 1] = s.y, sn[e + 2] = s.z, sn[e + 3] = s.w;
+    for (int e = 0; e < E; e += 2) {
+      const float2 none = make_float2(NAN, NAN);
+      const float2 c = angles != nullptr ? *reinterpret_cast<const float2*>(angles + unit * E + e) : none;
+      const float2 s = angles != nullptr ? *reinterpret_cast<const float2*>(angles + p.rotary / 2 + unit * E + e) : none;
+      cs[e] = c.x, cs[e + 1] = c.y;
+      sn[e] = s.x, sn[e + 1] = s.y;
     }
   }
   const bool norm = part.weight != nullptr;
-  uint4 w[2];  // packed: as floats, a quarter of the registers would be weights
+  Words<W> w[2];  // packed: as floats, a quarter of the registers would be weights
   if (norm && here) {
-    w[0] = *reinterpret_cast<const uint4*>(static_cast<const T*>(part.weight) + a);
-    w[1] = *reinterpret_cast<const uint4*>(static_cast<const T*>(part.weight) + b);
+    w[0].load(static_cast<const T*>(part.weight) + a);
+    w[1].load(static_cast<const T*>(part.weight) + b);
   }
 #pragma unroll
-  for (int n = 0; n < kHeadsPerGroup; ++n) {
+  for (int n = 0; n < kHeads; ++n) {
     const int h = head0 + n * kGroups;
     if (head0 - lane / kLanes + n * kGroups >= part.heads) break;  // the same for the whole warp
     float x[2 * E];
-    Vec<T>::widen_all(raw[n][0], x);
-    Vec<T>::widen_all(raw[n][1], x + E);
+    raw[n][0].template widen_all<T>(x);
+    raw[n][1].template widen_all<T>(x + E);
     if (norm) {
       float sum = 0.0f;
 #pragma unroll
@@ -109,10 +154,10 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
       for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       const float r = rsqrtf(sum / p.dim + p.eps);
       float f[E];
-      Vec<T>::widen_all(w[0], f);
+      w[0].template widen_all<T>(f);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = x[e] * r * f[e];
-      Vec<T>::widen_all(w[1], f);
+      w[1].template widen_all<T>(f);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[E + e] = x[E + e] * r * f[e];
     }
@@ -134,8 +179,11 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
       }
     }
     if (here && h < part.heads) {
-      *reinterpret_cast<uint4*>(row + h * part.out_head + a) = Vec<T>::narrow_all(x);
-      *reinterpret_cast<uint4*>(row + h * part.out_head + b) = Vec<T>::narrow_all(x + E);
+      Words<W> out;
+      out.template narrow_all<T>(x);
+      out.store(row + h * part.out_head + a);
+      out.template narrow_all<T>(x + E);
+      out.store(row + h * part.out_head + b);
     }
   }
 }
@@ -249,39 +297,45 @@ __global__ void document_spans_kernel(const int32_t* q_starts, const int32_t* k_
   }
 }
 
-// Whether every vector of a part, its weight's among them, starts on 16 bytes and is of the data's type.
+// Whether every vector of a part, its weight's among them, starts on `bytes` bytes and is of the data's type.
 template <typename T>
-bool part_aligned(const RotatePart& r) {
-  constexpr int64_t E = Vec<T>::kN;
-  return (r.weight == nullptr || (r.weight_dtype == kCode<T> && aligned_to(r.weight, 16))) && aligned_to(r.in, 16) &&
-         aligned_to(r.out, 16) && r.in_token % E == 0 && r.in_head % E == 0 &&
-         r.out_token % E == 0 && r.out_head % E == 0 && (!r.slotted || r.out_page % E == 0);
+bool part_aligned(const RotatePart& r, int64_t bytes) {
+  const int64_t n = bytes / static_cast<int64_t>(sizeof(T));
+  return (r.weight == nullptr || (r.weight_dtype == kCode<T> && aligned_to(r.weight, bytes))) && aligned_to(r.in, bytes) &&
+         aligned_to(r.out, bytes) && r.in_token % n == 0 && r.in_head % n == 0 && r.out_token % n == 0 &&
+         r.out_head % n == 0 && (!r.slotted || r.out_page % n == 0);
 }
 
-template <typename T, int kLanes>
-void launch_vectors(RotateParams& p, unsigned blocks, cudaStream_t stream) {
-  constexpr int kHeads = kHeadsPerGroup * 32 / kLanes;
+template <typename T, int W, int kLanes>
+void launch_lanes(RotateParams& p, unsigned blocks, cudaStream_t stream) {
+  constexpr int kHeads = 8 / W * 32 / kLanes;
   int slices = 0;
   for (int i = 0; i < p.n_parts; ++i) {
     p.part[i].slice = slices;
     slices += (p.part[i].heads + kHeads - 1) / kHeads;
   }
-  rotate_heads_kernel<T, kLanes><<<dim3(blocks, slices), kRotateThreads, 0, stream>>>(p);
+  rotate_heads_kernel<T, W, kLanes><<<dim3(blocks, slices), kRotateThreads, 0, stream>>>(p);
+}
+
+// By vectors of W words; false where sizes or addresses do not admit them.
+template <typename T, int W>
+bool launch_vectors(RotateParams& p, unsigned blocks, cudaStream_t stream) {
+  constexpr int kUnit = 2 * W * 4 / sizeof(T);  // elements
+  const int units = p.dim / kUnit;
+  bool fits = p.dim % kUnit == 0 && p.rotary % kUnit == 0 && units <= 32 && aligned_to(p.table, 8);
+  for (int i = 0; i < p.n_parts; ++i) fits = fits && part_aligned<T>(p.part[i], W * 4);
+  if (!fits) return false;
+  if (units <= 4) launch_lanes<T, W, 4>(p, blocks, stream);
+  else if (units <= 8) launch_lanes<T, W, 8>(p, blocks, stream);
+  else if (units <= 16) launch_lanes<T, W, 16>(p, blocks, stream);
+  else launch_lanes<T, W, 32>(p, blocks, stream);
+  return true;
 }
 
 template <typename T>
 cudaError_t launch_rotate(RotateParams p, cudaStream_t stream) {
-  constexpr int E = Vec<T>::kN;
   const unsigned blocks = static_cast<unsigned>((p.tokens + kRotateThreads / 32 - 1) / (kRotateThreads / 32));
-  bool vectors = p.dim % (2 * E) == 0 && p.rotary % (2 * E) == 0 && aligned_to(p.table, 16);
-  for (int i = 0; i < p.n_parts; ++i) vectors = vectors && part_aligned<T>(p.part[i]);
-  if (vectors) {
-    const int units = p.dim / (2 * E);
-    if (units <= 4) launch_vectors<T, 4>(p, blocks, stream);
-    else if (units <= 8) launch_vectors<T, 8>(p, blocks, stream);
-    else if (units <= 16) launch_vectors<T, 16>(p, blocks, stream);
-    else launch_vectors<T, 32>(p, blocks, stream);
-  } else {
+  if (!launch_vectors<T, 4>(p, blocks, stream) && !launch_vectors<T, 2>(p, blocks, stream)) {
     int heads = 0;
     for (int i = 0; i < p.n_parts; ++i) {
       p.part[i].slice = heads;

@@ -56,13 +56,42 @@ __device__ __forceinline__ void take(const float* x, float& top, float& sum) {
   }
 }
 
+// n logits from x on by kThreads threads: 16-byte vectors between the boundaries, the ends one by one.
+template <typename T, int kThreads>
+__device__ __forceinline__ void row_tail(const T* x, int n, int tid, float& top, float& sum) {
+  constexpr int E = Vec<T>::kN;
+  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
+  const int head = min(off ? E - off : 0, n), vectors = (n - head) / E, tail = head + vectors * E;
+  if (tid < head) {
+    const float one = widen(x[tid]);
+    take<1>(&one, top, sum);
+  }
+  if (tid < n - tail) {
+    const float one = widen(x[tail + tid]);
+    take<1>(&one, top, sum);
+  }
+  const uint4* v = reinterpret_cast<const uint4*>(x + head);
+  const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
+  for (int i = tid; i < vectors; i += kLossVectors * kThreads) {
+    uint4 raw[kLossVectors];
+#pragma unroll
+    for (int k = 0; k < kLossVectors; ++k) {
+      raw[k] = make_uint4(none, none, none, none);
+      if (i + k * kThreads < vectors) raw[k] = __ldcs(v + i + k * kThreads);
+    }
+    float f[kLossVectors * E];
+#pragma unroll
+    for (int k = 0; k < kLossVectors; ++k) Vec<T>::widen_all(raw[k], f + k * E);
+    take<kLossVectors * E>(f, top, sum);
+  }
+}
+
 // A token per CTA, or per cluster of CTAs that split the vocabulary where there
 // are fewer tokens than the SMs hold CTAs. One pass with the running maximum
 // and sum in registers; bound by HBM: each counted row is read once.
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads, kLossCtas)
     token_loss_kernel(const __grid_constant__ TokenLossParams p, int parts) {
-  constexpr int E = Vec<T>::kN;
   __shared__ float tops[kLossThreads / 32];
   __shared__ double sums[kLossThreads / 32];
   __shared__ float part_top;
@@ -80,32 +109,8 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   }
   const T* x = static_cast<const T*>(p.logits) + t * p.row;
   const int64_t from = p.vocab * rank / parts, to = p.vocab * (rank + 1) / parts;
-  const int64_t off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(x + from) % 16) / sizeof(T);
-  const int64_t head = min(from + (off ? E - off : 0), to), vectors = (to - head) / E;
-  float top = -3.402823466e38f, sum = 0.0f;
-  if (tid < head - from) {
-    const float one = widen(x[from + tid]);
-    take<1>(&one, top, sum);
-  }
-  if (tid < to - head - vectors * E) {
-    const float one = widen(x[head + vectors * E + tid]);
-    take<1>(&one, top, sum);
-  }
-  const uint4* v = reinterpret_cast<const uint4*>(x + head);
-  const int n = static_cast<int>(vectors);
-  const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
-  for (int i = tid; i < n; i += kLossVectors * kLossThreads) {
-    uint4 raw[kLossVectors];
-#pragma unroll
-    for (int k = 0; k < kLossVectors; ++k) {
-      raw[k] = make_uint4(none, none, none, none);
-      if (i + k * kLossThreads < n) raw[k] = __ldcs(v + i + k * kLossThreads);
-    }
-    float f[kLossVectors * E];
-#pragma unroll
-    for (int k = 0; k < kLossVectors; ++k) Vec<T>::widen_all(raw[k], f + k * E);
-    take<kLossVectors * E>(f, top, sum);
-  }
+  float top = kNone.top, sum = 0.0f;
+  row_tail<T, kLossThreads>(x + from, static_cast<int>(to - from), tid, top, sum);
   Tail mine = lanes_join<32>({top, sum});
   if ((tid & 31) == 0) {
     tops[tid >> 5] = mine.top;
@@ -135,6 +140,33 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   }
   if (rank == 0 && tid == 0) {
     const double nll = log(mine.sum) + (static_cast<double>(mine.top) - widen(x[target]));
+    p.rows[t] = nll;
+    if (p.nll != nullptr) p.nll[t] = static_cast<float>(nll);
+  }
+}
+
+// A token per warp, for small vocabularies: a CTA per token would come and go in more time than its row takes (4000 rows
+// of 2001, fp16: 41 us).
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) token_loss_warp_kernel(const __grid_constant__ TokenLossParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kLossThreads / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (t >= p.tokens) return;
+  const int64_t target = load_index(p.targets, t, p.target64);
+  if (target < 0 || target >= p.vocab) {
+    if (lane == 0) {
+      p.rows[t] = target < 0 ? 0.0 : NAN;
+      if (p.nll != nullptr) p.nll[t] = target < 0 ? 0.0f : NAN;
+    }
+    return;
+  }
+  const T* x = static_cast<const T*>(p.logits) + t * p.row;
+  float top = kNone.top, sum = 0.0f;
+  row_tail<T, 32>(x, static_cast<int>(p.vocab), lane, top, sum);
+  const Tail all = lanes_join<32>({top, sum});
+  if (lane == 0) {
+    const double nll = log(all.sum) + (static_cast<double>(all.top) - widen(x[target]));
     p.rows[t] = nll;
     if (p.nll != nullptr) p.nll[t] = static_cast<float>(nll);
   }
@@ -193,6 +225,13 @@ cudaError_t launch_with(F f, unsigned grid, unsigned threads, cudaLaunchAttribut
 
 template <typename T>
 cudaError_t launch_rows(const TokenLossParams& p, int sms, cudaStream_t stream) {
+  if (p.vocab <= 4096) {
+    constexpr int kRows = kLossThreads / 32;
+    token_loss_warp_kernel<T><<<static_cast<unsigned>((p.tokens + kRows - 1) / kRows), kLossThreads, 0, stream>>>(p);
+    return cudaGetLastError();
+  }
+  // as many parts as the SMs hold at once (100 rows of 151936, bf16: in 4 parts 12.8 us, in 8, two rounds, 17.5; 800 rows,
+  // fp32: in one part 77 us, in two 89), none with less than 4096 logits
   int parts = 1;
   while (parts < kMaxParts && p.tokens * parts * 2 <= kLossCtas * sms && p.vocab / (parts * 2) >= 4096) parts *= 2;
   cudaLaunchAttribute attr = {};
