@@ -32,22 +32,32 @@ bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int head
 
 namespace {
 
-constexpr int kRows = 128;           // query rows of a slot, keys of a load
+constexpr int kRows = 128;           // query rows of a slot
 constexpr int kKeys = 64;            // keys of a step
-constexpr int kMmaThreads = 384;
-constexpr int kSoftmaxWarps = 8;
-constexpr int kChunk = kRows * 128;  // bytes of 64 elements of 128 rows
+constexpr int kChunk = kRows * 128;  // bytes of 64 elements of a slot's queries
 constexpr float kSlack = 8.0f;       // log2: how far scores may pass the reference before the output is rescaled
 
-template <int D>
+// A CTA of two slots, one per SM, with keys and values by 128; or of one slot, two per SM, with keys and values by 64.
+template <int D, int kSlots>
 struct Plan {
-  static constexpr int kTile = D / 64 * kChunk;     // bytes of a tile of queries, keys or values
-  static constexpr int kStages = D == 128 ? 5 : 8;  // tiles of keys and values in turn
-  static constexpr int kBytes = (2 + kStages) * kTile + 1024;
+  static constexpr int kSteps = kSlots;                          // of a tile of keys and values
+  static constexpr int kQueries = D / 64 * kChunk;               // bytes of a slot's queries
+  static constexpr int kTileChunk = kSteps * kKeys * 128;        // bytes of 64 elements of a tile
+  static constexpr int kTile = D / 64 * kTileChunk;
+  static constexpr int kStages = kSlots == 1 ? 4 : D == 128 ? 5 : 8;  // tiles of keys and values in turn
+  static constexpr int kBytes = kSlots * kQueries + kStages * kTile + 1024;
+  static constexpr int kSoftmaxWarps = 4 * kSlots;
+  static constexpr int kThreads = kSlots == 1 ? 256 : 384;
+  static constexpr int kColumns = 256 * kSlots;                  // of tensor memory
+  static constexpr int kOutputs = 128 * kSlots;                  // the first column of the outputs
 };
 
+// Barriers of steps come in pairs, for even and odd steps. A wait by parity is sound while the barrier can be at most one
+// phase past the one waited for, and each of these cannot reach its next phase before the waiter has done its part: scores
+// c + 2 follow the weights c, weights c + 2 the scores c + 2, outputs c + 2 the weights c + 2, and a stage's next load
+// follows both slots' use of it. (One barrier for a slot's outputs could be two phases ahead of the last wait.)
 struct MmaShared {
-  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2][2], p_full[2][2], o_done[2], drain[2];
+  uint64_t q_full, kv_full[8], kv_empty[8], s_full[2][2], p_full[2][2], o_done[2][2], drain[2];
   int lo[2], hi[2];
   uint32_t tmem;
   int dead;
@@ -82,28 +92,32 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xFFFFF
 // The output is rescaled only when a row's maximum has passed the reference that
 // its weights are relative to by 2^8, which seldom happens after the first steps:
 // weights up to 256 lose nothing in 16 bits and their sum is fp32.
-template <typename T, int D, bool kCap, bool kBias>
-__global__ void __launch_bounds__(kMmaThreads, 1)
+template <typename T, int D, int kSlots, bool kCap, bool kBias>
+__global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     attention_mma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                          const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap o_map,
                          const __grid_constant__ AttentionParams p, int by_heads) {
-  using L = Plan<D>;
+  using L = Plan<D, kSlots>;
+  constexpr int kSoftmaxWarps = L::kSoftmaxWarps;
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
   extern __shared__ uint8_t raw[];
   __shared__ MmaShared sh;
   uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // queries of both slots, then the stages
-  uint8_t* stages = tiles + 2 * L::kTile;
+  uint8_t* stages = tiles + kSlots * L::kQueries;
   const int tid = threadIdx.x, warp = static_cast<int>(uniform(tid >> 5)), lane = tid & 31;
-  const int per = by_heads ? p.heads / 2 : p.heads;  // CTAs per tile of rows; the longest causal rows come first
-  const int item = blockIdx.x % per, block = gridDim.x / per - 1 - blockIdx.x / per;
-  const int head0 = by_heads ? item * 2 : item, kv_head = head0 / p.group;
+  const int heads_here = kSlots == 2 && by_heads ? 2 : 1, tiles_here = kSlots / heads_here;  // heads, tiles of rows
+  const int per = p.heads / heads_here;  // CTAs per tile of rows; the longest causal rows come first
+  const int item = blockIdx.x % per, block = (gridDim.x / per - 1 - blockIdx.x / per) * tiles_here;
+  const int head0 = item * heads_here, kv_head = head0 / p.group;
+  const auto head_of = [&](int s) { return heads_here == 2 ? head0 + s : head0; };
+  const auto block_of = [&](int s) { return tiles_here == 2 ? block + s : block; };
   volatile int* dead = &sh.dead;
 
   int64_t row = 0;
   int lo = 0, hi = 0, self = 0;
   const int slot = warp >> 2;
   if (warp < kSoftmaxWarps) {
-    row = (by_heads ? block : 2 * static_cast<int64_t>(block) + slot) * kRows + (tid & 127);
+    row = static_cast<int64_t>(block_of(slot)) * kRows + (tid & 127);
     if (row < p.q_tokens) {
       lo = max(p.spans[row], 0);
       hi = min(p.spans[p.q_tokens + row], static_cast<int>(p.k_tokens));
@@ -111,18 +125,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
     if (hi <= lo) lo = hi = 0;
   }
-  if (tid == (kSoftmaxWarps + 3) * 32) {
+  if (tid == (kSoftmaxWarps + kSlots + 1) * 32) {
     mbar_init(&sh.q_full, 1);
     for (int i = 0; i < L::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
-      mbar_init(&sh.kv_empty[i], 2);
+      mbar_init(&sh.kv_empty[i], kSlots);
     }
     for (int s = 0; s < 2; ++s) {
       for (int b = 0; b < 2; ++b) {
         mbar_init(&sh.s_full[s][b], 1);
         mbar_init(&sh.p_full[s][b], 4);
+        mbar_init(&sh.o_done[s][b], 1);
       }
-      mbar_init(&sh.o_done[s], 1);
       mbar_init(&sh.drain[s], 1);
       sh.lo[s] = 0x7FFFFFFF;
       sh.hi[s] = 0;
@@ -130,20 +144,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, 512);
-  if (tid == (kSoftmaxWarps + 2) * 32) {
+  if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, L::kColumns);
+  if (tid == (kSoftmaxWarps + kSlots) * 32) {
     prefetch_map(&q_map);
     prefetch_map(&k_map);
     prefetch_map(&v_map);
     prefetch_map(&o_map);
   }
   __syncthreads();
-  if (tid == (kSoftmaxWarps + 2) * 32) {  // the queries, before the spans are known
-    mbar_expect(&sh.q_full, 2 * L::kTile);
-    for (int s = 0; s < 2; ++s)
+  if (tid == (kSoftmaxWarps + kSlots) * 32) {  // the queries, before the spans are known
+    mbar_expect(&sh.q_full, kSlots * L::kQueries);
+    for (int s = 0; s < kSlots; ++s)
       for (int c = 0; c < D / 64; ++c)
-        tma_load_3d(tiles + s * L::kTile + c * kChunk, &q_map, c * 64, by_heads ? head0 + s : head0,
-                    (by_heads ? block : 2 * block + s) * kRows, &sh.q_full);
+        tma_load_3d(tiles + s * L::kQueries + c * kChunk, &q_map, c * 64, head_of(s), block_of(s) * kRows, &sh.q_full);
   }
   if (warp < kSoftmaxWarps) {
     const int least = __reduce_min_sync(0xFFFFFFFFu, hi > lo ? lo : 0x7FFFFFFF);
@@ -157,12 +170,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = uniform(sh.tmem);
-  const int begin = static_cast<int>(uniform(min(sh.lo[0], sh.lo[1])));
-  const int stop = static_cast<int>(uniform(max(sh.hi[0], sh.hi[1])));
+  const int begin = static_cast<int>(uniform(min(sh.lo[0], sh.lo[kSlots - 1])));
+  const int stop = static_cast<int>(uniform(max(sh.hi[0], sh.hi[kSlots - 1])));
   const int n = stop > begin ? (stop - begin + kKeys - 1) / kKeys : 0;  // steps
-  int from[2], to[2];                                                   // those that a slot sees
+  int from[kSlots], to[kSlots];                                         // those that a slot sees
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < kSlots; ++s) {
     from[s] = to[s] = 0;
     if (sh.hi[s] > sh.lo[s]) {
       from[s] = static_cast<int>(uniform((sh.lo[s] - begin) / kKeys));
@@ -170,16 +183,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
   }
 
-  if (warp == kSoftmaxWarps + 2) {
+  if (warp == kSoftmaxWarps + kSlots) {
     if (lane == 0) {
       int issued = 0;
-      for (int i = 0; i < (n + 1) / 2 * 2; ++i) {  // keys 0, values 0, keys 1, ...
+      for (int i = 0; i < (n + L::kSteps - 1) / L::kSteps * 2; ++i) {  // keys 0, values 0, keys 1, ...
         const int stage = i % L::kStages;
         if (i >= L::kStages && !mbar_wait(&sh.kv_empty[stage], (i / L::kStages - 1) & 1, dead)) break;
         mbar_expect(&sh.kv_full[stage], L::kTile);
         for (int c = 0; c < D / 64; ++c)
-          tma_load_3d(stages + stage * L::kTile + c * kChunk, i % 2 == 0 ? &k_map : &v_map, c * 64, kv_head,
-                      begin + (i / 2) * kRows, &sh.kv_full[stage]);
+          tma_load_3d(stages + stage * L::kTile + c * L::kTileChunk, i % 2 == 0 ? &k_map : &v_map, c * 64, kv_head,
+                      begin + (i / 2) * L::kSteps * kKeys, &sh.kv_full[stage]);
         ++issued;
       }
       if (*dead) {  // nothing may land in shared memory after the CTA is gone
@@ -189,20 +202,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         while (!mbar_try(&sh.q_full, 0) && clock64() - start < kWaitCycles) {}
       }
     }
-  } else if (warp == kSoftmaxWarps || warp == kSoftmaxWarps + 1) {
-    const int s = warp - kSoftmaxWarps, first = s ? from[1] : from[0], last = s ? to[1] : to[0];
+  } else if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kSlots) {
+    const int s = warp - kSoftmaxWarps;
+    const int first = s ? from[kSlots - 1] : from[0], last = s ? to[kSlots - 1] : to[0];
     const uint32_t at = uniform(smem_address(stages));
-    const uint64_t queries = operand_desc(uniform(smem_address(tiles)) + s * L::kTile, 16, 1024);
-    const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, kChunk, 1024);
+    const uint64_t queries = operand_desc(uniform(smem_address(tiles)) + s * L::kQueries, 16, 1024);
+    const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, L::kTileChunk, 1024);
     constexpr uint32_t kScores = mma_desc(kBf16, kKeys, false), kOutput = mma_desc(kBf16, D, true);
-    constexpr uint32_t kHalf = kKeys * 128;  // bytes from a tile's first 64 rows to its last
-    const uint32_t scores = tmem + s * 128, out = tmem + 256 + s * D;
+    constexpr uint32_t kHalf = kKeys * 128;  // bytes from a tile's first step to its second
+    const uint32_t scores = tmem + s * 128, out = tmem + L::kOutputs + s * D;
     const auto scores_of = [&](int j, uint64_t k) {  // of step j, its keys at k
       const int b = (j - first) & 1;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
-        mma_ss(scores + b * kKeys, queries + (d / 4 * kChunk + d % 4 * 32) / 16, k + (d / 4 * kChunk + d % 4 * 32) / 16,
-               kScores, d > 0);
+        mma_ss(scores + b * kKeys, queries + (d / 4 * kChunk + d % 4 * 32) / 16,
+               k + (d / 4 * L::kTileChunk + d % 4 * 32) / 16, kScores, d > 0);
       mma_commit(&sh.s_full[s][b]);
     };
     // Tile t's keys are the loads' 2 t, its values 2 t + 1. The stages and parities of tile t's values and tile t + 1's keys:
@@ -216,29 +230,39 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     };
     bool alive = n == 0 || mbar_wait_warp(&sh.q_full, 0, dead);
     if (n > 0 && alive) alive = mbar_wait_warp(&sh.kv_full[0], 0, dead);
-    if (n > 0 && alive && elect_one()) {  // the first two steps' scores
+    // The first two steps' scores: both of the first tile, or with a step per tile the first here and the second in front of
+    // the loop, which then has the stages of step i's values and of step i + 2's keys.
+    if (n > 0 && alive && elect_one()) {
       if (first == 0 && last > 0) scores_of(0, keys);
-      if (first <= 1 && last > 1) scores_of(1, keys + kHalf / 16);
+      if (L::kSteps == 2 && first <= 1 && last > 1) scores_of(1, keys + kHalf / 16);
       mma_commit(&sh.kv_empty[0]);
     }
+    if (L::kSteps == 1 && n > 1 && alive) {
+      alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
+      if (alive && elect_one()) {
+        if (first <= 1 && last > 1) scores_of(1, keys + static_cast<uint32_t>(k_stage) * L::kTile / 16);
+        mma_commit(&sh.kv_empty[k_stage]);
+      }
+      advance(k_stage, k_parity);
+    }
     for (int i = 0; i < n && alive; ++i) {  // step i's output, and step i + 2's scores in the place of step i's
-      const bool more = i / 2 * 2 + 2 < n;  // there is another tile
-      if (i % 2 == 0) {
+      const bool more = i / L::kSteps * L::kSteps + 2 < n;  // there is a tile of step i + 2
+      if (i % L::kSteps == 0) {
         if (i > 0) {
           advance(v_stage, v_parity);
           advance(k_stage, k_parity);
         }
         alive = mbar_wait_warp(&sh.kv_full[v_stage], v_parity, dead);
-        if (alive && more) alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
+        if (L::kSteps == 2 && alive && more) alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
         if (!alive) break;
-        const int rest = stop - (begin + i * kKeys), used = min(kRows, (n - i) * kKeys);
+        const int rest = stop - (begin + i * kKeys), used = min(L::kSteps, n - i) * kKeys;
         if (rest < used && stop < p.k_tokens) {
           // keys that no row sees (TMA gives zeros only beyond the last of all): their weight is 0, and 0 times what is
           // there has to be 0. A row's 16-byte vectors are swizzled among themselves.
           uint8_t* v = stages + v_stage * L::kTile + lane % 8 * 16;
           for (int r = rest + lane / 8; r < used; r += 4)
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(v + c * kChunk + r * 128) = make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(v + c * L::kTileChunk + r * 128) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
@@ -250,17 +274,22 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         if (!alive) break;
       }
       tmem_fence_after();
-      const uint64_t v = values + (static_cast<uint32_t>(v_stage) * L::kTile + i % 2 * kHalf) / 16;
-      const uint64_t k = keys + (static_cast<uint32_t>(k_stage) * L::kTile + i % 2 * kHalf) / 16;
+      const uint64_t v = values + (static_cast<uint32_t>(v_stage) * L::kTile + i % L::kSteps * kHalf) / 16;
+      const uint64_t k = keys + (static_cast<uint32_t>(k_stage) * L::kTile + i % L::kSteps * kHalf) / 16;
       if (elect_one()) {
         if (mine) {
           mma_ts(out, scores + b * kKeys, v, kOutput, c > 0);
 #pragma unroll
           for (int d = 1; d < kKeys / 16; ++d) mma_ts(out, scores + b * kKeys + d * 8, v + d * (2048 / 16), kOutput, true);
-          mma_commit(&sh.o_done[s]);
+          mma_commit(&sh.o_done[s][b]);
         }
+      }
+      // with four short tiles, step i + 2's keys may still be on their way
+      if (L::kSteps == 1 && more) alive = mbar_wait_warp(&sh.kv_full[k_stage], k_parity, dead);
+      if (!alive) break;
+      if (elect_one()) {
         if (i + 2 >= first && i + 2 < last) scores_of(i + 2, k);
-        if (i % 2 == 1 || i == n - 1) {
+        if (i % L::kSteps == L::kSteps - 1 || i == n - 1) {
           mma_commit(&sh.kv_empty[v_stage]);
           if (more) mma_commit(&sh.kv_empty[k_stage]);
         }
@@ -274,8 +303,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
     __syncwarp();
   } else if (warp < kSoftmaxWarps) {
-    const int h = by_heads ? head0 + slot : head0;
-    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + 256 + slot * D;
+    const int h = head_of(slot);
+    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + L::kOutputs + slot * D;
     const float scale2 = kCap ? p.scale / p.softcap : p.scale * kLog2e;
     const float cap2 = p.softcap * kLog2e, slope2 = kBias ? p.slopes[h] * kLog2e : 0.0f;
     const int steps = to[slot] - from[slot];
@@ -326,8 +355,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (__any_sync(0xFFFFFFFFu, moved)) {
         const float back = moved ? exp2_approx(base - top) : 1.0f;
         total *= back;
-        // the step before is in the output (the one before that is: these scores were issued behind it)
-        alive = mbar_wait_warp(&sh.o_done[slot], (c - 1) & 1, dead);
+        // the step before is in the output
+        alive = mbar_wait_warp(&sh.o_done[slot][b ^ 1], (c - 1) >> 1 & 1, dead);
         if (!alive) break;
         tmem_fence_after();
 #pragma unroll
@@ -366,17 +395,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
     const bool any = steps > 0;
     if (!any) alive = mbar_wait_warp(&sh.q_full, 0, dead);  // the queries' place is written below
-    // The last scores were issued behind the output's step before the last but one: a wait by parity for the last alone
-    // could be met by that one.
-    if (alive && steps > 1) alive = mbar_wait_warp(&sh.o_done[slot], (steps - 2) & 1, dead);
-    if (alive && any) alive = mbar_wait_warp(&sh.o_done[slot], (steps - 1) & 1, dead);
+    if (alive && any) alive = mbar_wait_warp(&sh.o_done[slot][(steps - 1) & 1], (steps - 1) >> 1 & 1, dead);
     tmem_fence_after();
     const bool seen = alive && any && total != 0.0f;
     const float over = seen ? 1.0f / total : 0.0f;
     bool finite = !seen || total < kInf;
     // Through shared memory, in the place of the slot's queries: a warp's rows of 64 elements as TMA stores them (rows
     // apart in memory, a thread's own stores took 3 us).
-    const uint32_t mine = smem_address(tiles + slot * L::kTile) + (warp & 3) * 32 * 128;
+    const uint32_t mine = smem_address(tiles + slot * L::kQueries) + (warp & 3) * 32 * 128;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[32];
@@ -425,31 +451,43 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __syncthreads();
   if (warp == kSoftmaxWarps) {
     tmem_fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, L::kColumns);
   }
 }
 
-template <typename T, int D, bool kCap, bool kBias>
+template <typename T, int D, int kSlots, bool kCap, bool kBias>
 cudaError_t launch_kind(const CUtensorMap (&m)[4], const AttentionParams& p, cudaStream_t stream) {
-  using L = Plan<D>;
-  const auto kernel = attention_mma_kernel<T, D, kCap, kBias>;
+  using L = Plan<D, kSlots>;
+  const auto kernel = attention_mma_kernel<T, D, kSlots, kCap, kBias>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (e != cudaSuccess) return e;
   const int by_heads = p.group % 2 == 0;
-  const int64_t rows = by_heads ? kRows : 2 * kRows;
-  const int64_t grid = (p.q_tokens + rows - 1) / rows * (by_heads ? p.heads / 2 : p.heads);
-  kernel<<<static_cast<unsigned>(grid), kMmaThreads, L::kBytes, stream>>>(m[0], m[1], m[2], m[3], p, by_heads);
+  const int heads_here = kSlots == 2 && by_heads ? 2 : 1;
+  const int64_t rows = kRows * (kSlots / heads_here);
+  const int64_t grid = (p.q_tokens + rows - 1) / rows * (p.heads / heads_here);
+  kernel<<<static_cast<unsigned>(grid), L::kThreads, L::kBytes, stream>>>(m[0], m[1], m[2], m[3], p, by_heads);
   return cudaGetLastError();
 }
 
-template <typename T, int D>
-cudaError_t launch_head(const CUtensorMap (&m)[4], const AttentionParams& p, cudaStream_t stream) {
+template <typename T, int D, int kSlots>
+cudaError_t launch_slots(const CUtensorMap (&m)[4], const AttentionParams& p, cudaStream_t stream) {
   if (p.softcap > 0.0f)
-    return p.slopes != nullptr ? launch_kind<T, D, true, true>(m, p, stream)
-                               : launch_kind<T, D, true, false>(m, p, stream);
-  return p.slopes != nullptr ? launch_kind<T, D, false, true>(m, p, stream)
-                             : launch_kind<T, D, false, false>(m, p, stream);
+    return p.slopes != nullptr ? launch_kind<T, D, kSlots, true, true>(m, p, stream)
+                               : launch_kind<T, D, kSlots, true, false>(m, p, stream);
+  return p.slopes != nullptr ? launch_kind<T, D, kSlots, false, true>(m, p, stream)
+                             : launch_kind<T, D, kSlots, false, false>(m, p, stream);
 }
+
+template <typename T>
+cudaError_t launch_head(const CUtensorMap (&m)[4], const AttentionParams& p, bool two, cudaStream_t stream) {
+  if (p.dim <= 64) return two ? launch_slots<T, 64, 2>(m, p, stream) : launch_slots<T, 64, 1>(m, p, stream);
+  return two ? launch_slots<T, 128, 2>(m, p, stream) : launch_slots<T, 128, 1>(m, p, stream);
+}
+
+// Whether a CTA takes two slots. The spans are on the device, so this goes by the keys there are: two CTAs of one slot per
+// SM hide each other's starts and ends (one document of 512 tokens 10.1 against 11.8 us, of 1024 18.8 / 17.2; 24 of at most
+// 256 24.9 / 28.7), two slots share their keys' tiles and issue ahead (one of 2048 tokens 40 / 32 us, of 8192 476 / 335).
+bool two_slots(const AttentionParams& p) { return p.k_tokens > 768; }
 
 }  // namespace
 
@@ -467,16 +505,14 @@ bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stre
       !vectors(p.out, p.out_token, p.out_head, p.q_tokens, p.heads))
     return false;
   CUtensorMap m[4];
-  const bool bf16 = dtype == 1;
+  const bool bf16 = dtype == 1, two = two_slots(p);
+  const int keys = two ? 2 * kKeys : kKeys;
   if (!make_head_map(&m[0], bf16, p.q, p.dim, p.heads, p.q_tokens, p.q_head, p.q_token, kRows) ||
-      !make_head_map(&m[1], bf16, p.k, p.dim, kv_heads, p.k_tokens, p.k_head, p.k_token, kRows) ||
-      !make_head_map(&m[2], bf16, p.v, p.dim, kv_heads, p.k_tokens, p.v_head, p.v_token, kRows) ||
+      !make_head_map(&m[1], bf16, p.k, p.dim, kv_heads, p.k_tokens, p.k_head, p.k_token, keys) ||
+      !make_head_map(&m[2], bf16, p.v, p.dim, kv_heads, p.k_tokens, p.v_head, p.v_token, keys) ||
       !make_head_map(&m[3], bf16, p.out, p.dim, p.heads, p.q_tokens, p.out_head, p.out_token, 32))
     return false;
-  if (bf16)
-    *e = p.dim <= 64 ? launch_head<__nv_bfloat16, 64>(m, p, stream) : launch_head<__nv_bfloat16, 128>(m, p, stream);
-  else
-    *e = p.dim <= 64 ? launch_head<__half, 64>(m, p, stream) : launch_head<__half, 128>(m, p, stream);
+  *e = bf16 ? launch_head<__nv_bfloat16>(m, p, two, stream) : launch_head<__half>(m, p, two, stream);
   return true;
 }
 

@@ -208,3 +208,21 @@ def test_few_rows_many_keys(dtype, tokens, keys):
         if tokens > 40:
             spans[1, 64:] = 0
             compare(q, k, v, spans)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=IDS[:2])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("docs,longest", [(6, 120), (1, 700), (8, 300), (3, 1000)])
+def test_many_launches_agree(dtype, dim, docs, longest):
+    """Many CTAs per SM, launch after launch on other data in between: the same bits every time, and none that a wait gave
+    up on (those are NaN)."""
+    g = gen(docs + dim)
+    lengths = [longest - (37 * i) % (longest // 2) for i in range(docs)]
+    t = sum(lengths)
+    spans = F.document_spans(starts(lengths), tokens=t)
+    sets = [[randn(g, t, 32, dim, dtype=dtype) for _ in range(3)] for _ in range(2)]
+    want = [compare(*x, spans)[0] for x in sets]
+    outs = [torch.empty_like(sets[0][0]) for _ in range(40)]
+    for i, out in enumerate(outs):
+        F.attention(*sets[i % 2], spans, out=out)
+    assert all(torch.equal(out, want[i % 2]) for i, out in enumerate(outs))
