@@ -39,6 +39,29 @@ __device__ __forceinline__ float weight_at(const RotatePart& part, int i) {
 template <typename T>
 constexpr int kCode = sizeof(T) == 4 ? 0 : __is_same(T, __nv_bfloat16) ? 1 : 2;  // zo_dtype
 
+// Two values: in one register pair for 16-bit types, whose instructions on two values at once halve what bounds them, and
+// as two for fp32, where the pairs' aligned registers would spill (130 against 161 us, 20000 tokens of 40 heads of 128).
+template <typename T>
+struct PairOf {
+  using type = uint64_t;
+};
+template <>
+struct PairOf<float> {
+  using type = float2;
+};
+__device__ __forceinline__ void set(uint64_t& p, float a, float b) { p = pack2(a, b); }
+__device__ __forceinline__ void set(float2& p, float a, float b) { p = make_float2(a, b); }
+__device__ __forceinline__ float lower(uint64_t p) { return low2(p); }
+__device__ __forceinline__ float lower(float2 p) { return p.x; }
+__device__ __forceinline__ float upper(uint64_t p) { return high2(p); }
+__device__ __forceinline__ float upper(float2 p) { return p.y; }
+__device__ __forceinline__ uint64_t times(uint64_t a, uint64_t b) { return mul2(a, b); }
+__device__ __forceinline__ float2 times(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ uint64_t times_plus(uint64_t a, uint64_t b, uint64_t c) { return fma2(a, b, c); }
+__device__ __forceinline__ float2 times_plus(float2 a, float2 b, float2 c) {
+  return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y));
+}
+
 // W words of 4 bytes in one load, W = 4 or 2.
 template <int W>
 struct Words {
@@ -57,30 +80,45 @@ struct Words {
     else *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   }
   template <typename T>
-  __device__ __forceinline__ void widen_all(float* f) const {
+  __device__ __forceinline__ void widen_all(typename PairOf<T>::type* f) const {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       if constexpr (sizeof(T) == 4) {
-        f[i] = __uint_as_float(w[i]);
+        if (i % 2 == 0) set(f[i / 2], __uint_as_float(w[i]), __uint_as_float(w[i + 1]));
       } else if constexpr (__is_same(T, __nv_bfloat16)) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        f[i] = static_cast<uint64_t>(w[i] & 0xFFFF0000u) << 32 | w[i] << 16;
       } else {
         const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        f[2 * i] = g.x;
-        f[2 * i + 1] = g.y;
+        set(f[i], g.x, g.y);
       }
     }
   }
   template <typename T>
-  __device__ __forceinline__ void narrow_all(const float* f) {
+  __device__ __forceinline__ void narrow_all(const typename PairOf<T>::type* f) {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
-      else w[i] = narrow2<T>(f[2 * i], f[2 * i + 1]);
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(i % 2 ? upper(f[i / 2]) : lower(f[i / 2]));
+      else w[i] = narrow2<T>(lower(f[i]), upper(f[i]));
     }
   }
 };
+
+// A lane's E angles as pairs.
+template <int E, typename P>
+__device__ __forceinline__ void load_angles(const float* at, P* f) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    if constexpr (E >= 8) {
+      if (e % 4 != 0) continue;
+      const float4 v = *reinterpret_cast<const float4*>(at + e);
+      set(f[e / 2], v.x, v.y);
+      set(f[e / 2 + 1], v.z, v.w);
+    } else {
+      const float2 v = *reinterpret_cast<const float2*>(at + e);
+      set(f[e / 2], v.x, v.y);
+    }
+  }
+}
 
 // A head lies on kLanes lanes, each with a unit of two vectors of W words: the
 // two halves of its pairs (layout half), or neighbours (interleaved, and what is
@@ -88,9 +126,9 @@ struct Words {
 // and sines at E times its number in both layouts. W is 4, or 2 where the size or
 // the rotated part leaves a half vector. A warp takes kHeads heads of each of its
 // groups of lanes; angles and weight are loaded once for them. Bound by HBM: 2
-// bytes in and 2 out per 16-bit element (50001 tokens of 80 heads of 128, fp16:
-// 361 us = 5.7 TB/s; two heads of 16-byte vectors per group of lanes 361, four on
-// fewer CTAs 365, one 521).
+// bytes in and 2 out per 16-bit element, and by its instructions (50001 tokens of
+// 80 heads of 128, fp16: 350 us = 5.9 TB/s; before the arithmetic by pairs of fp32
+// values 361, with four heads per group of lanes on fewer CTAs 365, with one 521).
 template <typename T, int W, int kLanes>
 __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
   constexpr int E = W * 4 / sizeof(T);
@@ -121,16 +159,19 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
       raw[n][1].load(in + h * part.in_head + b);
     }
   }
-  float cs[E], sn[E];
+  using P = typename PairOf<T>::type;
+  P cs[E / 2], sn[E / 2];
   if (turned) {
     const float* angles = table_row(p, t);
+    if (angles == nullptr) {
 #pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const float2 none = make_float2(NAN, NAN);
-      const float2 c = angles != nullptr ? *reinterpret_cast<const float2*>(angles + unit * E + e) : none;
-      const float2 s = angles != nullptr ? *reinterpret_cast<const float2*>(angles + p.rotary / 2 + unit * E + e) : none;
-      cs[e] = c.x, cs[e + 1] = c.y;
-      sn[e] = s.x, sn[e + 1] = s.y;
+      for (int e = 0; e < E / 2; ++e) {
+        set(cs[e], NAN, NAN);
+        set(sn[e], NAN, NAN);
+      }
+    } else {
+      load_angles<E>(angles + unit * E, cs);
+      load_angles<E>(angles + p.rotary / 2 + unit * E, sn);
     }
   }
   const bool norm = part.weight != nullptr;
@@ -143,38 +184,43 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
   for (int n = 0; n < kHeads; ++n) {
     const int h = head0 + n * kGroups;
     if (head0 - lane / kLanes + n * kGroups >= part.heads) break;  // the same for the whole warp
-    float x[2 * E];
+    P x[E];
     raw[n][0].template widen_all<T>(x);
-    raw[n][1].template widen_all<T>(x + E);
+    raw[n][1].template widen_all<T>(x + E / 2);
     if (norm) {
-      float sum = 0.0f;
+      P sums = times(x[0], x[0]);
 #pragma unroll
-      for (int e = 0; e < 2 * E; ++e) sum = fmaf(x[e], x[e], sum);
+      for (int e = 1; e < E; ++e) sums = times_plus(x[e], x[e], sums);
+      float sum = lower(sums) + upper(sums);
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       const float r = rsqrtf(sum / p.dim + p.eps);
-      float f[E];
+      P both, f[E];
+      set(both, r, r);
       w[0].template widen_all<T>(f);
+      w[1].template widen_all<T>(f + E / 2);
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = x[e] * r * f[e];
-      w[1].template widen_all<T>(f);
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[E + e] = x[E + e] * r * f[e];
+      for (int e = 0; e < E; ++e) x[e] = times(x[e], times(both, f[e]));
     }
     if (turned) {
+      P flip;  // a sine's signs for a pair's two elements, or for two pairs' first ones
+      set(flip, -1.0f, p.interleaved ? 1.0f : -1.0f);
       if (p.interleaved) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float u = x[2 * e], v = x[2 * e + 1];
-          x[2 * e] = u * cs[e] - v * sn[e];
-          x[2 * e + 1] = v * cs[e] + u * sn[e];
+          const float c = e % 2 ? upper(cs[e / 2]) : lower(cs[e / 2]), s = e % 2 ? upper(sn[e / 2]) : lower(sn[e / 2]);
+          P cc, ss, other;
+          set(cc, c, c);
+          set(ss, s, s);
+          set(other, upper(x[e]), lower(x[e]));
+          x[e] = times_plus(x[e], cc, times(other, times(ss, flip)));
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float u = x[e], v = x[E + e];
-          x[e] = u * cs[e] - v * sn[e];
-          x[E + e] = v * cs[e] + u * sn[e];
+        for (int e = 0; e < E / 2; ++e) {
+          const P u = x[e], v = x[E / 2 + e];
+          x[e] = times_plus(u, cs[e], times(v, times(sn[e], flip)));
+          x[E / 2 + e] = times_plus(v, cs[e], times(u, sn[e]));
         }
       }
     }
@@ -182,7 +228,7 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_heads_kern
       Words<W> out;
       out.template narrow_all<T>(x);
       out.store(row + h * part.out_head + a);
-      out.template narrow_all<T>(x + E);
+      out.template narrow_all<T>(x + E / 2);
       out.store(row + h * part.out_head + b);
     }
   }
@@ -322,7 +368,7 @@ template <typename T, int W>
 bool launch_vectors(RotateParams& p, unsigned blocks, cudaStream_t stream) {
   constexpr int kUnit = 2 * W * 4 / sizeof(T);  // elements
   const int units = p.dim / kUnit;
-  bool fits = p.dim % kUnit == 0 && p.rotary % kUnit == 0 && units <= 32 && aligned_to(p.table, 8);
+  bool fits = p.dim % kUnit == 0 && p.rotary % kUnit == 0 && units <= 32 && aligned_to(p.table, kUnit >= 16 ? 16 : 8);
   for (int i = 0; i < p.n_parts; ++i) fits = fits && part_aligned<T>(p.part[i], W * 4);
   if (!fits) return false;
   if (units <= 4) launch_lanes<T, W, 4>(p, blocks, stream);
