@@ -105,9 +105,8 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
   __syncthreads();
   const int64_t stop = range[1], begin = stop > 0 ? range[0] : 0;
 
-  const float slope2 = p.slopes != nullptr ? p.slopes[h] * kLog2e : 0.0f;
-  const float scale2 = p.softcap > 0.0f ? p.scale / p.softcap : p.scale * kLog2e;
-  const float cap2 = p.softcap * kLog2e;
+  // scores in their own units here, not in log2: with fp32 results their rounding would show
+  const float slope = p.slopes != nullptr ? p.slopes[h] : 0.0f, over_cap = p.softcap > 0.0f ? 1.0f / p.softcap : 0.0f;
   float acc[4][DP / 16], top[4], total[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -146,19 +145,20 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int j = tx * 4 + c;  // from the tile's first key, as the bounds
-        float x = p.softcap > 0.0f ? cap2 * tanhf(s[r][c] * scale2) : s[r][c] * scale2;
-        if (p.slopes != nullptr) x -= slope2 * fabsf(static_cast<float>(own[r] - j));
+        float x = s[r][c] * p.scale;
+        if (p.softcap > 0.0f) x = p.softcap * tanhf(x * over_cap);
+        if (p.slopes != nullptr) x -= slope * fabsf(static_cast<float>(own[r] - j));
         s[r][c] = j >= low[r] && j < high[r] ? x : -kInf;
         most_here = fmaxf(most_here, s[r][c]);
       }
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) most_here = fmaxf(most_here, __shfl_xor_sync(0xFFFFFFFFu, most_here, o));
       const float next = fmaxf(top[r], most_here), base = next == -kInf ? 0.0f : next;
-      const float back = exp2_approx(top[r] - base);
+      const float back = exp2_approx((top[r] - base) * kLog2e);
       float sum = 0.0f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[r][c] = exp2_approx(s[r][c] - base);
+        s[r][c] = exp2_approx((s[r][c] - base) * kLog2e);
         sum += s[r][c];
       }
 #pragma unroll
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
     }
 #pragma unroll
     for (int n = 0; n < kMaxParts; ++n) {
-      scale[n] = most == -kInf ? 1.0f : exp2_approx(scale[n] - most);  // without a maximum sums are 0, or NaN
+      scale[n] = most == -kInf ? 1.0f : exp2_approx((scale[n] - most) * kLog2e);  // without a maximum sums are 0, or NaN
       if (n < ranks) sum += peer_load(peer_address(&totals[r], n)) * scale[n];
     }
     const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
       finite = finite && (sum == 0.0f || fabsf(x) < kInf);
       if (d < p.dim) out[d] = narrow<T>(sum == 0.0f ? 0.0f : x * over);
     }
-    if (p.lse != nullptr && lane == 0) p.lse[h * p.q_tokens + i] = sum == 0.0f ? -kInf : (most + log2f(sum)) * kLn2;
+    if (p.lse != nullptr && lane == 0) p.lse[h * p.q_tokens + i] = sum == 0.0f ? -kInf : most + logf(sum);
     if (!__all_sync(0xFFFFFFFFu, finite)) attention_row<T>(p, i, h, lane);
   }
   if (ranks > 1) cluster_sync();  // no CTA leaves before its part is read

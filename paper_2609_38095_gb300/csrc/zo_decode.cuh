@@ -63,17 +63,19 @@ __device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePl
 }
 
 // Every thread of the cluster. outs: [kWarps][HB][DP] unscaled outputs, tops and
-// totals: [kWarps][HB] (log2 units), all in shared memory.
-template <typename T, int HB, int DP, int kWarps>
+// totals: [kWarps][HB], all in shared memory; tops in units of log2 (kLog2), or
+// of the scores.
+template <typename T, int HB, int DP, int kWarps, bool kLog2>
 __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodePlace& w, float* outs, const float* tops,
                                             const float* totals, DecodeJoin<HB>& join) {
   const int tid = threadIdx.x;
+  const auto less = [](float a, float b) { return exp2_approx(kLog2 ? a - b : (a - b) * kLog2e); };
   __syncthreads();
   if (tid < HB) {
     float top = -kInf, total = 0.0f;
     for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[i * HB + tid]);
     for (int i = 0; i < kWarps; ++i)
-      if (top > -kInf || totals[i * HB + tid] != 0.0f) total += totals[i * HB + tid] * exp2_approx(tops[i * HB + tid] - top);
+      if (top > -kInf || totals[i * HB + tid] != 0.0f) total += totals[i * HB + tid] * less(tops[i * HB + tid], top);
     join.top[tid] = top;
     join.total[tid] = total;
   }
@@ -82,7 +84,7 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     float top = -kInf, x = 0.0f;
     for (int n = 0; n < kWarps; ++n) top = fmaxf(top, tops[n * HB + h]);
     if (top > -kInf)
-      for (int n = 0; n < kWarps; ++n) x = fmaf(outs[n * HB * DP + i], exp2_approx(tops[n * HB + h] - top), x);
+      for (int n = 0; n < kWarps; ++n) x = fmaf(outs[n * HB * DP + i], less(tops[n * HB + h], top), x);
     outs[i] = x;
   }
   const uint32_t ranks = cluster_size(), rank = cluster_rank();
@@ -98,7 +100,7 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     float top = mine;
 #pragma unroll
     for (int o = kMaxCluster / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float scale = top == -kInf ? 0.0f : exp2_approx(mine - top);
+    const float scale = top == -kInf ? 0.0f : less(mine, top);
     float total = part * scale;
     if (part != part) total = part;  // a NaN where every score is one
 #pragma unroll
@@ -109,7 +111,7 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     join.scale[r][h] = scale;
     if (r == 0) {
       join.over[h] = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
-      join.lse[h] = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+      join.lse[h] = bad ? NAN : total == 0.0f ? -kInf : kLog2 ? (top + log2f(total)) * kLn2 : top + logf(total);
     }
   }
   __syncthreads();

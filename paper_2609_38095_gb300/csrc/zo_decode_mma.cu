@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         outs[(warp * HB + lane % 4 * 2 + (c & 1) + 8 * m) * DP + n * 16 + lane / 4 + c / 2 * 8] = acc[m][n][c];
-  decode_join<T, HB, DP, kWarps>(p, w, outs, tops, totals, join);
+  decode_join<T, HB, DP, kWarps, true>(p, w, outs, tops, totals, join);
 }
 
 template <typename T, int DP, int HB>

@@ -92,11 +92,12 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
     if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
-  const float scale2 = p.softcap > 0.0f ? p.scale / p.softcap : p.scale * kLog2e, cap2 = p.softcap * kLog2e;
-  float slope2[HB], top[HB], total[HB], acc[HB][DP / 32];
+  // scores in their own units here, not in log2: with fp32 results their rounding would show
+  const float over_cap = p.softcap > 0.0f ? 1.0f / p.softcap : 0.0f;
+  float slope[HB], top[HB], total[HB], acc[HB][DP / 32];
 #pragma unroll
   for (int h = 0; h < HB; ++h) {
-    slope2[h] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] * kLog2e : 0.0f;
+    slope[h] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] : 0.0f;
     top[h] = -kInf;
     total[h] = 0.0f;
 #pragma unroll
@@ -135,20 +136,21 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       float x = s[h] + __shfl_xor_sync(0xFFFFFFFFu, s[h], 16);
-      x = p.softcap > 0.0f ? cap2 * tanhf(x * scale2) : x * scale2;
-      x = j < w.len ? x - slope2[h] * away : -kInf;
+      x *= p.scale;
+      if (p.softcap > 0.0f) x = p.softcap * tanhf(x * over_cap);
+      x = j < w.len ? x - slope[h] * away : -kInf;
       float most = x;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
       const float next = fmaxf(top[h], most), base = next == -kInf ? 0.0f : next;
       if (next > top[h]) {  // the same for the whole warp
-        const float back = exp2_approx(top[h] - base);
+        const float back = exp2_approx((top[h] - base) * kLog2e);
         total[h] *= back;
 #pragma unroll
         for (int c = 0; c < DP / 32; ++c) acc[h][c] *= back;
         top[h] = next;
       }
-      s[h] = exp2_approx(x - base);
+      s[h] = exp2_approx((x - base) * kLog2e);
       total[h] += half == 0 ? s[h] : 0.0f;
     }
     if (half == 0) {
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
   for (int h = 0; h < HB; ++h)
 #pragma unroll
     for (int c = 0; c < DP / 32; ++c) tiles[(warp * HB + h) * DP + c * 32 + lane] = acc[h][c];
-  decode_join<T, HB, DP, S::kWarps>(p, w, tiles, tops, totals, join);
+  decode_join<T, HB, DP, S::kWarps, false>(p, w, tiles, tops, totals, join);
 }
 
 template <typename T, int DP, int HB, bool kAsync>

@@ -213,13 +213,16 @@ __device__ __forceinline__ float peer_load(uint32_t a) {
   return v;
 }
 
-// A score in units of log2: scale2 = scale log2(e), or with a cap
-// cap2 = cap log2(e) and scale over the cap.
+// cap2 tanh(s over_cap), a capped score in units of log2 (cap2 = cap log2(e),
+// over_cap = scale / cap). tanh(x) = 1 - 2 / (1 + e^{2x}) is off by about 1e-7
+// whatever x is, which for scores far below the cap would be more than their own
+// rounding: there, |x| < 0.3, by its series up to x^9 (5e-8 of x beyond).
 __device__ __forceinline__ float capped(float s, float over_cap, float cap2) {
-  // tanh(x) = 1 - 2 / (1 + e^{2x}); its error of about 1e-7 is absolute, like
-  // the rounding of the score that it is part of
-  const float e = exp2_approx(s * over_cap * (2.0f * kLog2e));
-  return cap2 - __fdividef(2.0f * cap2, 1.0f + fminf(e, 1e30f));
+  const float x = s * over_cap, y = x * x;
+  const float e = exp2_approx(x * (2.0f * kLog2e));
+  const float far = cap2 - __fdividef(2.0f * cap2, 1.0f + fminf(e, 1e30f));
+  const float series = fmaf(fmaf(fmaf(62.0f / 2835.0f, y, -17.0f / 315.0f), y, 2.0f / 15.0f), y, -1.0f / 3.0f);
+  return fabsf(x) < 0.3f ? cap2 * fmaf(x * y, series, x) : far;
 }
 
 // Row i of head h alone, by one warp, a key at a time: for rows whose tile gave
