@@ -1,6 +1,7 @@
 """GB300 (sm_103a) parameter-space hot path of 1.5-SPSA: probe generation,
 fused perturb, probe-space preconditioner and fused K-probe update, behind the
-C ABI of include/zo.h. The shared library is loaded on first use; a missing
+C ABI of include/zo.h; and, as .forward, the operators of a decoder's forward
+point (include/zo_forward.h). The shared library is loaded on first use; a missing
 library raises (there is no fallback).
 """
 from .zo import (ZO_ERR_ALIGN, ZO_ERR_ARG, ZO_ERR_CUDA, ZO_ERR_DTYPE, ZO_ERR_NONFINITE, ZO_ERR_TOO_MANY_PROBES,
