@@ -155,7 +155,8 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
  * lengths[b] keys of sequence b, of which the last is the row's own: key t is
  * row t % page_size of page pages[b * pages_stride + t / page_size] of the
  * caches. A length of zero or less gives a row that sees nothing; a page
- * outside 0 .. n_pages - 1, or a length above max_pages * page_size, NaN.
+ * outside 0 .. n_pages - 1, or a length above max_pages * page_size (or 2^31 -
+ * 65), NaN.
  * What lies in a page beyond the length does not reach the result.
  *   q, out  row b is sequence b's
  *   lse     fp32 [batch][heads] or NULL

@@ -85,9 +85,10 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xFFFFF
 //
 // What bounds it: the products with 64 columns read 6 KB of shared memory in the
 // 32 cycles that they would take, so a step is 384 + 256 cycles per slot, 2560 for
-// 128 keys and both slots (with 128 columns 2048, but then there is no tensor
-// memory for a second step, and a slot's softmax, 1600 cycles and two waits of
-// 400, is in series with its own products: 8192 tokens of 32 heads took 460 us).
+// 128 keys and both slots; it runs at some 2880 (8192 tokens, 32 / 8 heads of 128,
+// bf16: 333 us = 1.65 PFLOP/s). With 128 columns they would take 2048, but there is
+// no tensor memory for a second step's scores then, and a slot's softmax, 1600
+// cycles and two waits of 400, is in series with its own products (460 us).
 //
 // The output is rescaled only when a row's maximum has passed the reference that
 // its weights are relative to by 2^8, which seldom happens after the first steps:
@@ -323,11 +324,12 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       tie32(x[1]);
       const int key0 = begin + (from[slot] + c) * kKeys;
       if (kCap || kBias) {
+        const float away = static_cast<float>(self - key0);  // exact, and its differences, below 2^24
 #pragma unroll
         for (int e = 0; e < 64; ++e) {
           float s = __uint_as_float(x[e / 32][e % 32]);
           s = kCap ? capped(s, scale2, cap2) : s * scale2;
-          if (kBias) s -= slope2 * fabsf(static_cast<float>(self - (key0 + e)));
+          if (kBias) s -= slope2 * fabsf(away - e);
           x[e / 32][e % 32] = __float_as_uint(s);
         }
       }

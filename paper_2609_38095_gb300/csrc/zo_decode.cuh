@@ -40,7 +40,8 @@ __device__ __forceinline__ DecodePlace decode_place(const DecodeParams& p, uint3
   w.head0 = w.g * p.group + first;
   w.heads = min(HB, p.group - first);
   w.len = max(p.lengths[w.b], 0);
-  w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0);
+  // (keys, a last tile's end among them, are counted in 32 bits)
+  w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0) || w.len > 0x7FFFFFFF - 64;
   if (w.bad) w.len = 0;
   return w;
 }

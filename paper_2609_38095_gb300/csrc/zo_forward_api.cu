@@ -168,7 +168,7 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
   if (rc != ZO_OK) return rc;
   // a launch has at most 16 CTAs per sequence and query head
   if (batch < 0 || batch > kMaxIndex / 16 / heads || max_pages < 0 || n_pages < 0 || n_pages > kMaxIndex ||
-      page_size < 1 || pages_stride < 0 || max_pages > (INT64_C(1) << 40))
+      page_size < 1 || pages_stride < 0 || max_pages > kMaxIndex)
     return ZO_ERR_ARG;
   if (bad_strides(q->token, q->head, out->token) || bad_strides(out->head, k->page, k->token) ||
       bad_strides(k->head, v->page, v->token) || bad_strides(v->head, 0))

@@ -116,7 +116,7 @@ def test_decode_validation(L):
                                      cap, slopes, lse, None)
     for bad in ({"q": None}, {"k": None}, {"k": pages(0, 1, 1, 1)}, {"v": pages(FAKE, 1, -1, 1)}, {"out": rows(0, 1, 1)},
                 {"batch": -1}, {"batch": 1 << 30}, {"heads": 3, "kv": 2}, {"dim": 300}, {"table": None}, {"stride": -1},
-                {"most": -1}, {"n": -1}, {"page": 0}, {"lengths": None}, {"scale": float("inf")}, {"cap": -2.0}):
+                {"most": -1}, {"n": -1}, {"most": 1 << 31}, {"page": 0}, {"lengths": None}, {"scale": float("inf")}, {"cap": -2.0}):
         assert call(**bad) == zo.ZO_ERR_ARG, bad
     assert call(dtype=5) == zo.ZO_ERR_DTYPE
     for bad in ({"k": pages(FAKE + 1, 1, 1, 1)}, {"table": FAKE + 1}, {"lengths": FAKE + 2}, {"lse": FAKE + 2}):
