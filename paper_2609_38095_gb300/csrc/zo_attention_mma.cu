@@ -323,15 +323,30 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       tmem_wait_ld(x[0]);
       tie32(x[1]);
       const int key0 = begin + (from[slot] + c) * kKeys;
-      if (kCap || kBias) {
-        const float away = static_cast<float>(self - key0);  // exact, and its differences, below 2^24
+      if (kCap) {
+        float far = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 64; ++e) {
-          float s = __uint_as_float(x[e / 32][e % 32]);
-          s = kCap ? capped(s, scale2, cap2) : s * scale2;
-          if (kBias) s -= slope2 * fabsf(away - e);
-          x[e / 32][e % 32] = __float_as_uint(s);
+        for (int e = 0; e < 64; ++e) far = fmaxf(far, fabsf(__uint_as_float(x[e / 32][e % 32])));
+        if (__all_sync(0xFFFFFFFFu, far * scale2 < kNearCap)) {  // mostly: caps are there for the rare large score
+          const uint64_t over2 = pack2(scale2, scale2), caps = pack2(cap2, cap2);
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            uint32_t* at = &x[e / 32][e % 32];
+            const uint64_t s = capped_near(static_cast<uint64_t>(at[1]) << 32 | at[0], over2, caps);
+            at[0] = static_cast<uint32_t>(s), at[1] = static_cast<uint32_t>(s >> 32);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 64; ++e)
+            x[e / 32][e % 32] = __float_as_uint(capped(__uint_as_float(x[e / 32][e % 32]), scale2, cap2));
         }
+      }
+      if (kBias) {
+        const float away = static_cast<float>(self - key0);  // exact, and its differences, below 2^24
+        const float times = kCap ? 1.0f : scale2;
+#pragma unroll
+        for (int e = 0; e < 64; ++e)
+          x[e / 32][e % 32] = __float_as_uint(__uint_as_float(x[e / 32][e % 32]) * times - slope2 * fabsf(away - e));
       }
       if (!__all_sync(0xFFFFFFFFu, lo <= key0 && hi >= key0 + kKeys)) {
 #pragma unroll

@@ -213,16 +213,27 @@ __device__ __forceinline__ float peer_load(uint32_t a) {
   return v;
 }
 
+constexpr float kNearCap = 0.3f;
+
 // cap2 tanh(s over_cap), a capped score in units of log2 (cap2 = cap log2(e),
 // over_cap = scale / cap). tanh(x) = 1 - 2 / (1 + e^{2x}) is off by about 1e-7
 // whatever x is, which for scores far below the cap would be more than their own
-// rounding: there, |x| < 0.3, by its series up to x^9 (5e-8 of x beyond).
+// rounding: there, |x| < kNearCap, by its series up to x^9 (5e-8 of x beyond).
 __device__ __forceinline__ float capped(float s, float over_cap, float cap2) {
   const float x = s * over_cap, y = x * x;
   const float e = exp2_approx(x * (2.0f * kLog2e));
   const float far = cap2 - __fdividef(2.0f * cap2, 1.0f + fminf(e, 1e30f));
   const float series = fmaf(fmaf(fmaf(62.0f / 2835.0f, y, -17.0f / 315.0f), y, 2.0f / 15.0f), y, -1.0f / 3.0f);
-  return fabsf(x) < 0.3f ? cap2 * fmaf(x * y, series, x) : far;
+  return fabsf(x) < kNearCap ? cap2 * fmaf(x * y, series, x) : far;
+}
+
+// The same of two scores that are known to be below kNearCap of the cap.
+__device__ __forceinline__ uint64_t capped_near(uint64_t s, uint64_t over_cap, uint64_t cap2) {
+  const uint64_t x = mul2(s, over_cap), y = mul2(x, x);
+  uint64_t series = fma2(pack2(62.0f / 2835.0f, 62.0f / 2835.0f), y, pack2(-17.0f / 315.0f, -17.0f / 315.0f));
+  series = fma2(series, y, pack2(2.0f / 15.0f, 2.0f / 15.0f));
+  series = fma2(series, y, pack2(-1.0f / 3.0f, -1.0f / 3.0f));
+  return mul2(fma2(mul2(x, y), series, x), cap2);
 }
 
 // Row i of head h alone, by one warp, a key at a time: for rows whose tile gave
