@@ -16,38 +16,41 @@ template <typename T, int DP, bool kTransposed, bool kVec>
 __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stride, int64_t from, int64_t lo, int64_t hi,
                                           int dim) {
   constexpr int E = kVec ? Vec<T>::kN : 1;
-  constexpr int kChunks = DP / E;
-  if constexpr (kTransposed) {  // lanes on rows: stores without bank conflicts, a row's sectors from L1
-    const int r = threadIdx.x % kTile;
-    const int64_t row = from + r;
-    const bool in = row >= lo && row < hi;
-    for (int c = threadIdx.x / kTile; c < kChunks; c += kThreads256 / kTile) {
-      float f[E];
-      if constexpr (kVec) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (in && c * E < dim) u = *reinterpret_cast<const uint4*>(src + row * stride + c * E);
-        Vec<T>::widen_all(u, f);
-      } else {
-        f[0] = in && c < dim ? widen(src[row * stride + c]) : 0.0f;
-      }
+  constexpr int kChunks = DP / E, kEach = kChunks * kTile / kThreads256;  // loads of a thread
+  constexpr int kBatch = kEach % 8 == 0 ? 8 : kEach % 6 == 0 ? 6 : kEach;  // of them on their way together
+  for (int n0 = 0; n0 < kEach; n0 += kBatch) {
+    uint4 raw[kBatch];
+    float one[kBatch];
+    int row[kBatch], chunk[kBatch];
 #pragma unroll
-      for (int e = 0; e < E; ++e) dst[(c * E + e) * kTile + r] = f[e];
-    }
-  } else {
-    for (int i = threadIdx.x; i < kTile * kChunks; i += kThreads256) {
-      const int r = i / kChunks, c = i % kChunks;
-      const int64_t row = from + r;
-      const bool in = row >= lo && row < hi;
+    for (int n = 0; n < kBatch; ++n) {
+      const int i = threadIdx.x + (n0 + n) * kThreads256;
+      // transposed, lanes on rows: stores without bank conflicts, a row's sectors from L1
+      row[n] = kTransposed ? i % kTile : i / kChunks;
+      chunk[n] = kTransposed ? i / kTile : i % kChunks;
+      const int64_t r = from + row[n];
+      const bool in = r >= lo && r < hi && chunk[n] * E < dim;
       if constexpr (kVec) {
-        float f[E];
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (in && c * E < dim) u = *reinterpret_cast<const uint4*>(src + row * stride + c * E);
-        Vec<T>::widen_all(u, f);
+        raw[n] = make_uint4(0, 0, 0, 0);
+        if (in) raw[n] = *reinterpret_cast<const uint4*>(src + r * stride + chunk[n] * E);
+      } else {
+        one[n] = in ? widen(src[r * stride + chunk[n]]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      float f[E];
+      if constexpr (kVec) Vec<T>::widen_all(raw[n], f);
+      else f[0] = one[n];
+      if constexpr (kTransposed) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[(chunk[n] * E + e) * kTile + row[n]] = f[e];
+      } else if constexpr (kVec) {
 #pragma unroll
         for (int e = 0; e < E; e += 4)
-          *reinterpret_cast<float4*>(dst + r * DP + c * E + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+          *reinterpret_cast<float4*>(dst + row[n] * DP + chunk[n] * E + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       } else {
-        dst[r * DP + c] = in && c < dim ? widen(src[row * stride + c]) : 0.0f;
+        dst[row[n] * DP + chunk[n]] = f[0];
       }
     }
   }
