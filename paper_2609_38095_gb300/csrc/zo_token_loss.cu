@@ -88,7 +88,8 @@ __device__ __forceinline__ void row_tail(const T* x, int n, int tid, float& top,
 
 // A token per CTA, or per cluster of CTAs that split the vocabulary where there
 // are fewer tokens than the SMs hold CTAs. One pass with the running maximum
-// and sum in registers; bound by HBM: each counted row is read once.
+// and sum in registers; bound by HBM: each counted row is read once (3068 rows of
+// 151936, bf16: 154 us = 6.05 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads, kLossCtas)
     token_loss_kernel(const __grid_constant__ TokenLossParams p, int parts) {
