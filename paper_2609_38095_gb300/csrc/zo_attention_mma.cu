@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
   extern __shared__ uint8_t raw[];
   __shared__ MmaShared sh;
-  uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // queries of both slots, then the stages
+  uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // the slots' queries, then the stages
   uint8_t* stages = tiles + kSlots * L::kQueries;
   const int tid = threadIdx.x, warp = static_cast<int>(uniform(tid >> 5)), lane = tid & 31;
   const int heads_here = kSlots == 2 && by_heads ? 2 : 1, tiles_here = kSlots / heads_here;  // heads, tiles of rows
@@ -263,7 +263,8 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
           uint8_t* v = stages + v_stage * L::kTile + lane % 8 * 16;
           for (int r = rest + lane / 8; r < used; r += 4)
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(v + c * L::kTileChunk + r * 128) = make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < D / 64; ++c)
+              *reinterpret_cast<uint4*>(v + c * L::kTileChunk + r * 128) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       }
     }
     __syncwarp();
-    if (*dead && elect_one()) {
+    if (__any_sync(0xFFFFFFFFu, *dead != 0) && elect_one()) {  // the products that are on their way end first
       mma_commit(&sh.drain[s]);
       const long long start = clock64();
       while (!mbar_try(&sh.drain[s], 0) && clock64() - start < kWaitCycles) {}
