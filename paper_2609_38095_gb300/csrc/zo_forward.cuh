@@ -222,7 +222,7 @@ constexpr float kNearCap = 0.3f;
 __device__ __forceinline__ float capped(float s, float over_cap, float cap2) {
   const float x = s * over_cap, y = x * x;
   const float e = exp2_approx(x * (2.0f * kLog2e));
-  const float far = cap2 - __fdividef(2.0f * cap2, 1.0f + fminf(e, 1e30f));
+  const float far = cap2 - __fdividef(2.0f * cap2, 1.0f + (e > 1e30f ? 1e30f : e));  // (fminf would make a NaN a number)
   const float series = fmaf(fmaf(fmaf(62.0f / 2835.0f, y, -17.0f / 315.0f), y, 2.0f / 15.0f), y, -1.0f / 3.0f);
   return fabsf(x) < kNearCap ? cap2 * fmaf(x * y, series, x) : far;
 }
