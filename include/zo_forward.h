@@ -137,9 +137,11 @@ int zo_rotate_heads(const zo_head_part* parts, int32_t n_parts, int64_t tokens, 
  *   s_j = scale q_i . k_j;  softcap > 0: s_j = softcap tanh(s_j / softcap)
  *   slopes given: s_j = s_j - slopes[h] |self_i - j|
  *   out_i = sum_j exp(s_j) v_j / sum_j exp(s_j);  lse_i = log sum_j exp(s_j)
- * A row that sees nothing gets out = 0 and lse = -inf. What lies at keys that
- * a row does not see (NaN, infinities, memory never written) does not reach
- * its result.
+ * A row that sees nothing, or only scores of -inf, gets out = 0 and lse = -inf.
+ * What lies at keys that a row does not see (NaN, infinities, memory never
+ * written) does not reach its result. A column of out in which a row sees a
+ * value that is not finite is not finite; whether it is NaN or an infinity is
+ * left open.
  *   spans   int32 [3][q_tokens], zo_document_spans's or the caller's own; the
  *           third row (self) is read with slopes only
  *   slopes  fp32 [heads] or NULL

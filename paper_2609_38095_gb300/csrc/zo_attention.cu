@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
   float* ps = vs + DP * kTile;      // [64 rows][64 keys]
   __shared__ int64_t range[2];
   __shared__ float tops[kTile], totals[kTile];  // of this CTA's keys
+  __shared__ float lses[kTile];
+  __shared__ uint32_t left[kTile / 32];  // rows for attention_rows
   const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16, h = blockIdx.y, g = h / p.group;
   const int ranks = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
   const int64_t row0 = (static_cast<int64_t>(gridDim.x - 1 - blockIdx.x) / ranks) * kTile;  // the longest causal rows first
@@ -98,6 +100,7 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
   if (tid == 0) {
     range[0] = INT64_MAX;
     range[1] = 0;
+    for (int i = 0; i < kTile / 32; ++i) left[i] = 0;
   }
   __syncthreads();
   if (tx == 0 && most > 0) {
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
       if (n < ranks) sum += peer_load(peer_address(&totals[r], n)) * scale[n];
     }
     const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
-    bool finite = sum < kInf;
+    bool finite = true;
     T* out = static_cast<T*>(p.out) + i * p.out_token + h * p.out_head;
 #pragma unroll
     for (int d = lane; d < DP; d += 32) {
@@ -246,10 +249,17 @@ __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)
       finite = finite && (sum == 0.0f || fabsf(x) < kInf);
       if (d < p.dim) out[d] = narrow<T>(sum == 0.0f ? 0.0f : x * over);
     }
-    if (p.lse != nullptr && lane == 0) p.lse[h * p.q_tokens + i] = sum == 0.0f ? -kInf : most + logf(sum);
-    if (!__all_sync(0xFFFFFFFFu, finite)) attention_row<T>(p, i, h, lane);
+    const float lse = sum == 0.0f ? -kInf : most + logf(sum);
+    if (p.lse != nullptr && lane == 0) p.lse[h * p.q_tokens + i] = lse;
+    if (!__all_sync(0xFFFFFFFFu, finite) && sum < kInf && lane == 0) {  // (a sum that is NaN is that of seen scores)
+      lses[r] = lse;
+      atomicOr(&left[r / 32], 1u << r % 32);
+    }
   }
   if (ranks > 1) cluster_sync();  // no CTA leaves before its part is read
+  else __syncthreads();
+  if ((left[0] | left[1]) != 0)
+    attention_rows<T, DP, 1>(p, row0, h, left, lses, kTile / 32, tid / 32, kThreads256 / 32, lane);
 }
 
 template <typename T, int DP, bool kVec>

@@ -61,6 +61,8 @@ struct MmaShared {
   int lo[2], hi[2];
   uint32_t tmem;
   int dead;
+  uint32_t left[2][kRows / 32];  // rows for attention_rows
+  float lse[2][kRows];
 };
 
 // Bits 0 to n - 1.
@@ -417,7 +419,8 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     tmem_fence_after();
     const bool seen = alive && any && total != 0.0f;
     const float over = seen ? 1.0f / total : 0.0f;
-    bool finite = !seen || total < kInf;
+    const float lse = !alive ? NAN : seen ? (base + log2f(total)) * kLn2 : -kInf;
+    bool finite = true;
     // Through shared memory, in the place of the slot's queries: a warp's rows of 64 elements as TMA stores them (rows
     // apart in memory, a thread's own stores took 3 us).
     const uint32_t mine = smem_address(tiles + slot * L::kQueries) + (warp & 3) * 32 * 128;
@@ -452,18 +455,16 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         if (c * 64 < p.dim) tma_store_3d(&o_map, c * 64, h, static_cast<int>(row), mine + c * kChunk);
       tma_store_commit();
     }
-    if (row < p.q_tokens && p.lse != nullptr)
-      p.lse[h * p.q_tokens + row] = !alive ? NAN : seen ? (base + log2f(total)) * kLn2 : -kInf;
-    uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite);
+    if (row < p.q_tokens && p.lse != nullptr) p.lse[h * p.q_tokens + row] = lse;
+    // (a sum that is NaN is that of seen scores, and the outputs' too)
+    const uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite && total < kInf);
+    sh.lse[slot][tid & 127] = lse;
     if (lane == 0) {
-      if (left != 0) tma_stored<false>();  // those rows are written again
+      sh.left[slot][warp & 3] = left;
+      if (left != 0) tma_stored<false>();  // those rows are read again
       else tma_stored<true>();
     }
     __syncwarp();
-    for (; left != 0; left &= left - 1) {
-      const int r = __ffs(left) - 1;
-      attention_row<T>(p, row - lane + r, h, lane);
-    }
   }
   tmem_fence_before();
   __syncthreads();
@@ -471,6 +472,11 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     tmem_fence_after();
     tmem_free(tmem, L::kColumns);
   }
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s)
+    if ((sh.left[s][0] | sh.left[s][1] | sh.left[s][2] | sh.left[s][3]) != 0)
+      attention_rows<T, D, 2>(p, static_cast<int64_t>(block_of(s)) * kRows, head_of(s), sh.left[s], sh.lse[s],
+                                kRows / 32, warp, L::kThreads / 32, lane);
 }
 
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
