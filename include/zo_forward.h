@@ -26,7 +26,8 @@
  * Arithmetic. Values are read as fp32; norms, scores, softmax statistics and
  * sums are fp32 (fp64 across tokens) and each output is rounded once. One
  * exception, in zo_attention and zo_attention_decode on 16-bit types: the
- * softmax's weights are rounded to that type for the tensor cores.
+ * softmax's weights are rounded to that type for the tensor cores (in fp16 one
+ * below 2^-21 of its row's largest loses bits, and one below 2^-32 is lost).
  *
  * Strides are in elements; the elements of one head are contiguous.
  */

@@ -35,7 +35,6 @@ namespace {
 constexpr int kRows = 128;           // query rows of a slot
 constexpr int kKeys = 64;            // keys of a step
 constexpr int kChunk = kRows * 128;  // bytes of 64 elements of a slot's queries
-constexpr float kSlack = 8.0f;       // log2: how far scores may pass the reference before the output is rescaled
 
 // A CTA of two slots, one per SM, with keys and values by 128; or of one slot, two per SM, with keys and values by 64.
 template <int D, int kSlots>
@@ -94,7 +93,7 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xFFFFF
 //
 // The output is rescaled only when a row's maximum has passed the reference that
 // its weights are relative to by 2^8, which seldom happens after the first steps:
-// weights up to 256 lose nothing in 16 bits and their sum is fp32.
+// weights up to 2^8 (fp16: 2^15, kLift) lose nothing in 16 bits and their sum is fp32.
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
 __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     attention_mma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -369,6 +368,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       }
       float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
       if (!kCap && !kBias) top *= scale2;
+      top -= kLift<T>;
       // A row's first score sets its reference: its output so far is a sum of zeros (or of 0 times NaN, which shows at the
       // end), so there is nothing to rescale.
       const bool moved = base > -kInf && top > base + kSlack;

@@ -7,7 +7,6 @@ namespace zo {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr float kSlack = 8.0f;  // log2: how far scores may pass the reference before the output is rescaled
 
 template <int DP, int HB>
 struct Tiles {
@@ -216,6 +215,7 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 4));
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 8));
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 16));
+        most -= kLift<T>;
         back[m][c] = 1.0f;
         if (most > base[m][c] + kSlack || (base[m][c] == -kInf && most > -kInf)) {
           back[m][c] = exp2_approx(base[m][c] - most);

@@ -182,6 +182,13 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
   return r;
 }
 
+// Softmax weights in 16 bits are 2^kLift for a score at the reference, and up to kSlack (log2) more before the reference and
+// the output move. fp16 has 2^15 above 1 to spare and needs it below, where a weight under 2^-14 loses bits and one under
+// 2^-25 is lost while the sum counts it: thousands of keys that weigh little beside one of their row's.
+constexpr float kSlack = 8.0f;
+template <typename T>
+constexpr float kLift = __is_same(T, __half) ? 7.0f : 0.0f;
+
 __device__ __forceinline__ int64_t load_index(const void* p, int64_t i, int is64) {
   return is64 ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
 }
