@@ -9,6 +9,7 @@
 
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -42,7 +43,9 @@ const at::Tensor& cuda_tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) type_error(std::string(what) + " must be a CUDA tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) type_error(std::string(what) + " must be a CUDA tensor");
-  if (t.requires_grad() && at::GradMode::is_enabled())
+  // reverse mode, or a tangent of forward mode (which no_grad leaves on)
+  if ((t.requires_grad() && at::GradMode::is_enabled()) ||
+      (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(/*level=*/0).defined()))
     throw Refusal{PyExc_RuntimeError, std::string(what) + " asks for a gradient, which this operator does not have"};
   return t;
 }

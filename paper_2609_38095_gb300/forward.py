@@ -19,7 +19,7 @@ and of an answer's next token, over a paged cache (pages, page_size, kv_heads, h
     out = zo.forward.decode_attention(q, k_cache, v_cache, pages, lengths)
 
 The method has no backward pass: a tensor that asks for a gradient is refused
-where torch would record one.
+where torch would record one, and a tensor with a tangent of forward mode is.
 """
 import ctypes
 import importlib.machinery
