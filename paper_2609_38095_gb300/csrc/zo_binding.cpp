@@ -98,6 +98,7 @@ bool truth(PyObject* o) {
 struct Output {  // a tensor and the object that is returned for it
   at::Tensor t;
   PyObject* o = nullptr;
+  bool given = false;
   Output() = default;
   Output(const Output&) = delete;
   Output& operator=(const Output&) = delete;
@@ -105,13 +106,17 @@ struct Output {  // a tensor and the object that is returned for it
   void is(PyObject* other) {
     t = THPVariable_Unpack(other);
     o = Py_NewRef(other);
+    given = true;
   }
   void make(at::IntArrayRef shape, const at::Tensor& like, at::ScalarType type) {
     t = at::empty(shape, at::TensorOptions(like.device()).dtype(type));
     o = THPVariable_Wrap(t);
     if (o == nullptr) throw python_error();
   }
+  // The object, once the call is on its stream. A tensor of the caller's has a new version then, so that a backward pass
+  // that saved it before does not take it for the same (those of inference mode have none).
   PyObject* take() {
+    if (given && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
     PyObject* r = o;
     o = nullptr;
     return r;
