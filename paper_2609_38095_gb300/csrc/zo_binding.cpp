@@ -81,6 +81,12 @@ const at::Tensor& flat(PyObject* o, const char* what, std::initializer_list<at::
   return t;
 }
 
+// A count as the library takes it.
+int32_t count(int64_t n, const char* what) {
+  if (n > INT32_MAX) value_error(std::string(what) + " is " + std::to_string(n) + ", more than the library counts");
+  return static_cast<int32_t>(n);
+}
+
 bool given(PyObject* o) { return o != Py_None; }
 
 double number(PyObject* o) {
@@ -145,6 +151,7 @@ zo_pages pages_of(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.st
 // What attention and decode_attention share: q, k, v, slopes, out.
 struct Attention {
   const at::Tensor &q, &k, &v;
+  int32_t n = 0, kv = 0, size = 0;  // query heads, key-value heads, head size
   const float* slopes = nullptr;
   float scale = 0.0f, softcap = 0.0f;
   Output out, lse;
@@ -153,6 +160,7 @@ struct Attention {
       : q(heads(a[0], "q", 3)), k(heads(a[1], "k", dim, &q)), v(heads(a[2], "v", dim, &q)) {
     if (k.sizes() != v.sizes() || k.size(-1) != q.size(2)) value_error("k and v must have the same shape and q's head size");
     if (k.size(-2) == 0 || q.size(1) % k.size(-2) != 0) value_error("the key-value heads must divide the query heads");
+    n = count(q.size(1), "the number of heads"), kv = count(k.size(-2), "the number of heads"), size = count(q.size(2), "the head size");
     if (given(slopes_)) slopes = flat(slopes_, "slopes", {at::kFloat}, q, {q.size(1)}).const_data_ptr<float>();
     scale = given(scale_) ? static_cast<float>(number(scale_)) : static_cast<float>(1.0 / std::sqrt(static_cast<double>(q.size(2))));
     softcap = static_cast<float>(number(softcap_));
@@ -167,36 +175,36 @@ struct Attention {
 
 PyObject* attention(PyObject* const* a) {  // q, k, v, spans, scale, softcap, slopes, out, with_lse
   Attention c(a, 3, a[4], a[5], a[6], a[7]);
-  const int64_t tokens = c.q.size(0), n = c.q.size(1);
+  const int64_t tokens = c.q.size(0);
   const at::Tensor& spans = flat(a[3], "spans", {at::kInt}, c.q, {3, tokens});
   const bool with_lse = truth(a[8]);
-  if (with_lse) c.lse.make({n, tokens}, c.q, at::kFloat);
+  if (with_lse) c.lse.make({c.n, tokens}, c.q, at::kFloat);
   const zo_rows q = rows_of(c.q), k = rows_of(c.k), v = rows_of(c.v), out = rows_of(c.out.t);
   const int rc = on_stream(c.q, [&](void* stream) {
-    return g_attention(&q, &k, &v, &out, tokens, c.k.size(0), static_cast<int32_t>(n), static_cast<int32_t>(c.k.size(1)),
-                       static_cast<int32_t>(c.q.size(2)), code(c.q.scalar_type()), spans.const_data_ptr<int32_t>(), c.scale,
-                       c.softcap, c.slopes, with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
+    return g_attention(&q, &k, &v, &out, tokens, c.k.size(0), c.n, c.kv, c.size, code(c.q.scalar_type()),
+                       spans.const_data_ptr<int32_t>(), c.scale, c.softcap, c.slopes,
+                       with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
   });
   return rc != ZO_OK ? PyLong_FromLong(rc) : first_or_both(c.out, c.lse, with_lse);
 }
 
 PyObject* decode_attention(PyObject* const* a) {  // q, k, v, pages, lengths, scale, softcap, slopes, out, with_lse
   Attention c(a, 4, a[5], a[6], a[7], a[8]);
-  const int64_t batch = c.q.size(0), n = c.q.size(1);
+  const int64_t batch = c.q.size(0);
   const at::Tensor& pages = cuda_tensor(a[3], "pages");
   if (pages.scalar_type() != at::kInt || pages.device() != c.q.device()) type_error("pages must be an int32 tensor on q's device");
   if (pages.dim() != 2 || pages.size(0) != batch || (pages.size(1) > 1 && pages.stride(1) != 1))
     value_error("pages must have one row per sequence, contiguous");
   const at::Tensor& lengths = flat(a[4], "lengths", {at::kInt}, c.q, {batch});
   if (c.k.size(1) < 1) value_error("a page must hold at least one row");
+  const int32_t page_size = count(c.k.size(1), "the page size");
   const bool with_lse = truth(a[9]);
-  if (with_lse) c.lse.make({batch, n}, c.q, at::kFloat);
+  if (with_lse) c.lse.make({batch, c.n}, c.q, at::kFloat);
   const zo_rows q = rows_of(c.q), out = rows_of(c.out.t);
   const zo_pages k = pages_of(c.k), v = pages_of(c.v);
   const int rc = on_stream(c.q, [&](void* stream) {
-    return g_attention_decode(&q, &k, &v, &out, batch, static_cast<int32_t>(n), static_cast<int32_t>(c.k.size(2)),
-                              static_cast<int32_t>(c.q.size(2)), code(c.q.scalar_type()), pages.const_data_ptr<int32_t>(),
-                              pages.stride(0), pages.size(1), c.k.size(0), static_cast<int32_t>(c.k.size(1)),
+    return g_attention_decode(&q, &k, &v, &out, batch, c.n, c.kv, c.size, code(c.q.scalar_type()),
+                              pages.const_data_ptr<int32_t>(), pages.stride(0), pages.size(1), c.k.size(0), page_size,
                               lengths.const_data_ptr<int32_t>(), c.scale, c.softcap, c.slopes,
                               with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
   });
@@ -209,7 +217,7 @@ PyObject* rotate_heads(PyObject* const* a) {
   static const char* const weights[2] = {"q_weight", "k_weight"};
   static const char* const outs[3] = {"q_out", "k_out", "v_out"};
   const at::Tensor& q = heads(a[0], "q", 3);
-  const int64_t tokens = q.size(0), dim = q.size(2);
+  const int64_t tokens = q.size(0), dim = count(q.size(2), "the head size");
   if (!given(a[1]) && (given(a[2]) || given(a[6]) || given(a[10]))) value_error("v, k_weight and k_out need k");
   if (!given(a[2]) && given(a[11])) value_error("v_out needs v");
   const at::Tensor& table = cuda_tensor(a[3], "table");
@@ -229,6 +237,7 @@ PyObject* rotate_heads(PyObject* const* a) {
     if (!given(a[i])) continue;
     const at::Tensor& x = i == 0 ? q : heads(a[i], names[i], 3, &q);
     if (x.size(0) != tokens || x.size(2) != dim) value_error(std::string(names[i]) + " must have q's tokens and head size");
+    parts[n].heads = count(x.size(1), "the number of heads");
     const bool slotted = i > 0 && slots != nullptr;
     if (given(a[9 + i])) {
       const bool paged = slotted && THPVariable_Check(a[9 + i]) && THPVariable_Unpack(a[9 + i]).dim() == 4;
@@ -248,7 +257,6 @@ PyObject* rotate_heads(PyObject* const* a) {
       p.weight = w.const_data_ptr();
       p.weight_dtype = code(w.scalar_type());
     }
-    p.heads = static_cast<int32_t>(x.size(1));
     p.flags = (i < 2 ? ZO_HEADS_ROTATE : 0) | (slotted ? ZO_HEADS_SLOTTED : 0);
     if (slotted) {
       const int64_t per_page = o.dim() == 4 ? o.size(1) : o.size(0), all = o.dim() == 4 ? o.size(0) * per_page : per_page;
@@ -262,7 +270,7 @@ PyObject* rotate_heads(PyObject* const* a) {
   const int layout = truth(a[8]) ? ZO_ROTARY_INTERLEAVED : ZO_ROTARY_HALF;
   const int rc = on_stream(q, [&](void* stream) {
     return g_rotate_heads(parts, n, tokens, static_cast<int32_t>(dim), code(q.scalar_type()), table.const_data_ptr<float>(),
-                          table.size(0), static_cast<int32_t>(table.size(1)), layout, positions.const_data_ptr(),
+                          table.size(0), count(table.size(1), "the rotated part"), layout, positions.const_data_ptr(),
                           slots != nullptr ? slots->const_data_ptr() : nullptr, index_bytes(positions), rows,
                           page_size > 0 ? page_size : 1, static_cast<float>(eps), stream);
   });
