@@ -29,7 +29,10 @@
  * softmax's weights are rounded to that type for the tensor cores (in fp16 one
  * below 2^-21 of its row's largest loses bits, and one below 2^-32 is lost).
  *
- * Strides are in elements; the elements of one head are contiguous.
+ * Strides are in elements; the elements of one head are contiguous. An output
+ * over an input or another output, or with rows or heads over one another, is
+ * ZO_ERR_ARG as far as strides show it (layouts that interleave by unlike
+ * strides are the caller's to keep apart).
  */
 #ifndef ZO_FORWARD_H_
 #define ZO_FORWARD_H_
@@ -104,8 +107,8 @@ int zo_document_spans(const int32_t* q_starts, const int32_t* k_starts, const in
  * ZO_ROTARY_INTERLEAVED. With ZO_HEADS_SLOTTED token t goes to row slots[t] %
  * page_size of page slots[t] / page_size of `out` (nowhere if slots[t] is
  * negative or not below n_slots), else to row t (out_page is not used).
- * A part may be done in place (out = in, same strides); else out overlaps no
- * input.
+ * A part may be done in place (out = in, same strides; with slots each token to
+ * its own row); else an output overlaps no input, and never another output.
  *   weight        one per element of a head, of type weight_dtype, or NULL
  *   positions, slots  int32 or int64 by index_bytes (4 or 8); needed by the
  *                 parts that rotate / are slotted
@@ -161,7 +164,8 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
  * outside 0 .. n_pages - 1, or a length above max_pages * page_size (or 2^31 -
  * 65), NaN.
  * What lies in a page beyond the length does not reach the result.
- *   q, out  row b is sequence b's
+ *   q, out  row b is sequence b's; out may be q (same strides) and overlaps
+ *           nothing else
  *   lse     fp32 [batch][heads] or NULL
  * ------------------------------------------------------------------------- */
 int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, const zo_rows* out, int64_t batch,

@@ -1,7 +1,9 @@
 // zo_forward_api.cu -- the extern "C" entry points declared in
 // include/zo_forward.h: argument validation and the choice of kernel.
 // Everything here runs on the host and only enqueues kernels.
+#include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "zo_forward.cuh"
 #include "zo_forward.h"
@@ -28,6 +30,122 @@ int check_heads(int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype
 
 int check_scores(float scale, float softcap) {
   return std::isfinite(scale) && std::isfinite(softcap) && softcap >= 0.0f ? ZO_OK : ZO_ERR_ARG;
+}
+
+// A tensor's elements as its arguments give them: up to three dimensions of runs of contiguous bytes.
+struct Dimension {
+  int64_t count, stride;  // in elements
+};
+struct Tensor {
+  const void* ptr;
+  Dimension d[3];  // the outermost first, as the argument names them
+  int64_t run;
+  size_t size;
+  double bytes;  // from the first to the last, 0 where there are none
+};
+
+Tensor tensor(const void* p, int64_t run, size_t size, Dimension a, Dimension b, Dimension c) {
+  Tensor t = {p, {a, b, c}, run, size, 0.0};
+  if (p != nullptr && a.count > 0 && b.count > 0 && c.count > 0)
+    t.bytes = size * (static_cast<double>(a.count - 1) * a.stride + static_cast<double>(b.count - 1) * b.stride +
+                      static_cast<double>(c.count - 1) * c.stride + run);
+  return t;
+}
+Tensor tensor(const zo_rows& x, int64_t tokens, int64_t heads, int64_t run, size_t size) {
+  return tensor(x.ptr, run, size, {1, 0}, {tokens, x.token}, {heads, x.head});
+}
+Tensor tensor(const zo_pages& x, int64_t pages, int64_t page_size, int64_t heads, int64_t run, size_t size) {
+  return tensor(x.ptr, run, size, {pages, x.page}, {page_size, x.token}, {heads, x.head});
+}
+
+// The same in bytes: dimensions from the widest step down, what is contiguous together as one, the last a run.
+using Wide = __int128;  // any 64-bit strides and counts
+struct Places {
+  int n;
+  Wide count[4], step[4], extent[5];  // extent[i]: bytes from the first to the last of dimensions i ..
+};
+
+Places places(const Tensor& t) {
+  Dimension d[3] = {t.d[0], t.d[1], t.d[2]};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (d[i].stride < d[j].stride) std::swap(d[i], d[j]);
+  Wide count[4], step[4];
+  int n = 0;
+  count[n] = static_cast<Wide>(t.run) * t.size, step[n++] = 1;
+  for (int i = 2; i >= 0; --i) {  // from the innermost out
+    const Wide s = static_cast<Wide>(d[i].stride) * t.size;
+    if (d[i].count == 1) continue;
+    if (s == count[n - 1] * step[n - 1]) {
+      count[n - 1] *= d[i].count;
+    } else {
+      count[n] = d[i].count, step[n++] = s;
+    }
+  }
+  Places r;
+  r.n = n;
+  r.extent[n] = 1;
+  for (int i = n - 1; i >= 0; --i) {
+    r.count[i] = count[n - 1 - i], r.step[i] = step[n - 1 - i];
+    r.extent[i] = r.extent[i + 1] + (r.count[i] - 1) * r.step[i];
+  }
+  return r;
+}
+
+// Whether elements of an output lie over one another (rows or heads with a stride of less than what they hold).
+bool folds(const Tensor& t) {
+  double inner = static_cast<double>(t.run);
+  bool nested = true;  // each dimension's stride passes the ones behind it: mostly, and nothing more is to be looked at
+  for (int i = 2; i >= 0 && nested; --i) {
+    nested = t.d[i].count == 1 || t.d[i].stride >= inner;
+    inner += static_cast<double>(t.d[i].count - 1) * t.d[i].stride;
+  }
+  if (nested || t.bytes == 0.0) return false;
+  const Places a = places(t);
+  for (int i = 0; i + 1 < a.n; ++i)
+    if (a.step[i] < a.count[a.n - 1]) return true;
+  return false;
+}
+
+Wide floor_div(Wide a, Wide b) { return a / b - (a % b < 0); }
+
+// Whether dimensions i.. of a and j.. of b, which starts `delta` bytes behind a, share a byte. Exact where steps are equal,
+// or one step holds few of the other's; false where neither is so, since what cannot be shown is not refused.
+bool meet(Wide delta, const Places& a, int i, const Places& b, int j) {
+  const Wide ea = a.extent[i], eb = b.extent[j];
+  if (delta >= ea || -delta >= eb) return false;
+  const bool run_a = i == a.n - 1, run_b = j == b.n - 1;
+  if (run_a && run_b) return true;
+  if (run_a || (!run_b && a.step[i] < b.step[j])) return meet(-delta, b, j, a, i);  // a has the wider step
+  const Wide step = a.step[i], inner = a.extent[i + 1];
+  if (step == 0) return meet(delta, a, i + 1, b, j);
+  if (!run_b && b.step[j] == step && inner <= step && b.extent[j + 1] <= step) {  // rows k apart: at most two k matter
+    const Wide k0 = floor_div(-delta, step);
+    for (Wide k = k0; k <= k0 + 1; ++k)
+      if (k > -a.count[i] && k < b.count[j] && meet(delta + k * step, a, i + 1, b, j + 1)) return true;
+    return false;
+  }
+  const Wide from = std::max<Wide>(0, floor_div(delta - inner, step) + 1);
+  const Wide to = std::min<Wide>(a.count[i] - 1, floor_div(delta + eb - 1, step));
+  if (run_b && to - from > 1) return true;  // one between the first and the last starts within the run
+  if (to - from > 3) return false;
+  for (Wide x = from; x <= to; ++x)
+    if (meet(delta - x * step, a, i + 1, b, j)) return true;
+  return false;
+}
+
+bool meet(const Tensor& a, const Tensor& b) {
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.ptr), pb = reinterpret_cast<uintptr_t>(b.ptr);
+  // apart, or empty, mostly (a double's rounding aside, which the exact form settles)
+  if (a.bytes == 0.0 || b.bytes == 0.0 ||
+      (pa < pb ? static_cast<double>(pb - pa) > a.bytes * 1.000001 : static_cast<double>(pa - pb) > b.bytes * 1.000001))
+    return false;
+  return meet(static_cast<Wide>(pb) - static_cast<Wide>(pa), places(a), 0, places(b), 0);
+}
+
+// Each element of one at the other's own place.
+bool same_rows(const zo_rows& a, const void* ptr, int64_t token, int64_t head, int64_t tokens, int64_t heads) {
+  return a.ptr == ptr && (tokens <= 1 || a.token == token) && (heads <= 1 || a.head == head);
 }
 
 int finish(cudaError_t e, const char* what) { return e == cudaSuccess ? ZO_OK : zo::report_cuda_error(e, what); }
@@ -102,6 +220,22 @@ int zo_rotate_heads(const zo_head_part* parts, int32_t n_parts, int64_t tokens, 
     if (misaligned(slots, index_bytes)) return ZO_ERR_ALIGN;
   }
   if (n_parts == 0 || tokens == 0) return ZO_OK;
+  Tensor in[3], out[3];
+  for (int i = 0; i < n_parts; ++i) {
+    const zo_head_part& x = parts[i];
+    in[i] = tensor(x.in, tokens, x.heads, head_dim, size);
+    const zo_rows rows = {x.out.ptr, x.out.token, x.out.head};
+    out[i] = (x.flags & ZO_HEADS_SLOTTED) == 0
+                 ? tensor(rows, tokens, x.heads, head_dim, size)
+                 : tensor(x.out, n_slots > 0 ? (n_slots - 1) / page_size + 1 : 0, std::min(n_slots, page_size), x.heads, head_dim, size);
+  }
+  for (int i = 0; i < n_parts; ++i) {
+    const zo_head_part& x = parts[i];
+    const bool in_place = same_rows(x.in, x.out.ptr, x.out.token, x.out.head, tokens, x.heads);
+    if (folds(out[i])) return ZO_ERR_ARG;
+    for (int j = 0; j < n_parts; ++j)
+      if ((meet(out[i], in[j]) && !(i == j && in_place)) || (i < j && meet(out[i], out[j]))) return ZO_ERR_ARG;
+  }
   r.n_parts = n_parts;
   r.dim = head_dim;
   r.rotary = rotate ? rotary_dim : 0;
@@ -136,6 +270,10 @@ int zo_attention(const zo_rows* q, const zo_rows* k, const zo_rows* v, const zo_
   if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
       misaligned(spans, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
     return ZO_ERR_ALIGN;
+  const Tensor to = tensor(*out, q_tokens, heads, head_dim, size);
+  if (folds(to) || meet(to, tensor(*q, q_tokens, heads, head_dim, size)) ||
+      meet(to, tensor(*k, k_tokens, kv_heads, head_dim, size)) || meet(to, tensor(*v, k_tokens, kv_heads, head_dim, size)))
+    return ZO_ERR_ARG;
   const auto lone = [](int64_t stride, int64_t n) { return n > 1 ? stride : 0; };  // one element has no stride
   zo::AttentionParams p = {};
   p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
@@ -180,6 +318,11 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
   if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
       misaligned(pages, 4) || misaligned(lengths, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
     return ZO_ERR_ALIGN;
+  const Tensor to = tensor(*out, batch, heads, head_dim, size);
+  if (folds(to) || meet(to, tensor(*k, n_pages, page_size, kv_heads, head_dim, size)) ||
+      meet(to, tensor(*v, n_pages, page_size, kv_heads, head_dim, size)) ||
+      (!same_rows(*q, out->ptr, out->token, out->head, batch, heads) && meet(to, tensor(*q, batch, heads, head_dim, size))))
+    return ZO_ERR_ARG;
   int sms = 0;
   rc = zo::device_sms(&sms);
   if (rc != ZO_OK) return rc;

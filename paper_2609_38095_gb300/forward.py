@@ -133,7 +133,8 @@ def rotate_heads(q, k=None, v=None, *, table, positions, q_weight=None, k_weight
     """Norms (where a weight is given) and rotation of q (tokens, heads, head_dim) and k (tokens, kv_heads, head_dim);
     v is copied (zo_rotate_heads). Returns what was written, one tensor per tensor given: q alone, (q, k) or (q, k, v);
     new tensors where no *_out is given. With slots (one per token) k and v go to rows of a cache, k_out and v_out:
-    (rows, kv_heads, head_dim) or (pages, page_size, kv_heads, head_dim). q_out may be q, and k_out k."""
+    (rows, kv_heads, head_dim) or (pages, page_size, kv_heads, head_dim). q_out may be q, and k_out k; outputs overlap
+    nothing else."""
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(LAYOUTS)}")
     return _made("zo_rotate_heads", (_B or _binding()).rotate_heads(q, k, v, table, positions, q_weight, k_weight, eps,
@@ -144,7 +145,7 @@ def attention(q, k, v, spans, *, scale=None, softcap=0.0, slopes=None, out=None,
     """Attention of q (tokens, heads, head_dim) over k and v (keys, kv_heads, head_dim), each row over the keys of its
     span (zo_attention). spans: document_spans, or any int32 (3, tokens) of first key, end and own key. softcap: scores
     are softcap * tanh(score / softcap); slopes: float32 (heads), a bias of -slope * distance. Returns out, or (out,
-    lse) with lse float32 (heads, tokens)."""
+    lse) with lse float32 (heads, tokens). An `out` of the caller's overlaps no input."""
     return _made("zo_attention", (_B or _binding()).attention(q, k, v, spans, scale, softcap, slopes, out, with_lse))
 
 
@@ -152,7 +153,7 @@ def decode_attention(q, k_cache, v_cache, pages, lengths, *, scale=None, softcap
     """Attention of one new token per sequence, q (batch, heads, head_dim), over the first lengths[b] keys of each
     sequence, its own the last (zo_attention_decode). k_cache, v_cache: (pages, page_size, kv_heads, head_dim); pages:
     int32 (batch, pages of the longest); lengths: int32 (batch). Returns out, or (out, lse) with lse float32 (batch,
-    heads)."""
+    heads). An `out` of the caller's may be q, and overlaps nothing else."""
     return _made("zo_attention_decode", (_B or _binding()).decode_attention(q, k_cache, v_cache, pages, lengths, scale, softcap,
                                                                             slopes, out, with_lse))
 
