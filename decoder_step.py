@@ -123,7 +123,8 @@ class Answer:
         shape = (sum(need), page_size, model.kv_heads, model.head_dim)
         self.caches = [tuple(torch.empty(shape, dtype=model.dtype, device="cuda") for _ in range(2)) for _ in range(model.layers)]
         order = torch.randperm(sum(need), generator=torch.Generator().manual_seed(1)).tolist()
-        self.pages = torch.zeros(len(prompts), max(need), dtype=torch.int32)
+        self.pages = torch.full((len(prompts), max(need)), -1, dtype=torch.int32)   # -1: no page
+        self.rows_left = min(n * page_size - m for n, m in zip(need, lengths))
         for b, n in enumerate(need):
             self.pages[b, :n] = torch.tensor(order[:n])
             del order[:n]
@@ -144,10 +145,14 @@ class Answer:
         self.logits = model.logits(torch.cat([torch.as_tensor(p) for p in prompts]).cuda(), positions, attend)[starts[1:].long() - 1]
 
     def _slots(self, sequence, positions):
-        return self.pages[sequence, positions // self.page_size].long() * self.page_size + positions % self.page_size
+        page = self.pages[sequence, positions // self.page_size].long()
+        return torch.where(page < 0, -1, page * self.page_size + positions % self.page_size)
 
     def next(self, tokens):
-        """Appends one token to each sequence; returns the logits after it."""
+        """Appends one token to each sequence; returns the logits after it. ValueError when a sequence's pages are full."""
+        if self.rows_left == 0:
+            raise ValueError("a sequence's pages are full: there is no room for another token")
+        self.rows_left -= 1
         positions = self.lengths.long()
         slots = self._slots(torch.arange(len(positions), device="cuda"), positions)
         self.lengths += 1
