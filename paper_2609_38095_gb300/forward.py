@@ -86,13 +86,13 @@ def _made(what, result):
     return result
 
 
-def _flat(t, what, dtypes, device, n=None):
+def _flat(t, what, dtypes, device=None, n=None):
     """Checks a contiguous vector of numbers, of n elements."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor")
     if t.dtype not in dtypes:
         raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if t.device != device:
+    if device is not None and t.device != device:
         raise ValueError(f"{what} is on {t.device}, expected {device}")
     if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
         raise ValueError(f"{what} must be contiguous, with one dimension" + (f" and {n} elements" if n is not None else ""))
@@ -115,7 +115,7 @@ def rotary_table(rows, rotary_dim, base=10000.0, scale=1.0, original=0, low=1.0,
 def document_spans(q_starts, k_starts=None, prefix=None, *, tokens):
     """int32 (3, tokens): for each packed query row its first key, the end of its keys and its own key
     (zo_document_spans). q_starts and k_starts (q_starts by default): int32, one more than there are documents."""
-    _flat(q_starts, "q_starts", (torch.int32,), q_starts.device)
+    _flat(q_starts, "q_starts", (torch.int32,))
     dev, docs = q_starts.device, q_starts.numel() - 1
     if docs < 0:
         raise ValueError("q_starts must have one element more than there are documents")
