@@ -69,7 +69,7 @@ def _binding():
     global _B
     if _B is None:
         if not os.path.exists(BINDING_PATH):
-            raise RuntimeError(f"{BINDING_PATH} is not built; run paper_2609_38095_gb300.build.build()")
+            raise RuntimeError(f"{BINDING_PATH} is not built; run paper_2609_38095_gb300.build.build_binding()")
         loader = importlib.machinery.ExtensionFileLoader(__package__ + "._binding", BINDING_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
         loader.exec_module(module)
