@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         mbar_init(&sh.o_done[s][b], 1);
       }
       mbar_init(&sh.drain[s], 1);
+      for (int w = 0; w < kRows / 32; ++w) sh.left[s][w] = 0;
       sh.lo[s] = 0x7FFFFFFF;
       sh.hi[s] = 0;
     }
@@ -185,6 +186,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     }
   }
 
+  int again = 0;  // whether rows are left for attention_rows
   if (warp == kSoftmaxWarps + kSlots) {
     if (lane == 0) {
       int issued = 0;
@@ -458,25 +460,27 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     if (row < p.q_tokens && p.lse != nullptr) p.lse[h * p.q_tokens + row] = lse;
     // (a sum that is NaN is that of seen scores, and the outputs' too)
     const uint32_t left = __ballot_sync(0xFFFFFFFFu, alive && row < p.q_tokens && !finite && total < kInf);
-    sh.lse[slot][tid & 127] = lse;
+    if (left != 0) {
+      sh.lse[slot][tid & 127] = lse;
+      if (lane == 0) sh.left[slot][warp & 3] = left;
+      again = 1;
+    }
     if (lane == 0) {
-      sh.left[slot][warp & 3] = left;
       if (left != 0) tma_stored<false>();  // those rows are read again
       else tma_stored<true>();
     }
     __syncwarp();
   }
   tmem_fence_before();
-  __syncthreads();
+  again = __syncthreads_or(again);
   if (warp == kSoftmaxWarps) {
     tmem_fence_after();
     tmem_free(tmem, L::kColumns);
   }
-#pragma unroll
+  if (again == 0) return;
   for (int s = 0; s < kSlots; ++s)
-    if ((sh.left[s][0] | sh.left[s][1] | sh.left[s][2] | sh.left[s][3]) != 0)
-      attention_rows<T, D, 2>(p, static_cast<int64_t>(block_of(s)) * kRows, head_of(s), sh.left[s], sh.lse[s],
-                                kRows / 32, warp, L::kThreads / 32, lane);
+    attention_rows<T, D, 2>(p, static_cast<int64_t>(block_of(s)) * kRows, head_of(s), sh.left[s], sh.lse[s], kRows / 32,
+                            warp, L::kThreads / 32, lane);
 }
 
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
