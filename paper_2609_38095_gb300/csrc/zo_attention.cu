@@ -63,7 +63,7 @@ __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stri
 // joins its outputs over distributed shared memory, each CTA a part of the rows.
 // Bound by the multiply-adds and the shared-memory loads that feed them: 3000
 // causal tokens of 32 heads of 128 in fp32 2.29 ms = 32 TFLOP/s, 5 documents of at
-// most 333 over 100 cached keys (16 heads of 80, capped and biased) 88 us. Eight
+// most 333 over 100 cached keys (16 heads of 80, capped and biased) 88 to 99 us. Eight
 // rows per thread on half the threads: 2.90 ms and 102 us, for want of warps.
 template <typename T, int DP, bool kVec>
 __global__ void __launch_bounds__(kThreads256, DP <= 128 ? 2 : 1)

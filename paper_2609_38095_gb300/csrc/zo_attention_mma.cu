@@ -67,29 +67,34 @@ struct MmaShared {
 // Bits 0 to n - 1.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// A CTA has two slots of 128 query rows: two heads that share their keys (the
-// same rows, the same spans) where a group has an even number of them, else two
-// tiles of rows of one head. Keys and values come in tiles of 128 and go through
-// the products in steps of 64.
+// A slot is 128 query rows of a head. A CTA of two slots has two heads that share
+// their keys (the same rows, the same spans) where a group has an even number of
+// them, else two tiles of rows of one head; a CTA of one slot has one. Keys and
+// values come in tiles of 128 (one slot: 64) and go through the products in steps
+// of 64.
 //
-//   warps 0-3, 4-7   softmax of slot 0, 1: a thread has a row
-//   warps 8, 9       the matrix products of slot 0, 1, one thread each: a warp alone issues a step's in more time than
-//                    they take
-//   warp 10          TMA loads, one thread (11 only sets up the barriers)
+//   two slots        one slot
+//   warps 0-3, 4-7   0-3       softmax of slot 0, 1: a thread has a row
+//   warps 8, 9       4         the matrix products of slot 0, 1, one thread each: a warp alone issues a step's for both in
+//                              more time than they take
+//   warp 10          5         TMA loads, one thread (11 and 6 set up the barriers)
 //
-// Tensor memory (512 columns): a slot's scores of two steps, 64 columns each, the
-// weights of a step in 16 bits over the first half of its scores; outputs from
-// column 256 on. S = Q K^T has both operands in shared memory; O += P V takes P
-// from tensor memory and V as TMA left it, along N. Behind step i's output go
-// step i + 2's scores, into the place of the weights that it has read: a slot's
+// Tensor memory (512 columns, or 256): a slot's scores of two steps, 64 columns
+// each, the weights of a step in 16 bits over the first half of its scores; outputs
+// from column 256 (128) on. S = Q K^T has both operands in shared memory; O += P V
+// takes P from tensor memory and V as TMA left it, along N. Behind step i's output
+// go step i + 2's scores, into the place of the weights that it has read: a slot's
 // softmax always has its next scores, and its tensor-core warp one wait per step.
 //
-// What bounds it: the products with 64 columns read 6 KB of shared memory in the
-// 32 cycles that they would take, so a step is 384 + 256 cycles per slot, 2560 for
-// 128 keys and both slots; it runs at some 2880 (8192 tokens, 32 / 8 heads of 128,
-// bf16: 333 us = 1.65 PFLOP/s). With 128 columns they would take 2048, but there is
-// no tensor memory for a second step's scores then, and a slot's softmax, 1600
-// cycles and two waits of 400, is in series with its own products (460 us).
+// What bounds it, two slots and heads of 128: a product with 64 columns reads 6 KB
+// of shared memory in the 32 cycles that it would take; 16 of them and 8 with 128
+// columns, a slot's for 128 keys, were measured alone at 1262 cycles (1024 by the
+// columns), so 2524 for both slots, where the kernel takes some 2880. 8192 tokens,
+// 32 / 8 heads of 128, bf16: 334 to 339 us = 1.63 PFLOP/s for the first tens of
+// launches after a pause, 360 us = 1.53 once the GPU's clock has settled under the
+// load. With steps of 128 keys the products would take 2048 cycles, but there is no
+// tensor memory for a second step's scores then, and a slot's softmax, 1600 cycles
+// and two waits of 400, is in series with its own products (460 us).
 //
 // The output is rescaled only when a row's maximum has passed the reference that
 // its weights are relative to by 2^8, which seldom happens after the first steps:
@@ -512,9 +517,11 @@ cudaError_t launch_head(const CUtensorMap (&m)[4], const AttentionParams& p, boo
   return two ? launch_slots<T, 128, 2>(m, p, stream) : launch_slots<T, 128, 1>(m, p, stream);
 }
 
-// Whether a CTA takes two slots. The spans are on the device, so this goes by the keys there are: two CTAs of one slot per
-// SM hide each other's starts and ends (one document of 512 tokens 10.1 against 11.8 us, of 1024 18.8 / 17.2; 24 of at most
-// 256 24.9 / 28.7), two slots share their keys' tiles and issue ahead (one of 2048 tokens 40 / 32 us, of 8192 476 / 335).
+// Whether a CTA takes two slots: two CTAs of one slot per SM hide each other's starts and ends (one document of 512 tokens
+// 10.1 us with one slot, 11.8 with two; of 1024 18.8 / 17.2), two slots share their keys' tiles and issue ahead (of 2048 tokens
+// 40 / 32, of 8192 476 / 335). The spans are on the device, so this goes by all the keys of a call, as if they were one
+// document's: a packed batch beyond 768 keys takes two slots though its documents are short (24 of at most 256 24.9 / 28.7),
+// since two slots lose less there than one slot does on a long document.
 bool two_slots(const AttentionParams& p) { return p.k_tokens > 768; }
 
 }  // namespace

@@ -23,8 +23,9 @@ struct Scalar {
 // on its way (fp32 caches by cp.async; others are widened on the way and stored
 // before the products start). Scores: a lane has half of a key's dot product
 // with every head; outputs: a lane has DP / 32 elements of every head. Bound by
-// shared memory and instructions before HBM: 16 sequences of up to 4001 keys, fp32,
-// 32 / 8 heads of 128 in 120 us = 2.4 TB/s, 40 / 40 heads (2000 keys) 194 us = 3.6.
+// shared memory and instructions before HBM (134 KB of tiles and queries leave one
+// CTA of 4 warps per SM at heads of 128): 16 sequences of up to 4001 keys, fp32, 32 / 8
+// heads of 128 in 112 us = 2.5 TB/s, 40 / 40 heads (2000 keys) 194 us = 3.6.
 template <typename T, int DP, int HB, bool kAsync>
 __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
     decode_scalar_kernel(const __grid_constant__ DecodeParams p) {

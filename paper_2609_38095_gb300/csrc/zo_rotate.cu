@@ -343,7 +343,9 @@ __global__ void document_spans_kernel(const int32_t* q_starts, const int32_t* k_
   }
 }
 
-// Whether every vector of a part, its weight's among them, starts on `bytes` bytes and is of the data's type.
+// Whether every vector of a part, its weight's among them, starts on `bytes` bytes and is of the data's type. (A weight of
+// another type alone leaves aligned heads to rotate_heads_any_kernel: 4091 tokens of 40 heads of 128, bf16, with fp32 weights
+// 82 us against 16.7.)
 template <typename T>
 bool part_aligned(const RotatePart& r, int64_t bytes) {
   const int64_t n = bytes / static_cast<int64_t>(sizeof(T));

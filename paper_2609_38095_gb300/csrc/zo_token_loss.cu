@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
   }
 }
 
-// A token per warp, for small vocabularies: a CTA per token would come and go in more time than its row takes (4000 rows
-// of 2001, fp16: 41 us).
+// A token per warp, for vocabularies of at most 4096: a CTA per token would come and go in more time than its row takes (4000
+// rows of 2001, fp16: 21 us, with a CTA per token 41; the bytes alone 2.4).
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads) token_loss_warp_kernel(const __grid_constant__ TokenLossParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
