@@ -291,8 +291,8 @@ struct Elements<T, 2> {
 // which a key that the row sees has such a value stays as it is; the others are formed again from the seen keys alone,
 // kBatch at a time, with the weights exp(s - lse). The last key found for a column is the first looked at for the rows that
 // follow, so that a warp walks to a late one once and not once per row. kPer = 2: pairs of elements are aligned. (4096
-// tokens, 8 heads of 128: bf16 clean 51 us, an infinity or NaN in the first key's values 142, in key 3000's 1.26 ms, most
-// of it the 56 rows before that key in its tile; fp32 1.15, 1.30 and 2.67 ms.)
+// tokens, 8 heads of 128: bf16 clean 50 us, an infinity or NaN in the first key's values 140, in key 3000's 1.19 ms, most
+// of it the 56 rows before that key in its tile; fp32 1.12, 1.31 and 2.66 ms.)
 template <typename T, int kDim, int kPer>
 __device__ __noinline__ void attention_rows(const AttentionParams& p, int64_t row0, int h, const uint32_t* left,
                                             const float* lse, int words, int part, int parts, int lane) {
@@ -375,17 +375,17 @@ __device__ __noinline__ void attention_rows(const AttentionParams& p, int64_t ro
       float s[kRows * kBatch];
 #pragma unroll
       for (int n = 0; n < kBatch; ++n) {
-        Wide sums[kRows];
+        Wide dots[kRows];
 #pragma unroll
-        for (int m = 0; m < kRows; ++m) sums[m] = Load::twice(0.0f);
+        for (int m = 0; m < kRows; ++m) dots[m] = Load::twice(0.0f);
 #pragma unroll
         for (int c = 0; c < kLoads; ++c) {
           const Wide f = kk[n][c].wide();
 #pragma unroll
-          for (int m = 0; m < kRows; ++m) sums[m] = Load::times_plus(qr[m][c], f, sums[m]);
+          for (int m = 0; m < kRows; ++m) dots[m] = Load::times_plus(qr[m][c], f, dots[m]);
         }
 #pragma unroll
-        for (int m = 0; m < kRows; ++m) s[m * kBatch + n] = Load::at(sums[m], 0) + (kPer == 2 ? Load::at(sums[m], 1) : 0.0f);
+        for (int m = 0; m < kRows; ++m) s[m * kBatch + n] = Load::at(dots[m], 0) + (kPer == 2 ? Load::at(dots[m], 1) : 0.0f);
       }
       // the lanes' sums, each lane left with that of its key and row
 #pragma unroll
@@ -404,11 +404,31 @@ __device__ __noinline__ void attention_rows(const AttentionParams& p, int64_t ro
       if (p.slopes != nullptr) x -= slope * fabsf(static_cast<float>(self - static_cast<int64_t>(j)));
       const float w = j >= my_first && j < my_end ? __expf(x - my_lse) : 0.0f;
       total += w;
-      Wide zeros = Load::twice(0.0f);  // 0 times the values: NaN where one is not finite
+      Wide sums[kRows][kLoads];  // the batch's
+      const auto weigh = [&] {
 #pragma unroll
-      for (int n = 0; n < kBatch; ++n)
+        for (int m = 0; m < kRows; ++m)
 #pragma unroll
-        for (int c = 0; c < kLoads; ++c) zeros = Load::times_plus(vv[n][c].wide(), Load::twice(0.0f), zeros);
+          for (int c = 0; c < kLoads; ++c) sums[m][c] = Load::twice(0.0f);
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+          Wide wn[kRows];
+#pragma unroll
+          for (int m = 0; m < kRows; ++m) wn[m] = Load::twice(__shfl_sync(0xFFFFFFFFu, w, m * kBatch + n));
+#pragma unroll
+          for (int c = 0; c < kLoads; ++c) {
+            const Wide f = vv[n][c].wide();
+#pragma unroll
+            for (int m = 0; m < kRows; ++m) sums[m][c] = Load::times_plus(wn[m], f, sums[m][c]);
+          }
+        }
+      };
+      weigh();
+      Wide zeros = Load::twice(0.0f);  // 0 times the sums: NaN where a value is not finite
+#pragma unroll
+      for (int c = 0; c < kLoads; ++c)
+#pragma unroll
+        for (int m = 0; m < kRows; ++m) zeros = Load::times_plus(sums[m][c], Load::twice(0.0f), zeros);
       if (__any_sync(0xFFFFFFFFu, Load::at(zeros, 0) != 0.0f || Load::at(zeros, kPer - 1) != 0.0f)) {
 #pragma unroll
         for (int n = 0; n < kBatch; ++n)
@@ -424,19 +444,12 @@ __device__ __noinline__ void attention_rows(const AttentionParams& p, int64_t ro
                 for (int m = 0; m < kRows; ++m)
                   if (at >= first[m] && at < end[m]) open[m] &= ~(1u << (c * kPer + e));
               }
+        weigh();
       }
 #pragma unroll
-      for (int n = 0; n < kBatch; ++n) {
-        Wide wn[kRows];
+      for (int c = 0; c < kLoads; ++c)
 #pragma unroll
-        for (int m = 0; m < kRows; ++m) wn[m] = Load::twice(__shfl_sync(0xFFFFFFFFu, w, m * kBatch + n));
-#pragma unroll
-        for (int c = 0; c < kLoads; ++c) {
-          const Wide f = vv[n][c].wide();
-#pragma unroll
-          for (int m = 0; m < kRows; ++m) acc[m][c] = Load::times_plus(wn[m], f, acc[m][c]);
-        }
-      }
+        for (int m = 0; m < kRows; ++m) acc[m][c] = Load::times_plus(sums[m][c], Load::twice(1.0f), acc[m][c]);
     }
 #pragma unroll
     for (int m = 0; m < kRows; ++m) {
