@@ -11,11 +11,19 @@
  *   zo_attention_decode  attention of one new token per sequence over a paged cache
  *   zo_token_loss        -log p of every target token, summed into a loss table
  *
+ * and of learning from a model's own answers:
+ *
+ *   zo_draft_masks       what drafted tokens see of one another, from their parents
+ *   zo_attention_draft   attention of a tree of drafted tokens per sequence over a paged cache
+ *   zo_policy_loss       clipped policy loss of answers' tokens, with a KL term, and its gradient
+ *   zo_preference_loss   loss of pairs of answers, preferred and rejected, and its gradient
+ *
  * Conventions are those of zo.h: device memory owned by the caller, calls that
  * only enqueue work on `stream` of the current device, zo_status returned,
  * argument errors found before anything is enqueued, nothing allocated and
  * nothing kept. The method estimates its gradient from losses, so there are
- * no backward passes.
+ * no backward passes but those of the two losses over answers, which write
+ * the gradient in the logits beside the loss where they are asked to.
  *
  * Data-dependent errors (a position outside the table, a page outside the
  * cache, a target outside the vocabulary) cannot be seen on the host: the
@@ -196,6 +204,107 @@ int64_t zo_token_loss_workspace_size(int64_t tokens);
 int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
                   int32_t target_bytes, int32_t flags, void* loss, float* nll, void* workspace,
                   int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * zo_draft_masks -- masks[b][i]: bit j is set where node j is i itself or one
+ * of its ancestors in sequence b's tree of drafted tokens.
+ *   parents  int32 [batch][drafts]: a node's parent, which comes before it; -1:
+ *            it follows the sequence's last token. Anything else is no node:
+ *            its mask, and its descendants', is 0.
+ *   drafts   1 .. ZO_MAX_DRAFTS
+ *   masks    out, int64 [batch][drafts]
+ * ------------------------------------------------------------------------- */
+#define ZO_MAX_DRAFTS 64
+
+int zo_draft_masks(const int32_t* parents, int64_t batch, int32_t drafts, int64_t* masks, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * zo_attention_draft -- zo_attention_decode of several rows per sequence, the
+ * nodes of a tree of drafted tokens: keys 0 .. lengths[b] - 1 are the
+ * sequence's so far, key lengths[b] + j is node j's own. Node i sees the
+ * former, and key lengths[b] + j where bit j (< drafts) of its mask is set;
+ * without such a bit, or with a negative length, it sees nothing: out = 0, lse
+ * = -inf. The place of a key j < lengths[b], for the bias by distance, is j; a
+ * node's is lengths[b] + (bits of its mask) - 1.
+ * A node's key that no node sees is not looked up, nor is its page; what lies
+ * at one does not reach the result of a row that does not see it. A page
+ * outside the cache, or more keys than the page table or 31 bits hold, give
+ * NaN in all rows of the sequence that see anything.
+ *   q, out  node i of sequence b, head h at ptr[b * page + i * token + h * head];
+ *           out may be q (same strides) and overlaps nothing else
+ *   masks   int64 [batch][drafts], zo_draft_masks's or the caller's own
+ *   lse     fp32 [batch][drafts][heads] or NULL
+ * ------------------------------------------------------------------------- */
+int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, const zo_pages* out, int64_t batch,
+                       int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                       const int32_t* pages, int64_t pages_stride, int64_t max_pages, int64_t n_pages,
+                       int32_t page_size, const int32_t* lengths, const int64_t* masks, float scale, float softcap,
+                       const float* slopes, float* lse, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * zo_policy_loss -- with logp_t = x_t,target_t - log sum_v exp(x_tv), r_t =
+ * exp(logp_t - old_t) and d_t = ref_t - logp_t, over the counted tokens (those
+ * whose target is not negative; nothing of the others is read):
+ *   l_t = -min(r_t A_t, clamp(r_t, 1 - clip_low, 1 + clip_high) A_t)
+ *         + kl (exp(d_t) - d_t - 1)
+ *   loss = sum_t w_t l_t
+ * and, where grad is given, for every token and v
+ *   grad_tv = grad_scale dloss/dx_tv = grad_scale w_t c_t (1[v = target_t] - p_tv)
+ *   c_t = -r_t A_t, or 0 where the clamp is the smaller, + kl (1 - exp(d_t))
+ * (0 for tokens that do not count). The second form of the ratio's KL divergence
+ * is never negative and has the right mean. The order of additions depends on
+ * `tokens` alone.
+ *   old_logp, advantages  fp32 [tokens]
+ *   ref_logp     fp32 [tokens]; NULL (with kl = 0): no such term
+ *   weights      fp32 [tokens], or NULL: 1
+ *   clip_low     0 .. 1; clip_high and kl 0 or more, finite
+ *   flags        ZO_LOSS_MEAN: divided by the counted tokens' weights (NaN where
+ *                their sum is 0), the gradient too; ZO_LOSS_ADD, ZO_LOSS_F32 as
+ *                for zo_token_loss (the gradient is written, not added)
+ *   grad         [tokens][vocab] of the logits' type, grad_row elements from one
+ *                token to the next, or NULL; it may be the logits (same row) and
+ *                overlaps nothing else
+ *   grad_scale   e.g. to keep small gradients in fp16's range
+ *   logp         fp32 [tokens], 0 where the token does not count, or NULL
+ *   workspace    zo_policy_loss_workspace_size(tokens) bytes, 8-byte aligned
+ * ------------------------------------------------------------------------- */
+int64_t zo_policy_loss_workspace_size(int64_t tokens);
+int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
+                   int32_t target_bytes, const float* old_logp, const float* advantages, const float* ref_logp,
+                   const float* weights, float clip_low, float clip_high, float kl, int32_t flags, void* loss,
+                   void* grad, int64_t grad_row, float grad_scale, float* logp, void* workspace,
+                   int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * zo_preference_loss -- sequence j is rows starts[j] .. starts[j+1] - 1;
+ * sequence 2i is pair i's preferred answer, 2i + 1 its rejected one. s_j is the
+ * sum of logp_t over its counted tokens, with ZO_LOSS_BY_LENGTH divided by their
+ * number (if any). With e = smoothing, softplus(x) = log(1 + exp(x)):
+ *   m_i = beta ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)) - margin
+ *   loss = sum_i (1 - e) softplus(-m_i) + e softplus(m_i)
+ * and, where grad is given, grad_tv = grad_scale dloss/dx_tv; 0 for rows in no
+ * sequence (whose targets do not count) and tokens that do not count. Starts
+ * that descend or lie outside 0 .. tokens make the loss, every logp and the
+ * counted rows' gradient NaN.
+ *   starts       int32 [2 pairs + 1]
+ *   ref_logp     fp32 [2 pairs]: the sequences' s_j under the reference model, or
+ *                NULL: 0
+ *   beta         finite, 0 or more; smoothing 0 .. 1
+ *   flags        ZO_LOSS_MEAN: over the pairs (NaN if there are none), the
+ *                gradient too; ZO_LOSS_BY_LENGTH; ZO_LOSS_ADD, ZO_LOSS_F32
+ *   logp         fp32 [2 pairs], s_j, or NULL
+ *   workspace    zo_preference_loss_workspace_size(tokens, pairs) bytes, 8-byte
+ *                aligned
+ * The rest is zo_policy_loss's.
+ * ------------------------------------------------------------------------- */
+#define ZO_LOSS_BY_LENGTH 8
+
+int64_t zo_preference_loss_workspace_size(int64_t tokens, int64_t pairs);
+int zo_preference_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype,
+                       const void* targets, int32_t target_bytes, const int32_t* starts, int64_t pairs,
+                       const float* ref_logp, float beta, float margin, float smoothing, int32_t flags, void* loss,
+                       void* grad, int64_t grad_row, float grad_scale, float* logp, void* workspace,
+                       int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,11 @@ decltype(&zo_rotate_heads) g_rotate_heads = nullptr;
 decltype(&zo_attention) g_attention = nullptr;
 decltype(&zo_attention_decode) g_attention_decode = nullptr;
 decltype(&zo_token_loss) g_token_loss = nullptr;
+decltype(&zo_policy_loss) g_policy_loss = nullptr;
+decltype(&zo_preference_loss) g_preference_loss = nullptr;
+decltype(&zo_attention_draft) g_attention_draft = nullptr;
+decltype(&zo_policy_loss_workspace_size) g_policy_work = nullptr;
+decltype(&zo_preference_loss_workspace_size) g_preference_work = nullptr;
 
 // Whether tensors may have tangents in this call: within a level of forward mode. (Asked once per call; asking each tensor
 // took 0.5 us of a call of nine.)
@@ -143,19 +148,25 @@ int on_stream(const at::Tensor& t, F f) {
   return f(c10::cuda::getCurrentCUDAStream(t.device().index()).stream());
 }
 
-PyObject* first_or_both(Output& a, Output& b, bool both) {
-  if (!both) return a.take();
-  PyObject* r = PyTuple_New(2);
+// The first output alone, or a tuple of it and those of the others that there are.
+PyObject* with_others(Output& first, std::initializer_list<Output*> others) {
+  Py_ssize_t n = 1;
+  for (const Output* x : others) n += x->o != nullptr;
+  if (n == 1) return first.take();
+  PyObject* r = PyTuple_New(n);
   if (r == nullptr) throw python_error();
-  PyTuple_SET_ITEM(r, 0, a.take());
-  PyTuple_SET_ITEM(r, 1, b.take());
+  PyTuple_SET_ITEM(r, 0, first.take());
+  n = 1;
+  for (Output* x : others)
+    if (x->o != nullptr) PyTuple_SET_ITEM(r, n++, x->take());
   return r;
 }
 
 zo_rows rows_of(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.stride(1)}; }
 zo_pages pages_of(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)}; }
 
-// What attention and decode_attention share: q, k, v, slopes, out.
+// What attention, decode_attention and draft_attention share: q, k, v, slopes, out. Heads and their elements are the last
+// two dimensions.
 struct Attention {
   const at::Tensor &q, &k, &v;
   int32_t n = 0, kv = 0, size = 0;  // query heads, key-value heads, head size
@@ -163,16 +174,16 @@ struct Attention {
   float scale = 0.0f, softcap = 0.0f;
   Output out, lse;
 
-  Attention(PyObject* const* a, int64_t dim, PyObject* scale_, PyObject* softcap_, PyObject* slopes_, PyObject* out_)
-      : q(heads(a[0], "q", 3)), k(heads(a[1], "k", dim, &q)), v(heads(a[2], "v", dim, &q)) {
-    if (k.sizes() != v.sizes() || k.size(-1) != q.size(2)) value_error("k and v must have the same shape and q's head size");
-    if (k.size(-2) == 0 || q.size(1) % k.size(-2) != 0) value_error("the key-value heads must divide the query heads");
-    n = count(q.size(1), "the number of heads"), kv = count(k.size(-2), "the number of heads"), size = count(q.size(2), "the head size");
-    if (given(slopes_)) slopes = flat(slopes_, "slopes", {at::kFloat}, q, {q.size(1)}).const_data_ptr<float>();
-    scale = given(scale_) ? static_cast<float>(number(scale_)) : static_cast<float>(1.0 / std::sqrt(static_cast<double>(q.size(2))));
+  Attention(PyObject* const* a, int64_t q_dim, int64_t dim, PyObject* scale_, PyObject* softcap_, PyObject* slopes_, PyObject* out_)
+      : q(heads(a[0], "q", q_dim)), k(heads(a[1], "k", dim, &q)), v(heads(a[2], "v", dim, &q)) {
+    if (k.sizes() != v.sizes() || k.size(-1) != q.size(-1)) value_error("k and v must have the same shape and q's head size");
+    if (k.size(-2) == 0 || q.size(-2) % k.size(-2) != 0) value_error("the key-value heads must divide the query heads");
+    n = count(q.size(-2), "the number of heads"), kv = count(k.size(-2), "the number of heads"), size = count(q.size(-1), "the head size");
+    if (given(slopes_)) slopes = flat(slopes_, "slopes", {at::kFloat}, q, {q.size(-2)}).const_data_ptr<float>();
+    scale = given(scale_) ? static_cast<float>(number(scale_)) : static_cast<float>(1.0 / std::sqrt(static_cast<double>(q.size(-1))));
     softcap = static_cast<float>(number(softcap_));
     if (given(out_)) {
-      if (heads(out_, "out", 3, &q).sizes() != q.sizes()) value_error("out must have q's shape");
+      if (heads(out_, "out", q_dim, &q).sizes() != q.sizes()) value_error("out must have q's shape");
       out.is(out_);
     } else {
       out.make(q.sizes(), q, q.scalar_type());
@@ -181,7 +192,7 @@ struct Attention {
 };
 
 PyObject* attention(PyObject* const* a) {  // q, k, v, spans, scale, softcap, slopes, out, with_lse
-  Attention c(a, 3, a[4], a[5], a[6], a[7]);
+  Attention c(a, 3, 3, a[4], a[5], a[6], a[7]);
   const int64_t tokens = c.q.size(0);
   const at::Tensor& spans = flat(a[3], "spans", {at::kInt}, c.q, {3, tokens});
   const bool with_lse = truth(a[8]);
@@ -192,16 +203,21 @@ PyObject* attention(PyObject* const* a) {  // q, k, v, spans, scale, softcap, sl
                        spans.const_data_ptr<int32_t>(), c.scale, c.softcap, c.slopes,
                        with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
   });
-  return rc != ZO_OK ? PyLong_FromLong(rc) : first_or_both(c.out, c.lse, with_lse);
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.out, {&c.lse});
+}
+
+const at::Tensor& page_table(PyObject* o, const at::Tensor& q, int64_t batch) {
+  const at::Tensor& pages = cuda_tensor(o, "pages");
+  if (pages.scalar_type() != at::kInt || pages.device() != q.device()) type_error("pages must be an int32 tensor on q's device");
+  if (pages.dim() != 2 || pages.size(0) != batch || (pages.size(1) > 1 && pages.stride(1) != 1))
+    value_error("pages must have one row per sequence, contiguous");
+  return pages;
 }
 
 PyObject* decode_attention(PyObject* const* a) {  // q, k, v, pages, lengths, scale, softcap, slopes, out, with_lse
-  Attention c(a, 4, a[5], a[6], a[7], a[8]);
+  Attention c(a, 3, 4, a[5], a[6], a[7], a[8]);
   const int64_t batch = c.q.size(0);
-  const at::Tensor& pages = cuda_tensor(a[3], "pages");
-  if (pages.scalar_type() != at::kInt || pages.device() != c.q.device()) type_error("pages must be an int32 tensor on q's device");
-  if (pages.dim() != 2 || pages.size(0) != batch || (pages.size(1) > 1 && pages.stride(1) != 1))
-    value_error("pages must have one row per sequence, contiguous");
+  const at::Tensor& pages = page_table(a[3], c.q, batch);
   const at::Tensor& lengths = flat(a[4], "lengths", {at::kInt}, c.q, {batch});
   if (c.k.size(1) < 1) value_error("a page must hold at least one row");
   const int32_t page_size = count(c.k.size(1), "the page size");
@@ -215,7 +231,29 @@ PyObject* decode_attention(PyObject* const* a) {  // q, k, v, pages, lengths, sc
                               lengths.const_data_ptr<int32_t>(), c.scale, c.softcap, c.slopes,
                               with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
   });
-  return rc != ZO_OK ? PyLong_FromLong(rc) : first_or_both(c.out, c.lse, with_lse);
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.out, {&c.lse});
+}
+
+// q, k, v, pages, lengths, masks, scale, softcap, slopes, out, with_lse
+PyObject* draft_attention(PyObject* const* a) {
+  Attention c(a, 4, 4, a[6], a[7], a[8], a[9]);
+  const int64_t batch = c.q.size(0), drafts = c.q.size(1);
+  const at::Tensor& pages = page_table(a[3], c.q, batch);
+  const at::Tensor& lengths = flat(a[4], "lengths", {at::kInt}, c.q, {batch});
+  const at::Tensor& masks = flat(a[5], "masks", {at::kLong}, c.q, {batch, drafts});
+  if (drafts < 1 || drafts > ZO_MAX_DRAFTS) value_error("a sequence has 1 to " + std::to_string(ZO_MAX_DRAFTS) + " drafted tokens");
+  if (c.k.size(1) < 1) value_error("a page must hold at least one row");
+  const int32_t page_size = count(c.k.size(1), "the page size");
+  const bool with_lse = truth(a[10]);
+  if (with_lse) c.lse.make({batch, drafts, c.n}, c.q, at::kFloat);
+  const zo_pages q = pages_of(c.q), k = pages_of(c.k), v = pages_of(c.v), out = pages_of(c.out.t);
+  const int rc = on_stream(c.q, [&](void* stream) {
+    return g_attention_draft(&q, &k, &v, &out, batch, static_cast<int32_t>(drafts), c.n, c.kv, c.size, code(c.q.scalar_type()),
+                             pages.const_data_ptr<int32_t>(), pages.stride(0), pages.size(1), c.k.size(0), page_size,
+                             lengths.const_data_ptr<int32_t>(), masks.const_data_ptr<int64_t>(), c.scale, c.softcap, c.slopes,
+                             with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
+  });
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.out, {&c.lse});
 }
 
 // q, k, v, table, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, v_out, slots
@@ -310,7 +348,93 @@ PyObject* token_loss(PyObject* const* a) {  // logits, targets, mean, add, out, 
                         targets.const_data_ptr(), index_bytes(targets), flags, out.t.data_ptr(),
                         with_nll ? static_cast<float*>(nll.t.data_ptr()) : nullptr, work.data_ptr(), work.numel() * 8, stream);
   });
-  return rc != ZO_OK ? PyLong_FromLong(rc) : first_or_both(out, nll, with_nll);
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(out, {&nll});
+}
+
+// What the losses over answers share: logits, targets, and the outputs.
+struct AnswerLoss {
+  const at::Tensor& logits;
+  const at::Tensor& targets;
+  const int64_t tokens;
+  Output loss, grad, logp;
+  int flags = 0;
+  float grad_scale = 1.0f;
+
+  // o: out, f32, add, mean; g: with_grad, grad_out, grad_scale
+  AnswerLoss(PyObject* logits_, PyObject* targets_, PyObject* const* o, PyObject* const* g)
+      : logits(heads(logits_, "logits", 2)),
+        targets(flat(targets_, "targets", {at::kLong, at::kInt}, logits, {logits.size(0)})),
+        tokens(logits.size(0)) {
+    const bool add = truth(o[2]);
+    if (given(o[0])) {
+      flat(o[0], "out", {at::kDouble, at::kFloat}, logits, {1});
+      loss.is(o[0]);
+    } else {
+      if (add) value_error("add needs out");
+      loss.make({1}, logits, truth(o[1]) ? at::kFloat : at::kDouble);
+    }
+    flags = (truth(o[3]) ? ZO_LOSS_MEAN : 0) | (add ? ZO_LOSS_ADD : 0) | (loss.t.scalar_type() == at::kFloat ? ZO_LOSS_F32 : 0);
+    if (given(g[1])) {
+      if (heads(g[1], "grad_out", 2, &logits).sizes() != logits.sizes()) value_error("grad_out must have the logits' shape");
+      grad.is(g[1]);
+    } else if (truth(g[0])) {
+      grad.make(logits.sizes(), logits, logits.scalar_type());
+    }
+    grad_scale = static_cast<float>(number(g[2]));
+  }
+  const float* vector(PyObject* o, const char* what, int64_t n) const {
+    return given(o) ? flat(o, what, {at::kFloat}, logits, {n}).const_data_ptr<float>() : nullptr;
+  }
+  at::Tensor workspace(int64_t bytes) const {
+    return at::empty({bytes}, at::TensorOptions(logits.device()).dtype(at::kByte));
+  }
+  void* grad_ptr() const { return grad.t.defined() ? grad.t.data_ptr() : nullptr; }
+  int64_t grad_row() const { return grad.t.defined() ? grad.t.stride(0) : 0; }
+  float* logp_ptr() const { return logp.t.defined() ? static_cast<float*>(logp.t.data_ptr()) : nullptr; }
+};
+
+// logits, targets, old_logp, advantages, ref_logp, weights, clip low, clip high, kl, out, f32, add, mean, with_grad, grad_out,
+// grad_scale, with_logp
+PyObject* policy_loss(PyObject* const* a) {
+  AnswerLoss c(a[0], a[1], a + 9, a + 13);
+  if (truth(a[16])) c.logp.make({c.tokens}, c.logits, at::kFloat);
+  if (!given(a[2]) || !given(a[3])) type_error("old_logp and advantages must be CUDA tensors");
+  const float *old = c.vector(a[2], "old_logp", c.tokens), *advantages = c.vector(a[3], "advantages", c.tokens);
+  const float *ref = c.vector(a[4], "ref_logp", c.tokens), *weights = c.vector(a[5], "weights", c.tokens);
+  const float low = static_cast<float>(number(a[6])), high = static_cast<float>(number(a[7])), kl = static_cast<float>(number(a[8]));
+  if (kl != 0.0f && ref == nullptr) value_error("kl needs ref_logp");
+  const at::Tensor work = c.workspace(g_policy_work(c.tokens));
+  const int rc = on_stream(c.logits, [&](void* stream) {
+    return g_policy_loss(c.logits.const_data_ptr(), c.logits.stride(0), c.tokens, c.logits.size(1), code(c.logits.scalar_type()),
+                         c.targets.const_data_ptr(), index_bytes(c.targets), old, advantages, ref, weights, low, high, kl, c.flags,
+                         c.loss.t.data_ptr(), c.grad_ptr(), c.grad_row(), c.grad_scale, c.logp_ptr(), work.data_ptr(),
+                         work.numel(), stream);
+  });
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.loss, {&c.grad, &c.logp});
+}
+
+// logits, targets, starts, ref_logp, beta, margin, smoothing, by_length, out, f32, add, mean, with_grad, grad_out, grad_scale,
+// with_logp
+PyObject* preference_loss(PyObject* const* a) {
+  const at::Tensor& starts = cuda_tensor(a[2], "starts");
+  const int64_t n = starts.dim() == 1 ? starts.size(0) : 0;
+  if (n % 2 == 0) value_error("starts must have two elements per pair of answers, and one more");
+  AnswerLoss c(a[0], a[1], a + 8, a + 12);
+  flat(a[2], "starts", {at::kInt}, c.logits, {n});
+  if (truth(a[15])) c.logp.make({n - 1}, c.logits, at::kFloat);
+  const float* ref = c.vector(a[3], "ref_logp", n - 1);
+  const float beta = static_cast<float>(number(a[4])), margin = static_cast<float>(number(a[5])),
+              smoothing = static_cast<float>(number(a[6]));
+  if (truth(a[7])) c.flags |= ZO_LOSS_BY_LENGTH;
+  const at::Tensor work = c.workspace(g_preference_work(c.tokens, n / 2));
+  const int rc = on_stream(c.logits, [&](void* stream) {
+    return g_preference_loss(c.logits.const_data_ptr(), c.logits.stride(0), c.tokens, c.logits.size(1),
+                             code(c.logits.scalar_type()), c.targets.const_data_ptr(), index_bytes(c.targets),
+                             starts.const_data_ptr<int32_t>(), n / 2, ref, beta, margin, smoothing, c.flags,
+                             c.loss.t.data_ptr(), c.grad_ptr(), c.grad_row(), c.grad_scale, c.logp_ptr(), work.data_ptr(),
+                             work.numel(), stream);
+  });
+  return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.loss, {&c.grad, &c.logp});
 }
 
 // No exception leaves: a refusal becomes Python's, torch's own are translated by its macros.
@@ -331,13 +455,13 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {  // the addresses of the four entry points
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "four addresses expected");
+PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {  // the addresses of the entry points, in this order
+  void* p[9];
+  if (n != 9) {
+    PyErr_SetString(PyExc_TypeError, "nine addresses expected");
     return nullptr;
   }
-  void* p[4];
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 9; ++i) {
     p[i] = PyLong_AsVoidPtr(args[i]);
     if (p[i] == nullptr) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no address");
@@ -348,6 +472,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {  // the address
   g_attention = reinterpret_cast<decltype(g_attention)>(p[1]);
   g_attention_decode = reinterpret_cast<decltype(g_attention_decode)>(p[2]);
   g_token_loss = reinterpret_cast<decltype(g_token_loss)>(p[3]);
+  g_attention_draft = reinterpret_cast<decltype(g_attention_draft)>(p[4]);
+  g_policy_loss = reinterpret_cast<decltype(g_policy_loss)>(p[5]);
+  g_preference_loss = reinterpret_cast<decltype(g_preference_loss)>(p[6]);
+  g_policy_work = reinterpret_cast<decltype(g_policy_work)>(p[7]);
+  g_preference_work = reinterpret_cast<decltype(g_preference_work)>(p[8]);
   Py_RETURN_NONE;
 }
 
@@ -361,6 +490,9 @@ PyMethodDef g_methods[] = {{"bind", fast(&bind), METH_FASTCALL, nullptr},
                            {"attention", fast(&entry<attention, 9>), METH_FASTCALL, nullptr},
                            {"decode_attention", fast(&entry<decode_attention, 10>), METH_FASTCALL, nullptr},
                            {"token_loss", fast(&entry<token_loss, 7>), METH_FASTCALL, nullptr},
+                           {"draft_attention", fast(&entry<draft_attention, 11>), METH_FASTCALL, nullptr},
+                           {"policy_loss", fast(&entry<policy_loss, 17>), METH_FASTCALL, nullptr},
+                           {"preference_loss", fast(&entry<preference_loss, 16>), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

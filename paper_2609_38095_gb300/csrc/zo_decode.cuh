@@ -1,5 +1,6 @@
-// zo_decode.cuh -- what the kernels of one-token attention share: how a
-// cluster's CTAs and their warps split a sequence, and how they join.
+// zo_decode.cuh -- what the kernels of attention over a paged cache share, of
+// one token per sequence or a tree of them: how a cluster's CTAs and their warps
+// split a sequence, and how they join.
 //
 // A cluster of CTAs takes one sequence and key-value head. The keys go in tiles
 // of 16 or 32 to the cluster's warps in turn, so that warps differ by one tile at
@@ -63,12 +64,87 @@ __device__ __forceinline__ int2 decode_key(const DecodeParams& p, const DecodePl
   return make_int2(id, static_cast<int>(static_cast<uint32_t>(j) - decode_page(p, j) * static_cast<uint32_t>(p.page_size)));
 }
 
+// Where a row of the cluster goes, a query head of the sequence's token: for decode_join.
+template <typename T>
+struct DecodeRows {
+  T* out;
+  float* lse;  // or NULL
+  int64_t out_head;
+  __device__ __forceinline__ DecodeRows(const DecodeParams& p, const DecodePlace& w)
+      : out(static_cast<T*>(p.out) + w.b * p.out_token + w.head0 * p.out_head),
+        lse(p.lse != nullptr ? p.lse + static_cast<int64_t>(w.b) * p.heads + w.head0 : nullptr),
+        out_head(p.out_head) {}
+  __device__ __forceinline__ bool sees(int) const { return true; }
+  __device__ __forceinline__ T* row(int h) const { return out + h * out_head; }
+  __device__ __forceinline__ float* sum(int h) const { return lse + h; }
+};
+
+struct DraftPlace : DecodePlace {  // heads: rows here, head0: the first
+  int n;                           // keys ahead of the tree's
+  uint64_t any;                    // nodes that are seen
+};
+
+// Every thread of the CTA; masks: 64 words of shared memory, the nodes' masks without bits of no node (0 in a sequence of
+// negative length). A block of rows behind the last that sees anything has no keys.
+template <int HB>
+__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t cluster, uint64_t* masks) {
+  const int blocks = p.head_blocks, lane = threadIdx.x & 31;
+  DraftPlace w;
+  w.b = cluster / (p.kv_heads * blocks);
+  const int rest = cluster - w.b * (p.kv_heads * blocks);
+  w.g = rest / blocks;
+  w.head0 = (rest - w.g * blocks) * HB;
+  w.heads = min(HB, p.drafts * p.group - w.head0);
+  const int n = p.lengths[w.b];
+  if (threadIdx.x < 64) {
+    uint64_t m = 0;
+    if (threadIdx.x < p.drafts && n >= 0)
+      m = p.masks[static_cast<int64_t>(w.b) * p.drafts + threadIdx.x] & (~UINT64_C(0) >> (64 - p.drafts));
+    masks[threadIdx.x] = m;
+  }
+  __syncthreads();
+  const uint64_t a = masks[lane], b = masks[lane + 32], both = a | b;
+  w.any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
+          __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
+  const uint64_t live = static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, b != 0)) << 32 | __ballot_sync(0xFFFFFFFFu, a != 0);
+  w.n = max(n, 0);
+  w.len = w.any == 0 ? 0 : static_cast<int64_t>(w.n) + 64 - __clzll(w.any);
+  w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0) || w.len > 0x7FFFFFFF - 64;
+  if (w.bad || w.head0 >= (64 - __clzll(live)) * p.group) w.len = 0;
+  return w;
+}
+
+// Whether key j is one that the tree sees.
+__device__ __forceinline__ bool draft_sees(const DraftPlace& w, int64_t j) {
+  return j < w.n || (j < w.len && (w.any >> (j - w.n) & 1) != 0);
+}
+
+// The tree's rows: see DecodeRows.
+template <typename T>
+struct DraftRows {
+  const DraftParams& p;
+  const DraftPlace& w;
+  const uint64_t* masks;
+  __device__ __forceinline__ int node(int h) const { return (w.head0 + h) / p.group; }
+  __device__ __forceinline__ int head(int h) const { return w.g * p.group + (w.head0 + h) % p.group; }
+  __device__ __forceinline__ bool sees(int h) const { return masks[node(h)] != 0; }
+  __device__ __forceinline__ T* row(int h) const {
+    return static_cast<T*>(p.out) + w.b * p.out_token + node(h) * p.out_node + head(h) * p.out_head;
+  }
+  __device__ __forceinline__ float* sum(int h) const {
+    return p.lse + (static_cast<int64_t>(w.b) * p.drafts + node(h)) * p.heads + head(h);
+  }
+  __device__ __forceinline__ const T* query(int h) const {
+    return static_cast<const T*>(p.q) + w.b * p.q_token + node(h) * p.q_node + head(h) * p.q_head;
+  }
+};
+
 // Every thread of the cluster. outs: [kWarps][HB][DP] unscaled outputs, tops and
 // totals: [kWarps][HB], all in shared memory; tops in units of log2 (kLog2), or
 // of the scores.
-template <typename T, int HB, int DP, int kWarps, bool kLog2>
-__device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodePlace& w, float* outs, const float* tops,
-                                            const float* totals, DecodeJoin<HB>& join) {
+template <typename T, int HB, int DP, int kWarps, bool kLog2, typename R>
+__device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodePlace& w, const R& rows, float* outs,
+                                            const float* tops, const float* totals, DecodeJoin<HB>& join) {
   const int tid = threadIdx.x;
   const auto less = [](float a, float b) { return exp2_approx(kLog2 ? a - b : (a - b) * kLog2e); };
   __syncthreads();
@@ -111,23 +187,48 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     if (i >= HB * kMaxCluster) continue;
     join.scale[r][h] = scale;
     if (r == 0) {
+      if (h < w.heads && !rows.sees(h)) bad = false, total = 0.0f;
       join.over[h] = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
       join.lse[h] = bad ? NAN : total == 0.0f ? -kInf : kLog2 ? (top + log2f(total)) * kLn2 : top + logf(total);
     }
   }
   __syncthreads();
-  T* out = static_cast<T*>(p.out) + w.b * p.out_token;
   for (int i = rank * (kWarps * 32) + tid; i < w.heads * DP; i += ranks * (kWarps * 32)) {
     const int h = i / DP, d = i - h * DP;
     float x = 0.0f;
 #pragma unroll 4
     for (uint32_t r = 0; r < ranks; ++r) x = fmaf(peer_load(peer_address(outs + i, r)), join.scale[r][h], x);
-    const int head = w.head0 + h;
     const float over = join.over[h];
-    if (d < p.dim) out[head * p.out_head + d] = narrow<T>(over == 0.0f ? 0.0f : x * over);
-    if (d == 0 && p.lse != nullptr) p.lse[static_cast<int64_t>(w.b) * p.heads + head] = join.lse[h];
+    if (d < p.dim) rows.row(h)[d] = narrow<T>(over == 0.0f ? 0.0f : x * over);
+    if (d == 0 && p.lse != nullptr) *rows.sum(h) = join.lse[h];
   }
   cluster_sync();  // no CTA leaves before its part is read
+}
+
+// Fragments of tiles of 16-bit values in shared memory, and their products.
+__device__ __forceinline__ void load4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void load4_transposed(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (__is_same(T, __nv_bfloat16))
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 // CTAs of a cluster: a CTA per SM, none with less than 128 keys of the longest
@@ -142,8 +243,8 @@ inline int decode_cluster(int64_t items, int64_t longest, int sms, int per_sm) {
   return c;
 }
 
-template <typename K>
-cudaError_t launch_decode(K kernel, const DecodeParams& p, int64_t items, int cluster, int threads, int bytes,
+template <typename K, typename P>
+cudaError_t launch_decode(K kernel, const P& p, int64_t items, int cluster, int threads, int bytes,
                           cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

@@ -20,31 +20,6 @@ struct Tiles {
   static_assert(HB * DP * 4 <= kWarp, "a warp's output takes its tiles' place");
 };
 
-__device__ __forceinline__ void load4(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(at)
-               : "memory");
-}
-__device__ __forceinline__ void load4_transposed(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(at)
-               : "memory");
-}
-
-template <typename T>
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (__is_same(T, __nv_bfloat16))
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
 // An 8 x 8 matrix of 16-bit values, a row's pair per thread, transposed within the warp.
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t r;
@@ -283,7 +258,7 @@ __global__ void __launch_bounds__(kWarps * 32, HB == 8 && DP <= 128 ? 3 : 1) dec
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         outs[(warp * HB + lane % 4 * 2 + (c & 1) + 8 * m) * DP + n * 16 + lane / 4 + c / 2 * 8] = acc[m][n][c];
-  decode_join<T, HB, DP, kWarps, true>(p, w, outs, tops, totals, join);
+  decode_join<T, HB, DP, kWarps, true>(p, w, DecodeRows<T>(p, w), outs, tops, totals, join);
 }
 
 template <typename T, int DP, int HB>

@@ -1,5 +1,6 @@
-// zo_decode_scalar.cu -- one-token attention over a paged cache on the fp32
-// units: every type, head size, stride and alignment (zo_attention_decode).
+// zo_decode_scalar.cu -- attention of one token per sequence, or a tree of them,
+// over a paged cache on the fp32 units: every type, head size, stride and
+// alignment (zo_attention_decode, zo_attention_draft).
 #include "zo_decode.cuh"
 
 namespace zo {
@@ -26,10 +27,11 @@ struct Scalar {
 // shared memory and instructions before HBM (134 KB of tiles and queries leave one
 // CTA of 4 warps per SM at heads of 128): 16 sequences of up to 4001 keys, fp32, 32 / 8
 // heads of 128 in 112 us = 2.5 TB/s, 40 / 40 heads (2000 keys) 194 us = 3.6.
-template <typename T, int DP, int HB, bool kAsync>
-__global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
-    decode_scalar_kernel(const __grid_constant__ DecodeParams p) {
+// Of a tree, a cluster takes HB of the rows that share the key-value head.
+template <typename T, int DP, int HB, bool kAsync, typename P>
+__global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32) decode_scalar_kernel(const __grid_constant__ P p) {
   using S = Scalar<DP, HB>;
+  constexpr bool kDraft = __is_same(P, DraftParams);
   extern __shared__ __align__(16) float smem[];
   __shared__ DecodeJoin<HB> join;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -40,12 +42,22 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
   float* mine = tiles + warp * S::kWarp;
   float* weights = mine + S::kStages * S::kStage;  // [16][HB]
   const uint32_t ranks = cluster_size();
-  const DecodePlace w = decode_place<HB>(p, blockIdx.x / ranks);
+  __shared__ uint64_t masks[kDraft ? 64 : 1];
+  const auto w = [&] {
+    if constexpr (kDraft) return draft_place<HB>(p, blockIdx.x / ranks, masks);
+    else return decode_place<HB>(p, blockIdx.x / ranks);
+  }();
+  const auto rows = [&] {
+    if constexpr (kDraft) return DraftRows<T>{p, w, masks};
+    else return DecodeRows<T>(p, w);
+  }();
   if (threadIdx.x == 0) join.bad = w.bad;
-  const T* q = static_cast<const T*>(p.q) + w.b * p.q_token;
   for (int i = threadIdx.x; i < HB * DP; i += S::kWarps * 32) {
     const int h = i / DP, d = i - h * DP;
-    qs[i] = h < w.heads && d < p.dim ? widen(q[(w.head0 + h) * p.q_head + d]) : 0.0f;
+    const T* q;
+    if constexpr (kDraft) q = rows.query(h < w.heads ? h : 0);
+    else q = static_cast<const T*>(p.q) + w.b * p.q_token + (w.head0 + (h < w.heads ? h : 0)) * p.q_head;
+    qs[i] = h < w.heads && d < p.dim ? widen(q[d]) : 0.0f;
   }
   __syncthreads();
 
@@ -58,12 +70,19 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
   // a page is looked up a tile before its number is used, which would wait for the load
   const auto look = [&](int64_t tile) {
     const int64_t j = tile * kDecodeKeys + (lane & 15);
+    if constexpr (kDraft) {
+      if (!draft_sees(w, j)) return -1;
+    }
     return j < w.len ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
   };
   const auto fetch = [&](int64_t tile, int id, int stage) {
     float* ks = mine + stage * S::kStage;
     float* vs = ks + kDecodeKeys * S::kPitch;
-    const int2 key = decode_key(p, w, tile * kDecodeKeys + (lane & 15), id, bad);
+    int64_t j = tile * kDecodeKeys + (lane & 15);
+    if constexpr (kDraft) {
+      if (!draft_sees(w, j)) j = w.len;  // no key
+    }
+    const int2 key = decode_key(p, w, j, id, bad);
     const int64_t k_at = key.x >= 0 ? key.x * p.k_page + key.y * p.k_token : -1;
     const int64_t v_at = key.x >= 0 ? key.x * p.v_page + key.y * p.v_token : 0;
     for (int r = 0; r < kDecodeKeys; ++r) {
@@ -100,7 +119,8 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
   float slope[HB], top[HB], total[HB], acc[HB][DP / 32];
 #pragma unroll
   for (int h = 0; h < HB; ++h) {
-    slope[h] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] : 0.0f;
+    if constexpr (kDraft) slope[h] = p.slopes != nullptr && h < w.heads ? p.slopes[rows.head(h)] : 0.0f;
+    else slope[h] = p.slopes != nullptr && h < w.heads ? p.slopes[w.head0 + h] : 0.0f;
     top[h] = -kInf;
     total[h] = 0.0f;
 #pragma unroll
@@ -136,12 +156,26 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
       }
     }
     const float away = static_cast<float>(w.len - 1 - j);
+    bool nodes = false;  // whether the tile has keys of the tree
+    int place = 0;       // the key's, from the tree's first
+    if constexpr (kDraft) {
+      nodes = (tile + 1) * kDecodeKeys > w.n;
+      place = j < w.n ? static_cast<int>(j - w.n) : j < w.len ? __popcll(masks[j - w.n]) - 1 : 0;
+    }
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       float x = s[h] + __shfl_xor_sync(0xFFFFFFFFu, s[h], 16);
       x *= p.scale;
       if (p.softcap > 0.0f) x = p.softcap * tanhf(x * over_cap);
-      x = j < w.len ? x - slope[h] * away : -kInf;
+      bool seen = true;
+      if constexpr (kDraft) {
+        const uint64_t mask = masks[rows.node(h < w.heads ? h : 0)];
+        x -= slope[h] * fabsf(static_cast<float>(__popcll(mask) - 1 - place));
+        if (nodes) seen = j < w.n || (j < w.len && (mask >> (j - w.n) & 1) != 0);
+        if (!seen) x = -kInf;
+      } else {
+        x = j < w.len ? x - slope[h] * away : -kInf;
+      }
       float most = x;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
@@ -155,6 +189,7 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
       }
       s[h] = exp2_approx((x - base) * kLog2e);
       total[h] += half == 0 ? s[h] : 0.0f;
+      if (kDraft && !seen) s[h] = -1.0f;  // what is there does not reach the row
     }
     if (half == 0) {
 #pragma unroll
@@ -170,7 +205,8 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
       for (int c = 0; c < DP / 32; ++c) {
         const float x = vs[r * DP + c * 32 + lane];
 #pragma unroll
-        for (int h = 0; h < HB; ++h) acc[h][c] = fmaf(wr[h], x, acc[h][c]);
+        for (int h = 0; h < HB; ++h)
+          if (!(kDraft && wr[h] < 0.0f)) acc[h][c] = fmaf(wr[h], x, acc[h][c]);
       }
     }
     __syncwarp();  // the tile and the weights may be overwritten
@@ -191,47 +227,56 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32)
   for (int h = 0; h < HB; ++h)
 #pragma unroll
     for (int c = 0; c < DP / 32; ++c) tiles[(warp * HB + h) * DP + c * 32 + lane] = acc[h][c];
-  decode_join<T, HB, DP, S::kWarps, false>(p, w, tiles, tops, totals, join);
+  decode_join<T, HB, DP, S::kWarps, false>(p, w, rows, tiles, tops, totals, join);
 }
 
-template <typename T, int DP, int HB, bool kAsync>
-cudaError_t launch_heads(DecodeParams p, int64_t batch, int sms, cudaStream_t stream) {
+template <typename T, int DP, int HB, bool kAsync, typename P>
+cudaError_t launch_heads(P p, int64_t batch, int rows, int sms, cudaStream_t stream) {
   using S = Scalar<DP, HB>;
-  p.head_blocks = (p.group + HB - 1) / HB;
+  p.head_blocks = (rows + HB - 1) / HB;
   const int64_t items = batch * p.kv_heads * p.head_blocks;
   const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6);
-  return launch_decode(decode_scalar_kernel<T, DP, HB, kAsync>, p, items, c, S::kWarps * 32, S::kBytes, stream);
+  return launch_decode(decode_scalar_kernel<T, DP, HB, kAsync, P>, p, items, c, S::kWarps * 32, S::kBytes, stream);
 }
 
-// A cluster's query heads: no more than the group has, whose products would be of zeros.
-template <typename T, int DP, bool kAsync>
-cudaError_t launch_size(const DecodeParams& p, int64_t batch, int sms, cudaStream_t stream) {
-  if (p.group == 1) return launch_heads<T, DP, 1, kAsync>(p, batch, sms, stream);
-  return p.group <= 4 ? launch_heads<T, DP, 4, kAsync>(p, batch, sms, stream)
-                      : launch_heads<T, DP, 8, kAsync>(p, batch, sms, stream);
+// A cluster's rows: no more than share a key-value head, whose products would be of zeros.
+template <typename T, int DP, bool kAsync, typename P>
+cudaError_t launch_size(const P& p, int64_t batch, int rows, int sms, cudaStream_t stream) {
+  if (rows == 1) return launch_heads<T, DP, 1, kAsync>(p, batch, rows, sms, stream);
+  return rows <= 4 ? launch_heads<T, DP, 4, kAsync>(p, batch, rows, sms, stream)
+                   : launch_heads<T, DP, 8, kAsync>(p, batch, rows, sms, stream);
 }
 
-template <typename T>
-cudaError_t launch_type(const DecodeParams& p, int64_t batch, int sms, cudaStream_t stream) {
+template <typename T, typename P>
+cudaError_t launch_type(const P& p, int64_t batch, int rows, int sms, cudaStream_t stream) {
   if constexpr (sizeof(T) == 4) {
     if (p.dim % 4 == 0 && p.k_page % 4 == 0 && p.k_token % 4 == 0 && p.k_head % 4 == 0 && p.v_page % 4 == 0 &&
         p.v_token % 4 == 0 && p.v_head % 4 == 0 && aligned_to(p.k, 16) && aligned_to(p.v, 16)) {
-      if (p.dim <= 64) return launch_size<T, 64, true>(p, batch, sms, stream);
-      if (p.dim <= 128) return launch_size<T, 128, true>(p, batch, sms, stream);
-      return launch_size<T, 256, true>(p, batch, sms, stream);
+      if (p.dim <= 64) return launch_size<T, 64, true>(p, batch, rows, sms, stream);
+      if (p.dim <= 128) return launch_size<T, 128, true>(p, batch, rows, sms, stream);
+      return launch_size<T, 256, true>(p, batch, rows, sms, stream);
     }
   }
-  if (p.dim <= 64) return launch_size<T, 64, false>(p, batch, sms, stream);
-  if (p.dim <= 128) return launch_size<T, 128, false>(p, batch, sms, stream);
-  return launch_size<T, 256, false>(p, batch, sms, stream);
+  if (p.dim <= 64) return launch_size<T, 64, false>(p, batch, rows, sms, stream);
+  if (p.dim <= 128) return launch_size<T, 128, false>(p, batch, rows, sms, stream);
+  return launch_size<T, 256, false>(p, batch, rows, sms, stream);
+}
+
+template <typename P>
+cudaError_t launch(const P& p, int64_t batch, int rows, int dtype, int sms, cudaStream_t stream) {
+  if (dtype == 0) return launch_type<float>(p, batch, rows, sms, stream);
+  if (dtype == 1) return launch_type<__nv_bfloat16>(p, batch, rows, sms, stream);
+  return launch_type<__half>(p, batch, rows, sms, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream) {
-  if (dtype == 0) return launch_type<float>(p, batch, sms, stream);
-  if (dtype == 1) return launch_type<__nv_bfloat16>(p, batch, sms, stream);
-  return launch_type<__half>(p, batch, sms, stream);
+  return launch(p, batch, p.group, dtype, sms, stream);
+}
+
+cudaError_t launch_draft_scalar(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream) {
+  return launch(p, batch, p.drafts * p.group, dtype, sms, stream);
 }
 
 }  // namespace zo

@@ -62,6 +62,14 @@ struct DecodeParams {
   float* lse;
 };
 
+// Several rows per sequence, the nodes of a tree: row r of a key-value head is node r / group, query head r % group of its own.
+// A sequence's stride is q_token and out_token, head_blocks is of blocks of rows, and the tree's keys are behind `lengths`.
+struct DraftParams : DecodeParams {
+  int64_t q_node, out_node;
+  const int64_t* masks;
+  int32_t drafts;
+};
+
 struct TokenLossParams {
   const void* logits;
   int64_t row, tokens, vocab;
@@ -70,6 +78,39 @@ struct TokenLossParams {
   void* loss;
   float* nll;
   double* rows;  // a token's nll before its rounding
+  float2* lse;   // its logits' maximum, and what their log sum exp is above it, or NULL
+};
+
+// Losses over answers: a row's statistics, from them a coefficient per row, from it the row's gradient.
+struct PolicyLossParams {
+  TokenLossParams rows;  // loss and flags are the loss's; nll is not used
+  const float *old_logp, *advantages, *ref_logp, *weights;
+  float clip_low, clip_high, kl;
+  float* logp;
+  float* slopes;  // of the loss by a token's log-probability; NULL without a gradient
+};
+
+struct PreferenceLossParams {
+  TokenLossParams rows;
+  const int32_t* starts;
+  int64_t pairs;
+  const float* ref_logp;
+  float beta, margin, smoothing;
+  int32_t by_length;
+  float* logp;
+  double* sums;   // [2 pairs] of the sequences' tokens, then of the pairs' losses
+  float* slopes;  // of the loss by a token's log-probability, per token; NULL without a gradient
+};
+
+struct LogitsGradParams {
+  const void* logits;
+  void* grad;
+  int64_t row, grad_row, tokens, vocab;
+  const void* targets;
+  int32_t target64;
+  const float* slopes;
+  const float2* lse;
+  float scale;
 };
 
 cudaError_t launch_rotary_table(float* table, int64_t rows, int rotary, double base, double scale, int64_t original,
@@ -83,7 +124,13 @@ cudaError_t launch_attention_tiles(const AttentionParams& p, int dtype, int sms,
 bool launch_attention_mma(const AttentionParams& p, int dtype, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream);
 bool launch_decode_mma(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
+cudaError_t launch_draft_masks(const int32_t* parents, int64_t batch, int drafts, int64_t* masks, cudaStream_t stream);
+cudaError_t launch_draft_scalar(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream);
+bool launch_draft_mma(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams* g, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_preference_loss(const PreferenceLossParams& p, const LogitsGradParams* g, int dtype, int sms,
+                                   cudaStream_t stream);
 
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 

@@ -3,6 +3,7 @@
 // Everything here runs on the host and only enqueues kernels.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 
 #include "zo_forward.cuh"
@@ -146,6 +147,107 @@ bool meet(const Tensor& a, const Tensor& b) {
 // Each element of one at the other's own place.
 bool same_rows(const zo_rows& a, const void* ptr, int64_t token, int64_t head, int64_t tokens, int64_t heads) {
   return a.ptr == ptr && (tokens <= 1 || a.token == token) && (heads <= 1 || a.head == head);
+}
+
+Tensor vector(const void* p, int64_t n, size_t size) { return tensor(p, n, size, {1, 0}, {1, 0}, {n > 0, 0}); }
+
+// Attention of `nodes` rows per sequence over a paged cache: checks of the arguments, and from them the kernels' (but the masks).
+int check_paged(const zo_pages* q, const zo_pages* k, const zo_pages* v, const zo_pages* out, int64_t batch, int32_t nodes,
+                int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype, const int32_t* pages, int64_t pages_stride,
+                int64_t max_pages, int64_t n_pages, int32_t page_size, const int32_t* lengths, const void* masks, float scale,
+                float softcap, const float* slopes, float* lse, zo::DraftParams* params, int* sms) {
+  if (k == nullptr || v == nullptr) return ZO_ERR_ARG;
+  int rc = check_heads(heads, kv_heads, head_dim, dtype);
+  if (rc == ZO_OK) rc = check_scores(scale, softcap);
+  if (rc != ZO_OK) return rc;
+  // a launch has at most 16 CTAs per row and query head
+  if (batch < 0 || batch > kMaxIndex / 16 / heads / nodes || max_pages < 0 || n_pages < 0 || n_pages > kMaxIndex ||
+      page_size < 1 || pages_stride < 0 || max_pages > kMaxIndex)
+    return ZO_ERR_ARG;
+  for (const zo_pages* x : {q, k, v, out})
+    if (bad_strides(x->page, x->token, x->head)) return ZO_ERR_ARG;
+  if (batch == 0) return ZO_OK;
+  if (q->ptr == nullptr || out->ptr == nullptr || lengths == nullptr || masks == nullptr) return ZO_ERR_ARG;
+  if ((max_pages > 0 && pages == nullptr) || (n_pages > 0 && (k->ptr == nullptr || v->ptr == nullptr))) return ZO_ERR_ARG;
+  const size_t size = element_size(dtype);
+  if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
+      misaligned(pages, 4) || misaligned(lengths, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
+    return ZO_ERR_ALIGN;
+  const Tensor to = tensor(*out, batch, nodes, heads, head_dim, size);
+  const bool in_place = q->ptr == out->ptr && (batch <= 1 || q->page == out->page) && (nodes <= 1 || q->token == out->token) &&
+                        (heads <= 1 || q->head == out->head);
+  if (folds(to) || meet(to, tensor(*k, n_pages, page_size, kv_heads, head_dim, size)) ||
+      meet(to, tensor(*v, n_pages, page_size, kv_heads, head_dim, size)) ||
+      (!in_place && meet(to, tensor(*q, batch, nodes, heads, head_dim, size))))
+    return ZO_ERR_ARG;
+  rc = zo::device_sms(sms);
+  if (rc != ZO_OK) return rc;
+  const auto lone = [](int64_t stride, int64_t n) { return n > 1 ? stride : 0; };  // one element has no stride
+  zo::DraftParams& p = *params;
+  p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
+  p.q_token = q->page, p.q_head = q->head, p.out_token = out->page, p.out_head = out->head;
+  p.q_node = q->token, p.out_node = out->token;
+  p.k_page = lone(k->page, n_pages), p.k_token = lone(k->token, page_size), p.k_head = lone(k->head, kv_heads);
+  p.v_page = lone(v->page, n_pages), p.v_token = lone(v->token, page_size), p.v_head = lone(v->head, kv_heads);
+  p.pages_stride = pages_stride, p.max_pages = max_pages, p.n_pages = n_pages;
+  p.pages = pages, p.lengths = lengths;
+  p.heads = heads, p.kv_heads = kv_heads, p.group = heads / kv_heads, p.dim = head_dim, p.page_size = page_size;
+  p.page_shift = (page_size & (page_size - 1)) == 0 ? __builtin_ctz(page_size) : -1;
+  p.scale = scale, p.softcap = softcap;
+  p.slopes = slopes;
+  p.lse = lse;
+  p.drafts = nodes;
+  return ZO_OK;
+}
+
+// What the losses over rows of logits share.
+int check_rows(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
+               int32_t target_bytes, int32_t flags, int32_t known_flags, const void* loss) {
+  if (tokens < 0 || tokens > kMaxIndex / 8 || vocab < 1 || vocab > kMaxIndex || row < 0 ||
+      (target_bytes != 4 && target_bytes != 8) || (flags & ~known_flags) != 0)
+    return ZO_ERR_ARG;
+  if (!known(dtype)) return ZO_ERR_DTYPE;
+  if (loss == nullptr || (tokens > 0 && (logits == nullptr || targets == nullptr))) return ZO_ERR_ARG;
+  if (misaligned(logits, element_size(dtype)) || misaligned(targets, target_bytes) ||
+      misaligned(loss, flags & ZO_LOSS_F32 ? 4 : 8))
+    return ZO_ERR_ALIGN;
+  return ZO_OK;
+}
+
+// A loss's outputs, over none of its inputs (vectors) nor one another; the gradient may be the logits.
+int check_outputs(const void* logits, int64_t row, const void* grad, int64_t grad_row, float grad_scale, int64_t tokens,
+                  int64_t vocab, int32_t dtype, Tensor loss, Tensor logp, std::initializer_list<Tensor> inputs) {
+  const size_t size = element_size(dtype);
+  if (!std::isfinite(grad_scale) || (grad != nullptr && grad_row < 0)) return ZO_ERR_ARG;
+  if (misaligned(grad, size) || misaligned(logp.ptr, 4)) return ZO_ERR_ALIGN;
+  const Tensor in = tensor(logits, vocab, size, {1, 0}, {1, 0}, {tokens, row});
+  const Tensor out = tensor(grad, vocab, size, {1, 0}, {1, 0}, {grad != nullptr ? tokens : 0, grad_row});
+  const bool in_place = grad == logits && (tokens <= 1 || grad_row == row);
+  bool over = folds(out) || (!in_place && meet(out, in)) || meet(loss, in) || meet(logp, in) || meet(loss, out) ||
+              meet(logp, out) || meet(loss, logp);
+  for (const Tensor& t : inputs) {
+    if (misaligned(t.ptr, t.size)) return ZO_ERR_ALIGN;
+    over = over || meet(out, t) || meet(loss, t) || meet(logp, t);
+  }
+  return over ? ZO_ERR_ARG : ZO_OK;
+}
+
+// A workspace's parts, each on 8 bytes: the rows' nll and lse, their slopes, the sequences' sums.
+struct LossWork {
+  double* nll;
+  float2* lse;
+  double* sums;
+  float* slopes;
+};
+int64_t loss_work_size(int64_t tokens, int64_t sequences) {
+  const int64_t t = tokens > 0 ? tokens : 1;
+  return 16 * t + 8 * sequences + (4 * t + 7) / 8 * 8;
+}
+LossWork loss_work(void* p, int64_t tokens, int64_t sequences) {
+  char* at = static_cast<char*>(p);
+  const int64_t t = tokens > 0 ? tokens : 1;
+  return {reinterpret_cast<double*>(at), reinterpret_cast<float2*>(at + 8 * t), reinterpret_cast<double*>(at + 16 * t),
+          reinterpret_cast<float*>(at + 16 * t + 8 * sequences)};
 }
 
 int finish(cudaError_t e, const char* what) { return e == cudaSuccess ? ZO_OK : zo::report_cuda_error(e, what); }
@@ -300,49 +402,47 @@ int zo_attention_decode(const zo_rows* q, const zo_pages* k, const zo_pages* v, 
                         int64_t pages_stride, int64_t max_pages, int64_t n_pages, int32_t page_size,
                         const int32_t* lengths, float scale, float softcap, const float* slopes, float* lse,
                         void* stream) {
-  if (q == nullptr || k == nullptr || v == nullptr || out == nullptr) return ZO_ERR_ARG;
-  int rc = check_heads(heads, kv_heads, head_dim, dtype);
-  if (rc == ZO_OK) rc = check_scores(scale, softcap);
-  if (rc != ZO_OK) return rc;
-  // a launch has at most 16 CTAs per sequence and query head
-  if (batch < 0 || batch > kMaxIndex / 16 / heads || max_pages < 0 || n_pages < 0 || n_pages > kMaxIndex ||
-      page_size < 1 || pages_stride < 0 || max_pages > kMaxIndex)
-    return ZO_ERR_ARG;
-  if (bad_strides(q->token, q->head, out->token) || bad_strides(out->head, k->page, k->token) ||
-      bad_strides(k->head, v->page, v->token) || bad_strides(v->head, 0))
-    return ZO_ERR_ARG;
-  if (batch == 0) return ZO_OK;
-  if (q->ptr == nullptr || out->ptr == nullptr || lengths == nullptr) return ZO_ERR_ARG;
-  if ((max_pages > 0 && pages == nullptr) || (n_pages > 0 && (k->ptr == nullptr || v->ptr == nullptr))) return ZO_ERR_ARG;
-  const size_t size = element_size(dtype);
-  if (misaligned(q->ptr, size) || misaligned(k->ptr, size) || misaligned(v->ptr, size) || misaligned(out->ptr, size) ||
-      misaligned(pages, 4) || misaligned(lengths, 4) || misaligned(slopes, 4) || misaligned(lse, 4))
-    return ZO_ERR_ALIGN;
-  const Tensor to = tensor(*out, batch, heads, head_dim, size);
-  if (folds(to) || meet(to, tensor(*k, n_pages, page_size, kv_heads, head_dim, size)) ||
-      meet(to, tensor(*v, n_pages, page_size, kv_heads, head_dim, size)) ||
-      (!same_rows(*q, out->ptr, out->token, out->head, batch, heads) && meet(to, tensor(*q, batch, heads, head_dim, size))))
-    return ZO_ERR_ARG;
+  if (q == nullptr || out == nullptr) return ZO_ERR_ARG;
+  const zo_pages qs = {q->ptr, q->token, 0, q->head}, outs = {out->ptr, out->token, 0, out->head};
+  zo::DraftParams p = {};
   int sms = 0;
-  rc = zo::device_sms(&sms);
-  if (rc != ZO_OK) return rc;
-  zo::DecodeParams p = {};
-  p.q = q->ptr, p.k = k->ptr, p.v = v->ptr, p.out = out->ptr;
-  p.q_token = q->token, p.q_head = q->head, p.out_token = out->token, p.out_head = out->head;
-  const auto lone = [](int64_t stride, int64_t n) { return n > 1 ? stride : 0; };  // one element has no stride
-  p.k_page = lone(k->page, n_pages), p.k_token = lone(k->token, page_size), p.k_head = lone(k->head, kv_heads);
-  p.v_page = lone(v->page, n_pages), p.v_token = lone(v->token, page_size), p.v_head = lone(v->head, kv_heads);
-  p.pages_stride = pages_stride, p.max_pages = max_pages, p.n_pages = n_pages;
-  p.pages = pages, p.lengths = lengths;
-  p.heads = heads, p.kv_heads = kv_heads, p.group = heads / kv_heads, p.dim = head_dim, p.page_size = page_size;
-  p.page_shift = (page_size & (page_size - 1)) == 0 ? __builtin_ctz(page_size) : -1;
-  p.scale = scale, p.softcap = softcap;
-  p.slopes = slopes;
-  p.lse = lse;
+  const int rc = check_paged(&qs, k, v, &outs, batch, 1, heads, kv_heads, head_dim, dtype, pages, pages_stride, max_pages,
+                             n_pages, page_size, lengths, lengths, scale, softcap, slopes, lse, &p, &sms);
+  if (rc != ZO_OK || batch == 0) return rc;
   cudaError_t e = cudaSuccess;
   if (zo::launch_decode_mma(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
     return finish(e, "decode_mma_kernel");
   return finish(zo::launch_decode_scalar(p, batch, dtype, sms, static_cast<cudaStream_t>(stream)),
+                "decode_scalar_kernel");
+}
+
+int zo_draft_masks(const int32_t* parents, int64_t batch, int32_t drafts, int64_t* masks, void* stream) {
+  if (batch < 0 || batch > kMaxIndex / ZO_MAX_DRAFTS || drafts < 1 || drafts > ZO_MAX_DRAFTS) return ZO_ERR_ARG;
+  if (batch == 0) return ZO_OK;
+  if (parents == nullptr || masks == nullptr) return ZO_ERR_ARG;
+  if (misaligned(parents, 4) || misaligned(masks, 8)) return ZO_ERR_ALIGN;
+  if (meet(vector(masks, batch * drafts, 8), vector(parents, batch * drafts, 4))) return ZO_ERR_ARG;
+  return finish(zo::launch_draft_masks(parents, batch, drafts, masks, static_cast<cudaStream_t>(stream)),
+                "draft_masks_kernel");
+}
+
+int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, const zo_pages* out, int64_t batch,
+                       int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                       const int32_t* pages, int64_t pages_stride, int64_t max_pages, int64_t n_pages,
+                       int32_t page_size, const int32_t* lengths, const int64_t* masks, float scale, float softcap,
+                       const float* slopes, float* lse, void* stream) {
+  if (q == nullptr || out == nullptr || drafts < 1 || drafts > ZO_MAX_DRAFTS) return ZO_ERR_ARG;
+  zo::DraftParams p = {};
+  int sms = 0;
+  const int rc = check_paged(q, k, v, out, batch, drafts, heads, kv_heads, head_dim, dtype, pages, pages_stride, max_pages,
+                             n_pages, page_size, lengths, masks, scale, softcap, slopes, lse, &p, &sms);
+  if (rc != ZO_OK || batch == 0) return rc;
+  if (misaligned(masks, 8)) return ZO_ERR_ALIGN;
+  p.masks = masks;
+  cudaError_t e = cudaSuccess;
+  if (zo::launch_draft_mma(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
+    return finish(e, "draft_mma_kernel");
+  return finish(zo::launch_draft_scalar(p, batch, dtype, sms, static_cast<cudaStream_t>(stream)),
                 "decode_scalar_kernel");
 }
 
@@ -351,17 +451,13 @@ int64_t zo_token_loss_workspace_size(int64_t tokens) { return 8 * (tokens > 0 ? 
 int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
                   int32_t target_bytes, int32_t flags, void* loss, float* nll, void* workspace,
                   int64_t workspace_bytes, void* stream) {
-  if (tokens < 0 || tokens > kMaxIndex / 8 || vocab < 1 || vocab > kMaxIndex || row < 0 ||
-      (target_bytes != 4 && target_bytes != 8) || (flags & ~(ZO_LOSS_MEAN | ZO_LOSS_ADD | ZO_LOSS_F32)) != 0)
-    return ZO_ERR_ARG;
-  if (!known(dtype)) return ZO_ERR_DTYPE;
-  if (loss == nullptr || (tokens > 0 && (logits == nullptr || targets == nullptr))) return ZO_ERR_ARG;
-  if (misaligned(logits, element_size(dtype)) || misaligned(targets, target_bytes) ||
-      misaligned(loss, flags & ZO_LOSS_F32 ? 4 : 8) || misaligned(nll, 4) || misaligned(workspace, 8))
-    return ZO_ERR_ALIGN;
+  int rc = check_rows(logits, row, tokens, vocab, dtype, targets, target_bytes, flags,
+                      ZO_LOSS_MEAN | ZO_LOSS_ADD | ZO_LOSS_F32, loss);
+  if (rc != ZO_OK) return rc;
+  if (misaligned(nll, 4) || misaligned(workspace, 8)) return ZO_ERR_ALIGN;
   if (workspace == nullptr || workspace_bytes < zo_token_loss_workspace_size(tokens)) return ZO_ERR_WORKSPACE;
   int sms = 0;
-  const int rc = zo::device_sms(&sms);
+  rc = zo::device_sms(&sms);
   if (rc != ZO_OK) return rc;
   zo::TokenLossParams p = {};
   p.logits = logits;
@@ -371,6 +467,86 @@ int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab
   p.loss = loss, p.nll = nll;
   p.rows = static_cast<double*>(workspace);
   return finish(zo::launch_token_loss(p, dtype, sms, static_cast<cudaStream_t>(stream)), "token_loss_kernel");
+}
+
+int64_t zo_policy_loss_workspace_size(int64_t tokens) { return loss_work_size(tokens, 0); }
+
+int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
+                   int32_t target_bytes, const float* old_logp, const float* advantages, const float* ref_logp,
+                   const float* weights, float clip_low, float clip_high, float kl, int32_t flags, void* loss,
+                   void* grad, int64_t grad_row, float grad_scale, float* logp, void* workspace,
+                   int64_t workspace_bytes, void* stream) {
+  int rc = check_rows(logits, row, tokens, vocab, dtype, targets, target_bytes, flags,
+                      ZO_LOSS_MEAN | ZO_LOSS_ADD | ZO_LOSS_F32, loss);
+  if (rc != ZO_OK) return rc;
+  if (!(clip_low >= 0.0f && clip_low <= 1.0f) || !(std::isfinite(clip_high) && clip_high >= 0.0f) || !(std::isfinite(kl) && kl >= 0.0f) ||
+      (kl != 0.0f && ref_logp == nullptr && tokens > 0) || (tokens > 0 && (old_logp == nullptr || advantages == nullptr)))
+    return ZO_ERR_ARG;
+  rc = check_outputs(logits, row, grad, grad_row, grad_scale, tokens, vocab, dtype, vector(loss, 1, flags & ZO_LOSS_F32 ? 4 : 8),
+                     vector(logp, tokens, 4),
+                     {vector(targets, tokens, target_bytes), vector(old_logp, tokens, 4), vector(advantages, tokens, 4),
+                      vector(ref_logp, tokens, 4), vector(weights, tokens, 4)});
+  if (rc != ZO_OK) return rc;
+  if (misaligned(workspace, 8)) return ZO_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < zo_policy_loss_workspace_size(tokens)) return ZO_ERR_WORKSPACE;
+  int sms = 0;
+  rc = zo::device_sms(&sms);
+  if (rc != ZO_OK) return rc;
+  const LossWork work = loss_work(workspace, tokens, 0);
+  zo::PolicyLossParams p = {};
+  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags, loss, nullptr, work.nll,
+            grad != nullptr ? work.lse : nullptr};
+  p.old_logp = old_logp, p.advantages = advantages, p.weights = weights;
+  p.ref_logp = kl != 0.0f ? ref_logp : nullptr;
+  p.clip_low = clip_low, p.clip_high = clip_high, p.kl = kl;
+  p.logp = logp;
+  p.slopes = grad != nullptr ? work.slopes : nullptr;
+  const zo::LogitsGradParams g = {logits, grad, row, grad_row, tokens, vocab, targets, target_bytes == 8, work.slopes,
+                                  work.lse, grad_scale};
+  return finish(zo::launch_policy_loss(p, grad != nullptr ? &g : nullptr, dtype, sms, static_cast<cudaStream_t>(stream)),
+                "zo_policy_loss");
+}
+
+int64_t zo_preference_loss_workspace_size(int64_t tokens, int64_t pairs) {
+  return loss_work_size(tokens, 2 * (pairs > 0 ? pairs : 0));
+}
+
+int zo_preference_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype,
+                       const void* targets, int32_t target_bytes, const int32_t* starts, int64_t pairs,
+                       const float* ref_logp, float beta, float margin, float smoothing, int32_t flags, void* loss,
+                       void* grad, int64_t grad_row, float grad_scale, float* logp, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+  int rc = check_rows(logits, row, tokens, vocab, dtype, targets, target_bytes, flags,
+                      ZO_LOSS_MEAN | ZO_LOSS_ADD | ZO_LOSS_F32 | ZO_LOSS_BY_LENGTH, loss);
+  if (rc != ZO_OK) return rc;
+  if (pairs < 0 || pairs > kMaxIndex / 8 || starts == nullptr || !(std::isfinite(beta) && beta >= 0.0f) ||
+      !std::isfinite(margin) || !(smoothing >= 0.0f && smoothing <= 1.0f))
+    return ZO_ERR_ARG;
+  rc = check_outputs(logits, row, grad, grad_row, grad_scale, tokens, vocab, dtype, vector(loss, 1, flags & ZO_LOSS_F32 ? 4 : 8),
+                     vector(logp, 2 * pairs, 4),
+                     {vector(targets, tokens, target_bytes), vector(starts, 2 * pairs + 1, 4), vector(ref_logp, 2 * pairs, 4)});
+  if (rc != ZO_OK) return rc;
+  if (misaligned(workspace, 8)) return ZO_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < zo_preference_loss_workspace_size(tokens, pairs)) return ZO_ERR_WORKSPACE;
+  int sms = 0;
+  rc = zo::device_sms(&sms);
+  if (rc != ZO_OK) return rc;
+  const LossWork work = loss_work(workspace, tokens, 2 * pairs);
+  zo::PreferenceLossParams p = {};
+  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags & ~ZO_LOSS_BY_LENGTH, loss, nullptr, work.nll,
+            grad != nullptr ? work.lse : nullptr};
+  p.starts = starts;
+  p.pairs = pairs;
+  p.ref_logp = ref_logp;
+  p.beta = beta, p.margin = margin, p.smoothing = smoothing;
+  p.by_length = (flags & ZO_LOSS_BY_LENGTH) != 0;
+  p.logp = logp;
+  p.sums = work.sums;
+  p.slopes = grad != nullptr ? work.slopes : nullptr;
+  const zo::LogitsGradParams g = {logits, grad, row, grad_row, tokens, vocab, targets, target_bytes == 8, work.slopes,
+                                  work.lse, grad_scale};
+  return finish(zo::launch_preference_loss(p, grad != nullptr ? &g : nullptr, dtype, sms, static_cast<cudaStream_t>(stream)),
+                "zo_preference_loss");
 }
 
 }  // extern "C"

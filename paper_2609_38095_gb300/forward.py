@@ -18,8 +18,21 @@ and of an answer's next token, over a paged cache (pages, page_size, kv_heads, h
     q, _, _ = zo.forward.rotate_heads(q, k, v, k_out=k_cache, v_out=v_cache, slots=slots, ...)
     out = zo.forward.decode_attention(q, k_cache, v_cache, pages, lengths)
 
+and of several, a tree of drafted tokens per sequence that are verified at once
+(keys and values of node j to the slot of position lengths + j):
+
+    masks = zo.forward.draft_masks(parents)                                      # once per tree
+    out = zo.forward.draft_attention(q, k_cache, v_cache, pages, lengths, masks)
+
+and the losses over such answers, each into the loss table or with its gradient:
+
+    zo.forward.policy_loss(logits, targets, old_logp, advantages, out=losses[probe, 0:1])
+    loss, grad = zo.forward.preference_loss(logits, targets, starts, ref_logp=ref, with_grad=True)
+    loss, grad = zo.forward.policy_loss(logits.detach(), ..., with_grad=True); logits.backward(grad)
+
 The method has no backward pass: a tensor that asks for a gradient is refused
 where torch would record one, and a tensor with a tangent of forward mode is.
+The two losses over answers return their gradients in the logits instead.
 """
 import ctypes
 import importlib.machinery
@@ -31,9 +44,11 @@ import torch
 from . import zo as _zo
 
 EXPORTS = ["zo_rotary_table", "zo_document_spans", "zo_rotate_heads", "zo_attention", "zo_attention_decode",
-           "zo_token_loss_workspace_size", "zo_token_loss"]
+           "zo_token_loss_workspace_size", "zo_token_loss", "zo_draft_masks", "zo_attention_draft",
+           "zo_policy_loss_workspace_size", "zo_policy_loss", "zo_preference_loss_workspace_size", "zo_preference_loss"]
 MAX_HEAD_DIM = 256
 MAX_HEADS = 1024
+MAX_DRAFTS = 64
 LAYOUTS = {"half": False, "interleaved": True}
 BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")
 
@@ -56,6 +71,15 @@ def _lib():
                                      vp], ctypes.c_int),
             "zo_token_loss_workspace_size": ([i64], i64),
             "zo_token_loss": ([vp, i64, i64, i64, i32, vp, i32, i32, vp, vp, vp, i64, vp], ctypes.c_int),
+            "zo_draft_masks": ([vp, i64, i32, vp, vp], ctypes.c_int),
+            "zo_attention_draft": ([vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, i64, i64, i64, i32, vp, vp, f32, f32,
+                                    vp, vp, vp], ctypes.c_int),
+            "zo_policy_loss_workspace_size": ([i64], i64),
+            "zo_policy_loss": ([vp, i64, i64, i64, i32, vp, i32, vp, vp, vp, vp, f32, f32, f32, i32, vp, vp, i64, f32, vp, vp,
+                                i64, vp], ctypes.c_int),
+            "zo_preference_loss_workspace_size": ([i64, i64], i64),
+            "zo_preference_loss": ([vp, i64, i64, i64, i32, vp, i32, vp, i64, vp, f32, f32, f32, i32, vp, vp, i64, f32, vp, vp,
+                                    i64, vp], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -74,7 +98,8 @@ def _binding():
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
         loader.exec_module(module)
         module.bind(*(ctypes.cast(getattr(_lib(), "zo_" + n), ctypes.c_void_p).value
-                      for n in ("rotate_heads", "attention", "attention_decode", "token_loss")))
+                      for n in ("rotate_heads", "attention", "attention_decode", "token_loss", "attention_draft", "policy_loss",
+                                "preference_loss", "policy_loss_workspace_size", "preference_loss_workspace_size")))
         _B = module
     return _B
 
@@ -158,6 +183,30 @@ def decode_attention(q, k_cache, v_cache, pages, lengths, *, scale=None, softcap
                                                                             slopes, out, with_lse))
 
 
+def draft_masks(parents):
+    """int64, what draft_attention's nodes see of one another: for each node of parents, int32 (batch, drafts), the bits of
+    its ancestors and its own (zo_draft_masks). A parent comes before its children; -1: the sequence's last token; below:
+    no node, whose mask is 0."""
+    _flat(parents.flatten() if isinstance(parents, torch.Tensor) and parents.is_contiguous() else parents, "parents", (torch.int32,))
+    if parents.dim() != 2 or not 1 <= parents.shape[1] <= MAX_DRAFTS:
+        raise ValueError(f"parents must have two dimensions, sequences and their 1 to {MAX_DRAFTS} nodes")
+    masks = torch.empty(parents.shape, dtype=torch.int64, device=parents.device)
+    _zo._launch("zo_draft_masks", _zo._index(parents.device), _lib().zo_draft_masks, parents.data_ptr(), parents.shape[0],
+                parents.shape[1], masks.data_ptr())
+    return masks
+
+
+def draft_attention(q, k_cache, v_cache, pages, lengths, masks, *, scale=None, softcap=0.0, slopes=None, out=None, with_lse=False):
+    """Attention of a tree of drafted tokens per sequence, q (batch, drafts, heads, head_dim), over the sequence's lengths[b]
+    keys so far and, at keys lengths[b] + j, the nodes' own: node i sees node j where bit j of masks[b, i] is set
+    (zo_attention_draft). masks: draft_masks, or any int64 (batch, drafts); a node without a bit sees nothing. k_cache,
+    v_cache, pages, lengths: as for decode_attention, but for the lengths, which are those ahead of the drafted tokens.
+    Returns out, or (out, lse) with lse float32 (batch, drafts, heads). An `out` of the caller's may be q, and overlaps
+    nothing else."""
+    return _made("zo_attention_draft", (_B or _binding()).draft_attention(q, k_cache, v_cache, pages, lengths, masks, scale,
+                                                                          softcap, slopes, out, with_lse))
+
+
 def token_loss(logits, targets, *, mean=False, add=False, out=None, dtype=torch.float64, with_nll=False):
     """-log p of the targets under logits (tokens, vocab), summed over the tokens whose target is not negative, or their
     mean (zo_token_loss). Returns a one-element tensor: `out` (for instance losses[k, 0:1] of a step's loss table; added
@@ -165,3 +214,33 @@ def token_loss(logits, targets, *, mean=False, add=False, out=None, dtype=torch.
     if dtype is not torch.float64 and dtype is not torch.float32:
         raise ValueError("dtype must be torch.float64 or torch.float32")
     return _made("zo_token_loss", (_B or _binding()).token_loss(logits, targets, mean, add, out, dtype is torch.float32, with_nll))
+
+
+def policy_loss(logits, targets, old_logp, advantages, *, ref_logp=None, weights=None, clip=(0.2, 0.2), kl=0.0, mean=False,
+                add=False, out=None, dtype=torch.float64, with_grad=False, grad_out=None, grad_scale=1.0, with_logp=False):
+    """The clipped policy loss of answers' tokens under logits (tokens, vocab), with a term kl times their divergence from a
+    reference where ref_logp is given, summed over the tokens whose target is not negative or averaged by their weights
+    (zo_policy_loss). old_logp, advantages, ref_logp, weights: float32 (tokens); clip: how far below and above 1 the ratio
+    exp(logp - old_logp) counts, or one number for both. out, add, dtype: as for token_loss. Returns the loss, or a tuple of
+    it and, with with_grad or grad_out, its gradient in the logits times grad_scale (a new tensor, or grad_out, which may be
+    logits and overlaps nothing else), and with with_logp the targets' log-probabilities, float32."""
+    if dtype is not torch.float64 and dtype is not torch.float32:
+        raise ValueError("dtype must be torch.float64 or torch.float32")
+    low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
+    return _made("zo_policy_loss", (_B or _binding()).policy_loss(
+        logits, targets, old_logp, advantages, ref_logp, weights, low, high, kl, out, dtype is torch.float32, add, mean, with_grad,
+        grad_out, grad_scale, with_logp))
+
+
+def preference_loss(logits, targets, starts, *, ref_logp=None, beta=0.1, margin=0.0, smoothing=0.0, by_length=False, mean=False,
+                    add=False, out=None, dtype=torch.float64, with_grad=False, grad_out=None, grad_scale=1.0, with_logp=False):
+    """The loss of pairs of answers by their log-ratios to a reference, summed over the pairs or their mean
+    (zo_preference_loss). The answers' tokens are rows starts[j] .. starts[j + 1] - 1 of logits (tokens, vocab), int32 and one
+    more than there are answers: first a pair's preferred one, then its rejected one. ref_logp: float32, the answers' sums of
+    log-probabilities under the reference (by_length: their means over the counted tokens), or none. out, add, dtype: as
+    for token_loss; gradient as for policy_loss. with_logp: also the answers' sums (or means), float32."""
+    if dtype is not torch.float64 and dtype is not torch.float32:
+        raise ValueError("dtype must be torch.float64 or torch.float32")
+    return _made("zo_preference_loss", (_B or _binding()).preference_loss(
+        logits, targets, starts, ref_logp, beta, margin, smoothing, by_length, out, dtype is torch.float32, add, mean, with_grad,
+        grad_out, grad_scale, with_logp))
