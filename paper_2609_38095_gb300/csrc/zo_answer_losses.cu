@@ -14,7 +14,8 @@ namespace zo {
 namespace {
 
 constexpr int kSumThreads = 1024;
-constexpr int kGradThreads = 256;
+constexpr int kMaxParts = 8;      // CTAs of a cluster
+constexpr int kWarpVocab = 4096;  // vocabularies up to which a warp has a row
 
 struct Term {
   float value, slope;
@@ -43,16 +44,22 @@ __device__ __forceinline__ Term policy_term(const PolicyLossParams& p, int64_t t
   return term;
 }
 
+// The counted tokens' weights, on thread 0.
+__device__ __forceinline__ double counted_weight(const PolicyLossParams& p) {
+  const TokenLossParams& r = p.rows;
+  double weight = 0.0;
+  for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x)
+    if (load_index(r.targets, t, r.target64) >= 0) weight += p.weights != nullptr ? p.weights[t] : 1.0;
+  return cta_sums({weight, 0.0}).a;
+}
+
 // The tokens' terms and their sum, in one CTA and an order of their number alone.
 __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_constant__ PolicyLossParams p) {
   __shared__ double over;
   const TokenLossParams& r = p.rows;
-  double weight = 0.0;
   if (r.flags & 1) {
-    for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x)
-      if (load_index(r.targets, t, r.target64) >= 0) weight += p.weights != nullptr ? p.weights[t] : 1.0;
-    const Sums all = cta_sums({weight, 0.0});
-    if (threadIdx.x == 0) over = all.a != 0.0 ? 1.0 / all.a : NAN;
+    const double weight = counted_weight(p);
+    if (threadIdx.x == 0) over = weight != 0.0 ? 1.0 / weight : NAN;
     __syncthreads();
   }
   const double unit = r.flags & 1 ? over : 1.0;
@@ -146,87 +153,238 @@ __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __gri
   }
 }
 
-// grad_v = slope scale (1[v = target] - exp(x_v - lse)). A CTA has kPerRow threads per row's part of kPart vectors. x - lse is
-// formed from the row's maximum first, then from the rest in the product's rounding. Rows of slope 0 are not read. The target's own
-// element is -expm1(x - lse), which 1 - p would lose where p is near 1.
-template <typename T, int kPerRow>
-__global__ void __launch_bounds__(kGradThreads) logits_grad_kernel(const __grid_constant__ LogitsGradParams p, int parts) {
-  constexpr int E = Vec<T>::kN, kLoads = 4, kRows = kGradThreads / kPerRow;
-  const int tid = threadIdx.x % kPerRow;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kPerRow;
-  const int64_t t = item / parts, part = item - t * parts;
-  if (t >= p.tokens) return;
-  const T* x = static_cast<const T*>(p.logits) + t * p.row;
-  T* g = static_cast<T*>(p.grad) + t * p.grad_row;
-  const float slope = p.slopes[t];
-  const int64_t target = load_index(p.targets, t, p.target64);
-  const bool reads = slope != 0.0f;
-  float2 lse = make_float2(0.0f, 0.0f);
-  if (reads) lse = p.lse[t];
-  const float times = slope * p.scale, low = -lse.y * kLog2e;
-  const auto one = [&](float v, int64_t at) {
-    if (!reads) return 0.0f;
-    const float away = v - lse.x;
-    return at == target ? times * -expm1f(away - lse.y) : -times * exp2_approx(fmaf(away, kLog2e, low));
-  };
-  const int64_t chunk = static_cast<int64_t>(kLoads) * kPerRow;
-  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
-  if (reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T) != off) {  // no vector of one is a vector of the other
-    const int64_t from = part * chunk * E, to = min(p.vocab, from + chunk * E);
-    for (int64_t i = from + tid; i < to; i += kPerRow) g[i] = narrow<T>(one(reads ? widen(x[i]) : 0.0f, i));
-    return;
+// log of a sum of exponentials, without the fp64 units' log (whose 2 us every row would wait for): the exponent's part in fp64
+// and the mantissa's, at most 0.35, in fp32.
+__device__ __forceinline__ double log_split(double sum) {
+  int e;
+  const float f = static_cast<float>(sum);
+  float m = frexpf(f, &e);
+  if (!(f > 0.0f && f < kInf)) return logf(f);
+  if (m < 0.70710678f) m *= 2.0f, --e;
+  return e * 0.69314718055994530942 + logf(m);
+}
+
+// The gradient of a row's logits in place of the logits: grad_v = slope scale (1[v = target] - exp(x_v - lse)). x - lse is formed
+// from the row's maximum first, then from the rest in the product's rounding. The target's own element is -expm1(x - lse),
+// which 1 - p would lose where p is near 1.
+struct Slope {
+  float times, top, rest, low;  // slope scale; of lse; -rest log2(e)
+  __device__ __forceinline__ Slope(float slope, float scale, float2 lse)
+      : times(slope * scale), top(lse.x), rest(lse.y), low(-lse.y * kLog2e) {}
+  __device__ __forceinline__ float other(float x) const { return -times * exp2_approx(fmaf(x - top, kLog2e, low)); }
+  __device__ __forceinline__ float target(float x) const { return times * -expm1f(x - top - rest); }
+};
+
+// Which elements of a row a CTA has: the vectors of 16 bytes between its boundaries in `parts` equal parts, the elements in
+// front of them with the first part, those behind with the last.
+template <typename T>
+struct Part {
+  static constexpr int E = Vec<T>::kN;
+  int first;  // element of the first vector
+  int vectors;
+  int edge;  // this thread's element in front or behind, -1: none
+  __device__ __forceinline__ Part(const T* x, int64_t n, int rank, int parts) {
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
+    const int head = min(off ? E - off : 0, static_cast<int>(n)), all = (static_cast<int>(n) - head) / E, tail = head + all * E;
+    const int each = (all + parts - 1) / parts, from = min(rank * each, all);
+    first = head + from * E;
+    vectors = min(each, all - from);
+    edge = -1;
+    if (rank == 0 && threadIdx.x < head) edge = threadIdx.x;
+    if (rank == parts - 1 && threadIdx.x >= 32 && threadIdx.x - 32 < n - tail) edge = tail + threadIdx.x - 32;
   }
-  const int64_t head = min(static_cast<int64_t>(off ? E - off : 0), p.vocab), vectors = (p.vocab - head) / E;
-  const int64_t tail = head + vectors * E;
-  if (part == 0) {
-    if (tid < head) g[tid] = narrow<T>(one(reads ? widen(x[tid]) : 0.0f, tid));
-    if (tid < p.vocab - tail) g[tail + tid] = narrow<T>(one(reads ? widen(x[tail + tid]) : 0.0f, tail + tid));
-  }
-  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-  uint4* gv = reinterpret_cast<uint4*>(g + head);
-  const int64_t from = part * chunk + tid;
-  uint4 raw[kLoads];
+};
+
+constexpr int kPartThreads = 256;
+
+// Writes a part's gradient from its logits in shared memory (each thread reads what it has put there itself), or zeros.
+template <typename T>
+__device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4* x, float edge, bool zero, const Slope& s,
+                                         int64_t target) {
+  constexpr int E = Vec<T>::kN;
+  const int tid = threadIdx.x;
+  if (part.edge >= 0) g[part.edge] = narrow<T>(zero ? 0.0f : part.edge == target ? s.target(edge) : s.other(edge));
+  const int64_t at = target - part.first;  // the target's element among the part's, and its vector
+  const int64_t here = at >= 0 ? at / E : -1;
+  T* to = g + part.first;
+  const bool vector = reinterpret_cast<uintptr_t>(to) % 16 == 0;
+  for (int i = tid; i < part.vectors; i += kPartThreads) {
+    float f[E] = {};
+    if (!zero) {
+      float w[E];
+      Vec<T>::widen_all(x[i], w);
 #pragma unroll
-  for (int k = 0; k < kLoads; ++k) {
-    raw[k] = make_uint4(0, 0, 0, 0);
-    if (reads && from + k * kPerRow < vectors) raw[k] = __ldcs(xv + from + k * kPerRow);
-  }
+      for (int e = 0; e < E; ++e) f[e] = s.other(w[e]);
+      if (here == i) {
 #pragma unroll
-  for (int k = 0; k < kLoads; ++k) {
-    const int64_t i = from + k * kPerRow, first = head + i * E;
-    if (i >= vectors) continue;
-    float f[E];
-    Vec<T>::widen_all(raw[k], f);
-    const bool here = target >= first && target < first + E;
-    float own = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (here && first + e == target) own = f[e];
-      f[e] = reads ? -times * exp2_approx(fmaf(f[e] - lse.x, kLog2e, low)) : 0.0f;
+        for (int e = 0; e < E; ++e)
+          if (at % E == e) f[e] = s.target(w[e]);
+      }
     }
-    if (here) {
-      own = one(own, target);
+    if (vector) {
+      __stcs(reinterpret_cast<uint4*>(to) + i, Vec<T>::narrow_all(f));
+    } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (first + e == target) f[e] = own;
+      for (int e = 0; e < E; ++e) to[static_cast<int64_t>(i) * E + e] = narrow<T>(f[e]);
     }
-    __stcs(gv + i, Vec<T>::narrow_all(f));
   }
 }
 
 template <typename T>
-cudaError_t launch_grad(const LogitsGradParams& p, cudaStream_t stream) {
-  constexpr int E = Vec<T>::kN;
-  if (p.vocab <= 4096) {
-    constexpr int kRows = kGradThreads / 32;
-    const int parts = static_cast<int>((p.vocab + 128 * E - 1) / (128 * E));
-    const int64_t grid = (p.tokens * parts + kRows - 1) / kRows;
-    logits_grad_kernel<T, 32><<<static_cast<unsigned>(grid), kGradThreads, 0, stream>>>(p, parts);
-  } else {
-    constexpr int kPart = 4 * kGradThreads * E;
-    const int parts = static_cast<int>((p.vocab + kPart - 1) / kPart);
-    logits_grad_kernel<T, kGradThreads><<<static_cast<unsigned>(p.tokens * parts), kGradThreads, 0, stream>>>(p, parts);
+__device__ __forceinline__ void fetch_part(const T* x, const Part<T>& part, uint4* to) {
+  const uint4* from = reinterpret_cast<const uint4*>(x + part.first);
+  for (int i = threadIdx.x; i < part.vectors; i += kPartThreads)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + i))),
+                 "l"(from + i)
+                 : "memory");
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+// A row's gradient from its slope and log-sum: parts of a row, the rows from the last to the first, since the last ones read
+// for their sums may still be in L2. Rows of slope 0 are not read.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads) logits_grad_kernel(const __grid_constant__ LogitsGradParams p, int parts) {
+  extern __shared__ __align__(16) uint4 tile[];
+  const int64_t t = p.tokens - 1 - blockIdx.x / parts;
+  const T* x = static_cast<const T*>(p.logits) + t * p.row;
+  const Part<T> part(x, p.vocab, blockIdx.x % parts, parts);
+  const float slope = p.slopes[t];
+  const bool zero = slope == 0.0f;
+  float2 lse = make_float2(0.0f, 0.0f);
+  float edge = 0.0f;
+  if (!zero) {
+    fetch_part(x, part, tile);
+    lse = p.lse[t];
+    if (part.edge >= 0) edge = widen(x[part.edge]);
   }
+  const int64_t target = load_index(p.targets, t, p.target64);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  put_part(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
+}
+
+// The same for vocabularies of at most 4096: a warp per row.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads) logits_grad_warp_kernel(const __grid_constant__ LogitsGradParams p) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kPartThreads / 32) + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
+  const T* x = static_cast<const T*>(p.logits) + t * p.row;
+  T* g = static_cast<T*>(p.grad) + t * p.grad_row;
+  const float slope = p.slopes[t];
+  const bool zero = slope == 0.0f;
+  const Slope s(slope, p.scale, zero ? make_float2(0.0f, 0.0f) : p.lse[t]);
+  const int64_t target = load_index(p.targets, t, p.target64);
+  for (int64_t i = threadIdx.x & 31; i < p.vocab; i += 32) {
+    const float v = zero ? 0.0f : widen(x[i]);
+    g[i] = narrow<T>(zero ? 0.0f : i == target ? s.target(v) : s.other(v));
+  }
+}
+
+// A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
+                                                                   const __grid_constant__ LogitsGradParams g, int parts) {
+  extern __shared__ __align__(16) uint4 tile[];
+  constexpr int kWarps = kPartThreads / 32;
+  __shared__ float tops[kWarps];
+  __shared__ double sums[kWarps];
+  __shared__ float part_top;
+  __shared__ float part_sum[2];  // high and low part
+  __shared__ float shared_slope;
+  __shared__ float2 shared_lse;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const TokenLossParams& r = p.rows;
+  const int tid = threadIdx.x, rank = blockIdx.x % parts;
+  const int64_t t = blockIdx.x / parts;
+  const T* x = static_cast<const T*>(r.logits) + t * r.row;
+  const Part<T> part(x, r.vocab, rank, parts);
+  const int64_t target = load_index(r.targets, t, r.target64);
+  const bool counts = target >= 0, known = counts && target < r.vocab;
+  T* grad = static_cast<T*>(g.grad) + t * g.grad_row;
+  if (!known) {  // the whole cluster
+    if (rank == 0 && tid == 0) r.rows[t] = counts ? NAN : 0.0;
+    const float nan = NAN;
+    put_part(grad, part, tile, nan, !counts, Slope(nan, 1.0f, make_float2(0.0f, 0.0f)), -1);
+    if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");  // what follows may count on the kernel before
+    return;
+  }
+  fetch_part(x, part, tile);
+  float edge = -kInf, own = 0.0f;
+  if (part.edge >= 0) edge = widen(x[part.edge]);
+  if (tid == 0) own = widen(x[target]);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  constexpr int E = Vec<T>::kN;
+  float top = kNone.top, sum = 0.0f;
+  if (part.edge >= 0) take<1>(&edge, top, sum);
+  int i = tid;
+  for (; i + (kRowVectors - 1) * kPartThreads < part.vectors; i += kRowVectors * kPartThreads) {
+    float f[kRowVectors * E];
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k) Vec<T>::widen_all(tile[i + k * kPartThreads], f + k * E);
+    take<kRowVectors * E>(f, top, sum);
+  }
+  for (; i < part.vectors; i += kPartThreads) {
+    float f[E];
+    Vec<T>::widen_all(tile[i], f);
+    take<E>(f, top, sum);
+  }
+  Tail mine = lanes_join<32>({top, sum});
+  if ((tid & 31) == 0) {
+    tops[tid >> 5] = mine.top;
+    sums[tid >> 5] = mine.sum;
+  }
+  __syncthreads();
+  if (tid < 32) {
+    mine = lanes_join<kWarps>(tid < kWarps ? Tail{tops[tid], sums[tid]} : kNone);
+    if (tid == 0 && parts > 1) {
+      part_top = mine.top;
+      part_sum[0] = static_cast<float>(mine.sum);
+      part_sum[1] = static_cast<float>(mine.sum - part_sum[0]);
+    }
+  }
+  if (parts > 1) {
+    cluster_sync();
+    if (tid < 32) {
+      mine = kNone;
+      if (tid < parts)
+        mine = {peer_load(peer_address(&part_top, tid)),
+                static_cast<double>(peer_load(peer_address(&part_sum[0], tid))) +
+                    peer_load(peer_address(&part_sum[1], tid))};
+      mine = lanes_join<kMaxParts>(mine);
+    }
+  }
+  if (tid == 0) {
+    const double rest = log_split(mine.sum), logp = (static_cast<double>(own) - mine.top) - rest;
+    const double w = p.weights != nullptr ? p.weights[t] : 1.0;
+    if (rank == 0) r.rows[t] = -logp;
+    const Term term = policy_term(p, t, logp);
+    if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");
+    shared_slope = static_cast<float>(w * (p.unit != nullptr ? __ldcg(p.unit) : 1.0) * term.slope);
+    shared_lse = make_float2(mine.top, static_cast<float>(rest));
+  }
+  __syncthreads();
+  const float slope = shared_slope;
+  put_part(grad, part, tile, edge, slope == 0.0f, Slope(slope, g.scale, shared_lse), target);
+  if (parts > 1) cluster_sync();  // no CTA leaves before its part is read
+}
+
+// 1 over the counted tokens' weights.
+__global__ void __launch_bounds__(kSumThreads) policy_unit_kernel(const __grid_constant__ PolicyLossParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const double weight = counted_weight(p);
+  if (threadIdx.x == 0) *p.unit = weight != 0.0 ? 1.0 / weight : NAN;
+}
+
+template <typename T>
+cudaError_t launch_grad(const LogitsGradParams& p, cudaStream_t stream) {
+  if (p.vocab <= kWarpVocab) {
+    constexpr int kRows = kPartThreads / 32;
+    logits_grad_warp_kernel<T><<<static_cast<unsigned>((p.tokens + kRows - 1) / kRows), kPartThreads, 0, stream>>>(p);
+    return cudaGetLastError();
+  }
+  constexpr int kMost = 24 * 1024;
+  const int64_t bytes = p.vocab * static_cast<int64_t>(sizeof(T));
+  const int parts = static_cast<int>((bytes + kMost - 1) / kMost);
+  logits_grad_kernel<T><<<static_cast<unsigned>(p.tokens * parts), kPartThreads, (bytes / parts + 31) / 16 * 16, stream>>>(p, parts);
   return cudaGetLastError();
 }
 
@@ -235,6 +393,40 @@ cudaError_t launch_logits_grad(const LogitsGradParams& p, int dtype, cudaStream_
   return dtype == 0   ? launch_grad<float>(p, stream)
          : dtype == 1 ? launch_grad<__nv_bfloat16>(p, stream)
                       : launch_grad<__half>(p, stream);
+}
+
+constexpr int64_t kMostPart = 200 * 1024;
+
+// Whether rows of that many bytes are taken at once: beyond the vocabularies that a warp takes, up to what a cluster holds.
+bool rows_at_once(int64_t vocab, int64_t bytes) { return vocab > kWarpVocab && bytes <= kMaxParts * (kMostPart - 16); }
+
+template <typename T>
+cudaError_t launch_rows(const PolicyLossParams& p, const LogitsGradParams& g, int sms, cudaStream_t stream) {
+  const int64_t bytes = g.vocab * static_cast<int64_t>(sizeof(T));
+  int parts = 1;
+  while (parts < kMaxParts && (bytes / parts > 40 * 1024 || (g.tokens * parts * 2 <= 5 * sms && g.vocab / (parts * 2) >= 4096))) parts *= 2;
+  const int tile = static_cast<int>((bytes / parts + 31) / 16 * 16);
+  cudaError_t e = cudaFuncSetAttribute(policy_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile);
+  if (e != cudaSuccess) return e;
+  if (p.unit != nullptr) {
+    policy_unit_kernel<<<1, kSumThreads, 0, stream>>>(p);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = parts;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(static_cast<unsigned>(g.tokens * parts));
+  c.blockDim = dim3(kPartThreads);
+  c.dynamicSmemBytes = tile;
+  c.stream = stream;
+  c.attrs = attr;
+  c.numAttrs = p.unit != nullptr ? 2 : 1;
+  return cudaLaunchKernelEx(&c, policy_rows_kernel<T>, p, g, parts);
 }
 
 template <typename F, typename P>
@@ -249,6 +441,15 @@ cudaError_t launch_sum(F kernel, const P& p, int64_t items, cudaStream_t stream)
 }  // namespace
 
 cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams* g, int dtype, int sms, cudaStream_t stream) {
+  if (g != nullptr && g->tokens > 0 && rows_at_once(g->vocab, g->vocab * (dtype == 0 ? 4 : 2))) {
+    PolicyLossParams at_once = p;
+    at_once.slopes = nullptr;
+    if ((p.rows.flags & 1) == 0) at_once.unit = nullptr;
+    cudaError_t e = dtype == 0   ? launch_rows<float>(at_once, *g, sms, stream)
+                    : dtype == 1 ? launch_rows<__nv_bfloat16>(at_once, *g, sms, stream)
+                                 : launch_rows<__half>(at_once, *g, sms, stream);
+    return e != cudaSuccess ? e : launch_sum(policy_sum_kernel, at_once, p.rows.tokens, stream);
+  }
   cudaError_t e = launch_token_rows(p.rows, dtype, sms, stream);
   if (e == cudaSuccess) e = launch_sum(policy_sum_kernel, p, p.rows.tokens, stream);
   if (e == cudaSuccess && g != nullptr) e = launch_logits_grad(*g, dtype, stream);

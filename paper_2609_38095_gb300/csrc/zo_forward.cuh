@@ -87,6 +87,7 @@ struct PolicyLossParams {
   const float *old_logp, *advantages, *ref_logp, *weights;
   float clip_low, clip_high, kl;
   float* logp;
+  double* unit;   // place for what a mean's weights are multiplied by
   float* slopes;  // of the loss by a token's log-probability; NULL without a gradient
 };
 

@@ -232,7 +232,7 @@ int check_outputs(const void* logits, int64_t row, const void* grad, int64_t gra
   return over ? ZO_ERR_ARG : ZO_OK;
 }
 
-// A workspace's parts, each on 8 bytes: the rows' nll and lse, their slopes, the sequences' sums.
+// A workspace's parts, each on 8 bytes: the rows' nll and lse, the sequences' sums (or a mean's weight), the rows' slopes.
 struct LossWork {
   double* nll;
   float2* lse;
@@ -469,7 +469,7 @@ int zo_token_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab
   return finish(zo::launch_token_loss(p, dtype, sms, static_cast<cudaStream_t>(stream)), "token_loss_kernel");
 }
 
-int64_t zo_policy_loss_workspace_size(int64_t tokens) { return loss_work_size(tokens, 0); }
+int64_t zo_policy_loss_workspace_size(int64_t tokens) { return loss_work_size(tokens, 1); }
 
 int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t vocab, int32_t dtype, const void* targets,
                    int32_t target_bytes, const float* old_logp, const float* advantages, const float* ref_logp,
@@ -492,7 +492,7 @@ int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t voca
   int sms = 0;
   rc = zo::device_sms(&sms);
   if (rc != ZO_OK) return rc;
-  const LossWork work = loss_work(workspace, tokens, 0);
+  const LossWork work = loss_work(workspace, tokens, 1);
   zo::PolicyLossParams p = {};
   p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags, loss, nullptr, work.nll,
             grad != nullptr ? work.lse : nullptr};
@@ -500,6 +500,7 @@ int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t voca
   p.ref_logp = kl != 0.0f ? ref_logp : nullptr;
   p.clip_low = clip_low, p.clip_high = clip_high, p.kl = kl;
   p.logp = logp;
+  p.unit = work.sums;
   p.slopes = grad != nullptr ? work.slopes : nullptr;
   const zo::LogitsGradParams g = {logits, grad, row, grad_row, tokens, vocab, targets, target_bytes == 8, work.slopes,
                                   work.lse, grad_scale};
