@@ -29,7 +29,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["zo_api.cu", "zo_stream_kernels.cu", "zo_update_lut8.cu", "zo_small_kernels.cu",
            "zo_quad_step.cu", "zo_update_items.cu", "zo_update_blocks.cu",
            "zo_forward_api.cu", "zo_rotate.cu", "zo_attention.cu", "zo_attention_mma.cu",
-           "zo_decode_mma.cu", "zo_decode_scalar.cu", "zo_token_loss.cu", "zo_answer_losses.cu", "zo_draft.cu"]
+           "zo_decode_mma.cu", "zo_decode_scalar.cu", "zo_token_loss.cu", "zo_answer_losses.cu", "zo_draft.cu", "zo_draft_wide.cu"]
 HEADERS = ["zo_blocks.cuh", "zo_decode.cuh", "zo_device.cuh", "zo_forward.cuh", "zo_items.h", "zo_launch.h",
            "zo_logits.cuh", "zo_precond.cuh", "zo_tcgen05.cuh"]
 ABI_HEADERS = ["zo.h", "zo_forward.h"]

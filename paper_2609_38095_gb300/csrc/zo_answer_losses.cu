@@ -28,16 +28,26 @@ __device__ __forceinline__ float expm1_less(float d) {
   return d * d * fmaf(c, d, 0.5f);
 }
 
+struct Token {  // what stands beside its logits
+  float old_logp, advantage, ref_logp, weight;
+  __device__ __forceinline__ Token(const PolicyLossParams& p, int64_t t)
+      : old_logp(p.old_logp[t]),
+        advantage(p.advantages[t]),
+        ref_logp(p.ref_logp != nullptr ? p.ref_logp[t] : 0.0f),
+        weight(p.weights != nullptr ? p.weights[t] : 1.0f) {}
+  __device__ __forceinline__ Token() {}
+};
+
 // A token's loss and its slope by its log-probability. With r = exp(logp - old):
 // -min(r A, clip(r) A) + kl (exp(d) - 1 - d), d = ref - logp. A NaN stays one:
 // each comparison is written so that it picks the side that is NaN.
-__device__ __forceinline__ Term policy_term(const PolicyLossParams& p, int64_t t, double logp) {
-  const float a = p.advantages[t], r = expf(static_cast<float>(logp - p.old_logp[t]));
+__device__ __forceinline__ Term policy_term(const PolicyLossParams& p, const Token& t, double logp) {
+  const float a = t.advantage, r = expf(static_cast<float>(logp - t.old_logp));
   const float lo = 1.0f - p.clip_low, hi = 1.0f + p.clip_high;
   const float whole = r * a, cut = (r < lo ? lo : r > hi ? hi : r) * a;
   Term term = {whole > cut ? -cut : -whole, whole > cut ? 0.0f : -whole};
   if (p.ref_logp != nullptr) {
-    const float d = static_cast<float>(p.ref_logp[t] - logp);
+    const float d = static_cast<float>(t.ref_logp - logp);
     term.value += p.kl * expm1_less(d);
     term.slope -= p.kl * expm1f(d);
   }
@@ -69,9 +79,13 @@ __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_co
     const bool counts = load_index(r.targets, t, r.target64) >= 0;
     const double logp = -r.rows[t];
     Term term = {0.0f, 0.0f};
-    if (counts) term = policy_term(p, t, logp);
-    const double w = !counts ? 0.0 : p.weights != nullptr ? p.weights[t] : 1.0;
-    if (counts) sum += w * term.value;
+    double w = 0.0;
+    if (counts) {
+      const Token token(p, t);
+      term = policy_term(p, token, logp);
+      w = token.weight;
+      sum += w * term.value;
+    }
     if (p.logp != nullptr) p.logp[t] = counts ? static_cast<float>(logp) : 0.0f;
     if (p.slopes != nullptr) p.slopes[t] = counts ? static_cast<float>(w * unit * term.slope) : 0.0f;
   }
@@ -172,6 +186,10 @@ struct Slope {
   __device__ __forceinline__ Slope(float slope, float scale, float2 lse)
       : times(slope * scale), top(lse.x), rest(lse.y), low(-lse.y * kLog2e) {}
   __device__ __forceinline__ float other(float x) const { return -times * exp2_approx(fmaf(x - top, kLog2e, low)); }
+  __device__ __forceinline__ uint64_t other2(float a, float b) const {
+    const uint64_t y = fma2(add2(pack2(a, b), pack2(-top, -top)), pack2(kLog2e, kLog2e), pack2(low, low));
+    return mul2(pack2(exp2_approx(low2(y)), exp2_approx(high2(y))), pack2(-times, -times));
+  }
   __device__ __forceinline__ float target(float x) const { return times * -expm1f(x - top - rest); }
 };
 
@@ -197,8 +215,17 @@ struct Part {
 
 constexpr int kPartThreads = 256;
 
+template <int kThreads, typename T>
+__device__ __forceinline__ void fetch_part(const T* x, const Part<T>& part, uint4* to) {
+  const uint4* from = reinterpret_cast<const uint4*>(x + part.first);
+  for (int i = threadIdx.x; i < part.vectors; i += kThreads)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + i))),
+                 "l"(from + i)
+                 : "memory");
+}
+
 // Writes a part's gradient from its logits in shared memory (each thread reads what it has put there itself), or zeros.
-template <typename T>
+template <int kThreads, typename T>
 __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4* x, float edge, bool zero, const Slope& s,
                                          int64_t target) {
   constexpr int E = Vec<T>::kN;
@@ -208,13 +235,17 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
   const int64_t here = at >= 0 ? at / E : -1;
   T* to = g + part.first;
   const bool vector = reinterpret_cast<uintptr_t>(to) % 16 == 0;
-  for (int i = tid; i < part.vectors; i += kPartThreads) {
+#pragma unroll 2
+  for (int i = tid; i < part.vectors; i += kThreads) {
     float f[E] = {};
     if (!zero) {
       float w[E];
       Vec<T>::widen_all(x[i], w);
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[e] = s.other(w[e]);
+      for (int e = 0; e < E; e += 2) {
+        const uint64_t y = s.other2(w[e], w[e + 1]);
+        f[e] = low2(y), f[e + 1] = high2(y);
+      }
       if (here == i) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -230,16 +261,6 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void fetch_part(const T* x, const Part<T>& part, uint4* to) {
-  const uint4* from = reinterpret_cast<const uint4*>(x + part.first);
-  for (int i = threadIdx.x; i < part.vectors; i += kPartThreads)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + i))),
-                 "l"(from + i)
-                 : "memory");
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-
 // A row's gradient from its slope and log-sum: parts of a row, the rows from the last to the first, since the last ones read
 // for their sums may still be in L2. Rows of slope 0 are not read.
 template <typename T>
@@ -253,13 +274,13 @@ __global__ void __launch_bounds__(kPartThreads) logits_grad_kernel(const __grid_
   float2 lse = make_float2(0.0f, 0.0f);
   float edge = 0.0f;
   if (!zero) {
-    fetch_part(x, part, tile);
+    fetch_part<kPartThreads>(x, part, tile);
     lse = p.lse[t];
     if (part.edge >= 0) edge = widen(x[part.edge]);
   }
   const int64_t target = load_index(p.targets, t, p.target64);
   asm volatile("cp.async.wait_all;" ::: "memory");
-  put_part(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
+  put_part<kPartThreads>(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
 }
 
 // The same for vocabularies of at most 4096: a warp per row.
@@ -279,92 +300,150 @@ __global__ void __launch_bounds__(kPartThreads) logits_grad_warp_kernel(const __
   }
 }
 
+template <typename T>
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (__is_same(T, __nv_bfloat16)) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// take() of vectors; 16-bit values are compared as they are, two at a time. (Where both are NaN the larger is one, and so the sum.)
+template <typename T, int N>
+__device__ __forceinline__ void take_raw(const uint4 (&raw)[N], float& top, float& sum) {
+  constexpr int E = Vec<T>::kN;
+  float most;
+  if constexpr (sizeof(T) == 4) {
+    most = __uint_as_float(raw[0].x);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      most = fmaxf(fmaxf(fmaxf(most, __uint_as_float(raw[k].x)), __uint_as_float(raw[k].y)),
+                   fmaxf(__uint_as_float(raw[k].z), __uint_as_float(raw[k].w)));
+  } else {
+    uint32_t m = raw[0].x;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m = max2<T>(max2<T>(max2<T>(m, raw[k].x), raw[k].y), max2<T>(raw[k].z, raw[k].w));
+    const T* two = reinterpret_cast<const T*>(&m);
+    most = fmaxf(widen(two[0]), widen(two[1]));
+  }
+  if (most > top) {
+    sum *= exp2_approx((top - most) * kLog2e);
+    top = most;
+  }
+  const uint64_t away = pack2(-top, -top), unit = pack2(kLog2e, kLog2e);
+  uint64_t s[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float f[E];
+    Vec<T>::widen_all(raw[k], f);
+#pragma unroll
+    for (int i = 0; i < E; i += 2) {
+      const uint64_t d = mul2(add2(pack2(f[i], f[i + 1]), away), unit);
+      s[i / 2 & 1] = add2(s[i / 2 & 1], pack2(exp2_approx(low2(d)), exp2_approx(high2(d))));
+    }
+  }
+  const uint64_t all = add2(s[0], s[1]);
+  sum += low2(all) + high2(all);
+}
+
+// lanes_join in fp32, for sums of some hundred values: the fp64 units would take as long for the joins of a part as the fp32
+// units for the part.
+template <int kLanes>
+__device__ __forceinline__ void lanes_join_f32(float& top, float& sum) {
+  float all = top;
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, o));
+  sum *= exp2_approx((top - all) * kLog2e);
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  top = all;
+}
+
 // A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory.
 template <typename T>
-__global__ void __launch_bounds__(kPartThreads) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
-                                                                   const __grid_constant__ LogitsGradParams g, int parts) {
+__global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
+                                                                     const __grid_constant__ LogitsGradParams g, int parts) {
   extern __shared__ __align__(16) uint4 tile[];
   constexpr int kWarps = kPartThreads / 32;
   __shared__ float tops[kWarps];
-  __shared__ double sums[kWarps];
-  __shared__ float part_top;
-  __shared__ float part_sum[2];  // high and low part
+  __shared__ float sums[kWarps];
+  __shared__ float part_top, part_sum;
   __shared__ float shared_slope;
   __shared__ float2 shared_lse;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const TokenLossParams& r = p.rows;
-  const int tid = threadIdx.x, rank = blockIdx.x % parts;
-  const int64_t t = blockIdx.x / parts;
+  const int tid = threadIdx.x, rank = static_cast<int>(cluster_rank());
+  const int64_t t = blockIdx.x / static_cast<unsigned>(parts), target = load_index(r.targets, t, r.target64);
   const T* x = static_cast<const T*>(r.logits) + t * r.row;
-  const Part<T> part(x, r.vocab, rank, parts);
-  const int64_t target = load_index(r.targets, t, r.target64);
-  const bool counts = target >= 0, known = counts && target < r.vocab;
   T* grad = static_cast<T*>(g.grad) + t * g.grad_row;
-  if (!known) {  // the whole cluster
-    if (rank == 0 && tid == 0) r.rows[t] = counts ? NAN : 0.0;
+  const Part<T> part(x, r.vocab, rank, parts);
+  const bool counts = target >= 0;
+  if (!counts || target >= r.vocab) {  // the same for the whole cluster
     const float nan = NAN;
-    put_part(grad, part, tile, nan, !counts, Slope(nan, 1.0f, make_float2(0.0f, 0.0f)), -1);
+    if (rank == 0 && tid == 0) r.rows[t] = counts ? NAN : 0.0;
+    put_part<kPartThreads>(grad, part, tile, nan, !counts, Slope(nan, 1.0f, make_float2(0.0f, 0.0f)), -1);
     if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");  // what follows may count on the kernel before
     return;
   }
-  fetch_part(x, part, tile);
-  float edge = -kInf, own = 0.0f;
+  fetch_part<kPartThreads>(x, part, tile);
+  float edge = 0.0f, own = 0.0f;
   if (part.edge >= 0) edge = widen(x[part.edge]);
-  if (tid == 0) own = widen(x[target]);
+  Token token;
+  if (tid == 0) {
+    own = widen(x[target]);
+    token = Token(p, t);
+  }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  constexpr int E = Vec<T>::kN;
   float top = kNone.top, sum = 0.0f;
   if (part.edge >= 0) take<1>(&edge, top, sum);
   int i = tid;
-  for (; i + (kRowVectors - 1) * kPartThreads < part.vectors; i += kRowVectors * kPartThreads) {
-    float f[kRowVectors * E];
+  for (; i + 3 * kPartThreads < part.vectors; i += 4 * kPartThreads) {
+    uint4 raw[4];
 #pragma unroll
-    for (int k = 0; k < kRowVectors; ++k) Vec<T>::widen_all(tile[i + k * kPartThreads], f + k * E);
-    take<kRowVectors * E>(f, top, sum);
+    for (int k = 0; k < 4; ++k) raw[k] = tile[i + k * kPartThreads];
+    take_raw<T>(raw, top, sum);
   }
   for (; i < part.vectors; i += kPartThreads) {
-    float f[E];
-    Vec<T>::widen_all(tile[i], f);
-    take<E>(f, top, sum);
+    const uint4 raw[1] = {tile[i]};
+    take_raw<T>(raw, top, sum);
   }
-  Tail mine = lanes_join<32>({top, sum});
+  lanes_join_f32<32>(top, sum);
   if ((tid & 31) == 0) {
-    tops[tid >> 5] = mine.top;
-    sums[tid >> 5] = mine.sum;
+    tops[tid >> 5] = top;
+    sums[tid >> 5] = sum;
   }
   __syncthreads();
   if (tid < 32) {
-    mine = lanes_join<kWarps>(tid < kWarps ? Tail{tops[tid], sums[tid]} : kNone);
-    if (tid == 0 && parts > 1) {
-      part_top = mine.top;
-      part_sum[0] = static_cast<float>(mine.sum);
-      part_sum[1] = static_cast<float>(mine.sum - part_sum[0]);
-    }
+    top = tid < kWarps ? tops[tid] : kNone.top;
+    sum = tid < kWarps ? sums[tid] : 0.0f;
+    lanes_join_f32<kWarps>(top, sum);
+    if (tid == 0) part_top = top, part_sum = sum;
+    __syncwarp();
   }
   if (parts > 1) {
-    cluster_sync();
+    if (tid < 32) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (tid < 32) {
-      mine = kNone;
-      if (tid < parts)
-        mine = {peer_load(peer_address(&part_top, tid)),
-                static_cast<double>(peer_load(peer_address(&part_sum[0], tid))) +
-                    peer_load(peer_address(&part_sum[1], tid))};
-      mine = lanes_join<kMaxParts>(mine);
+      top = tid < parts ? peer_load(peer_address(&part_top, tid)) : kNone.top;
+      sum = tid < parts ? peer_load(peer_address(&part_sum, tid)) : 0.0f;
+      lanes_join_f32<kMaxParts>(top, sum);
+      __syncwarp();
     }
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // its peers' parts are read
   }
   if (tid == 0) {
-    const double rest = log_split(mine.sum), logp = (static_cast<double>(own) - mine.top) - rest;
-    const double w = p.weights != nullptr ? p.weights[t] : 1.0;
+    const double rest = log_split(sum), logp = (static_cast<double>(own) - top) - rest;
     if (rank == 0) r.rows[t] = -logp;
-    const Term term = policy_term(p, t, logp);
+    const Term term = policy_term(p, token, logp);
     if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");
-    shared_slope = static_cast<float>(w * (p.unit != nullptr ? __ldcg(p.unit) : 1.0) * term.slope);
-    shared_lse = make_float2(mine.top, static_cast<float>(rest));
+    shared_slope = static_cast<float>(token.weight * (p.unit != nullptr ? __ldcg(p.unit) : 1.0) * term.slope);
+    shared_lse = make_float2(top, static_cast<float>(rest));
   }
   __syncthreads();
   const float slope = shared_slope;
-  put_part(grad, part, tile, edge, slope == 0.0f, Slope(slope, g.scale, shared_lse), target);
-  if (parts > 1) cluster_sync();  // no CTA leaves before its part is read
+  put_part<kPartThreads>(grad, part, tile, edge, slope == 0.0f, Slope(slope, g.scale, shared_lse), target);
+  if (parts > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // no CTA leaves before its part is read
 }
 
 // 1 over the counted tokens' weights.

@@ -231,6 +231,12 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Whether every key's and value's elements are whole 16-byte vectors of a 16-bit type.
+inline bool paged_vectors(const DecodeParams& p) {
+  return p.dim % 8 == 0 && p.k_page % 8 == 0 && p.k_token % 8 == 0 && p.k_head % 8 == 0 && p.v_page % 8 == 0 &&
+         p.v_token % 8 == 0 && p.v_head % 8 == 0 && aligned_to(p.k, 16) && aligned_to(p.v, 16);
+}
+
 // CTAs of a cluster: a CTA per SM, none with less than 128 keys of the longest
 // sequence that the page table can hold; up to `per_sm` where each keeps 512,
 // because a CTA's start and its part in the join cost as much as some 200 keys

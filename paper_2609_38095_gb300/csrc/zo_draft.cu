@@ -365,9 +365,7 @@ cudaError_t launch_draft_masks(const int32_t* parents, int64_t batch, int drafts
 }
 
 bool launch_draft_mma(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e) {
-  if (dtype == 0 || p.dim % 8 != 0 || p.k_page % 8 != 0 || p.k_token % 8 != 0 || p.k_head % 8 != 0 || p.v_page % 8 != 0 ||
-      p.v_token % 8 != 0 || p.v_head % 8 != 0 || !aligned_to(p.k, 16) || !aligned_to(p.v, 16))
-    return false;
+  if (dtype == 0 || !paged_vectors(p)) return false;
   *e = dtype == 1 ? launch_type<__nv_bfloat16>(p, batch, sms, stream) : launch_type<__half>(p, batch, sms, stream);
   return true;
 }

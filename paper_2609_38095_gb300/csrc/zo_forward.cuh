@@ -127,12 +127,16 @@ cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype
 bool launch_decode_mma(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_draft_masks(const int32_t* parents, int64_t batch, int drafts, int64_t* masks, cudaStream_t stream);
 cudaError_t launch_draft_scalar(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream);
+bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 bool launch_draft_mma(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream);
 cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams* g, int dtype, int sms, cudaStream_t stream);
 cudaError_t launch_preference_loss(const PreferenceLossParams& p, const LogitsGradParams* g, int dtype, int sms,
                                    cudaStream_t stream);
 
+#ifdef __CUDACC__
+__host__ __device__
+#endif
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 #ifdef __CUDACC__

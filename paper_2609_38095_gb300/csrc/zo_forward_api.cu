@@ -440,6 +440,8 @@ int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, 
   if (misaligned(masks, 8)) return ZO_ERR_ALIGN;
   p.masks = masks;
   cudaError_t e = cudaSuccess;
+  if (zo::launch_draft_wide(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
+    return finish(e, "draft_wide_kernel");
   if (zo::launch_draft_mma(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
     return finish(e, "draft_mma_kernel");
   return finish(zo::launch_draft_scalar(p, batch, dtype, sms, static_cast<cudaStream_t>(stream)),
