@@ -81,36 +81,47 @@ struct DecodeRows {
 
 struct DraftPlace : DecodePlace {  // heads: rows here, head0: the first
   int n;                           // keys ahead of the tree's
+  int live;                        // rows here up to the last that sees anything
   uint64_t any;                    // nodes that are seen
 };
 
-// Every thread of the CTA; masks: 64 words of shared memory, the nodes' masks without bits of no node (0 in a sequence of
-// negative length). A block of rows behind the last that sees anything has no keys.
 template <int HB>
-__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t cluster, uint64_t* masks) {
-  const int blocks = p.head_blocks, lane = threadIdx.x & 31;
+struct DraftShared {
+  uint64_t masks[64];  // the nodes', without bits of no node; 0 in a sequence of negative length
+  uint16_t node[HB], head[HB];  // of the rows here
+};
+
+// Every thread of the CTA. A block of rows behind the last that sees anything has no keys.
+template <int HB>
+__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t cluster, DraftShared<HB>& sh) {
+  const uint32_t blocks = p.head_blocks, lane = threadIdx.x & 31;
   DraftPlace w;
   w.b = cluster / (p.kv_heads * blocks);
-  const int rest = cluster - w.b * (p.kv_heads * blocks);
+  const uint32_t rest = cluster - w.b * (p.kv_heads * blocks);
   w.g = rest / blocks;
   w.head0 = (rest - w.g * blocks) * HB;
   w.heads = min(HB, p.drafts * p.group - w.head0);
   const int n = p.lengths[w.b];
   if (threadIdx.x < 64) {
-    uint64_t m = 0;
-    if (threadIdx.x < p.drafts && n >= 0)
-      m = p.masks[static_cast<int64_t>(w.b) * p.drafts + threadIdx.x] & (~UINT64_C(0) >> (64 - p.drafts));
-    masks[threadIdx.x] = m;
+    uint64_t m = 0;  // (both loads on their way at once)
+    if (threadIdx.x < p.drafts) m = p.masks[static_cast<int64_t>(w.b) * p.drafts + threadIdx.x] & (~UINT64_C(0) >> (64 - p.drafts));
+    sh.masks[threadIdx.x] = n >= 0 ? m : 0;
+  }
+  for (uint32_t h = threadIdx.x; h < HB; h += blockDim.x) {
+    const uint32_t r = w.head0 + min(h, static_cast<uint32_t>(w.heads) - 1), node = r / static_cast<uint32_t>(p.group);
+    sh.node[h] = static_cast<uint16_t>(node);
+    sh.head[h] = static_cast<uint16_t>(w.g * p.group + r - node * p.group);
   }
   __syncthreads();
-  const uint64_t a = masks[lane], b = masks[lane + 32], both = a | b;
+  const uint64_t a = sh.masks[lane], b = sh.masks[lane + 32], both = a | b;
   w.any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
           __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
-  const uint64_t live = static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, b != 0)) << 32 | __ballot_sync(0xFFFFFFFFu, a != 0);
+  const uint64_t nodes = static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, b != 0)) << 32 | __ballot_sync(0xFFFFFFFFu, a != 0);
   w.n = max(n, 0);
   w.len = w.any == 0 ? 0 : static_cast<int64_t>(w.n) + 64 - __clzll(w.any);
   w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0) || w.len > 0x7FFFFFFF - 64;
-  if (w.bad || w.head0 >= (64 - __clzll(live)) * p.group) w.len = 0;
+  w.live = max(0, min(w.heads, (64 - __clzll(nodes)) * p.group - w.head0));
+  if (w.bad || w.live == 0) w.len = w.live = 0;
   return w;
 }
 
@@ -119,15 +130,16 @@ __device__ __forceinline__ bool draft_sees(const DraftPlace& w, int64_t j) {
   return j < w.n || (j < w.len && (w.any >> (j - w.n) & 1) != 0);
 }
 
-// The tree's rows: see DecodeRows.
-template <typename T>
+// The tree's rows: see DecodeRows. (A row that is none is the last.)
+template <typename T, int HB>
 struct DraftRows {
   const DraftParams& p;
   const DraftPlace& w;
-  const uint64_t* masks;
-  __device__ __forceinline__ int node(int h) const { return (w.head0 + h) / p.group; }
-  __device__ __forceinline__ int head(int h) const { return w.g * p.group + (w.head0 + h) % p.group; }
-  __device__ __forceinline__ bool sees(int h) const { return masks[node(h)] != 0; }
+  const DraftShared<HB>& sh;
+  __device__ __forceinline__ int node(int h) const { return sh.node[h]; }
+  __device__ __forceinline__ int head(int h) const { return sh.head[h]; }
+  __device__ __forceinline__ uint64_t mask(int h) const { return sh.masks[sh.node[h]]; }
+  __device__ __forceinline__ bool sees(int h) const { return mask(h) != 0; }
   __device__ __forceinline__ T* row(int h) const {
     return static_cast<T*>(p.out) + w.b * p.out_token + node(h) * p.out_node + head(h) * p.out_head;
   }
@@ -203,6 +215,81 @@ __device__ __forceinline__ void decode_join(const DecodeParams& p, const DecodeP
     if (d == 0 && p.lse != nullptr) *rows.sum(h) = join.lse[h];
   }
   cluster_sync();  // no CTA leaves before its part is read
+}
+
+// Every thread of the cluster: the join of its CTAs alone, each with tops and totals of its HB rows (tops in units of log2) and
+// unscaled outputs, kPitch floats from one row to the next, on 16 bytes. A warp has a row at a time: its lanes the CTAs'
+// statistics, then four columns each. Returns when the peers are done with this CTA's part.
+template <typename T, int DP, int kPitch, int kThreads, typename R>
+__device__ __forceinline__ void rows_join(const DecodeParams& p, const DecodePlace& w, const R& rows, const float* outs,
+                                          const float* tops, const float* totals, const int* bad_here) {
+  constexpr int kLanes = DP / 4 < 32 ? DP / 4 : 32, kVectors = DP / 4 / kLanes;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int ranks = static_cast<int>(cluster_size());
+  cluster_sync();
+  const bool peer = lane < ranks;
+  const bool bad_any =
+      __any_sync(0xFFFFFFFFu, peer && __float_as_int(peer_load(peer_address(bad_here, peer ? lane : 0))) != 0);
+  for (int r = static_cast<int>(cluster_rank()) * (kThreads / 32) + warp; r < w.heads; r += ranks * (kThreads / 32)) {
+    const float mine = peer ? peer_load(peer_address(tops + r, lane)) : -kInf;
+    const float part = peer ? peer_load(peer_address(totals + r, lane)) : 0.0f;
+    float top = mine;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float scale = mine == -kInf ? 0.0f : exp2_approx(mine - top);
+    float total = part * scale;
+    if (part != part) total = part;  // a NaN where every score is one
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    top = __shfl_sync(0xFFFFFFFFu, top, 0);
+    total = __shfl_sync(0xFFFFFFFFu, total, 0);
+    const bool sees = rows.sees(r), bad = bad_any && sees;
+    if (!sees) total = 0.0f;
+    const uint32_t has = __ballot_sync(0xFFFFFFFFu, mine > -kInf);  // CTAs in which the row saw something
+    float4 x[kVectors];
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) x[v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (total != 0.0f && !bad) {
+      constexpr int kBatch = kVectors == 1 ? 8 : 4;
+      for (int first = 0; first < ranks; first += kBatch) {
+        float4 y[kBatch][kVectors];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const bool in = first + i < ranks && (has >> (first + i) & 1) != 0 && lane < kLanes;
+#pragma unroll
+          for (int v = 0; v < kVectors; ++v) {
+            y[i][v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (in)
+              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                           : "=f"(y[i][v].x), "=f"(y[i][v].y), "=f"(y[i][v].z), "=f"(y[i][v].w)
+                           : "r"(peer_address(outs + r * kPitch + v * 128 + lane * 4, first + i)));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float s = __shfl_sync(0xFFFFFFFFu, scale, (first + i) & 31);
+#pragma unroll
+          for (int v = 0; v < kVectors; ++v) {
+            x[v].x = fmaf(y[i][v].x, s, x[v].x), x[v].y = fmaf(y[i][v].y, s, x[v].y);
+            x[v].z = fmaf(y[i][v].z, s, x[v].z), x[v].w = fmaf(y[i][v].w, s, x[v].w);
+          }
+        }
+      }
+    }
+    const float over = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
+    const auto value = [&](float f) { return narrow<T>(over == 0.0f ? 0.0f : f * over); };
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+      const int d = v * 128 + lane * 4;
+      T* to = rows.row(r) + d;
+      if (d < p.dim) to[0] = value(x[v].x);
+      if (d + 1 < p.dim) to[1] = value(x[v].y);
+      if (d + 2 < p.dim) to[2] = value(x[v].z);
+      if (d + 3 < p.dim) to[3] = value(x[v].w);
+    }
+    if (lane == 0 && p.lse != nullptr) *rows.sum(r) = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+  }
+  cluster_sync();
 }
 
 // Fragments of tiles of 16-bit values in shared memory, and their products.

@@ -42,20 +42,20 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32) decode_scalar_ker
   float* mine = tiles + warp * S::kWarp;
   float* weights = mine + S::kStages * S::kStage;  // [16][HB]
   const uint32_t ranks = cluster_size();
-  __shared__ uint64_t masks[kDraft ? 64 : 1];
+  __shared__ DraftShared<kDraft ? HB : 1> sh;
   const auto w = [&] {
-    if constexpr (kDraft) return draft_place<HB>(p, blockIdx.x / ranks, masks);
+    if constexpr (kDraft) return draft_place<HB>(p, blockIdx.x / ranks, sh);
     else return decode_place<HB>(p, blockIdx.x / ranks);
   }();
   const auto rows = [&] {
-    if constexpr (kDraft) return DraftRows<T>{p, w, masks};
+    if constexpr (kDraft) return DraftRows<T, HB>{p, w, sh};
     else return DecodeRows<T>(p, w);
   }();
   if (threadIdx.x == 0) join.bad = w.bad;
   for (int i = threadIdx.x; i < HB * DP; i += S::kWarps * 32) {
     const int h = i / DP, d = i - h * DP;
     const T* q;
-    if constexpr (kDraft) q = rows.query(h < w.heads ? h : 0);
+    if constexpr (kDraft) q = rows.query(h);
     else q = static_cast<const T*>(p.q) + w.b * p.q_token + (w.head0 + (h < w.heads ? h : 0)) * p.q_head;
     qs[i] = h < w.heads && d < p.dim ? widen(q[d]) : 0.0f;
   }
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32) decode_scalar_ker
     int place = 0;       // the key's, from the tree's first
     if constexpr (kDraft) {
       nodes = (tile + 1) * kDecodeKeys > w.n;
-      place = j < w.n ? static_cast<int>(j - w.n) : j < w.len ? __popcll(masks[j - w.n]) - 1 : 0;
+      place = j < w.n ? static_cast<int>(j - w.n) : j < w.len ? __popcll(sh.masks[j - w.n]) - 1 : 0;
     }
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(Scalar<DP, HB>::kWarps * 32) decode_scalar_ker
       if (p.softcap > 0.0f) x = p.softcap * tanhf(x * over_cap);
       bool seen = true;
       if constexpr (kDraft) {
-        const uint64_t mask = masks[rows.node(h < w.heads ? h : 0)];
+        const uint64_t mask = rows.mask(h);
         x -= slope[h] * fabsf(static_cast<float>(__popcll(mask) - 1 - place));
         if (nodes) seen = j < w.n || (j < w.len && (mask >> (j - w.n) & 1) != 0);
         if (!seen) x = -kInf;

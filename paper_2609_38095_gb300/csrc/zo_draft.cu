@@ -35,7 +35,7 @@ struct Tiles {
   static constexpr int kRow = DP * 2;                  // bytes of a key
   static constexpr int kStage = 2 * kKeys * kRow;      // keys, then values
   static constexpr int kWarp = kStages * kStage;
-  static constexpr int kBytes = kWarps * kWarp + 2 * kWarps * kRows * 4;
+  static constexpr int kBytes = kWarps * kWarp;
   static_assert(kRows * DP * 4 <= kWarp, "a warp's output takes its tiles' place");
 };
 
@@ -53,21 +53,21 @@ __device__ __forceinline__ bool not_finite2(uint32_t v) {
 // O += P V, so that a step's scores are the next product's left operand as they
 // are. What a row sees of the tree's own keys is a bit of its node's mask.
 template <typename T, int DP, int MB>
-__global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
+__global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 64 ? 3 : 2)
     draft_mma_kernel(const __grid_constant__ DraftParams p) {
   using L = Tiles<DP, MB>;
   constexpr int kVectors = DP / 8, kDeep = L::kBlocksOfKeys, kRows = L::kRows;  // a key's 16-byte vectors
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ DecodeJoin<kRows> join;
-  __shared__ uint64_t masks[64];
+  __shared__ DraftShared<kRows> sh;
+  __shared__ float tops[kWarps][kRows], totals[kWarps][kRows];  // then the first the warps' scales
+  __shared__ float top[kRows], sum[kRows];
+  __shared__ int bad_here;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t tiles = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * L::kWarp;
-  float* tops = reinterpret_cast<float*>(smem + kWarps * L::kWarp);
-  float* totals = tops + kWarps * kRows;
   const uint32_t ranks = cluster_size();
-  const DraftPlace w = draft_place<kRows>(p, blockIdx.x / ranks, masks);
-  const DraftRows<T> rows = {p, w, masks};
-  if (threadIdx.x == 0) join.bad = w.bad;
+  if (threadIdx.x == 0) bad_here = 0;
+  const DraftPlace w = draft_place<kRows>(p, blockIdx.x / ranks, sh);
+  const DraftRows<T, kRows> rows = {p, w, sh};
 
   const T* kc = static_cast<const T*>(p.k) + w.g * p.k_head;
   const T* vc = static_cast<const T*>(p.v) + w.g * p.v_head;
@@ -125,27 +125,30 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   // the queries as left operands: rows lane / 4 and 8 more of each block of 16, elements 2 (lane mod 4) and 8 more
+  const bool pairs = aligned_to(p.q, 4) && (p.q_token | p.q_node | p.q_head) % 2 == 0;
   uint32_t qa[MB][DP / 16][4];
-  float slope2[MB][2];
-  int depth[MB][2];  // a row's place from the tree's first
+  float slope2[MB][2], depth[MB][2];  // depth: a row's place from the tree's first
 #pragma unroll
   for (int m = 0; m < MB; ++m)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int h = 16 * m + 8 * r + lane / 4;
-      const bool in = h < w.heads;
-      const T* q = rows.query(in ? h : 0);
-      slope2[m][r] = p.slopes != nullptr ? p.slopes[rows.head(in ? h : 0)] * kLog2e : 0.0f;
-      depth[m][r] = __popcll(masks[rows.node(in ? h : 0)]) - 1;
+      const T* q = rows.query(h);
+      slope2[m][r] = p.slopes != nullptr ? p.slopes[rows.head(h)] * kLog2e : 0.0f;
+      depth[m][r] = static_cast<float>(__popcll(rows.mask(h)) - 1);
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int d = s * 16 + c * 8 + lane % 4 * 2;
           qa[m][s][r + 2 * c] = 0;
-          if (in && d < p.dim) {
-            const uint16_t* x = reinterpret_cast<const uint16_t*>(q + d);
-            qa[m][s][r + 2 * c] = x[0] | static_cast<uint32_t>(x[1]) << 16;
+          if (d < p.dim) {
+            if (pairs) {
+              qa[m][s][r + 2 * c] = *reinterpret_cast<const uint32_t*>(q + d);
+            } else {
+              const uint16_t* x = reinterpret_cast<const uint16_t*>(q + d);
+              qa[m][s][r + 2 * c] = x[0] | static_cast<uint32_t>(x[1]) << 16;
+            }
           }
         }
     }
@@ -194,52 +197,100 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
     }
     const int64_t key0 = tile * L::kKeys;
     const bool nodes = key0 + L::kKeys > w.n;  // keys of the tree, or beyond the last
-    const int from = static_cast<int>(key0 - w.n) + lane % 4 * 2;  // the thread's first key, from the tree's first
+    float times = scale2;  // what the scores are in, times
+    if (p.softcap > 0.0f) {
+      times = 1.0f;
+      float far = 0.0f;
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int n = 0; n < 2 * kDeep; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) far = fmaxf(far, fabsf(s[m][n][c]));
+      const bool near = __all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap);  // mostly: caps are there for the rare large score
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int n = 0; n < 2 * kDeep; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; c += 2) {
+            float* const y = &s[m][n][c];
+            if (near) {
+              const uint64_t two = capped_near(pack2(y[0], y[1]), pack2(scale2, scale2), pack2(cap2, cap2));
+              y[0] = low2(two), y[1] = high2(two);
+            } else {
+              y[0] = capped(y[0], scale2, cap2), y[1] = capped(y[1], scale2, cap2);
+            }
+          }
+    } else if (p.slopes != nullptr || nodes || p.scale <= 0.0f) {
+      times = 1.0f;
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int n = 0; n < 2 * kDeep; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[m][n][c] *= scale2;
+    }
+    if (nodes) {
+      const int from = static_cast<int>(key0 - w.n) + lane % 4 * 2;  // the thread's first key, from the tree's first
+#pragma unroll
+      for (int n = 0; n < 2 * kDeep; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int node = from + n * 8 + c;
+          const bool tree = node >= 0 && node < 64;
+          const float place = static_cast<float>(node < 0 ? node : tree ? __popcll(sh.masks[node]) - 1 : 0);
+#pragma unroll
+          for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              float& y = s[m][n][2 * r + c];
+              if (p.slopes != nullptr) y -= slope2[m][r] * fabsf(depth[m][r] - place);
+              if (node >= 0 && !(tree && (rows.mask(16 * m + 8 * r + lane / 4) >> node & 1))) y = -kInf;
+            }
+        }
+    } else if (p.slopes != nullptr) {
+      const float from = static_cast<float>(static_cast<int>(w.n - key0) - lane % 4 * 2);  // exact, and its sums, below 2^24
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float away = depth[m][r] + from;
+#pragma unroll
+          for (int n = 0; n < 2 * kDeep; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              s[m][n][2 * r + c] = fmaf(-slope2[m][r], away - static_cast<float>(n * 8 + c), s[m][n][2 * r + c]);
+        }
+    }
     bool moved = false;
     float back[MB][2];
 #pragma unroll
     for (int m = 0; m < MB; ++m)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int h = 16 * m + 8 * r + lane / 4;
-        const uint64_t mask = nodes ? masks[rows.node(h < w.heads ? h : 0)] : 0;
-        float most = -kInf;
+        float most = fmaxf(s[m][0][2 * r], s[m][0][2 * r + 1]);
 #pragma unroll
-        for (int n = 0; n < 2 * kDeep; ++n)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float y = s[m][n][2 * r + c];
-            y = p.softcap > 0.0f ? capped(y, scale2, cap2) : y * scale2;
-            int place = from + n * 8 + c;
-            bool seen = true;
-            if (nodes && place >= 0) {
-              seen = place < 64 && (mask >> place & 1) != 0;
-              place = place < 64 ? __popcll(masks[place]) - 1 : 0;
-            }
-            if (p.slopes != nullptr) y -= slope2[m][r] * fabsf(static_cast<float>(depth[m][r] - place));
-            if (!seen) y = -kInf;
-            s[m][n][2 * r + c] = y;
-            most = fmaxf(most, y);
-          }
+        for (int n = 1; n < 2 * kDeep; ++n) most = fmaxf(fmaxf(most, s[m][n][2 * r]), s[m][n][2 * r + 1]);
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-        most -= kLift<T>;
+        most = most * times - kLift<T>;
         back[m][r] = 1.0f;
         if (most > base[m][r] + kSlack || (base[m][r] == -kInf && most > -kInf)) {
           back[m][r] = exp2_approx(base[m][r] - most);
           base[m][r] = most;
           moved = true;
         }
-        const float shift = base[m][r] == -kInf ? 0.0f : base[m][r];
-        total[m][r] *= back[m][r];
+        const float shift = base[m][r] == -kInf ? 0.0f : -base[m][r];
+        uint64_t sums = 0;
 #pragma unroll
-        for (int n = 0; n < 2 * kDeep; ++n)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float e = exp2_approx(s[m][n][2 * r + c] - shift);
-            s[m][n][2 * r + c] = e;
-            total[m][r] += e;
-          }
+        for (int n = 0; n < 2 * kDeep; ++n) {
+          const uint64_t t = fma2(pack2(s[m][n][2 * r], s[m][n][2 * r + 1]), pack2(times, times), pack2(shift, shift));
+          const uint64_t e = pack2(exp2_approx(low2(t)), exp2_approx(high2(t)));
+          s[m][n][2 * r] = low2(e), s[m][n][2 * r + 1] = high2(e);
+          sums = add2(sums, e);
+        }
+        total[m][r] = fmaf(total[m][r], back[m][r], low2(sums) + high2(sums));
       }
     if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
@@ -268,7 +319,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               const int h = 16 * m + 8 * r + lane / 4;
-              if (!(masks[rows.node(h < w.heads ? h : 0)] >> node & 1)) continue;
+              if (!(rows.mask(h) >> node & 1)) continue;
 #pragma unroll
               for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
@@ -318,16 +369,16 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
   for (int m = 0; m < MB; ++m)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      float sum = total[m][r];
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+      float all = total[m][r];
+      all += __shfl_xor_sync(0xFFFFFFFFu, all, 1);
+      all += __shfl_xor_sync(0xFFFFFFFFu, all, 2);
       if (lane % 4 == 0) {
-        tops[warp * kRows + 16 * m + 8 * r + lane / 4] = base[m][r];
-        totals[warp * kRows + 16 * m + 8 * r + lane / 4] = sum;
+        tops[warp][16 * m + 8 * r + lane / 4] = base[m][r];
+        totals[warp][16 * m + 8 * r + lane / 4] = all;
       }
     }
-  __syncthreads();  // join.bad is set, and every warp is done with its tiles: the outputs take their place
-  if (bad) join.bad = 1;
+  if (bad || w.bad) bad_here = 1;
+  __syncthreads();  // every warp is done with its tiles: the outputs take their place
   float* outs = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int m = 0; m < MB; ++m)
@@ -337,7 +388,32 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 ? 3 : 2)
       for (int r = 0; r < 2; ++r)
         *reinterpret_cast<float2*>(outs + (warp * kRows + 16 * m + 8 * r + lane / 4) * DP + n * 8 + lane % 4 * 2) =
             make_float2(acc[m][n][2 * r], acc[m][n][2 * r + 1]);
-  decode_join<T, kRows, DP, kWarps, true>(p, w, rows, outs, tops, totals, join);
+  if (threadIdx.x < kRows) {  // the warps' scales
+    const int h = threadIdx.x;
+    float most = -kInf, all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) most = fmaxf(most, tops[i][h]);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float scale = tops[i][h] == -kInf ? 0.0f : exp2_approx(tops[i][h] - most);
+      all += totals[i][h] != totals[i][h] ? totals[i][h] : totals[i][h] * scale;
+      tops[i][h] = scale;
+    }
+    top[h] = most, sum[h] = all;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x * 4; i < w.live * DP; i += kWarps * 32 * 4) {
+    const int h = i / DP;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int n = 0; n < kWarps; ++n) {
+      const float scale = tops[n][h];
+      const float4 y = *reinterpret_cast<const float4*>(outs + n * kRows * DP + i);
+      x.x = fmaf(y.x, scale, x.x), x.y = fmaf(y.y, scale, x.y), x.z = fmaf(y.z, scale, x.z), x.w = fmaf(y.w, scale, x.w);
+    }
+    *reinterpret_cast<float4*>(outs + i) = x;
+  }
+  rows_join<T, DP, DP, kWarps * 32>(p, w, rows, outs, top, sum, &bad_here);
 }
 
 template <typename T, int DP, int MB>

@@ -38,7 +38,7 @@ struct Plan {
 template <int kSlots>
 struct Shared {
   uint64_t full[12], empty[12], s_full[2][2], p_full[2][2], o_done[2][2], drain[2];
-  uint64_t masks[64];
+  DraftShared<kSlots * kRows> rows;
   uint32_t odd[64][4];  // a node's columns whose value is not finite
   float top[kSlots * kRows], total[kSlots * kRows];
   uint32_t tmem;
@@ -72,17 +72,15 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   uint8_t* stages = tiles + kSlots * L::kQueries;
   const int tid = threadIdx.x, warp = static_cast<int>(uniform(tid >> 5)), lane = tid & 31;
   const uint32_t ranks = cluster_size(), rank = cluster_rank();
-  const DraftPlace w = draft_place<L::kBlock>(p, blockIdx.x / ranks, sh.masks);
-  const DraftRows<T> rows = {p, w, sh.masks};
+  const DraftPlace w = draft_place<L::kBlock>(p, blockIdx.x / ranks, sh.rows);
+  const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
   volatile int* dead = &sh.dead;
 
   // steps here, and rows up to the last that sees anything
   const int all = static_cast<int>((w.len + kKeys - 1) / kKeys);
   const int begin = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
   const int n = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - begin;
-  const uint64_t live_nodes = static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, sh.masks[lane + 32] != 0)) << 32 |
-                              __ballot_sync(0xFFFFFFFFu, sh.masks[lane] != 0);
-  const int live = n == 0 ? 0 : min(w.heads, (64 - __clzll(live_nodes)) * p.group - w.head0);
+  const int live = n == 0 ? 0 : w.live;
   const auto warps_of = [&](int s) { return max(0, min(4, (live - s * kRows + 31) / 32)); };
 
   if (tid == L::kThreads - 32) {
@@ -111,19 +109,22 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
     for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
       const int r = i / kVectors, v = i % kVectors;
+      uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
       uint4 x = make_uint4(0, 0, 0, 0);
       if (r < live && v * 8 < p.dim) {
         const T* q = rows.query(r) + v * 8;
         if (whole) {
-          x = *reinterpret_cast<const uint4*>(q);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
+          continue;
         } else {
           const uint16_t* u = reinterpret_cast<const uint16_t*>(q);
           const auto two = [&](int e) { return u[e] | static_cast<uint32_t>(u[e + 1]) << 16; };
           x = make_uint4(two(0), two(2), two(4), two(6));
         }
       }
-      *reinterpret_cast<uint4*>(tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4)) = x;
+      *reinterpret_cast<uint4*>(to) = x;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   tmem_fence_before();
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   } else {
     const int slot = warp >> 2, r = tid;  // the thread's row
     const bool in = r < live;
-    const uint64_t mask = in ? sh.masks[rows.node(r)] : 0;
+    const uint64_t mask = in ? rows.mask(r) : 0;
     const int depth = __popcll(mask) - 1;
     const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + L::kOutputs + slot * D;
     const float scale2 = kCap ? p.scale / p.softcap : p.scale * kLog2e;
@@ -311,7 +312,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
 #pragma unroll
           for (int e = 0; e < 64; ++e) {
             const int64_t node = key0 + e - w.n;
-            const float far = node < 0 ? away - e : node < 64 ? fabsf(static_cast<float>(depth + 1 - __popcll(sh.masks[node]))) : 0.0f;
+            const float far = node < 0 ? away - e : node < 64 ? fabsf(static_cast<float>(depth + 1 - __popcll(sh.rows.masks[node]))) : 0.0f;
             x[e / 32][e % 32] = __float_as_uint(__uint_as_float(x[e / 32][e % 32]) * times - slope2 * far);
           }
         }
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   float* outs = reinterpret_cast<float*>(tiles);
   if (warp < kSoftmaxWarps && warp * 32 < live && sh.dead == 0) {
     const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + L::kOutputs + (warp >> 2) * D;
-    const uint64_t mask = tid < live ? sh.masks[rows.node(tid)] : 0;
+    const uint64_t mask = tid < live ? rows.mask(tid) : 0;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[32];
@@ -409,53 +410,13 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   }
   if (tid == 0 && sh.dead != 0) sh.bad = 1;
   tmem_fence_before();
-  cluster_sync();
+  __syncthreads();
   if (warp == kSoftmaxWarps) {
     tmem_fence_after();
     tmem_free(tmem, L::kColumns);
   }
-  // The cluster's CTAs joined: a warp per row, the rows in turn; lanes have the CTAs' statistics, then 4 columns each.
-  const int shares = ranks * (L::kThreads / 32);
-  for (int r = static_cast<int>(rank) * (L::kThreads / 32) + warp; r < w.heads; r += shares) {
-    const bool peer = lane < static_cast<int>(ranks);
-    const float mine = peer ? peer_load(peer_address(&sh.top[r], lane)) : -kInf;
-    const float part = peer ? peer_load(peer_address(&sh.total[r], lane)) : 0.0f;
-    bool bad = peer && __float_as_int(peer_load(peer_address(&sh.bad, lane))) != 0;
-    bad = __any_sync(0xFFFFFFFFu, bad);
-    float top = mine;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float scale = mine == -kInf ? 0.0f : exp2_approx(mine - top);
-    float total = part * scale;
-    if (part != part) total = part;  // a NaN where every score is one
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-    if (!rows.sees(r)) bad = false, total = 0.0f;
-    const float over = bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
-    const uint32_t has = __ballot_sync(0xFFFFFFFFu, mine > -kInf);  // CTAs in which the row saw something
-    float x[4] = {};
-    if (!bad && total != 0.0f) {
-      for (uint32_t left = has; left != 0; left &= left - 1) {
-        const int from = __ffs(left) - 1;
-        const float s = __shfl_sync(0xFFFFFFFFu, scale, from);
-        if (lane * 4 < D) {
-          const uint32_t a = peer_address(outs + r * L::kPitch + lane * 4, from);
-          float4 y;
-          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w)
-                       : "r"(a)
-                       : "memory");
-          x[0] = fmaf(y.x, s, x[0]), x[1] = fmaf(y.y, s, x[1]), x[2] = fmaf(y.z, s, x[2]), x[3] = fmaf(y.w, s, x[3]);
-        }
-      }
-    }
-    T* to = rows.row(r) + lane * 4;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane * 4 + e < p.dim) to[e] = narrow<T>(over == 0.0f ? 0.0f : x[e] * over);
-    if (lane == 0 && p.lse != nullptr) *rows.sum(r) = bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
-  }
-  cluster_sync();  // no CTA leaves before its part is read
+  __syncwarp();
+  rows_join<T, D, L::kPitch, L::kThreads>(p, w, rows, outs, sh.top, sh.total, &sh.bad);
 }
 
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
