@@ -234,12 +234,16 @@ int zo_draft_masks(const int32_t* parents, int64_t batch, int32_t drafts, int64_
  *           out may be q (same strides) and overlaps nothing else
  *   masks   int64 [batch][drafts], zo_draft_masks's or the caller's own
  *   lse     fp32 [batch][drafts][heads] or NULL
+ *   workspace  zo_attention_draft_workspace_size(...) bytes, 16-byte aligned
+ *           (0, where it takes none: NULL)
  * ------------------------------------------------------------------------- */
+int64_t zo_attention_draft_workspace_size(int64_t batch, int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                          int32_t dtype);
 int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, const zo_pages* out, int64_t batch,
                        int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
                        const int32_t* pages, int64_t pages_stride, int64_t max_pages, int64_t n_pages,
                        int32_t page_size, const int32_t* lengths, const int64_t* masks, float scale, float softcap,
-                       const float* slopes, float* lse, void* stream);
+                       const float* slopes, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
  * zo_policy_loss -- with logp_t = x_t,target_t - log sum_v exp(x_tv), r_t =

@@ -32,6 +32,7 @@ decltype(&zo_preference_loss) g_preference_loss = nullptr;
 decltype(&zo_attention_draft) g_attention_draft = nullptr;
 decltype(&zo_policy_loss_workspace_size) g_policy_work = nullptr;
 decltype(&zo_preference_loss_workspace_size) g_preference_work = nullptr;
+decltype(&zo_attention_draft_workspace_size) g_draft_work = nullptr;
 
 // Whether tensors may have tangents in this call: within a level of forward mode. (Asked once per call; asking each tensor
 // took 0.5 us of a call of nine.)
@@ -247,11 +248,14 @@ PyObject* draft_attention(PyObject* const* a) {
   const bool with_lse = truth(a[10]);
   if (with_lse) c.lse.make({batch, drafts, c.n}, c.q, at::kFloat);
   const zo_pages q = pages_of(c.q), k = pages_of(c.k), v = pages_of(c.v), out = pages_of(c.out.t);
+  const int64_t bytes = g_draft_work(batch, static_cast<int32_t>(drafts), c.n, c.kv, c.size, code(c.q.scalar_type()));
+  const at::Tensor work = bytes > 0 ? at::empty({bytes}, at::TensorOptions(c.q.device()).dtype(at::kByte)) : at::Tensor();
   const int rc = on_stream(c.q, [&](void* stream) {
     return g_attention_draft(&q, &k, &v, &out, batch, static_cast<int32_t>(drafts), c.n, c.kv, c.size, code(c.q.scalar_type()),
                              pages.const_data_ptr<int32_t>(), pages.stride(0), pages.size(1), c.k.size(0), page_size,
                              lengths.const_data_ptr<int32_t>(), masks.const_data_ptr<int64_t>(), c.scale, c.softcap, c.slopes,
-                             with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, stream);
+                             with_lse ? static_cast<float*>(c.lse.t.data_ptr()) : nullptr, bytes > 0 ? work.data_ptr() : nullptr,
+                             bytes, stream);
   });
   return rc != ZO_OK ? PyLong_FromLong(rc) : with_others(c.out, {&c.lse});
 }
@@ -456,12 +460,12 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {  // the addresses of the entry points, in this order
-  void* p[9];
-  if (n != 9) {
-    PyErr_SetString(PyExc_TypeError, "nine addresses expected");
+  void* p[10];
+  if (n != 10) {
+    PyErr_SetString(PyExc_TypeError, "ten addresses expected");
     return nullptr;
   }
-  for (int i = 0; i < 9; ++i) {
+  for (int i = 0; i < 10; ++i) {
     p[i] = PyLong_AsVoidPtr(args[i]);
     if (p[i] == nullptr) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no address");
@@ -477,6 +481,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {  // the address
   g_preference_loss = reinterpret_cast<decltype(g_preference_loss)>(p[6]);
   g_policy_work = reinterpret_cast<decltype(g_policy_work)>(p[7]);
   g_preference_work = reinterpret_cast<decltype(g_preference_work)>(p[8]);
+  g_draft_work = reinterpret_cast<decltype(g_draft_work)>(p[9]);
   Py_RETURN_NONE;
 }
 

@@ -91,15 +91,32 @@ struct DraftShared {
   uint16_t node[HB], head[HB];  // of the rows here
 };
 
-// Every thread of the CTA. A block of rows behind the last that sees anything has no keys.
+// A warp with each lane's two masks of a sequence (0 where there is no node): which nodes are seen, how many there are up to the
+// last that sees anything, the keys, and whether there are more than the page table or 32 bits hold, a last tile's end among them.
+struct DraftKeys {
+  uint64_t any;
+  int64_t len;
+  int nodes, bad;
+};
+__device__ __forceinline__ DraftKeys draft_keys(const DraftParams& p, int n, uint64_t a, uint64_t b) {
+  const uint64_t both = a | b;
+  DraftKeys k;
+  k.any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
+          __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
+  const uint32_t high = __ballot_sync(0xFFFFFFFFu, b != 0), low = __ballot_sync(0xFFFFFFFFu, a != 0);
+  k.nodes = 64 - __clzll(static_cast<uint64_t>(high) << 32 | low);
+  k.len = k.any == 0 ? 0 : static_cast<int64_t>(n) + 64 - __clzll(k.any);
+  k.bad = k.len > p.max_pages * p.page_size || (k.len > 0 && p.n_pages == 0) || k.len > 0x7FFFFFFF - 64;
+  return k;
+}
+
+// Every thread of the CTA: sequence b, key-value head g and the block'th HB rows. One behind the last row that sees anything
+// has no keys.
 template <int HB>
-__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t cluster, DraftShared<HB>& sh) {
-  const uint32_t blocks = p.head_blocks, lane = threadIdx.x & 31;
+__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, int b, int g, int block, DraftShared<HB>& sh) {
+  const uint32_t lane = threadIdx.x & 31;
   DraftPlace w;
-  w.b = cluster / (p.kv_heads * blocks);
-  const uint32_t rest = cluster - w.b * (p.kv_heads * blocks);
-  w.g = rest / blocks;
-  w.head0 = (rest - w.g * blocks) * HB;
+  w.b = b, w.g = g, w.head0 = block * HB;
   w.heads = min(HB, p.drafts * p.group - w.head0);
   const int n = p.lengths[w.b];
   if (threadIdx.x < 64) {
@@ -113,16 +130,20 @@ __device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t
     sh.head[h] = static_cast<uint16_t>(w.g * p.group + r - node * p.group);
   }
   __syncthreads();
-  const uint64_t a = sh.masks[lane], b = sh.masks[lane + 32], both = a | b;
-  w.any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
-          __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
-  const uint64_t nodes = static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, b != 0)) << 32 | __ballot_sync(0xFFFFFFFFu, a != 0);
+  const DraftKeys k = draft_keys(p, max(n, 0), sh.masks[lane], sh.masks[lane + 32]);
   w.n = max(n, 0);
-  w.len = w.any == 0 ? 0 : static_cast<int64_t>(w.n) + 64 - __clzll(w.any);
-  w.bad = w.len > p.max_pages * p.page_size || (w.len > 0 && p.n_pages == 0) || w.len > 0x7FFFFFFF - 64;
-  w.live = max(0, min(w.heads, (64 - __clzll(nodes)) * p.group - w.head0));
+  w.any = k.any;
+  w.len = k.len;
+  w.bad = k.bad;
+  w.live = max(0, min(w.heads, k.nodes * p.group - w.head0));
   if (w.bad || w.live == 0) w.len = w.live = 0;
   return w;
+}
+template <int HB>
+__device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t cluster, DraftShared<HB>& sh) {
+  const uint32_t blocks = p.head_blocks, b = cluster / (p.kv_heads * blocks), rest = cluster - b * (p.kv_heads * blocks);
+  const uint32_t g = rest / blocks;
+  return draft_place<HB>(p, b, g, rest - g * blocks, sh);
 }
 
 // Whether key j is one that the tree sees.

@@ -1,6 +1,8 @@
 // zo_draft_wide.cu -- attention of trees of drafted tokens over a paged cache
 // where many rows share a key (zo_attention_draft): tcgen05, 16-bit types, heads
 // of up to 128 elements, vectors aligned to 16 bytes.
+#include <algorithm>
+
 #include "zo_decode.cuh"
 #include "zo_tcgen05.cuh"
 
@@ -23,10 +25,7 @@ struct Plan {
   // Tiles on their way before the oldest is waited for. A tile of values is fetched into the place of one that the products
   // are done with only when the next step's scores are, whose keys have to be known to be there by then: at most kStages - 2.
   static constexpr int kAhead = kSlots == 2 ? (D == 128 ? 5 : 9) : (D == 128 ? 2 : 6);
-  static constexpr int kPitch = D + 4;                  // floats of a row of outputs: rows' vectors on distinct banks
-  static constexpr int kOuts = kBlock * kPitch * 4;
-  static constexpr int kUsed = kSlots * kQueries + kStages * kTile;
-  static constexpr int kBytes = (kUsed > kOuts ? kUsed : kOuts) + 1024;
+  static constexpr int kBytes = kSlots * kQueries + kStages * kTile + 1024;
   static constexpr int kSoftmaxWarps = 4 * kSlots;
   static constexpr int kThreads = 32 * (kSoftmaxWarps + kSlots + kLoaders);
   static constexpr int kColumns = 256 * kSlots;         // of tensor memory
@@ -40,9 +39,8 @@ struct Shared {
   uint64_t full[12], empty[12], s_full[2][2], p_full[2][2], o_done[2][2], drain[2];
   DraftShared<kSlots * kRows> rows;
   uint32_t odd[64][4];  // a node's columns whose value is not finite
-  float top[kSlots * kRows], total[kSlots * kRows];
   uint32_t tmem;
-  int dead, bad, any_odd;
+  int dead, any_odd;
 };
 
 template <typename T>
@@ -51,18 +49,95 @@ __device__ __forceinline__ bool odd16(uint32_t v) {  // infinite or NaN
   return (v & kExponent) == kExponent;
 }
 
-// A CTA has up to 128 kSlots rows of a sequence and key-value head, and its
-// cluster splits the keys: rows are what they are in zo_draft.cu, products and
-// barriers as in zo_attention_mma.cu (a slot's scores of two steps and their
-// weights in tensor memory, a step's scores issued behind the output of the one
-// two before it).
+// The work of all sequences, heads and blocks of rows in a line of steps, cut into as many equal runs as there are CTAs: with
+// runs, unlike clusters, every SM has a CTA and each as many steps (+- 1), whatever the lengths. A CTA takes its run piece by
+// piece, a piece being the steps of one block of rows; one that is not the whole block leaves its unscaled outputs and
+// statistics in the workspace (the first in place 2 i of CTA i, the last in 2 i + 1), and draft_wide_join_kernel puts the
+// pieces together.
+constexpr int kMaxCtas = 304;  // of one slot; of two, half as many
+constexpr int kFewest = 4;     // steps of a CTA
+
+struct WideParams : DraftParams {
+  int64_t batch;
+  int64_t* prefix;   // [batch + 1] steps in front of a sequence
+  int2* shape;       // [batch] steps of a block of rows, blocks that see anything
+  int32_t* bad;      // [batch]
+  float2* stats;     // [2 CTAs][rows of a block] log2 of what the weights are relative to, their sum
+  float* outs;       // [2 CTAs][rows of a block][D]
+  int32_t ctas, block;
+};
+
+// The first step of CTA i (or of none, i = ctas), and the CTA of a step.
+struct Runs {
+  int64_t each, more;  // steps of a CTA; CTAs with one more
+  int ctas;
+  __device__ __forceinline__ Runs(int64_t steps, int most) {
+    ctas = static_cast<int>(min(static_cast<int64_t>(most), (steps + kFewest - 1) / kFewest));
+    each = ctas > 0 ? steps / ctas : 0;
+    more = steps - each * ctas;
+  }
+  __device__ __forceinline__ int64_t first(int64_t i) const { return i * each + min(i, more); }
+  __device__ __forceinline__ int64_t cta(int64_t step) const {
+    return step < more * (each + 1) ? step / (each + 1) : more + (step - more * (each + 1)) / each;
+  }
+};
+
+// The sequences' shapes and the sums of their steps, in one CTA; a warp has a sequence.
+__global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_constant__ WideParams p) {
+  __shared__ int64_t steps[1024];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int64_t before = 0;
+  for (int64_t first = 0; first < p.batch; first += 1024) {
+    const int64_t here = min(static_cast<int64_t>(1024), p.batch - first);
+    for (int64_t i = warp; i < here; i += 32) {
+      const int n = p.lengths[first + i];
+      const auto mask = [&](int node) {
+        return node < p.drafts ? p.masks[(first + i) * p.drafts + node] & (~UINT64_C(0) >> (64 - p.drafts)) : UINT64_C(0);
+      };
+      const uint64_t a = mask(lane), b = mask(lane + 32);
+      const DraftKeys k = draft_keys(p, max(n, 0), n >= 0 ? a : 0, n >= 0 ? b : 0);
+      const int64_t each = k.bad ? 0 : (k.len + kKeys - 1) / kKeys;
+      const int blocks = (k.nodes * p.group + p.block - 1) / p.block;
+      if (lane == 0) {
+        p.shape[first + i] = make_int2(static_cast<int>(each), blocks);
+        p.bad[first + i] = k.bad;
+        steps[i] = each * blocks * p.kv_heads;
+      }
+    }
+    __syncthreads();
+    int64_t mine = tid < here ? steps[tid] : 0, all = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xFFFFFFFFu, all, o);
+      if (lane >= o) all += x;
+    }
+    __syncthreads();
+    if (lane == 31) steps[warp] = all;
+    __syncthreads();
+    int64_t sum = before;
+    for (int i = 0; i < 32; ++i) {
+      if (i < warp) all += steps[i];
+      sum += steps[i];
+    }
+    if (tid < here) p.prefix[first + tid] = before + all - mine;
+    before = sum;
+    __syncthreads();
+  }
+  if (tid == 0) p.prefix[p.batch] = before;
+}
+
+// A block of up to 128 kSlots rows at a time: rows are what they are in zo_draft.cu,
+// products and barriers as in zo_attention_mma.cu (a slot's scores of two steps
+// and their weights in tensor memory, a step's scores issued behind the output
+// of the one two before it).
 //
 //   warps 0-3 (4-7)   softmax of slot 0 (1): a thread has a row; those without a row that sees anything stay out
 //   the next (two)    the products of slot 0 (1)
 //   the last two      keys and values by cp.async, a lane per key's page: any size of page
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
 __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
-    draft_wide_kernel(const __grid_constant__ DraftParams p) {
+    draft_wide_kernel(const __grid_constant__ WideParams p) {
   using L = Plan<D, kSlots>;
   constexpr int kSoftmaxWarps = L::kSoftmaxWarps, kVectors = D / 8;
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
@@ -71,39 +146,62 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   uint8_t* tiles = raw + (1024 - smem_address(raw) % 1024) % 1024;  // the slots' queries, then the stages
   uint8_t* stages = tiles + kSlots * L::kQueries;
   const int tid = threadIdx.x, warp = static_cast<int>(uniform(tid >> 5)), lane = tid & 31;
-  const uint32_t ranks = cluster_size(), rank = cluster_rank();
-  const DraftPlace w = draft_place<L::kBlock>(p, blockIdx.x / ranks, sh.rows);
-  const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
   volatile int* dead = &sh.dead;
-
-  // steps here, and rows up to the last that sees anything
-  const int all = static_cast<int>((w.len + kKeys - 1) / kKeys);
-  const int begin = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
-  const int n = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - begin;
-  const int live = n == 0 ? 0 : w.live;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, L::kColumns);
+  if (tid == 0) sh.dead = 0;
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = uniform(sh.tmem);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Runs runs(p.prefix[p.batch], p.ctas);
+  const int64_t start = blockIdx.x < runs.ctas ? runs.first(blockIdx.x) : 0;
+  const int64_t stop = blockIdx.x < runs.ctas ? runs.first(blockIdx.x + 1) : 0;
+  bool again = false;
+  for (int64_t at_step = start; at_step < stop;) {
+  // the last sequence whose steps begin here or before: by 32 places at a time
+  int64_t b = 0;
+  for (int64_t end = p.batch; end - b > 1;) {
+    const int64_t stride = (end - b + 31) / 32, mine = b + lane * stride;
+    const uint32_t before = __ballot_sync(0xFFFFFFFFu, mine < end && p.prefix[mine] <= at_step);
+    b += (31 - __clz(before)) * stride;
+    end = min(end, b + stride);
+  }
+  const int2 shape = p.shape[b];
+  const int64_t inside = at_step - p.prefix[b];
+  const int unit = static_cast<int>(inside / shape.x), begin = static_cast<int>(inside - static_cast<int64_t>(unit) * shape.x);
+  const int n = static_cast<int>(min(static_cast<int64_t>(shape.x - begin), stop - at_step));
+  const int g = unit / shape.y;
+  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, unit - g * shape.y, sh.rows);
+  const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
+  const int live = w.live;
   const auto warps_of = [&](int s) { return max(0, min(4, (live - s * kRows + 31) / 32)); };
 
   if (tid == L::kThreads - 32) {
     const int slots = (live + kRows - 1) / kRows;
+    const auto barrier = [&](uint64_t* x, int count) {
+      if (again) mbar_inval(x);
+      mbar_init(x, count > 0 ? count : 1);
+    };
     for (int i = 0; i < L::kStages; ++i) {
-      mbar_init(&sh.full[i], kLoaders);
-      mbar_init(&sh.empty[i], slots > 0 ? slots : 1);
+      barrier(&sh.full[i], kLoaders);
+      barrier(&sh.empty[i], slots);
     }
     for (int s = 0; s < kSlots; ++s) {
       for (int b = 0; b < 2; ++b) {
-        mbar_init(&sh.s_full[s][b], 1);
-        mbar_init(&sh.p_full[s][b], warps_of(s) > 0 ? warps_of(s) : 1);
-        mbar_init(&sh.o_done[s][b], 1);
+        barrier(&sh.s_full[s][b], 1);
+        barrier(&sh.p_full[s][b], warps_of(s));
+        barrier(&sh.o_done[s][b], 1);
       }
-      mbar_init(&sh.drain[s], 1);
+      barrier(&sh.drain[s], 1);
     }
-    sh.dead = sh.any_odd = 0;
-    sh.bad = w.bad;
+    sh.any_odd = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  again = true;
   for (int i = tid; i < 64 * 4; i += L::kThreads) (&sh.odd[0][0])[i] = 0;
-  if (warp == kSoftmaxWarps) tmem_alloc(&sh.tmem, L::kColumns);
-  if (warp < kSoftmaxWarps && live > 0) {
+  if (warp < kSoftmaxWarps) {
     // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
     // elements. Rows that are none are zeros.
     const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
@@ -127,10 +225,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     asm volatile("cp.async.wait_all;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  tmem_fence_before();
   __syncthreads();
-  tmem_fence_after();
-  const uint32_t tmem = uniform(sh.tmem);
 
   if (warp >= kSoftmaxWarps + kSlots) {
     // Tile l is step l / 2's keys (even) or values. Each of the two warps has 32 of its keys, a lane one of their places.
@@ -180,7 +275,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     int64_t k_at = -1, v_at = -1;
     bool alive = true;
     int issued = 0;
-    for (int l = 0; l < (live > 0 ? 2 * n : 0) && alive; ++l) {
+    for (int l = 0; l < 2 * n && alive; ++l) {
       if (l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
       if (!alive) break;
       if (l % 2 == 0) {
@@ -207,7 +302,10 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (alive)
       for (int l = max(0, issued - L::kAhead); l < issued; ++l) arrived(l);
-    if (bad) sh.bad = 1;
+    // the barriers are made anew for the next block: every arrival has come before that
+    for (int l = max(0, 2 * n - L::kStages); l < 2 * n && alive; ++l)
+      alive = mbar_wait_warp(&sh.empty[l % L::kStages], l / L::kStages & 1, dead);
+    if (bad) p.bad[w.b] = 1;
   } else if (warp >= kSoftmaxWarps) {
     const int s = warp - kSoftmaxWarps;
     const uint32_t at = uniform(smem_address(stages));
@@ -380,76 +478,201 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.p_full[slot][b]);
     }
-    if (steps > 0 && alive) alive = mbar_wait_warp(&sh.o_done[slot][(steps - 1) & 1], (steps - 1) >> 1 & 1, dead);
-    sh.top[r] = steps > 0 ? base : -kInf;
-    sh.total[r] = steps > 0 ? total : 0.0f;
+    for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
     tmem_fence_after();
-  }
-  __syncthreads();  // the products are done: the outputs take the place of what they read
-  float* outs = reinterpret_cast<float*>(tiles);
-  if (warp < kSoftmaxWarps && warp * 32 < live && sh.dead == 0) {
-    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + L::kOutputs + (warp >> 2) * D;
-    const uint64_t mask = tid < live ? rows.mask(tid) : 0;
+    if (steps > 0 && alive) {
+      const bool whole = n == shape.x, seen = total != 0.0f;
+      const float over = seen ? 1.0f / total : 0.0f;
+      const int64_t place = (2 * static_cast<int64_t>(blockIdx.x) + (at_step > start)) * L::kBlock + r;
+      T* const to = rows.row(r);
+      const bool vectors = reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_load32(o, at + c * 32);
-      tmem_wait_ld(o);
-      if (sh.any_odd) {
-        uint32_t odd = 0;
-        for (int j = 0; j < 64; ++j)
-          if (mask >> j & 1) odd |= sh.odd[j][c];
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tmem_load32(o, out + c * 32);
+        tmem_wait_ld(o);
+        if (sh.any_odd) {
+          uint32_t odd = 0;
+          for (int j = 0; j < 64; ++j)
+            if (mask >> j & 1) odd |= sh.odd[j][c];
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (odd >> e & 1) o[e] = 0x7FC00000u;
+          for (int e = 0; e < 32; ++e)
+            if (odd >> e & 1) o[e] = 0x7FC00000u;
+        }
+        if (!in) continue;
+        if (whole) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = seen ? __uint_as_float(o[e + i]) * over : 0.0f;
+            const uint4 u = Vec<T>::narrow_all(f);
+            if (c * 32 + e >= p.dim) continue;
+            if (vectors) {
+              *reinterpret_cast<uint4*>(to + c * 32 + e) = u;
+            } else {
+              const uint32_t two[4] = {u.x, u.y, u.z, u.w};
+              uint16_t* one = reinterpret_cast<uint16_t*>(to + c * 32 + e);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) one[i] = static_cast<uint16_t>(two[i / 2] >> 16 * (i & 1));
+            }
+          }
+        } else {
+          uint4* part = reinterpret_cast<uint4*>(p.outs + place * D + c * 32);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) part[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
       }
-#pragma unroll
-      for (int e = 0; e < 32; e += 4)
-        *reinterpret_cast<uint4*>(outs + tid * L::kPitch + c * 32 + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      if (in && whole) {
+        if (p.lse != nullptr) *rows.sum(r) = seen ? (base + log2f(total)) * kLn2 : -kInf;
+      } else if (in) {
+        p.stats[place] = make_float2(base, total);
+      }
+      tmem_fence_before();
     }
   }
-  if (tid == 0 && sh.dead != 0) sh.bad = 1;
+  __syncthreads();
+  tmem_fence_after();
+  if (sh.dead != 0) {  // what is left of the run is not formed
+    if (tid == 0) p.bad[w.b] = 1;
+    at_step += n;
+    for (b += 1; b < p.batch && p.prefix[b] < stop; ++b)
+      if (tid == 0) p.bad[b] = 1;
+    break;
+  }
+  at_step += n;
+  }
   tmem_fence_before();
   __syncthreads();
   if (warp == kSoftmaxWarps) {
     tmem_fence_after();
     tmem_free(tmem, L::kColumns);
   }
-  __syncwarp();
-  rows_join<T, D, L::kPitch, L::kThreads>(p, w, rows, outs, sh.top, sh.total, &sh.bad);
+}
+
+// A warp per row: the pieces of its block, if there is more than one; rows that see nothing, and those of sequences whose pages
+// are none.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_constant__ WideParams p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5), per = p.drafts * static_cast<int64_t>(p.heads);
+  const int64_t b = item / per;
+  if (b >= p.batch) return;
+  const int node = static_cast<int>((item - b * per) / p.heads), head = static_cast<int>((item - b * per) % p.heads);
+  const bool sees = p.lengths[b] >= 0 && (p.masks[b * p.drafts + node] & (~UINT64_C(0) >> (64 - p.drafts))) != 0;
+  T* const to = static_cast<T*>(p.out) + b * p.out_token + node * p.out_node + head * p.out_head;
+  float* const lse = p.lse != nullptr ? p.lse + (b * p.drafts + node) * p.heads + head : nullptr;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!sees || p.bad[b] != 0) {
+    for (int d = lane; d < p.dim; d += 32) to[d] = narrow<T>(sees ? NAN : 0.0f);
+    if (lane == 0 && lse != nullptr) *lse = sees ? NAN : -kInf;
+    return;
+  }
+  const int g = head / p.group, r = node * p.group + head - g * p.group, block = r / p.block;
+  const int2 shape = p.shape[b];
+  const Runs runs(p.prefix[p.batch], p.ctas);
+  const int64_t first = p.prefix[b] + (static_cast<int64_t>(g) * shape.y + block) * shape.x;
+  const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
+  if (from == last) return;
+  const auto place = [&](int64_t i) {
+    return (2 * i + (i == from && runs.first(i) < first)) * p.block + r - block * static_cast<int64_t>(p.block);
+  };
+  float top = -kInf, total = 0.0f;
+  for (int64_t i = from + lane; i <= last; i += 32) top = fmaxf(top, p.stats[place(i)].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int64_t i = from; i <= last; ++i) {
+    const int64_t at = place(i);
+    const float2 part = p.stats[at];
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (lane * 4 < D) y = *reinterpret_cast<const float4*>(p.outs + at * D + lane * 4);
+    const float scale = part.x == -kInf ? 0.0f : exp2_approx(part.x - top);
+    total += part.y != part.y ? part.y : part.y * scale;
+    if (part.x > -kInf) x.x = fmaf(y.x, scale, x.x), x.y = fmaf(y.y, scale, x.y), x.z = fmaf(y.z, scale, x.z), x.w = fmaf(y.w, scale, x.w);
+  }
+  const float over = total == 0.0f ? 0.0f : 1.0f / total;
+  const auto value = [&](float f) { return narrow<T>(over == 0.0f ? 0.0f : f * over); };
+  const int d = lane * 4;
+  if (d < p.dim) to[d] = value(x.x);
+  if (d + 1 < p.dim) to[d + 1] = value(x.y);
+  if (d + 2 < p.dim) to[d + 2] = value(x.z);
+  if (d + 3 < p.dim) to[d + 3] = value(x.w);
+  if (lane == 0 && lse != nullptr) *lse = total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+}
+
+template <typename P, typename F>
+cudaError_t launch_behind(F kernel, int64_t grid, int threads, int bytes, cudaStream_t stream, const P& p) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(static_cast<unsigned>(grid));
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = bytes;
+  c.stream = stream;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, p);
 }
 
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
-cudaError_t launch_kind(DraftParams p, int64_t batch, int sms, cudaStream_t stream) {
+cudaError_t launch_kind(const WideParams& p, cudaStream_t stream) {
   using L = Plan<D, kSlots>;
-  p.head_blocks = (p.drafts * p.group + L::kBlock - 1) / L::kBlock;
-  const int64_t items = batch * p.kv_heads * p.head_blocks;
-  const int c = decode_cluster(items, p.max_pages * p.page_size, sms, 6);
-  return launch_decode(draft_wide_kernel<T, D, kSlots, kCap, kBias>, p, items, c, L::kThreads, L::kBytes, stream);
+  const auto kernel = draft_wide_kernel<T, D, kSlots, kCap, kBias>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  if (e != cudaSuccess) return e;
+  draft_wide_plan_kernel<<<1, 1024, 0, stream>>>(p);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = launch_behind(kernel, p.ctas, L::kThreads, L::kBytes, stream, p);
+  const int64_t rows = p.batch * p.drafts * p.heads;
+  return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, (rows + 7) / 8, 256, 0, stream, p);
 }
 
 template <typename T, int D, int kSlots>
-cudaError_t launch_slots(const DraftParams& p, int64_t batch, int sms, cudaStream_t stream) {
+cudaError_t launch_slots(const WideParams& p, cudaStream_t stream) {
   if (p.softcap > 0.0f)
-    return p.slopes != nullptr ? launch_kind<T, D, kSlots, true, true>(p, batch, sms, stream)
-                               : launch_kind<T, D, kSlots, true, false>(p, batch, sms, stream);
-  return p.slopes != nullptr ? launch_kind<T, D, kSlots, false, true>(p, batch, sms, stream)
-                             : launch_kind<T, D, kSlots, false, false>(p, batch, sms, stream);
+    return p.slopes != nullptr ? launch_kind<T, D, kSlots, true, true>(p, stream) : launch_kind<T, D, kSlots, true, false>(p, stream);
+  return p.slopes != nullptr ? launch_kind<T, D, kSlots, false, true>(p, stream) : launch_kind<T, D, kSlots, false, false>(p, stream);
 }
 
 template <typename T>
-cudaError_t launch_head(const DraftParams& p, int64_t batch, int sms, cudaStream_t stream) {
-  const bool two = p.drafts * p.group > kRows;
-  if (p.dim <= 64) return two ? launch_slots<T, 64, 2>(p, batch, sms, stream) : launch_slots<T, 64, 1>(p, batch, sms, stream);
-  return two ? launch_slots<T, 128, 2>(p, batch, sms, stream) : launch_slots<T, 128, 1>(p, batch, sms, stream);
+cudaError_t launch_head(const WideParams& p, cudaStream_t stream) {
+  const bool two = p.block > kRows;
+  if (p.dim <= 64) return two ? launch_slots<T, 64, 2>(p, stream) : launch_slots<T, 64, 1>(p, stream);
+  return two ? launch_slots<T, 128, 2>(p, stream) : launch_slots<T, 128, 1>(p, stream);
 }
+
+// Whether so many rows share a key, of that type and head size: here, if strides, alignment and scale admit it.
+bool wide(int64_t rows, int dim, int dtype) { return dtype != 0 && dim <= 128 && rows > 32; }
+
+constexpr int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 }  // namespace
 
-bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e) {
+int64_t draft_wide_work(int64_t batch, int64_t rows, int dim, int dtype) {
+  if (!wide(rows, dim, dtype)) return 0;
+  const int64_t places = static_cast<int64_t>(2 * kMaxCtas) * kRows;  // two slots: half as many CTAs, twice the rows
+  return up16(8 * (batch + 1)) + up16(8 * batch) + up16(4 * batch) + places * (8 + 4 * (dim <= 64 ? 64 : 128));
+}
+
+bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, void* work, cudaStream_t stream, cudaError_t* e) {
   // The scores' maximum is taken before the scale, and -inf times it has to stay -inf: it is positive
-  if (dtype == 0 || p.dim > 128 || !paged_vectors(p) || !(p.scale > 0.0f) || p.drafts * p.group <= 32) return false;
-  *e = dtype == 1 ? launch_head<__nv_bfloat16>(p, batch, sms, stream) : launch_head<__half>(p, batch, sms, stream);
+  const int64_t rows = static_cast<int64_t>(p.drafts) * p.group;
+  if (!wide(rows, p.dim, dtype) || !paged_vectors(p) || !(p.scale > 0.0f)) return false;
+  WideParams q = {};
+  static_cast<DraftParams&>(q) = p;
+  q.batch = batch;
+  q.block = rows > kRows ? 2 * kRows : kRows;
+  q.ctas = std::min(sms * (rows > kRows ? 1 : 2), kMaxCtas / (rows > kRows ? 2 : 1));
+  char* at = static_cast<char*>(work);
+  q.prefix = reinterpret_cast<int64_t*>(at), at += up16(8 * (batch + 1));
+  q.shape = reinterpret_cast<int2*>(at), at += up16(8 * batch);
+  q.bad = reinterpret_cast<int32_t*>(at), at += up16(4 * batch);
+  q.stats = reinterpret_cast<float2*>(at), at += static_cast<int64_t>(2 * kMaxCtas) * kRows * 8;
+  q.outs = reinterpret_cast<float*>(at);
+  *e = dtype == 1 ? launch_head<__nv_bfloat16>(q, stream) : launch_head<__half>(q, stream);
   return true;
 }
 

@@ -127,7 +127,9 @@ cudaError_t launch_decode_scalar(const DecodeParams& p, int64_t batch, int dtype
 bool launch_decode_mma(const DecodeParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_draft_masks(const int32_t* parents, int64_t batch, int drafts, int64_t* masks, cudaStream_t stream);
 cudaError_t launch_draft_scalar(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream);
-bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
+// For many rows; work: draft_wide_work's bytes on 16 of them (0: not for these).
+int64_t draft_wide_work(int64_t batch, int64_t rows, int dim, int dtype);
+bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, void* work, cudaStream_t stream, cudaError_t* e);
 bool launch_draft_mma(const DraftParams& p, int64_t batch, int dtype, int sms, cudaStream_t stream, cudaError_t* e);
 cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream);
 cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams* g, int dtype, int sms, cudaStream_t stream);

@@ -426,21 +426,30 @@ int zo_draft_masks(const int32_t* parents, int64_t batch, int32_t drafts, int64_
                 "draft_masks_kernel");
 }
 
+int64_t zo_attention_draft_workspace_size(int64_t batch, int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                          int32_t dtype) {
+  if (batch < 0 || batch > kMaxIndex || drafts < 1 || drafts > ZO_MAX_DRAFTS || check_heads(heads, kv_heads, head_dim, dtype) != ZO_OK)
+    return 0;
+  return zo::draft_wide_work(batch, static_cast<int64_t>(drafts) * (heads / kv_heads), head_dim, dtype);
+}
+
 int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, const zo_pages* out, int64_t batch,
                        int32_t drafts, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
                        const int32_t* pages, int64_t pages_stride, int64_t max_pages, int64_t n_pages,
                        int32_t page_size, const int32_t* lengths, const int64_t* masks, float scale, float softcap,
-                       const float* slopes, float* lse, void* stream) {
+                       const float* slopes, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   if (q == nullptr || out == nullptr || drafts < 1 || drafts > ZO_MAX_DRAFTS) return ZO_ERR_ARG;
   zo::DraftParams p = {};
   int sms = 0;
   const int rc = check_paged(q, k, v, out, batch, drafts, heads, kv_heads, head_dim, dtype, pages, pages_stride, max_pages,
                              n_pages, page_size, lengths, masks, scale, softcap, slopes, lse, &p, &sms);
   if (rc != ZO_OK || batch == 0) return rc;
-  if (misaligned(masks, 8)) return ZO_ERR_ALIGN;
+  if (misaligned(masks, 8) || misaligned(workspace, 16)) return ZO_ERR_ALIGN;
+  const int64_t work = zo_attention_draft_workspace_size(batch, drafts, heads, kv_heads, head_dim, dtype);
+  if (work > 0 && (workspace == nullptr || workspace_bytes < work)) return ZO_ERR_WORKSPACE;
   p.masks = masks;
   cudaError_t e = cudaSuccess;
-  if (zo::launch_draft_wide(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
+  if (zo::launch_draft_wide(p, batch, dtype, sms, workspace, static_cast<cudaStream_t>(stream), &e))
     return finish(e, "draft_wide_kernel");
   if (zo::launch_draft_mma(p, batch, dtype, sms, static_cast<cudaStream_t>(stream), &e))
     return finish(e, "draft_mma_kernel");

@@ -44,7 +44,7 @@ import torch
 from . import zo as _zo
 
 EXPORTS = ["zo_rotary_table", "zo_document_spans", "zo_rotate_heads", "zo_attention", "zo_attention_decode",
-           "zo_token_loss_workspace_size", "zo_token_loss", "zo_draft_masks", "zo_attention_draft",
+           "zo_token_loss_workspace_size", "zo_token_loss", "zo_draft_masks", "zo_attention_draft_workspace_size", "zo_attention_draft",
            "zo_policy_loss_workspace_size", "zo_policy_loss", "zo_preference_loss_workspace_size", "zo_preference_loss"]
 MAX_HEAD_DIM = 256
 MAX_HEADS = 1024
@@ -73,7 +73,8 @@ def _lib():
             "zo_token_loss": ([vp, i64, i64, i64, i32, vp, i32, i32, vp, vp, vp, i64, vp], ctypes.c_int),
             "zo_draft_masks": ([vp, i64, i32, vp, vp], ctypes.c_int),
             "zo_attention_draft": ([vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, i64, i64, i64, i32, vp, vp, f32, f32,
-                                    vp, vp, vp], ctypes.c_int),
+                                    vp, vp, vp, i64, vp], ctypes.c_int),
+            "zo_attention_draft_workspace_size": ([i64, i32, i32, i32, i32, i32], i64),
             "zo_policy_loss_workspace_size": ([i64], i64),
             "zo_policy_loss": ([vp, i64, i64, i64, i32, vp, i32, vp, vp, vp, vp, f32, f32, f32, i32, vp, vp, i64, f32, vp, vp,
                                 i64, vp], ctypes.c_int),
@@ -99,7 +100,8 @@ def _binding():
         loader.exec_module(module)
         module.bind(*(ctypes.cast(getattr(_lib(), "zo_" + n), ctypes.c_void_p).value
                       for n in ("rotate_heads", "attention", "attention_decode", "token_loss", "attention_draft", "policy_loss",
-                                "preference_loss", "policy_loss_workspace_size", "preference_loss_workspace_size")))
+                                "preference_loss", "policy_loss_workspace_size", "preference_loss_workspace_size",
+                                "attention_draft_workspace_size")))
         _B = module
     return _B
 

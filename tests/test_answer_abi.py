@@ -39,9 +39,9 @@ def test_draft_masks(L):
 def test_attention_draft(L):
     def call(q=pages(FAR[0], 1024, 128, 64), k=pages(FAR[1], 1024, 64, 64), v=pages(FAR[2], 1024, 64, 64),
              out=pages(FAR[3], 1024, 128, 64), batch=2, drafts=8, heads=2, kv=1, dim=64, dtype=1, table=FAKE, stride=4, most=4, n=9,
-             page=16, lengths=FAKE, masks=FAKE, scale=1.0, cap=0.0, slopes=None, lse=None):
+             page=16, lengths=FAKE, masks=FAKE, scale=1.0, cap=0.0, slopes=None, lse=None, work=FAR[5], wb=1 << 30):
         return L.zo_attention_draft(q, k, v, out, batch, drafts, heads, kv, dim, dtype, table, stride, most, n, page, lengths, masks,
-                                    scale, cap, slopes, lse, None)
+                                    scale, cap, slopes, lse, work, wb, None)
     for bad in ({"q": None}, {"k": None}, {"v": None}, {"out": None}, {"q": pages(0, 1, 1, 1)}, {"k": pages(0, 1, 1, 1)},
                 {"v": pages(FAKE, 1, -1, 1)}, {"q": pages(FAKE, -1, 1, 1)}, {"out": pages(0, 1, 1, 1)}, {"batch": -1}, {"batch": 1 << 26},
                 {"drafts": 0}, {"drafts": 65}, {"heads": 3, "kv": 2}, {"heads": 1025}, {"dim": 300}, {"table": None}, {"stride": -1},
@@ -58,6 +58,10 @@ def test_attention_draft(L):
                 {"lse": FAKE + 2}, {"slopes": FAKE + 1}):
         assert call(**bad) == zo.ZO_ERR_ALIGN, bad
     assert call(batch=0, lengths=None, masks=None) == zo.ZO_OK
+    size = L.zo_attention_draft_workspace_size
+    for few in ((2, 8, 2, 1, 64, 1), (2, 64, 4, 1, 64, 0), (2, 64, 4, 1, 200, 1), (2, 0, 2, 1, 64, 1), (2, 8, 3, 2, 64, 1), (-1, 64, 4, 1, 64, 1)):
+        assert size(*few) == 0, few
+    assert size(2, 64, 4, 1, 64, 1) % 16 == 0 and size(500, 64, 4, 1, 64, 1) > size(2, 64, 4, 1, 64, 1) > 0
 
 
 def test_policy_loss(L):
