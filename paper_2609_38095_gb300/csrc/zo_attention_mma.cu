@@ -6,8 +6,10 @@
 
 namespace zo {
 
-bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
-                   int64_t token_stride, int rows) {
+namespace {
+
+bool encode_map(CUtensorMap* map, bool bf16, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                const cuuint32_t* box) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -19,15 +21,33 @@ bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int head
       f = nullptr;
     return reinterpret_cast<Encode>(f);
   }();
-  if (encode == nullptr) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
-  // a dimension of one element has no stride of its own
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? head_stride * 2 : 16),
-                                 static_cast<cuuint64_t>(tokens > 1 ? token_stride * 2 : 16)};
-  const cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)}, steps[3] = {1, 1, 1};
-  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims,
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
+  return encode != nullptr &&
+         encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(p), dims,
                 strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// a dimension of one element has no stride of its own
+cuuint64_t stride_of(int64_t n, int64_t stride) { return static_cast<cuuint64_t>(n > 1 ? stride * 2 : 16); }
+
+}  // namespace
+
+bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
+                   int64_t token_stride, int rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+  const cuuint64_t strides[2] = {stride_of(heads, head_stride), stride_of(tokens, token_stride)};
+  const cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)};
+  return encode_map(map, bf16, p, 3, dims, strides, box);
+}
+
+bool make_page_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t page_rows, int64_t pages, int64_t head_stride,
+                   int64_t row_stride, int64_t page_stride, int rows) {
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(page_rows),
+                              static_cast<cuuint64_t>(pages)};
+  const cuuint64_t strides[3] = {stride_of(heads, head_stride), stride_of(page_rows, row_stride), stride_of(pages, page_stride)};
+  const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(rows), 1};
+  return encode_map(map, bf16, p, 4, dims, strides, box);
 }
 
 namespace {

@@ -56,29 +56,31 @@ __device__ __forceinline__ bool odd16(uint32_t v) {  // infinite or NaN
 // pieces together.
 constexpr int kMaxCtas = 304;  // of one slot; of two, half as many
 constexpr int kFewest = 4;     // steps of a CTA
+constexpr int kStart = 6;      // what a piece's start and end cost, in steps: a block of rows counts as that many more
 
 struct WideParams : DraftParams {
   int64_t batch;
-  int64_t* prefix;   // [batch + 1] steps in front of a sequence
-  int2* shape;       // [batch] steps of a block of rows, blocks that see anything
+  int64_t* prefix;   // [batch + 1] units in front of a sequence
+  int2* shape;       // [batch] units of a block of rows (kStart and its steps), blocks that see anything
   int32_t* bad;      // [batch]
   float2* stats;     // [2 CTAs][rows of a block] log2 of what the weights are relative to, their sum
   float* outs;       // [2 CTAs][rows of a block][D]
   int32_t ctas, block;
+  int32_t rows_at_once;  // of a page by TMA, 0: none
 };
 
-// The first step of CTA i (or of none, i = ctas), and the CTA of a step.
+// The first unit of CTA i (or of none, i = ctas), and the CTA of a unit.
 struct Runs {
-  int64_t each, more;  // steps of a CTA; CTAs with one more
+  int64_t each, more;  // units of a CTA; CTAs with one more
   int ctas;
-  __device__ __forceinline__ Runs(int64_t steps, int most) {
-    ctas = static_cast<int>(min(static_cast<int64_t>(most), (steps + kFewest - 1) / kFewest));
-    each = ctas > 0 ? steps / ctas : 0;
-    more = steps - each * ctas;
+  __device__ __forceinline__ Runs(int64_t units, int most) {
+    ctas = static_cast<int>(min(static_cast<int64_t>(most), (units + kStart + kFewest - 1) / (kStart + kFewest)));
+    each = ctas > 0 ? units / ctas : 0;
+    more = units - each * ctas;
   }
   __device__ __forceinline__ int64_t first(int64_t i) const { return i * each + min(i, more); }
-  __device__ __forceinline__ int64_t cta(int64_t step) const {
-    return step < more * (each + 1) ? step / (each + 1) : more + (step - more * (each + 1)) / each;
+  __device__ __forceinline__ int64_t cta(int64_t unit) const {
+    return unit < more * (each + 1) ? unit / (each + 1) : more + (unit - more * (each + 1)) / each;
   }
 };
 
@@ -97,7 +99,7 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
       };
       const uint64_t a = mask(lane), b = mask(lane + 32);
       const DraftKeys k = draft_keys(p, max(n, 0), n >= 0 ? a : 0, n >= 0 ? b : 0);
-      const int64_t each = k.bad ? 0 : (k.len + kKeys - 1) / kKeys;
+      const int64_t each = k.bad || k.len == 0 ? 0 : kStart + (k.len + kKeys - 1) / kKeys;
       const int blocks = (k.nodes * p.group + p.block - 1) / p.block;
       if (lane == 0) {
         p.shape[first + i] = make_int2(static_cast<int>(each), blocks);
@@ -134,10 +136,12 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
 //
 //   warps 0-3 (4-7)   softmax of slot 0 (1): a thread has a row; those without a row that sees anything stay out
 //   the next (two)    the products of slot 0 (1)
-//   the last two      keys and values by cp.async, a lane per key's page: any size of page
+//   the last two      keys and values: by TMA, a lane per page, where a step has no key of the tree and pages and steps begin
+//                     together; else by cp.async, a lane per key
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
 __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
-    draft_wide_kernel(const __grid_constant__ WideParams p) {
+    draft_wide_kernel(const __grid_constant__ WideParams p, const __grid_constant__ CUtensorMap k_map,
+                      const __grid_constant__ CUtensorMap v_map) {
   using L = Plan<D, kSlots>;
   constexpr int kSoftmaxWarps = L::kSoftmaxWarps, kVectors = D / 8;
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
@@ -159,21 +163,26 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   const int64_t start = blockIdx.x < runs.ctas ? runs.first(blockIdx.x) : 0;
   const int64_t stop = blockIdx.x < runs.ctas ? runs.first(blockIdx.x + 1) : 0;
   bool again = false;
-  for (int64_t at_step = start; at_step < stop;) {
+  for (int64_t at_unit = start; at_unit < stop;) {
   // the last sequence whose steps begin here or before: by 32 places at a time
   int64_t b = 0;
   for (int64_t end = p.batch; end - b > 1;) {
     const int64_t stride = (end - b + 31) / 32, mine = b + lane * stride;
-    const uint32_t before = __ballot_sync(0xFFFFFFFFu, mine < end && p.prefix[mine] <= at_step);
+    const uint32_t before = __ballot_sync(0xFFFFFFFFu, mine < end && p.prefix[mine] <= at_unit);
     b += (31 - __clz(before)) * stride;
     end = min(end, b + stride);
   }
   const int2 shape = p.shape[b];
-  const int64_t inside = at_step - p.prefix[b];
-  const int unit = static_cast<int>(inside / shape.x), begin = static_cast<int>(inside - static_cast<int64_t>(unit) * shape.x);
-  const int n = static_cast<int>(min(static_cast<int64_t>(shape.x - begin), stop - at_step));
-  const int g = unit / shape.y;
-  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, unit - g * shape.y, sh.rows);
+  const int64_t inside = at_unit - p.prefix[b];
+  const int item = static_cast<int>(inside / shape.x), from = static_cast<int>(inside - static_cast<int64_t>(item) * shape.x);
+  const int units = static_cast<int>(min(static_cast<int64_t>(shape.x - from), stop - at_unit));
+  const int begin = max(0, from - kStart), n = max(0, from + units - kStart) - begin;  // the block's steps here
+  if (n == 0) {
+    at_unit += units;
+    continue;
+  }
+  const int g = item / shape.y;
+  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.y, sh.rows);
   const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
   const int live = w.live;
   const auto warps_of = [&](int s) { return max(0, min(4, (live - s * kRows + 31) / 32)); };
@@ -271,37 +280,76 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.full[l % L::kStages]);
     };
-    int id = look(0);
+    // by TMA: a lane has rows_at_once keys of the step
+    const int boxes = p.rows_at_once > 0 ? kKeys / p.rows_at_once : 0;
+    const auto whole = [&](int step) { return boxes > 0 && static_cast<int64_t>(begin + step + 1) * kKeys <= w.n; };
+    const auto look_page = [&](int step) {
+      const int64_t j = static_cast<int64_t>(begin + step) * kKeys + lane * p.rows_at_once;
+      return lane < boxes && j < w.n ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+    };
+    const auto look_ahead = [&](int step) { return whole(step) ? look_page(step) : look(step); };
+    int id = look_ahead(0), box_page = 0, box_row = 0;
     int64_t k_at = -1, v_at = -1;
     bool alive = true;
     int issued = 0;
     for (int l = 0; l < 2 * n && alive; ++l) {
       if (l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
       if (!alive) break;
+      const bool tiled = whole(l / 2);
       if (l % 2 == 0) {
-        const int64_t j = key_of(l / 2);
-        const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
-        k_at = key.x >= 0 ? (key.x * p.k_page + key.y * p.k_token) * 2 : -1;
-        v_at = key.x >= 0 ? (key.x * p.v_page + key.y * p.v_token) * 2 : -1;
-        id = look(l / 2 + 1);
+        if (tiled) {
+          const uint32_t j = static_cast<uint32_t>(begin + l / 2) * kKeys + lane * p.rows_at_once;
+          box_page = id;
+          box_row = static_cast<int>(j - decode_page(p, j) * static_cast<uint32_t>(p.page_size));
+          if (lane < boxes && (id < 0 || id >= p.n_pages)) bad = 1;  // (and zeros come)
+        } else {
+          const int64_t j = key_of(l / 2);
+          const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
+          k_at = key.x >= 0 ? (key.x * p.k_page + key.y * p.k_token) * 2 : -1;
+          v_at = key.x >= 0 ? (key.x * p.v_page + key.y * p.v_token) * 2 : -1;
+        }
+        id = look_ahead(l / 2 + 1);
       }
+      if (tiled) {  // one of the two warps has the keys, the other the values
+        uint64_t* const full = &sh.full[l % L::kStages];
+        if (lane == 0) {
+          if (half == l % 2) mbar_expect(full, L::kTile);
+          else mbar_arrive(full);
+        }
+        __syncwarp();
+        if (half == l % 2 && lane < boxes) {
+          uint8_t* const to = stages + l % L::kStages * L::kTile + lane * p.rows_at_once * 128;
 #pragma unroll
-      for (int i = 0; i < 32 / kAtOnce; ++i) {
-        const int64_t at = __shfl_sync(0xFFFFFFFFu, l % 2 == 0 ? k_at : v_at, i * kAtOnce + lane / kVectors);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_address(place_of(l, i))),
-                     "l"((l % 2 == 0 ? kl : vl) + (at >= 0 ? at : 0)), "r"(at >= 0 ? bytes : 0)
-                     : "memory");
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_4d(to + c * L::kTileChunk, l % 2 == 0 ? &k_map : &v_map, c * 64, w.g, box_row, box_page, full);
+        }
+        __syncwarp();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+          const int64_t at = __shfl_sync(0xFFFFFFFFu, l % 2 == 0 ? k_at : v_at, i * kAtOnce + lane / kVectors);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_address(place_of(l, i))),
+                       "l"((l % 2 == 0 ? kl : vl) + (at >= 0 ? at : 0)), "r"(at >= 0 ? bytes : 0)
+                       : "memory");
+        }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
       ++issued;
       if (l >= L::kAhead) {
         asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
-        arrived(l - L::kAhead);
+        if (!whole((l - L::kAhead) / 2)) arrived(l - L::kAhead);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (alive)
-      for (int l = max(0, issued - L::kAhead); l < issued; ++l) arrived(l);
+      for (int l = max(0, issued - L::kAhead); l < issued; ++l)
+        if (!whole(l / 2)) arrived(l);
+    if (lane == 0 && *dead) {  // nothing may land in shared memory after the CTA is gone
+      const long long start = clock64();
+      for (int l = max(0, issued - L::kStages); l < issued; ++l)
+        while (whole(l / 2) && !mbar_try(&sh.full[l % L::kStages], l / L::kStages & 1) && clock64() - start < kWaitCycles) {}
+    }
+    __syncwarp();
     // the barriers are made anew for the next block: every arrival has come before that
     for (int l = max(0, 2 * n - L::kStages); l < 2 * n && alive; ++l)
       alive = mbar_wait_warp(&sh.empty[l % L::kStages], l / L::kStages & 1, dead);
@@ -481,9 +529,9 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
     tmem_fence_after();
     if (steps > 0 && alive) {
-      const bool whole = n == shape.x, seen = total != 0.0f;
+      const bool whole = n == shape.x - kStart, seen = total != 0.0f;
       const float over = seen ? 1.0f / total : 0.0f;
-      const int64_t place = (2 * static_cast<int64_t>(blockIdx.x) + (at_step > start)) * L::kBlock + r;
+      const int64_t place = (2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start)) * L::kBlock + r;
       T* const to = rows.row(r);
       const bool vectors = reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
@@ -535,12 +583,12 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   tmem_fence_after();
   if (sh.dead != 0) {  // what is left of the run is not formed
     if (tid == 0) p.bad[w.b] = 1;
-    at_step += n;
+    at_unit += units;
     for (b += 1; b < p.batch && p.prefix[b] < stop; ++b)
       if (tid == 0) p.bad[b] = 1;
     break;
   }
-  at_step += n;
+  at_unit += units;
   }
   tmem_fence_before();
   __syncthreads();
@@ -573,17 +621,24 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
   const Runs runs(p.prefix[p.batch], p.ctas);
   const int64_t first = p.prefix[b] + (static_cast<int64_t>(g) * shape.y + block) * shape.x;
   const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
-  if (from == last) return;
+  // a CTA's steps of the block: it may have no more than a part of what the block counts beyond them
+  const auto steps_of = [&](int64_t i) {
+    const int64_t end = min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)) - kStart, begin = runs.first(i) - first - kStart;
+    return max(end, static_cast<int64_t>(0)) - max(begin, static_cast<int64_t>(0));
+  };
+  if (steps_of(last) == shape.x - kStart) return;  // (the last one's are never none)
   const auto place = [&](int64_t i) {
     return (2 * i + (i == from && runs.first(i) < first)) * p.block + r - block * static_cast<int64_t>(p.block);
   };
   float top = -kInf, total = 0.0f;
-  for (int64_t i = from + lane; i <= last; i += 32) top = fmaxf(top, p.stats[place(i)].x);
+  for (int64_t i = from + lane; i <= last; i += 32)
+    if (steps_of(i) > 0) top = fmaxf(top, p.stats[place(i)].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
   for (int64_t i = from; i <= last; ++i) {
+    if (steps_of(i) == 0) continue;
     const int64_t at = place(i);
     const float2 part = p.stats[at];
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -602,8 +657,8 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
   if (lane == 0 && lse != nullptr) *lse = total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
 }
 
-template <typename P, typename F>
-cudaError_t launch_behind(F kernel, int64_t grid, int threads, int bytes, cudaStream_t stream, const P& p) {
+template <typename F, typename... A>
+cudaError_t launch_behind(F kernel, int64_t grid, int threads, int bytes, cudaStream_t stream, const A&... a) {
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
@@ -614,20 +669,28 @@ cudaError_t launch_behind(F kernel, int64_t grid, int threads, int bytes, cudaSt
   c.stream = stream;
   c.attrs = &attr;
   c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, kernel, p);
+  return cudaLaunchKernelEx(&c, kernel, a...);
 }
 
 template <typename T, int D, int kSlots, bool kCap, bool kBias>
-cudaError_t launch_kind(const WideParams& p, cudaStream_t stream) {
+cudaError_t launch_kind(WideParams p, cudaStream_t stream) {
   using L = Plan<D, kSlots>;
   const auto kernel = draft_wide_kernel<T, D, kSlots, kCap, kBias>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (e != cudaSuccess) return e;
+  // pages that hold whole steps, or of which a step holds whole ones, by 8 rows (the swizzle's) at least
+  CUtensorMap k_map = {}, v_map = {};
+  constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+  const bool fits = p.page_size % kKeys == 0 || (p.page_size >= 8 && kKeys % p.page_size == 0);
+  const int rows = std::min(p.page_size, kKeys);
+  if (fits && make_page_map(&k_map, kBf16, p.k, p.dim, p.kv_heads, p.page_size, p.n_pages, p.k_head, p.k_token, p.k_page, rows) &&
+      make_page_map(&v_map, kBf16, p.v, p.dim, p.kv_heads, p.page_size, p.n_pages, p.v_head, p.v_token, p.v_page, rows))
+    p.rows_at_once = rows;
   draft_wide_plan_kernel<<<1, 1024, 0, stream>>>(p);
   e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_behind(kernel, p.ctas, L::kThreads, L::kBytes, stream, p);
-  const int64_t rows = p.batch * p.drafts * p.heads;
-  return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, (rows + 7) / 8, 256, 0, stream, p);
+  if (e == cudaSuccess) e = launch_behind(kernel, p.ctas, L::kThreads, L::kBytes, stream, p, k_map, v_map);
+  const int64_t all = p.batch * p.drafts * p.heads;
+  return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, (all + 7) / 8, 256, 0, stream, p);
 }
 
 template <typename T, int D, int kSlots>

@@ -84,6 +84,14 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_address(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_address(bar))
+      : "memory");
+}
+
 // From shared memory; what lies beyond the tensor is not written. tma_stored: the thread's stores have been read from
 // shared memory (kRead) or are done.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
@@ -196,5 +204,8 @@ __device__ __forceinline__ void tie32(uint32_t (&v)[32]) {
 // last are read as zeros. False if the strides admit none.
 bool make_head_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t tokens, int64_t head_stride,
                    int64_t token_stride, int rows);
+// The same of a paged cache: boxes of 64 elements x 1 head x `rows` rows of a page x 1 page.
+bool make_page_map(CUtensorMap* map, bool bf16, const void* p, int dim, int heads, int64_t page_rows, int64_t pages, int64_t head_stride,
+                   int64_t row_stride, int64_t page_stride, int rows);
 
 }  // namespace zo
