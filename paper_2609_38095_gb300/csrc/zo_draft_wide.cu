@@ -49,6 +49,11 @@ __device__ __forceinline__ bool odd16(uint32_t v) {  // infinite or NaN
   return (v & kExponent) == kExponent;
 }
 
+template <typename T>
+__device__ __forceinline__ bool odd32(uint32_t v) {  // either of two values
+  return odd16<T>(v) || odd16<T>(v >> 16);
+}
+
 // The work of all sequences, heads and blocks of rows in a line of steps, cut into as many equal runs as there are CTAs: with
 // runs, unlike clusters, every SM has a CTA and each as many steps (+- 1), whatever the lengths. A CTA takes its run piece by
 // piece, a piece being the steps of one block of rows; one that is not the whole block leaves its unscaled outputs and
@@ -56,7 +61,7 @@ __device__ __forceinline__ bool odd16(uint32_t v) {  // infinite or NaN
 // pieces together.
 constexpr int kMaxCtas = 304;  // of one slot; of two, half as many
 constexpr int kFewest = 4;     // steps of a CTA
-constexpr int kStart = 6;      // what a piece's start and end cost, in steps: a block of rows counts as that many more
+constexpr int kStart = 10;      // what a piece's start and end cost, in steps: a block of rows counts as that many more
 
 struct WideParams : DraftParams {
   int64_t batch;
@@ -64,7 +69,7 @@ struct WideParams : DraftParams {
   int2* shape;       // [batch] units of a block of rows (kStart and its steps), blocks that see anything
   int32_t* bad;      // [batch]
   float2* stats;     // [2 CTAs][rows of a block] log2 of what the weights are relative to, their sum
-  float* outs;       // [2 CTAs][rows of a block][D]
+  float4* outs;      // [2 CTAs][D / 4][rows of a block]: neighbouring rows' columns together, as threads have them
   int32_t ctas, block;
   int32_t rows_at_once;  // of a page by TMA, 0: none
 };
@@ -262,10 +267,12 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         if (key0 + kKeys > w.n) {
           // Values of the tree's keys that are not finite are noted and taken out: a row that does not see one has the
           // weight 0 there, and 0 times it is NaN.
+#pragma unroll 4
           for (int i = 0; i < 32 / kAtOnce; ++i) {
             const int64_t node = key0 + half * 32 + i * kAtOnce + lane / kVectors - w.n;
             uint16_t* x = reinterpret_cast<uint16_t*>(place_of(l, i));
-            if (node < 0 || node >= 64) continue;
+            const uint4 u = *reinterpret_cast<const uint4*>(x);
+            if (node < 0 || node >= 64 || !(odd32<T>(u.x) || odd32<T>(u.y) || odd32<T>(u.z) || odd32<T>(u.w))) continue;
             for (int e = 0; e < 8; ++e)
               if (odd16<T>(x[e])) {
                 const int column = vector * 8 + e;
@@ -531,7 +538,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     if (steps > 0 && alive) {
       const bool whole = n == shape.x - kStart, seen = total != 0.0f;
       const float over = seen ? 1.0f / total : 0.0f;
-      const int64_t place = (2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start)) * L::kBlock + r;
+      const int64_t place_of_cta = 2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start);
       T* const to = rows.row(r);
       const bool vectors = reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
@@ -566,15 +573,17 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
             }
           }
         } else {
-          uint4* part = reinterpret_cast<uint4*>(p.outs + place * D + c * 32);
+          float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + r;
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) part[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int e = 0; e < 32; e += 4)
+            part[e / 4 * L::kBlock] = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
+                                                  __uint_as_float(o[e + 3]));
         }
       }
       if (in && whole) {
         if (p.lse != nullptr) *rows.sum(r) = seen ? (base + log2f(total)) * kLn2 : -kInf;
       } else if (in) {
-        p.stats[place] = make_float2(base, total);
+        p.stats[place_of_cta * L::kBlock + r] = make_float2(base, total);
       }
       tmem_fence_before();
     }
@@ -598,63 +607,98 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   }
 }
 
-// A warp per row: the pieces of its block, if there is more than one; rows that see nothing, and those of sequences whose pages
-// are none.
+// 32 rows of a block, a lane per row: the pieces of their block, if there is more than one; rows that see nothing, and those of
+// sequences whose pages are none. Warps share the columns, and the rows leave through shared memory.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_constant__ WideParams p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5), per = p.drafts * static_cast<int64_t>(p.heads);
-  const int64_t b = item / per;
-  if (b >= p.batch) return;
-  const int node = static_cast<int>((item - b * per) / p.heads), head = static_cast<int>((item - b * per) % p.heads);
-  const bool sees = p.lengths[b] >= 0 && (p.masks[b * p.drafts + node] & (~UINT64_C(0) >> (64 - p.drafts))) != 0;
-  T* const to = static_cast<T*>(p.out) + b * p.out_token + node * p.out_node + head * p.out_head;
-  float* const lse = p.lse != nullptr ? p.lse + (b * p.drafts + node) * p.heads + head : nullptr;
+  constexpr int kWarps = 8, kMine = D / 4 / kWarps;  // a warp's vectors of 4 columns
+  constexpr int kPitch = D + 8;                      // 16-bit elements of a row
+  __shared__ __align__(16) T tile[32 * kPitch];
+  __shared__ int64_t to_row[32];  // where its elements go, -1: nowhere
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t chunks = p.block / 32, rows = p.drafts * p.group, blocks = (rows + p.block - 1) / p.block;
+  const uint32_t item = blockIdx.x / chunks, chunk = blockIdx.x - item * chunks;
+  const uint32_t head_block = item / blocks, block = item - head_block * blocks;
+  const uint32_t b = head_block / p.kv_heads, g = head_block - b * p.kv_heads;
+  const uint32_t in_block = chunk * 32 + lane, r = block * p.block + in_block;
+  if (block * p.block + chunk * 32 >= rows) return;
+  const bool in = r < rows;
+  const uint32_t node = (in ? r : rows - 1) / p.group, head = g * p.group + (in ? r : rows - 1) - node * p.group;
+  const uint64_t mask = p.masks[static_cast<int64_t>(b) * p.drafts + node] & (~UINT64_C(0) >> (64 - p.drafts));
+  const bool sees = p.lengths[b] >= 0 && mask != 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (!sees || p.bad[b] != 0) {
-    for (int d = lane; d < p.dim; d += 32) to[d] = narrow<T>(sees ? NAN : 0.0f);
-    if (lane == 0 && lse != nullptr) *lse = sees ? NAN : -kInf;
-    return;
-  }
-  const int g = head / p.group, r = node * p.group + head - g * p.group, block = r / p.block;
   const int2 shape = p.shape[b];
-  const Runs runs(p.prefix[p.batch], p.ctas);
-  const int64_t first = p.prefix[b] + (static_cast<int64_t>(g) * shape.y + block) * shape.x;
-  const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
-  // a CTA's steps of the block: it may have no more than a part of what the block counts beyond them
-  const auto steps_of = [&](int64_t i) {
-    const int64_t end = min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)) - kStart, begin = runs.first(i) - first - kStart;
-    return max(end, static_cast<int64_t>(0)) - max(begin, static_cast<int64_t>(0));
-  };
-  if (steps_of(last) == shape.x - kStart) return;  // (the last one's are never none)
-  const auto place = [&](int64_t i) {
-    return (2 * i + (i == from && runs.first(i) < first)) * p.block + r - block * static_cast<int64_t>(p.block);
-  };
+  const int64_t before = p.prefix[b], all = p.prefix[p.batch];
+  const bool bad = p.bad[b] != 0;
   float top = -kInf, total = 0.0f;
-  for (int64_t i = from + lane; i <= last; i += 32)
-    if (steps_of(i) > 0) top = fmaxf(top, p.stats[place(i)].x);
+  float4 x[kMine];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int64_t i = from; i <= last; ++i) {
-    if (steps_of(i) == 0) continue;
-    const int64_t at = place(i);
-    const float2 part = p.stats[at];
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (lane * 4 < D) y = *reinterpret_cast<const float4*>(p.outs + at * D + lane * 4);
-    const float scale = part.x == -kInf ? 0.0f : exp2_approx(part.x - top);
-    total += part.y != part.y ? part.y : part.y * scale;
-    if (part.x > -kInf) x.x = fmaf(y.x, scale, x.x), x.y = fmaf(y.y, scale, x.y), x.z = fmaf(y.z, scale, x.z), x.w = fmaf(y.w, scale, x.w);
+  for (int k = 0; k < kMine; ++k) x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  bool whole = false;
+  if (shape.x > 0 && static_cast<int>(block) < shape.y && !bad) {
+    const Runs runs(all, p.ctas);
+    const int64_t first = before + (static_cast<int64_t>(g) * shape.y + block) * shape.x;
+    const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
+    // a CTA's steps of the block: it may have no more than a part of what the block counts beyond them
+    const auto steps_of = [&](int64_t i) {
+      const int64_t end = min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)) - kStart, begin = runs.first(i) - first - kStart;
+      return max(end, static_cast<int64_t>(0)) - max(begin, static_cast<int64_t>(0));
+    };
+    whole = steps_of(last) == shape.x - kStart;  // (the last one's are never none)
+    if (!whole) {
+      const auto place = [&](int64_t i) { return 2 * i + (i == from && runs.first(i) < first); };
+      for (int64_t i = from; i <= last; ++i)
+        if (steps_of(i) > 0) top = fmaxf(top, p.stats[place(i) * p.block + in_block].x);
+#pragma unroll 2
+      for (int64_t i = from; i <= last; ++i) {
+        if (steps_of(i) == 0) continue;
+        const float2 part = p.stats[place(i) * p.block + in_block];
+        const float4* outs = p.outs + (place(i) * (D / 4) + warp) * p.block + in_block;
+        float4 y[kMine];
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) y[k] = outs[k * kWarps * p.block];
+        const float scale = part.x == -kInf ? 0.0f : exp2_approx(part.x - top);
+        total += part.y != part.y ? part.y : part.y * scale;
+        if (part.x > -kInf) {
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) {
+            x[k].x = fmaf(y[k].x, scale, x[k].x), x[k].y = fmaf(y[k].y, scale, x[k].y);
+            x[k].z = fmaf(y[k].z, scale, x[k].z), x[k].w = fmaf(y[k].w, scale, x[k].w);
+          }
+        }
+      }
+    }
   }
-  const float over = total == 0.0f ? 0.0f : 1.0f / total;
-  const auto value = [&](float f) { return narrow<T>(over == 0.0f ? 0.0f : f * over); };
-  const int d = lane * 4;
-  if (d < p.dim) to[d] = value(x.x);
-  if (d + 1 < p.dim) to[d + 1] = value(x.y);
-  if (d + 2 < p.dim) to[d + 2] = value(x.z);
-  if (d + 3 < p.dim) to[d + 3] = value(x.w);
-  if (lane == 0 && lse != nullptr) *lse = total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+  if (!sees) total = 0.0f;
+  const float over = sees && bad ? NAN : total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const float f[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+    uint2 two;
+    two.x = narrow2<T>(over == 0.0f ? 0.0f : f[0] * over, over == 0.0f ? 0.0f : f[1] * over);
+    two.y = narrow2<T>(over == 0.0f ? 0.0f : f[2] * over, over == 0.0f ? 0.0f : f[3] * over);
+    *reinterpret_cast<uint2*>(tile + lane * kPitch + (warp + k * kWarps) * 4) = two;
+  }
+  if (warp == 0) {
+    const bool writes = in && !(whole && sees);  // a whole block's rows are written
+    to_row[lane] = writes ? b * p.out_token + node * p.out_node + head * p.out_head : -1;
+    if (writes && p.lse != nullptr)
+      p.lse[(static_cast<int64_t>(b) * p.drafts + node) * p.heads + head] =
+          sees && bad ? NAN : total == 0.0f ? -kInf : (top + log2f(total)) * kLn2;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * (D / 8); i += 256) {
+    const int row = i / (D / 8), d = i % (D / 8) * 8;
+    if (to_row[row] < 0 || d >= p.dim) continue;
+    T* to = static_cast<T*>(p.out) + to_row[row] + d;
+    const T* from = tile + row * kPitch + d;
+    if (reinterpret_cast<uintptr_t>(to) % 16 == 0) {
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) to[e] = from[e];
+    }
+  }
 }
 
 template <typename F, typename... A>
@@ -689,8 +733,9 @@ cudaError_t launch_kind(WideParams p, cudaStream_t stream) {
   draft_wide_plan_kernel<<<1, 1024, 0, stream>>>(p);
   e = cudaGetLastError();
   if (e == cudaSuccess) e = launch_behind(kernel, p.ctas, L::kThreads, L::kBytes, stream, p, k_map, v_map);
-  const int64_t all = p.batch * p.drafts * p.heads;
-  return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, (all + 7) / 8, 256, 0, stream, p);
+  const int64_t blocks = (static_cast<int64_t>(p.drafts) * p.group + p.block - 1) / p.block;
+  const int64_t chunks = p.batch * p.kv_heads * blocks * (p.block / 32);
+  return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, chunks, 256, 0, stream, p);
 }
 
 template <typename T, int D, int kSlots>
@@ -734,7 +779,7 @@ bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, 
   q.shape = reinterpret_cast<int2*>(at), at += up16(8 * batch);
   q.bad = reinterpret_cast<int32_t*>(at), at += up16(4 * batch);
   q.stats = reinterpret_cast<float2*>(at), at += static_cast<int64_t>(2 * kMaxCtas) * kRows * 8;
-  q.outs = reinterpret_cast<float*>(at);
+  q.outs = reinterpret_cast<float4*>(at);
   *e = dtype == 1 ? launch_head<__nv_bfloat16>(q, stream) : launch_head<__half>(q, stream);
   return true;
 }
