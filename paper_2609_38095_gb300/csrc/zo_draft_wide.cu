@@ -60,13 +60,20 @@ __device__ __forceinline__ bool odd32(uint32_t v) {  // either of two values
 // statistics in the workspace (the first in place 2 i of CTA i, the last in 2 i + 1), and draft_wide_join_kernel puts the
 // pieces together.
 constexpr int kMaxCtas = 304;  // of one slot; of two, half as many
-constexpr int kFewest = 4;     // steps of a CTA
-constexpr int kStart = 10;      // what a piece's start and end cost, in steps: a block of rows counts as that many more
+constexpr int kFewest = 110;   // units of a CTA
+constexpr int kStart = 120;    // units that a piece's start and end cost (10 us); a block of rows counts as that many more
+// Units of a step, measured at 0.08 us each: up to 64 rows are bound by HBM, more by their softmax.
+__device__ __forceinline__ int units_of_step(int rows) { return rows > 128 ? 11 : rows > 64 ? 10 : 8; }
+
+// Steps that lie wholly in front of a unit of a block of rows.
+__device__ __forceinline__ int steps_before(int64_t unit, int per_step) {
+  return unit <= kStart ? 0 : static_cast<int>(static_cast<uint32_t>(unit - kStart) / static_cast<uint32_t>(per_step));
+}
 
 struct WideParams : DraftParams {
   int64_t batch;
   int64_t* prefix;   // [batch + 1] units in front of a sequence
-  int2* shape;       // [batch] units of a block of rows (kStart and its steps), blocks that see anything
+  int4* shape;       // [batch] units of a block of rows (kStart and its steps'), steps, units of a step, blocks that see anything
   int32_t* bad;      // [batch]
   float2* stats;     // [2 CTAs][rows of a block] log2 of what the weights are relative to, their sum
   float4* outs;      // [2 CTAs][D / 4][rows of a block]: neighbouring rows' columns together, as threads have them
@@ -79,7 +86,7 @@ struct Runs {
   int64_t each, more;  // units of a CTA; CTAs with one more
   int ctas;
   __device__ __forceinline__ Runs(int64_t units, int most) {
-    ctas = static_cast<int>(min(static_cast<int64_t>(most), (units + kStart + kFewest - 1) / (kStart + kFewest)));
+    ctas = static_cast<int>(min(static_cast<int64_t>(most), (units + kFewest - 1) / kFewest));
     each = ctas > 0 ? units / ctas : 0;
     more = units - each * ctas;
   }
@@ -104,10 +111,11 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
       };
       const uint64_t a = mask(lane), b = mask(lane + 32);
       const DraftKeys k = draft_keys(p, max(n, 0), n >= 0 ? a : 0, n >= 0 ? b : 0);
-      const int64_t each = k.bad || k.len == 0 ? 0 : kStart + (k.len + kKeys - 1) / kKeys;
+      const int count = k.bad ? 0 : static_cast<int>((k.len + kKeys - 1) / kKeys), per_step = units_of_step(min(k.nodes * p.group, p.block));
+      const int64_t each = count == 0 ? 0 : kStart + count * static_cast<int64_t>(per_step);
       const int blocks = (k.nodes * p.group + p.block - 1) / p.block;
       if (lane == 0) {
-        p.shape[first + i] = make_int2(static_cast<int>(each), blocks);
+        p.shape[first + i] = make_int4(static_cast<int>(each), count, per_step, blocks);
         p.bad[first + i] = k.bad;
         steps[i] = each * blocks * p.kv_heads;
       }
@@ -177,17 +185,17 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     b += (31 - __clz(before)) * stride;
     end = min(end, b + stride);
   }
-  const int2 shape = p.shape[b];
+  const int4 shape = p.shape[b];
   const int64_t inside = at_unit - p.prefix[b];
   const int item = static_cast<int>(inside / shape.x), from = static_cast<int>(inside - static_cast<int64_t>(item) * shape.x);
   const int units = static_cast<int>(min(static_cast<int64_t>(shape.x - from), stop - at_unit));
-  const int begin = max(0, from - kStart), n = max(0, from + units - kStart) - begin;  // the block's steps here
+  const int begin = steps_before(from, shape.z), n = steps_before(from + static_cast<int64_t>(units), shape.z) - begin;
   if (n == 0) {
     at_unit += units;
     continue;
   }
-  const int g = item / shape.y;
-  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.y, sh.rows);
+  const int g = item / shape.w;
+  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.w, sh.rows);
   const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
   const int live = w.live;
   const auto warps_of = [&](int s) { return max(0, min(4, (live - s * kRows + 31) / 32)); };
@@ -214,31 +222,9 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   again = true;
+  // the warps of the softmax and the products; the loads need not wait for the queries
+  const auto queries_there = [] { asm volatile("bar.sync 1, %0;" ::"n"((kSoftmaxWarps + kSlots) * 32) : "memory"); };
   for (int i = tid; i < 64 * 4; i += L::kThreads) (&sh.odd[0][0])[i] = 0;
-  if (warp < kSoftmaxWarps) {
-    // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
-    // elements. Rows that are none are zeros.
-    const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
-    for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
-      const int r = i / kVectors, v = i % kVectors;
-      uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (r < live && v * 8 < p.dim) {
-        const T* q = rows.query(r) + v * 8;
-        if (whole) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
-          continue;
-        } else {
-          const uint16_t* u = reinterpret_cast<const uint16_t*>(q);
-          const auto two = [&](int e) { return u[e] | static_cast<uint32_t>(u[e + 1]) << 16; };
-          x = make_uint4(two(0), two(2), two(4), two(6));
-        }
-      }
-      *reinterpret_cast<uint4*>(to) = x;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
   __syncthreads();
 
   if (warp >= kSoftmaxWarps + kSlots) {
@@ -380,6 +366,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       mma_commit(&sh.empty[stage]);
     };
     const auto there = [&](int l) { return mbar_wait_warp(&sh.full[l % L::kStages], l / L::kStages & 1, dead); };
+    queries_there();
     bool alive = true;
     for (int i = 0; i < min(2, mine) && alive; ++i) {
       alive = there(2 * i);
@@ -413,6 +400,29 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     }
     __syncwarp();
   } else {
+    // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
+    // elements. Rows that are none are zeros.
+    const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
+    for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
+      const int r = i / kVectors, v = i % kVectors;
+      uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (r < live && v * 8 < p.dim) {
+        const T* q = rows.query(r) + v * 8;
+        if (whole) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
+          continue;
+        } else {
+          const uint16_t* u = reinterpret_cast<const uint16_t*>(q);
+          const auto two = [&](int e) { return u[e] | static_cast<uint32_t>(u[e + 1]) << 16; };
+          x = make_uint4(two(0), two(2), two(4), two(6));
+        }
+      }
+      *reinterpret_cast<uint4*>(to) = x;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    queries_there();
     const int slot = warp >> 2, r = tid;  // the thread's row
     const bool in = r < live;
     const uint64_t mask = in ? rows.mask(r) : 0;
@@ -536,7 +546,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
     tmem_fence_after();
     if (steps > 0 && alive) {
-      const bool whole = n == shape.x - kStart, seen = total != 0.0f;
+      const bool whole = n == shape.y, seen = total != 0.0f;
       const float over = seen ? 1.0f / total : 0.0f;
       const int64_t place_of_cta = 2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start);
       T* const to = rows.row(r);
@@ -627,7 +637,7 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
   const uint64_t mask = p.masks[static_cast<int64_t>(b) * p.drafts + node] & (~UINT64_C(0) >> (64 - p.drafts));
   const bool sees = p.lengths[b] >= 0 && mask != 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int2 shape = p.shape[b];
+  const int4 shape = p.shape[b];
   const int64_t before = p.prefix[b], all = p.prefix[p.batch];
   const bool bad = p.bad[b] != 0;
   float top = -kInf, total = 0.0f;
@@ -635,16 +645,14 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
 #pragma unroll
   for (int k = 0; k < kMine; ++k) x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   bool whole = false;
-  if (shape.x > 0 && static_cast<int>(block) < shape.y && !bad) {
+  if (shape.x > 0 && static_cast<int>(block) < shape.w && !bad) {
     const Runs runs(all, p.ctas);
-    const int64_t first = before + (static_cast<int64_t>(g) * shape.y + block) * shape.x;
+    const int64_t first = before + (static_cast<int64_t>(g) * shape.w + block) * shape.x;
     const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
-    // a CTA's steps of the block: it may have no more than a part of what the block counts beyond them
-    const auto steps_of = [&](int64_t i) {
-      const int64_t end = min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)) - kStart, begin = runs.first(i) - first - kStart;
-      return max(end, static_cast<int64_t>(0)) - max(begin, static_cast<int64_t>(0));
+    const auto steps_of = [&](int64_t i) {  // a CTA's of the block: it may have units of it but no step
+      return steps_before(min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)), shape.z) - steps_before(runs.first(i) - first, shape.z);
     };
-    whole = steps_of(last) == shape.x - kStart;  // (the last one's are never none)
+    for (int64_t i = from; i <= last && !whole; ++i) whole = steps_of(i) == shape.y;
     if (!whole) {
       const auto place = [&](int64_t i) { return 2 * i + (i == from && runs.first(i) < first); };
       for (int64_t i = from; i <= last; ++i)
@@ -762,7 +770,7 @@ constexpr int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 int64_t draft_wide_work(int64_t batch, int64_t rows, int dim, int dtype) {
   if (!wide(rows, dim, dtype)) return 0;
   const int64_t places = static_cast<int64_t>(2 * kMaxCtas) * kRows;  // two slots: half as many CTAs, twice the rows
-  return up16(8 * (batch + 1)) + up16(8 * batch) + up16(4 * batch) + places * (8 + 4 * (dim <= 64 ? 64 : 128));
+  return up16(8 * (batch + 1)) + 16 * batch + up16(4 * batch) + places * (8 + 4 * (dim <= 64 ? 64 : 128));
 }
 
 bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, void* work, cudaStream_t stream, cudaError_t* e) {
@@ -776,7 +784,7 @@ bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, 
   q.ctas = std::min(sms * (rows > kRows ? 1 : 2), kMaxCtas / (rows > kRows ? 2 : 1));
   char* at = static_cast<char*>(work);
   q.prefix = reinterpret_cast<int64_t*>(at), at += up16(8 * (batch + 1));
-  q.shape = reinterpret_cast<int2*>(at), at += up16(8 * batch);
+  q.shape = reinterpret_cast<int4*>(at), at += 16 * batch;
   q.bad = reinterpret_cast<int32_t*>(at), at += up16(4 * batch);
   q.stats = reinterpret_cast<float2*>(at), at += static_cast<int64_t>(2 * kMaxCtas) * kRows * 8;
   q.outs = reinterpret_cast<float4*>(at);
