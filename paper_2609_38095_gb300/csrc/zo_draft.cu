@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
 #pragma unroll
           for (int c = 0; c < 4; c += 2) {
             float* const y = &s[m][n][c];
-            if (near) {
+            if (__builtin_expect(near, 1)) {
               const uint64_t two = capped_near(pack2(y[0], y[1]), pack2(scale2, scale2), pack2(cap2, cap2));
               y[0] = low2(two), y[1] = high2(two);
             } else {
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
 #pragma unroll
           for (int c = 0; c < 4; ++c) s[m][n][c] *= scale2;
     }
-    if (nodes) {
+    if (__builtin_expect(nodes, 0)) {
       const int from = static_cast<int>(key0 - w.n) + lane % 4 * 2;  // the thread's first key, from the tree's first
 #pragma unroll
       for (int n = 0; n < 2 * kDeep; ++n)
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
 #pragma unroll
           for (int c = 0; c < 4; ++c) acc[m][n][c] *= back[m][c >> 1];
     }
-    if (nodes) {
+    if (__builtin_expect(nodes, 0)) {
       // Values of the tree's keys that are not finite: a row that sees one has NaN in its column, for the others (whose
       // weight is 0, and 0 times it is NaN) it is taken out.
       uint4* const v = reinterpret_cast<uint4*>(smem + warp * L::kWarp + stage * L::kStage + L::kKeys * L::kRow);

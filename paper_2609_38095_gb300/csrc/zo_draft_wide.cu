@@ -39,9 +39,13 @@ struct Shared {
   uint64_t full[12], empty[12], s_full[2][2], p_full[2][2], o_done[2][2], drain[2];
   DraftShared<kSlots * kRows> rows;
   uint32_t odd[64][4];  // a node's columns whose value is not finite
+  float2 part[kRows];   // the copies' statistics
   uint32_t tmem;
   int dead, any_odd;
 };
+
+// A copy's output in the joint one's units; one that has seen nothing has none.
+__device__ __forceinline__ float times_scale(uint32_t o, float scale) { return scale == 0.0f ? 0.0f : __uint_as_float(o) * scale; }
 
 template <typename T>
 __device__ __forceinline__ bool odd16(uint32_t v) {  // infinite or NaN
@@ -142,6 +146,9 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
   if (tid == 0) p.prefix[p.batch] = before;
 }
 
+// With up to 32 or 64 rows, which would leave three warps or two of a slot's four without any, the rows are there four times
+// or twice, in lanes of their own, and each copy takes its part of every step's keys: its weights for the others are zero.
+//
 // A block of up to 128 kSlots rows at a time: rows are what they are in zo_draft.cu,
 // products and barriers as in zo_attention_mma.cu (a slot's scores of two steps
 // and their weights in tensor memory, a step's scores issued behind the output
@@ -151,12 +158,14 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
 //   the next (two)    the products of slot 0 (1)
 //   the last two      keys and values: by TMA, a lane per page, where a step has no key of the tree and pages and steps begin
 //                     together; else by cp.async, a lane per key
-template <typename T, int D, int kSlots, bool kCap, bool kBias>
+template <typename T, int D, int kSlots, int kCopies, bool kPlain>
 __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     draft_wide_kernel(const __grid_constant__ WideParams p, const __grid_constant__ CUtensorMap k_map,
                       const __grid_constant__ CUtensorMap v_map) {
   using L = Plan<D, kSlots>;
   constexpr int kSoftmaxWarps = L::kSoftmaxWarps, kVectors = D / 8;
+  constexpr int kSpan = L::kBlock / kCopies, kColumns = kKeys / kCopies;  // rows of a copy, a step's keys that are its own
+  static_assert(kSlots == 1 || kCopies == 1, "");
   constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
   extern __shared__ uint8_t raw[];
   __shared__ Shared<kSlots> sh;
@@ -198,7 +207,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.w, sh.rows);
   const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
   const int live = w.live;
-  const auto warps_of = [&](int s) { return max(0, min(4, (live - s * kRows + 31) / 32)); };
+  const auto warps_of = [&](int s) { return kCopies > 1 ? kCopies * ((live + 31) / 32) : max(0, min(4, (live - s * kRows + 31) / 32)); };
 
   if (tid == L::kThreads - 32) {
     const int slots = (live + kRows - 1) / kRows;
@@ -223,6 +232,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   }
   again = true;
   // the warps of the softmax and the products; the loads need not wait for the queries
+  const auto softmax_warps = [] { asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory"); };
   const auto queries_there = [] { asm volatile("bar.sync 1, %0;" ::"n"((kSoftmaxWarps + kSlots) * 32) : "memory"); };
   for (int i = tid; i < 64 * 4; i += L::kThreads) (&sh.odd[0][0])[i] = 0;
   __syncthreads();
@@ -273,15 +283,16 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.full[l % L::kStages]);
     };
-    // by TMA: a lane has rows_at_once keys of the step
-    const int boxes = p.rows_at_once > 0 ? kKeys / p.rows_at_once : 0;
+    // by TMA: a box of rows_at_once keys of a page; lanes hold the pages of as many steps as there is room for, and of the next as
+    // many (a page looked up a step ahead would be waited for: 1.0 us of a step of 64 x 64 elements, which takes 0.7)
+    const int boxes = p.rows_at_once > 0 ? kKeys / p.rows_at_once : 0, held = boxes > 0 ? 32 / boxes : 1;
     const auto whole = [&](int step) { return boxes > 0 && static_cast<int64_t>(begin + step + 1) * kKeys <= w.n; };
-    const auto look_page = [&](int step) {
+    const auto look_pages = [&](int step) {
       const int64_t j = static_cast<int64_t>(begin + step) * kKeys + lane * p.rows_at_once;
-      return lane < boxes && j < w.n ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+      return boxes > 0 && j < w.n ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
     };
-    const auto look_ahead = [&](int step) { return whole(step) ? look_page(step) : look(step); };
-    int id = look_ahead(0), box_page = 0, box_row = 0;
+    int ids = look_pages(0), next_ids = look_pages(held), at_id = 0;
+    int id = whole(0) ? 0 : look(0), box_page = 0, box_row = 0;
     int64_t k_at = -1, v_at = -1;
     bool alive = true;
     int issued = 0;
@@ -292,16 +303,21 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       if (l % 2 == 0) {
         if (tiled) {
           const uint32_t j = static_cast<uint32_t>(begin + l / 2) * kKeys + lane * p.rows_at_once;
-          box_page = id;
+          box_page = __shfl_sync(0xFFFFFFFFu, ids, (at_id * boxes + lane) & 31);
           box_row = static_cast<int>(j - decode_page(p, j) * static_cast<uint32_t>(p.page_size));
-          if (lane < boxes && (id < 0 || id >= p.n_pages)) bad = 1;  // (and zeros come)
+          if (lane < boxes && (box_page < 0 || box_page >= p.n_pages)) bad = 1;  // (and zeros come)
+          if (++at_id == held) {
+            at_id = 0;
+            ids = next_ids;
+            next_ids = look_pages(l / 2 + 1 + held);
+          }
         } else {
           const int64_t j = key_of(l / 2);
           const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
           k_at = key.x >= 0 ? (key.x * p.k_page + key.y * p.k_token) * 2 : -1;
           v_at = key.x >= 0 ? (key.x * p.v_page + key.y * p.v_token) * 2 : -1;
         }
-        id = look_ahead(l / 2 + 1);
+        if (!whole(l / 2 + 1)) id = look(l / 2 + 1);
       }
       if (tiled) {  // one of the two warps has the keys, the other the values
         uint64_t* const full = &sh.full[l % L::kStages];
@@ -401,14 +417,14 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     __syncwarp();
   } else {
     // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
-    // elements. Rows that are none are zeros.
+    // elements, a copy behind another. Rows that are none are zeros.
     const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
     for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
       const int r = i / kVectors, v = i % kVectors;
       uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
       uint4 x = make_uint4(0, 0, 0, 0);
-      if (r < live && v * 8 < p.dim) {
-        const T* q = rows.query(r) + v * 8;
+      if (r % kSpan < live && v * 8 < p.dim) {
+        const T* q = rows.query(r % kSpan) + v * 8;
         if (whole) {
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
           continue;
@@ -423,14 +439,14 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     asm volatile("cp.async.wait_all;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     queries_there();
-    const int slot = warp >> 2, r = tid;  // the thread's row
-    const bool in = r < live;
+    const int slot = warp >> 2, r = tid % kSpan, copy = kCopies > 1 ? warp / (4 / kCopies) : 0;  // the thread's row
+    const bool in = r < live, cap = !kPlain && p.softcap > 0.0f, bias = !kPlain && p.slopes != nullptr;
     const uint64_t mask = in ? rows.mask(r) : 0;
     const int depth = __popcll(mask) - 1;
     const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + L::kOutputs + slot * D;
-    const float scale2 = kCap ? p.scale / p.softcap : p.scale * kLog2e;
-    const float cap2 = p.softcap * kLog2e, slope2 = kBias && in ? p.slopes[rows.head(r)] * kLog2e : 0.0f;
-    const int steps = warp * 32 < live ? n : 0;
+    const float scale2 = cap ? p.scale / p.softcap : p.scale * kLog2e;
+    const float cap2 = p.softcap * kLog2e, slope2 = bias && in ? p.slopes[rows.head(r)] * kLog2e : 0.0f;
+    const int steps = warp * 32 % kSpan < live ? n : 0;
     float base = -kInf, total = 0.0f;  // log2 of what the weights are relative to, and their sum
     bool alive = true;
     for (int c = 0; c < steps; ++c) {
@@ -439,71 +455,74 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       alive = mbar_wait_warp(&sh.s_full[slot][b], c >> 1 & 1, dead);
       if (!alive) break;
       tmem_fence_after();
-      uint32_t x[2][32];
-      tmem_load32(x[0], scores);
-      tmem_load32(x[1], scores + 32);
-      tmem_wait_ld(x[0]);
-      tie32(x[1]);
-      const int64_t key0 = static_cast<int64_t>(begin + c) * kKeys;
-      const bool nodes = key0 + kKeys > w.n;  // keys of the tree, or beyond the last
-      if (kCap) {
-        float far = 0.0f;
+      constexpr int kWidth = kColumns < 32 ? kColumns : 32;
+      uint32_t x[kColumns / kWidth][kWidth];
+      if constexpr (kWidth == 16) {
+        tmem_load16_wait(x[0], scores + copy * kColumns);
+      } else {
+        tmem_load32(x[0], scores + copy * kColumns);
+        if constexpr (kColumns == 64) tmem_load32(x[1], scores + 32);
+        tmem_wait_ld(x[0]);
+        if constexpr (kColumns == 64) tie32(x[1]);
+      }
+      const auto score = [&](int e) -> uint32_t& { return x[e / kWidth][e % kWidth]; };
+      const int key0 = (begin + c) * kKeys + copy * kColumns;  // (the last step's end is below 2^31)
+      const bool nodes = key0 + kColumns > w.n;  // keys of the tree, or beyond the last
+      if (cap) {
+        float fars[4] = {};
 #pragma unroll
-        for (int e = 0; e < 64; ++e) far = fmaxf(far, fabsf(__uint_as_float(x[e / 32][e % 32])));
-        if (__all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap)) {
+        for (int e = 0; e < kColumns; ++e) fars[e % 4] = fmaxf(fars[e % 4], fabsf(__uint_as_float(score(e))));
+        const float far = fmaxf(fmaxf(fars[0], fars[1]), fmaxf(fars[2], fars[3]));
+        if (__builtin_expect(__all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap), 1)) {
           const uint64_t over2 = pack2(scale2, scale2), caps = pack2(cap2, cap2);
 #pragma unroll
-          for (int e = 0; e < 64; e += 2) {
-            uint32_t* two = &x[e / 32][e % 32];
-            const uint64_t y = capped_near(static_cast<uint64_t>(two[1]) << 32 | two[0], over2, caps);
-            two[0] = static_cast<uint32_t>(y), two[1] = static_cast<uint32_t>(y >> 32);
+          for (int e = 0; e < kColumns; e += 2) {
+            const uint64_t y = capped_near(static_cast<uint64_t>(score(e + 1)) << 32 | score(e), over2, caps);
+            score(e) = static_cast<uint32_t>(y), score(e + 1) = static_cast<uint32_t>(y >> 32);
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 64; ++e)
-            x[e / 32][e % 32] = __float_as_uint(capped(__uint_as_float(x[e / 32][e % 32]), scale2, cap2));
+          for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(capped(__uint_as_float(score(e)), scale2, cap2));
         }
-      }
-      if (kBias) {
-        const float times = kCap ? 1.0f : scale2;
-        const float away = static_cast<float>(w.n + depth - key0);  // exact, and its differences, below 2^24
-        if (!nodes) {
+      } else if (!kPlain) {
 #pragma unroll
-          for (int e = 0; e < 64; ++e)
-            x[e / 32][e % 32] = __float_as_uint(__uint_as_float(x[e / 32][e % 32]) * times - slope2 * (away - e));
+        for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(__uint_as_float(score(e)) * scale2);
+      }
+      if (bias) {
+        const float away = static_cast<float>(w.n - key0 + depth);  // exact, and its differences, below 2^24
+        if (__builtin_expect(!nodes, 1)) {
+#pragma unroll
+          for (int e = 0; e < kColumns; ++e)
+            score(e) = __float_as_uint(fmaf(-slope2, away - static_cast<float>(e), __uint_as_float(score(e))));
         } else {
 #pragma unroll
-          for (int e = 0; e < 64; ++e) {
-            const int64_t node = key0 + e - w.n;
+          for (int e = 0; e < kColumns; ++e) {
+            const int node = key0 - w.n + e;
             const float far = node < 0 ? away - e : node < 64 ? fabsf(static_cast<float>(depth + 1 - __popcll(sh.rows.masks[node]))) : 0.0f;
-            x[e / 32][e % 32] = __float_as_uint(__uint_as_float(x[e / 32][e % 32]) * times - slope2 * far);
+            score(e) = __float_as_uint(fmaf(-slope2, far, __uint_as_float(score(e))));
           }
         }
       }
-      if (nodes || __any_sync(0xFFFFFFFFu, mask == 0)) {
-        const int64_t ahead = w.n - key0;  // the step's first keys that are not the tree's
+      if (__builtin_expect(nodes || __any_sync(0xFFFFFFFFu, mask == 0), 0)) {
+        const int ahead = w.n - key0;  // the columns' first keys that are not the tree's
         uint64_t seen = mask == 0 || ahead <= 0 ? 0 : ahead >= 64 ? ~UINT64_C(0) : (UINT64_C(1) << ahead) - 1;
         if (ahead < 64 && ahead > -64) seen |= ahead >= 0 ? mask << ahead : mask >> -ahead;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kColumns / kWidth; ++h) {
           const uint32_t bits = static_cast<uint32_t>(seen >> 32 * h);
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
+          for (int e = 0; e < kWidth; ++e)
             if (!(bits >> e & 1)) x[h][e] = __float_as_uint(-kInf);
         }
       }
       float most[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        most[e] = __uint_as_float(x[e / 2][e % 2 * 16]);
-#pragma unroll
-        for (int i = 1; i < 16; ++i) most[e] = fmaxf(most[e], __uint_as_float(x[e / 2][e % 2 * 16 + i]));
-      }
+      for (int e = 0; e < kColumns; ++e) most[e % 4] = e < 4 ? __uint_as_float(score(e)) : fmaxf(most[e % 4], __uint_as_float(score(e)));
       float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-      if (!kCap && !kBias) top *= scale2;
+      if (kPlain) top *= scale2;
       top -= kLift<T>;
       const bool moved = base > -kInf && top > base + kSlack;
-      if (__any_sync(0xFFFFFFFFu, moved)) {
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, moved), 0)) {
         const float back = moved ? exp2_approx(base - top) : 1.0f;
         total *= back;
         alive = mbar_wait_warp(&sh.o_done[slot][b ^ 1], (c - 1) >> 1 & 1, dead);  // the step before is in the output
@@ -520,21 +539,26 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       }
       if (moved || base == -kInf) base = top;
       const float shift = base == -kInf ? 0.0f : -base;
-      const float times = kCap || kBias ? 1.0f : scale2;
+      const float times = kPlain ? scale2 : 1.0f;
       const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
       uint64_t sums[2] = {0, 0};
+      uint32_t weights[kColumns / 2];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t weights[16];
+      for (int i = 0; i < kColumns / 2; ++i) {
+        const uint64_t t = fma2(pack2(__uint_as_float(score(2 * i)), __uint_as_float(score(2 * i + 1))), times2, shift2);
+        const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
+        sums[i & 1] = add2(sums[i & 1], pack2(u, v));
+        weights[i] = narrow2<T>(u, v);
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {  // the other copies' keys weigh nothing here
+        uint32_t all[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const uint64_t t =
-              fma2(pack2(__uint_as_float(x[half][2 * i]), __uint_as_float(x[half][2 * i + 1])), times2, shift2);
-          const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
-          sums[i & 1] = add2(sums[i & 1], pack2(u, v));
-          weights[i] = narrow2<T>(u, v);
+          constexpr int kMine = kColumns / 2;
+          all[i] = kCopies == 1 || (half * 16 + i) / kMine == copy ? weights[(half * 16 + i) % kMine] : 0;
         }
-        tmem_store16(scores + half * 16, weights);
+        tmem_store16(scores + half * 16, all);
       }
       const uint64_t sum = add2(sums[0], sums[1]);
       total += low2(sum) + high2(sum);
@@ -545,7 +569,38 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     }
     for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
     tmem_fence_after();
-    if (steps > 0 && alive) {
+    float scale = 1.0f;  // of a copy's outputs
+    float* const gathered = reinterpret_cast<float*>(stages);  // the copies' behind the first, in place of keys and values
+    constexpr int kPitch = D + 4;
+    if constexpr (kCopies > 1) {  // the copies' statistics, then their outputs, as one
+      sh.part[tid] = make_float2(base, total);
+      softmax_warps();
+      float most = -kInf, all = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kCopies; ++k) most = fmaxf(most, sh.part[k * kSpan + r].x);
+#pragma unroll
+      for (int k = 0; k < kCopies; ++k) {
+        const float2 part = sh.part[k * kSpan + r];
+        all += part.y != part.y ? part.y : part.x == -kInf ? 0.0f : part.y * exp2_approx(part.x - most);
+      }
+      scale = base == -kInf ? 0.0f : exp2_approx(base - most);
+      base = most, total = all;
+      if (copy > 0 && steps > 0 && alive) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_load32(o, out + c * 32);
+          tmem_wait_ld(o);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4*>(gathered + ((copy - 1) * kSpan + r) * kPitch + c * 32 + e) =
+                make_float4(times_scale(o[e], scale), times_scale(o[e + 1], scale), times_scale(o[e + 2], scale), times_scale(o[e + 3], scale));
+        }
+        tmem_fence_before();
+      }
+      softmax_warps();
+    }
+    if (steps > 0 && alive && copy == 0) {
       const bool whole = n == shape.y, seen = total != 0.0f;
       const float over = seen ? 1.0f / total : 0.0f;
       const int64_t place_of_cta = 2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start);
@@ -556,6 +611,19 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         uint32_t o[32];
         tmem_load32(o, out + c * 32);
         tmem_wait_ld(o);
+        if constexpr (kCopies > 1) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            float y[4] = {times_scale(o[e], scale), times_scale(o[e + 1], scale), times_scale(o[e + 2], scale), times_scale(o[e + 3], scale)};
+#pragma unroll
+            for (int k = 0; k < kCopies - 1; ++k) {
+              const float4 z = *reinterpret_cast<const float4*>(gathered + (k * kSpan + r) * kPitch + c * 32 + e);
+              y[0] += z.x, y[1] += z.y, y[2] += z.z, y[3] += z.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[e + i] = __float_as_uint(y[i]);
+          }
+        }
         if (sh.any_odd) {
           uint32_t odd = 0;
           for (int j = 0; j < 64; ++j)
@@ -583,7 +651,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
             }
           }
         } else {
-          float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + r;
+          float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + tid;
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
             part[e / 4 * L::kBlock] = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
@@ -593,10 +661,11 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       if (in && whole) {
         if (p.lse != nullptr) *rows.sum(r) = seen ? (base + log2f(total)) * kLn2 : -kInf;
       } else if (in) {
-        p.stats[place_of_cta * L::kBlock + r] = make_float2(base, total);
+        p.stats[place_of_cta * L::kBlock + tid] = make_float2(base, total);
       }
       tmem_fence_before();
     }
+    if constexpr (kCopies > 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // TMA's turn
   }
   __syncthreads();
   tmem_fence_after();
@@ -648,30 +717,46 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
   if (shape.x > 0 && static_cast<int>(block) < shape.w && !bad) {
     const Runs runs(all, p.ctas);
     const int64_t first = before + (static_cast<int64_t>(g) * shape.w + block) * shape.x;
-    const int64_t from = runs.cta(first), last = runs.cta(first + shape.x - 1);
-    const auto steps_of = [&](int64_t i) {  // a CTA's of the block: it may have units of it but no step
-      return steps_before(min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)), shape.z) - steps_before(runs.first(i) - first, shape.z);
-    };
-    for (int64_t i = from; i <= last && !whole; ++i) whole = steps_of(i) == shape.y;
+    int64_t from = runs.cta(first);
+    const int64_t last = runs.cta(first + shape.x - 1);
+    const auto end_of = [&](int64_t i) { return min(runs.first(i + 1) - first, static_cast<int64_t>(shape.x)); };
+    const bool split = from < last && runs.first(from) < first;  // the first CTA's is not its first piece
+    const int64_t from_first = from;
+    while (from < last && steps_before(end_of(from), shape.z) == 0) ++from;  // CTAs with units of the block but no step
+    whole = from == last;
     if (!whole) {
-      const auto place = [&](int64_t i) { return 2 * i + (i == from && runs.first(i) < first); };
-      for (int64_t i = from; i <= last; ++i)
-        if (steps_of(i) > 0) top = fmaxf(top, p.stats[place(i) * p.block + in_block].x);
-#pragma unroll 2
-      for (int64_t i = from; i <= last; ++i) {
-        if (steps_of(i) == 0) continue;
-        const float2 part = p.stats[place(i) * p.block + in_block];
-        const float4* outs = p.outs + (place(i) * (D / 4) + warp) * p.block + in_block;
-        float4 y[kMine];
+      const auto place = [&](int64_t i) { return 2 * i + (split && i == from_first); };
+      constexpr int kAtOnce = 4;
+      for (int64_t i0 = from; i0 <= last; i0 += kAtOnce) {
+        float2 part[kAtOnce];
+        float4 y[kAtOnce][kMine];
 #pragma unroll
-        for (int k = 0; k < kMine; ++k) y[k] = outs[k * kWarps * p.block];
-        const float scale = part.x == -kInf ? 0.0f : exp2_approx(part.x - top);
-        total += part.y != part.y ? part.y : part.y * scale;
-        if (part.x > -kInf) {
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int64_t at = place(min(i0 + k, last));
+          part[k] = p.stats[at * p.block + in_block];
+          const float4* outs = p.outs + (at * (D / 4) + warp) * p.block + in_block;
 #pragma unroll
-          for (int k = 0; k < kMine; ++k) {
-            x[k].x = fmaf(y[k].x, scale, x[k].x), x[k].y = fmaf(y[k].y, scale, x[k].y);
-            x[k].z = fmaf(y[k].z, scale, x[k].z), x[k].w = fmaf(y[k].w, scale, x[k].w);
+          for (int m = 0; m < kMine; ++m) y[k][m] = outs[m * kWarps * p.block];
+          if (i0 + k > last) part[k] = make_float2(-kInf, 0.0f);
+        }
+        float most = top;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) most = fmaxf(most, part[k].x);
+        const float back = top == -kInf ? 0.0f : exp2_approx(top - most);
+        top = most;
+        total *= back;  // (a NaN stays one)
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) x[m].x *= back, x[m].y *= back, x[m].z *= back, x[m].w *= back;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const float scale = part[k].x == -kInf ? 0.0f : exp2_approx(part[k].x - top);
+          total += part[k].y != part[k].y ? part[k].y : part[k].y * scale;
+          if (part[k].x > -kInf) {
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) {
+              x[m].x = fmaf(y[k][m].x, scale, x[m].x), x[m].y = fmaf(y[k][m].y, scale, x[m].y);
+              x[m].z = fmaf(y[k][m].z, scale, x[m].z), x[m].w = fmaf(y[k][m].w, scale, x[m].w);
+            }
           }
         }
       }
@@ -724,10 +809,10 @@ cudaError_t launch_behind(F kernel, int64_t grid, int threads, int bytes, cudaSt
   return cudaLaunchKernelEx(&c, kernel, a...);
 }
 
-template <typename T, int D, int kSlots, bool kCap, bool kBias>
+template <typename T, int D, int kSlots, int kCopies, bool kPlain>
 cudaError_t launch_kind(WideParams p, cudaStream_t stream) {
   using L = Plan<D, kSlots>;
-  const auto kernel = draft_wide_kernel<T, D, kSlots, kCap, kBias>;
+  const auto kernel = draft_wide_kernel<T, D, kSlots, kCopies, kPlain>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (e != cudaSuccess) return e;
   // pages that hold whole steps, or of which a step holds whole ones, by 8 rows (the swizzle's) at least
@@ -746,22 +831,35 @@ cudaError_t launch_kind(WideParams p, cudaStream_t stream) {
   return e != cudaSuccess ? e : launch_behind(draft_wide_join_kernel<T, D>, chunks, 256, 0, stream, p);
 }
 
-template <typename T, int D, int kSlots>
-cudaError_t launch_slots(const WideParams& p, cudaStream_t stream) {
-  if (p.softcap > 0.0f)
-    return p.slopes != nullptr ? launch_kind<T, D, kSlots, true, true>(p, stream) : launch_kind<T, D, kSlots, true, false>(p, stream);
-  return p.slopes != nullptr ? launch_kind<T, D, kSlots, false, true>(p, stream) : launch_kind<T, D, kSlots, false, false>(p, stream);
+template <typename T, int D, int kSlots, int kCopies>
+cudaError_t launch_rows(const WideParams& p, cudaStream_t stream) {
+  return p.softcap > 0.0f || p.slopes != nullptr ? launch_kind<T, D, kSlots, kCopies, false>(p, stream)
+                                                 : launch_kind<T, D, kSlots, kCopies, true>(p, stream);
+}
+
+template <typename T, int D>
+cudaError_t launch_size(const WideParams& p, cudaStream_t stream) {
+  const int64_t rows = static_cast<int64_t>(p.drafts) * p.group;
+  if (rows > kRows) return launch_rows<T, D, 2, 1>(p, stream);
+  if (rows > 64) return launch_rows<T, D, 1, 1>(p, stream);
+  return rows > 32 ? launch_rows<T, D, 1, 2>(p, stream) : launch_rows<T, D, 1, 4>(p, stream);
 }
 
 template <typename T>
 cudaError_t launch_head(const WideParams& p, cudaStream_t stream) {
-  const bool two = p.block > kRows;
-  if (p.dim <= 64) return two ? launch_slots<T, 64, 2>(p, stream) : launch_slots<T, 64, 1>(p, stream);
-  return two ? launch_slots<T, 128, 2>(p, stream) : launch_slots<T, 128, 1>(p, stream);
+  return p.dim <= 64 ? launch_size<T, 64>(p, stream) : launch_size<T, 128>(p, stream);
 }
 
-// Whether so many rows share a key, of that type and head size: here, if strides, alignment and scale admit it.
-bool wide(int64_t rows, int dim, int dtype) { return dtype != 0 && dim <= 128 && rows > 32; }
+// What can be taken here, if strides, alignment and scale admit it: more than 16 rows, 16-bit types.
+bool wide(int64_t rows, int dim, int dtype) { return dtype != 0 && dim <= 128 && rows > 16; }
+
+// Whether it is: three launches and the pieces' way through memory take 27 us at least, where draft_mma_kernel begins at 13 but
+// reads every key once per 32 rows. By the most keys that the page table holds, times blocks of 32 rows and the head size, 20e6
+// (32 / 8 heads of 128; rows, sequences of up to so many keys, this kernel / that one, us: 32, 8 x 1000, 33 / 23; 32, 8 x 4000,
+// 40 / 45; 96, 8 x 1000, 33 / 36; 256, 1 x 1000, 31 / 25; 256, 1 x 8000, 36 / 85; 256, 8 x 4000, 48 / 149).
+bool worth(const DraftParams& p, int64_t batch, int64_t rows) {
+  return static_cast<double>(batch) * p.kv_heads * p.max_pages * p.page_size * ((rows + 31) / 32) * (p.dim <= 64 ? 64 : 128) > 20e6;
+}
 
 constexpr int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
@@ -776,7 +874,7 @@ int64_t draft_wide_work(int64_t batch, int64_t rows, int dim, int dtype) {
 bool launch_draft_wide(const DraftParams& p, int64_t batch, int dtype, int sms, void* work, cudaStream_t stream, cudaError_t* e) {
   // The scores' maximum is taken before the scale, and -inf times it has to stay -inf: it is positive
   const int64_t rows = static_cast<int64_t>(p.drafts) * p.group;
-  if (!wide(rows, p.dim, dtype) || !paged_vectors(p) || !(p.scale > 0.0f)) return false;
+  if (!wide(rows, p.dim, dtype) || !worth(p, batch, rows) || !paged_vectors(p) || !(p.scale > 0.0f)) return false;
   WideParams q = {};
   static_cast<DraftParams&>(q) = p;
   q.batch = batch;

@@ -59,7 +59,7 @@ def test_attention_draft(L):
         assert call(**bad) == zo.ZO_ERR_ALIGN, bad
     assert call(batch=0, lengths=None, masks=None) == zo.ZO_OK
     size = L.zo_attention_draft_workspace_size
-    for few in ((2, 8, 2, 1, 64, 1), (2, 64, 4, 1, 64, 0), (2, 64, 4, 1, 200, 1), (2, 0, 2, 1, 64, 1), (2, 8, 3, 2, 64, 1), (-1, 64, 4, 1, 64, 1)):
+    for few in ((2, 8, 2, 1, 64, 1), (2, 8, 4, 2, 64, 2), (2, 64, 4, 1, 64, 0), (2, 64, 4, 1, 200, 1), (2, 0, 2, 1, 64, 1), (2, 8, 3, 2, 64, 1), (-1, 64, 4, 1, 64, 1)):
         assert size(*few) == 0, few
     assert size(2, 64, 4, 1, 64, 1) % 16 == 0 and size(500, 64, 4, 1, 64, 1) > size(2, 64, 4, 1, 64, 1) > 0
 

@@ -146,6 +146,46 @@ def test_splits(dtype, batch, kv, length, drafts):
     compare(q, args, rows, lengths, masks, slopes=slopes, scale=-0.07)
 
 
+@pytest.mark.parametrize("dtype", DTYPES[:2], ids=IDS[:2])
+@pytest.mark.parametrize("heads,kv,dim,drafts,page", [(32, 32, 64, 26, 16), (8, 8, 128, 17, 24), (16, 8, 128, 32, 64), (16, 4, 80, 24, 256),
+                                                      (32, 8, 128, 64, 16), (8, 1, 96, 64, 8), (12, 1, 64, 64, 128), (40, 8, 128, 31, 7)])
+def test_much_work(dtype, heads, kv, dim, drafts, page):
+    """Sequences of many and of few keys and no tree at all, in a page table with room for much more: work that is cut across
+    sequences, heads and blocks of rows; blocks that begin in one CTA's share and end in another's, and whole ones."""
+    lengths = [3000, 0, 63, 1, 700, -2, 129, 64, 2000, 5, 190, 1]
+    sizes = [drafts, drafts, 1, drafts // 2, drafts, 3, 2, drafts, 5, drafts, drafts, 1]
+    masks = padded(trees(heads + drafts, sizes), drafts)
+    masks[6] = [0] * drafts
+    g = gen(dim + drafts)
+    args, rows = paged(g, lengths, masks, page, kv, dim, dtype)
+    table = torch.full((len(lengths), -(-60_000 // page)), 1 << 30, dtype=torch.int32, device="cuda")
+    table[:, :args[2].shape[1]] = args[2]
+    args = (*args[:2], table, *args[3:])
+    q = randn(g, len(lengths), drafts, heads, dim, dtype=dtype, scale=1.5)
+    out, lse = compare(q, args, rows, lengths, masks)
+    for _ in range(2):
+        again = F.draft_attention(q, *args, with_lse=True)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+    slopes = torch.tensor([2.0 ** -(8 * (h + 1) / heads) for h in range(heads)], device="cuda")
+    compare(q, args, rows, lengths, masks, softcap=20.0, slopes=slopes)
+    assert torch.equal(F.draft_attention(q, *args, out=q), out)
+    # values that are not finite at a node, for those that see it and those that do not; a page that is none
+    j = lengths[4] + 1
+    args[1][table[4, j // page], j % page, 0, 3] = math.inf
+    out2 = F.draft_attention(q, *args)
+    assert not torch.isfinite(out2[4, 1, 0, 3])
+    clean = [i for i in range(drafts) if not masks[4][i] >> 1 & 1]
+    assert torch.isfinite(out2[4, clean]).all()
+    table[0, 100 // page] = -3
+    table[8, 1999 // page] = args[0].shape[0]
+    out3, lse3 = F.draft_attention(q, *args, with_lse=True)
+    for b in (0, 8):
+        sees = torch.tensor([m != 0 for m in masks[b]], device="cuda")
+        assert torch.isnan(out3[b, sees]).all() and torch.isnan(lse3[b, sees]).all() and not out3[b, ~sees].any()
+    others = [b for b in range(len(lengths)) if b not in (0, 4, 8)]
+    assert torch.equal(out3[others], out2[others])
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 @pytest.mark.parametrize("drafts", [3, 40, 64])
 def test_masks_of_the_callers_own(dtype, drafts):
