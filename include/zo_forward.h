@@ -248,7 +248,7 @@ int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, 
 /* ---------------------------------------------------------------------------
  * zo_policy_loss -- with logp_t = x_t,target_t - log sum_v exp(x_tv), r_t =
  * exp(logp_t - old_t) and d_t = ref_t - logp_t, over the counted tokens (those
- * whose target is not negative; nothing of the others is read):
+ * whose target is not negative; nothing of the others reaches a result):
  *   l_t = -min(r_t A_t, clamp(r_t, 1 - clip_low, 1 + clip_high) A_t)
  *         + kl (exp(d_t) - d_t - 1)
  *   loss = sum_t w_t l_t

@@ -17,6 +17,56 @@ constexpr int kSumThreads = 1024;
 constexpr int kMaxParts = 8;      // CTAs of a cluster
 constexpr int kWarpVocab = 4096;  // vocabularies up to which a warp has a row
 
+// Sums here are pairs of fp32, the second what the first has lost: the fp64 units take 16 cycles for a warp's addition, and a
+// CTA's joins of fp64 took more time than the rows they joined.
+struct Pair {
+  float high, low;
+};
+// a + b and the rounding error of that (Knuth, The Art of Computer Programming 2, 4.2.2).
+__device__ __forceinline__ Pair two_sum(float a, float b) {
+  const float s = __fadd_rn(a, b), bb = __fadd_rn(s, -a);
+  const float error = __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -bb)), __fadd_rn(b, -bb));
+  return {s, fabsf(s) < kInf ? error : 0.0f};
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+  const Pair s = two_sum(a.high, b.high);
+  return two_sum(s.high, __fadd_rn(s.low, __fadd_rn(a.low, b.low)));
+}
+__device__ __forceinline__ Pair operator-(Pair a) { return {-a.high, -a.low}; }
+__device__ __forceinline__ Pair over(Pair a, float n) {
+  const float q = __fdiv_rn(a.high, n);
+  return two_sum(q, __fdiv_rn(__fadd_rn(fmaf(-q, n, a.high), a.low), n));
+}
+__device__ __forceinline__ double wide(Pair a) { return static_cast<double>(a.high) + a.low; }
+__device__ __forceinline__ Pair pair_of(float2 v) { return {v.x, v.y}; }
+
+__device__ __forceinline__ Pair warp_sum(Pair s) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    s = s + Pair{__shfl_xor_sync(0xFFFFFFFFu, s.high, o), __shfl_xor_sync(0xFFFFFFFFu, s.low, o)};
+  return s;
+}
+// Over the CTA's threads, in an order of their number alone; on warp 0. The CTA comes to a barrier before it is called again.
+__device__ __forceinline__ Pair cta_sum(Pair s) {
+  __shared__ float2 warps[kSumThreads / 32];
+  s = warp_sum(s);
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = make_float2(s.high, s.low);
+  __syncthreads();
+  if (threadIdx.x < 32) s = warp_sum(threadIdx.x < blockDim.x / 32 ? pair_of(warps[threadIdx.x]) : Pair{0.0f, 0.0f});
+  return s;
+}
+
+// log of a sum: the mantissa's, at most 0.35, and the exponent's times log 2 = 355 / 512 - 2.1219444e-4, the first exactly.
+__device__ __forceinline__ Pair log_pair(float sum) {
+  int e;
+  float m = frexpf(sum, &e);
+  if (!(sum > 0.0f && sum < kInf)) return {logf(sum), 0.0f};
+  if (m < 0.70710678f) m *= 2.0f, --e;
+  return two_sum(e * 0.693359375f, fmaf(static_cast<float>(e), -2.12194440e-4f, logf(m)));
+}
+// x - (top + rest)
+__device__ __forceinline__ Pair logp_of(float x, float top, Pair rest) { return two_sum(x, -top) + -rest; }
+
 struct Term {
   float value, slope;
 };
@@ -41,65 +91,98 @@ struct Token {  // what stands beside its logits
 // A token's loss and its slope by its log-probability. With r = exp(logp - old):
 // -min(r A, clip(r) A) + kl (exp(d) - 1 - d), d = ref - logp. A NaN stays one:
 // each comparison is written so that it picks the side that is NaN.
-__device__ __forceinline__ Term policy_term(const PolicyLossParams& p, const Token& t, double logp) {
-  const float a = t.advantage, r = expf(static_cast<float>(logp - t.old_logp));
+__device__ __forceinline__ Term policy_term(const PolicyLossParams& p, const Token& t, Pair logp) {
+  const float a = t.advantage, r = expf((logp.high - t.old_logp) + logp.low);
   const float lo = 1.0f - p.clip_low, hi = 1.0f + p.clip_high;
   const float whole = r * a, cut = (r < lo ? lo : r > hi ? hi : r) * a;
   Term term = {whole > cut ? -cut : -whole, whole > cut ? 0.0f : -whole};
   if (p.ref_logp != nullptr) {
-    const float d = static_cast<float>(t.ref_logp - logp);
+    const float d = (t.ref_logp - logp.high) - logp.low;
     term.value += p.kl * expm1_less(d);
     term.slope -= p.kl * expm1f(d);
   }
   return term;
 }
 
-// The counted tokens' weights, on thread 0.
-__device__ __forceinline__ double counted_weight(const PolicyLossParams& p) {
-  const TokenLossParams& r = p.rows;
-  double weight = 0.0;
-  for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x)
-    if (load_index(r.targets, t, r.target64) >= 0) weight += p.weights != nullptr ? p.weights[t] : 1.0;
-  return cta_sums({weight, 0.0}).a;
-}
-
-// The tokens' terms and their sum, in one CTA and an order of their number alone.
-__global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_constant__ PolicyLossParams p) {
-  __shared__ double over;
-  const TokenLossParams& r = p.rows;
-  if (r.flags & 1) {
-    const double weight = counted_weight(p);
-    if (threadIdx.x == 0) over = weight != 0.0 ? 1.0 / weight : NAN;
-    __syncthreads();
-  }
-  const double unit = r.flags & 1 ? over : 1.0;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  double sum = 0.0;
+// 1 over the counted tokens' weights, on thread 0.
+__device__ __forceinline__ float mean_unit(const PolicyLossParams& p) {
+  const AnswerRows& r = p.rows;
+  Pair weight = {0.0f, 0.0f};
+#pragma unroll 4
   for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x) {
-    const bool counts = load_index(r.targets, t, r.target64) >= 0;
-    const double logp = -r.rows[t];
-    Term term = {0.0f, 0.0f};
-    double w = 0.0;
-    if (counts) {
-      const Token token(p, t);
-      term = policy_term(p, token, logp);
-      w = token.weight;
-      sum += w * term.value;
-    }
-    if (p.logp != nullptr) p.logp[t] = counts ? static_cast<float>(logp) : 0.0f;
-    if (p.slopes != nullptr) p.slopes[t] = counts ? static_cast<float>(w * unit * term.slope) : 0.0f;
+    const float w = p.weights != nullptr ? p.weights[t] : 1.0f;
+    if (load_index(r.targets, t, r.target64) >= 0) weight = weight + Pair{w, 0.0f};
   }
-  const Sums all = cta_sums({sum, 0.0});
-  if (threadIdx.x == 0) put_loss(r.loss, r.flags, r.flags & 1 ? all.a * unit : all.a);
+  weight = cta_sum(weight);
+  return weight.high != 0.0f ? static_cast<float>(1.0 / wide(weight)) : NAN;
 }
 
-// The sequences' sums, the pairs' losses and their sum, and each token's slope,
-// in one CTA; a warp has a sequence.
+// The tokens' terms and their sum, in one CTA and an order of their number alone. What it costs is latency: what stands beside
+// the logits is read ahead of the rows' sums, whether a token counts or not, and four tokens of a thread at once.
+__global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_constant__ PolicyLossParams p) {
+  __shared__ float shared_unit;
+  constexpr int kAtOnce = 4;
+  const AnswerRows& r = p.rows;
+  Token token[kAtOnce];
+  bool counts[kAtOnce];
+  const auto read = [&](int64_t first) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t t = first + k * static_cast<int64_t>(blockDim.x);
+      counts[k] = false;
+      if (t < r.tokens) {
+        token[k] = Token(p, t);
+        counts[k] = load_index(r.targets, t, r.target64) >= 0;
+      }
+    }
+  };
+  read(threadIdx.x);
+  float unit = 1.0f;
+  if (p.unit != nullptr) {
+    unit = mean_unit(p);
+    if (threadIdx.x == 0) shared_unit = unit;
+    __syncthreads();
+    unit = shared_unit;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  Pair sum = {0.0f, 0.0f};
+  for (int64_t first = threadIdx.x; first < r.tokens; first += kAtOnce * static_cast<int64_t>(blockDim.x)) {
+    if (first != threadIdx.x) read(first);
+    Pair logp[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t t = first + k * static_cast<int64_t>(blockDim.x);
+      logp[k] = t < r.tokens ? pair_of(r.logp[t]) : Pair{0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t t = first + k * static_cast<int64_t>(blockDim.x);
+      if (t >= r.tokens) continue;
+      Term term = {0.0f, 0.0f};
+      if (counts[k]) {
+        term = policy_term(p, token[k], logp[k]);
+        sum = sum + Pair{token[k].weight * term.value, 0.0f};
+      }
+      if (p.logp != nullptr) p.logp[t] = logp[k].high;
+      if (p.slopes != nullptr) p.slopes[t] = counts[k] ? token[k].weight * unit * term.slope : 0.0f;
+    }
+  }
+  sum = cta_sum(sum);
+  if (threadIdx.x == 0) put_loss(r.loss, r.flags, p.unit != nullptr ? wide(sum) * unit : wide(sum));
+}
+
+// The sequences' sums, the pairs' losses and their sum, and each token's slope, in one CTA. A sequence has one warp, or where
+// there are few as many as it takes for all to have some; a token that does not count has a log-probability of 0 already.
 __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __grid_constant__ PreferenceLossParams p) {
   __shared__ int unsorted;
-  const TokenLossParams& r = p.rows;
+  __shared__ float2 part_sum[kSumThreads / 32];
+  __shared__ int part_count[kSumThreads / 32];
+  const AnswerRows& r = p.rows;
   const int warps = blockDim.x / 32, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t sequences = 2 * p.pairs;
+  int per = 1;  // warps of a sequence
+  while (sequences > 0 && 2 * per * sequences <= warps) per *= 2;
+  const int at_once = warps / per, mine = warp / per, share = warp - mine * per;  // sequences at once; the warp's, its place
   if (threadIdx.x == 0) unsorted = 0;
   __syncthreads();
   for (int64_t j = threadIdx.x; j <= sequences; j += blockDim.x) {
@@ -109,73 +192,69 @@ __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __gri
   __syncthreads();
   const bool bad = unsorted != 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int64_t j = warp; j < sequences && !bad; j += warps) {
-    double sum = 0.0, count = 0.0;
-    for (int64_t t = p.starts[j] + lane; t < p.starts[j + 1]; t += 32)
-      if (load_index(r.targets, t, r.target64) >= 0) {
-        sum -= r.rows[t];
-        count += 1.0;
+  for (int64_t first = 0; first < sequences && !bad; first += at_once) {
+    const int64_t j = first + mine;
+    Pair sum = {0.0f, 0.0f};
+    int count = 0;
+    if (j < sequences && mine < at_once) {
+      const int64_t from = p.starts[j] + share * 32 + lane, to = p.starts[j + 1];
+#pragma unroll 4
+      for (int64_t t = from; t < to; t += per * 32) sum = sum + pair_of(r.logp[t]);
+      if (p.by_length) {
+#pragma unroll 4
+        for (int64_t t = from; t < to; t += per * 32) count += load_index(r.targets, t, r.target64) >= 0;
       }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-      count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
     }
-    if (lane == 0) p.sums[j] = p.by_length ? sum / fmax(count, 1.0) : sum;
+    sum = warp_sum(sum);
+    count = __reduce_add_sync(0xFFFFFFFFu, count);
+    if (lane == 0) part_sum[warp] = make_float2(sum.high, sum.low), part_count[warp] = count;
+    __syncthreads();
+    if (j < sequences && mine < at_once && share == 0 && lane == 0) {
+      for (int i = 1; i < per; ++i) sum = sum + pair_of(part_sum[warp + i]), count += part_count[warp + i];
+      const float by = p.by_length && count > 1 ? static_cast<float>(count) : 1.0f;
+      if (by > 1.0f) sum = over(sum, by);
+      p.sums[j] = make_float2(sum.high, sum.low);
+      p.counts[j] = by;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  double loss = 0.0;
-  const double over = r.flags & 1 ? 1.0 / p.pairs : 1.0;
+  Pair loss = {0.0f, 0.0f};
+  const float per_pair = r.flags & 1 ? 1.0f / static_cast<float>(p.pairs) : 1.0f;
   for (int64_t i = threadIdx.x; i < p.pairs; i += blockDim.x) {
-    const double chosen = bad ? NAN : p.sums[2 * i], rejected = bad ? NAN : p.sums[2 * i + 1];
-    double away = chosen - rejected;
-    if (p.ref_logp != nullptr) away -= static_cast<double>(p.ref_logp[2 * i]) - p.ref_logp[2 * i + 1];
-    const float m = static_cast<float>(p.beta * away - p.margin);
+    const Pair chosen = bad ? Pair{NAN, 0.0f} : pair_of(p.sums[2 * i]), rejected = bad ? Pair{NAN, 0.0f} : pair_of(p.sums[2 * i + 1]);
+    Pair away = chosen + -rejected;
+    if (p.ref_logp != nullptr) away = away + two_sum(p.ref_logp[2 * i + 1], -p.ref_logp[2 * i]);
+    const float m = p.beta * away.high - p.margin;
     // softplus(x) = max(x, 0) + log1p(exp(-|x|)), and its derivative
     const float e = expf(-fabsf(m)), tail = log1pf(e), small = e / (1.0f + e), large = 1.0f / (1.0f + e);
     const float up = m > 0.0f ? large : m <= 0.0f ? small : NAN, down = m > 0.0f ? small : m <= 0.0f ? large : NAN;
-    loss += (1.0 - p.smoothing) * (fmaxf(-m, 0.0f) + tail) + p.smoothing * (fmaxf(m, 0.0f) + tail);
+    loss = loss + Pair{(1.0f - p.smoothing) * (fmaxf(-m, 0.0f) + tail), p.smoothing * (fmaxf(m, 0.0f) + tail)};
     if (p.logp != nullptr) {
-      p.logp[2 * i] = static_cast<float>(chosen);
-      p.logp[2 * i + 1] = static_cast<float>(rejected);
+      p.logp[2 * i] = chosen.high;
+      p.logp[2 * i + 1] = rejected.high;
     }
     if (p.slopes != nullptr) {
-      const double slope = over * p.beta * (p.smoothing * up - (1.0 - p.smoothing) * down);
-      p.sums[2 * i] = slope;
-      p.sums[2 * i + 1] = -slope;
+      const float slope = per_pair * p.beta * (p.smoothing * up - (1.0f - p.smoothing) * down);
+      p.sums[2 * i] = make_float2(slope, 0.0f);
+      p.sums[2 * i + 1] = make_float2(-slope, 0.0f);
     }
   }
-  const Sums all = cta_sums({loss, 0.0});
-  if (threadIdx.x == 0) put_loss(r.loss, r.flags, all.a * over);
+  loss = cta_sum(loss);
+  if (threadIdx.x == 0) put_loss(r.loss, r.flags, r.flags & 1 ? wide(loss) / static_cast<double>(p.pairs) : wide(loss));
   if (p.slopes == nullptr) return;
   __syncthreads();  // the slopes are in p.sums
-  const int64_t first = bad ? 0 : p.starts[0], end = bad ? r.tokens : p.starts[sequences];
-  for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x)
-    if (bad || t < first || t >= end)
-      p.slopes[t] = load_index(r.targets, t, r.target64) >= 0 && bad ? NAN : 0.0f;
-  for (int64_t j = warp; j < sequences && !bad; j += warps) {
-    const int64_t from = p.starts[j], to = p.starts[j + 1];
-    double count = 1.0;
-    if (p.by_length) {
-      count = 0.0;
-      for (int64_t t = from + lane; t < to; t += 32) count += load_index(r.targets, t, r.target64) >= 0 ? 1.0 : 0.0;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
-    }
-    const float slope = static_cast<float>(p.sums[j] / fmax(count, 1.0));
-    for (int64_t t = from + lane; t < to; t += 32) p.slopes[t] = load_index(r.targets, t, r.target64) >= 0 ? slope : 0.0f;
+  if (bad) {
+    for (int64_t t = threadIdx.x; t < r.tokens; t += blockDim.x) p.slopes[t] = NAN;
+    return;
   }
-}
-
-// log of a sum of exponentials, without the fp64 units' log (whose 2 us every row would wait for): the exponent's part in fp64
-// and the mantissa's, at most 0.35, in fp32.
-__device__ __forceinline__ double log_split(double sum) {
-  int e;
-  const float f = static_cast<float>(sum);
-  float m = frexpf(f, &e);
-  if (!(f > 0.0f && f < kInf)) return logf(f);
-  if (m < 0.70710678f) m *= 2.0f, --e;
-  return e * 0.69314718055994530942 + logf(m);
+  // rows in no sequence, and the sequences' (whether they count: the gradient's kernel goes by that too)
+  const int64_t begin = p.starts[0], end = p.starts[sequences];
+  for (int64_t t = threadIdx.x; t < begin; t += blockDim.x) p.slopes[t] = 0.0f;
+  for (int64_t t = end + threadIdx.x; t < r.tokens; t += blockDim.x) p.slopes[t] = 0.0f;
+  for (int64_t j = mine; j < sequences && mine < at_once; j += at_once) {
+    const float slope = p.sums[j].x / p.counts[j];
+    for (int64_t t = p.starts[j] + share * 32 + lane; t < p.starts[j + 1]; t += per * 32) p.slopes[t] = slope;
+  }
 }
 
 // The gradient of a row's logits in place of the logits: grad_v = slope scale (1[v = target] - exp(x_v - lse)). x - lse is formed
@@ -215,17 +294,17 @@ struct Part {
 
 constexpr int kPartThreads = 256;
 
-template <int kThreads, typename T>
+template <typename T>
 __device__ __forceinline__ void fetch_part(const T* x, const Part<T>& part, uint4* to) {
   const uint4* from = reinterpret_cast<const uint4*>(x + part.first);
-  for (int i = threadIdx.x; i < part.vectors; i += kThreads)
+  for (int i = threadIdx.x; i < part.vectors; i += kPartThreads)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + i))),
                  "l"(from + i)
                  : "memory");
 }
 
 // Writes a part's gradient from its logits in shared memory (each thread reads what it has put there itself), or zeros.
-template <int kThreads, typename T>
+template <typename T>
 __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4* x, float edge, bool zero, const Slope& s,
                                          int64_t target) {
   constexpr int E = Vec<T>::kN;
@@ -236,7 +315,7 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
   T* to = g + part.first;
   const bool vector = reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll 2
-  for (int i = tid; i < part.vectors; i += kThreads) {
+  for (int i = tid; i < part.vectors; i += kPartThreads) {
     float f[E] = {};
     if (!zero) {
       float w[E];
@@ -270,17 +349,17 @@ __global__ void __launch_bounds__(kPartThreads) logits_grad_kernel(const __grid_
   const T* x = static_cast<const T*>(p.logits) + t * p.row;
   const Part<T> part(x, p.vocab, blockIdx.x % parts, parts);
   const float slope = p.slopes[t];
-  const bool zero = slope == 0.0f;
+  const int64_t target = load_index(p.targets, t, p.target64);
+  const bool zero = slope == 0.0f || target < 0;
   float2 lse = make_float2(0.0f, 0.0f);
   float edge = 0.0f;
   if (!zero) {
-    fetch_part<kPartThreads>(x, part, tile);
+    fetch_part(x, part, tile);
     lse = p.lse[t];
     if (part.edge >= 0) edge = widen(x[part.edge]);
   }
-  const int64_t target = load_index(p.targets, t, p.target64);
   asm volatile("cp.async.wait_all;" ::: "memory");
-  put_part<kPartThreads>(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
+  put_part(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
 }
 
 // The same for vocabularies of at most 4096: a warp per row.
@@ -291,9 +370,9 @@ __global__ void __launch_bounds__(kPartThreads) logits_grad_warp_kernel(const __
   const T* x = static_cast<const T*>(p.logits) + t * p.row;
   T* g = static_cast<T*>(p.grad) + t * p.grad_row;
   const float slope = p.slopes[t];
-  const bool zero = slope == 0.0f;
-  const Slope s(slope, p.scale, zero ? make_float2(0.0f, 0.0f) : p.lse[t]);
   const int64_t target = load_index(p.targets, t, p.target64);
+  const bool zero = slope == 0.0f || target < 0;
+  const Slope s(slope, p.scale, zero ? make_float2(0.0f, 0.0f) : p.lse[t]);
   for (int64_t i = threadIdx.x & 31; i < p.vocab; i += 32) {
     const float v = zero ? 0.0f : widen(x[i]);
     g[i] = narrow<T>(zero ? 0.0f : i == target ? s.target(v) : s.other(v));
@@ -359,54 +438,14 @@ __device__ __forceinline__ void lanes_join_f32(float& top, float& sum) {
   top = all;
 }
 
-// A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory.
-template <typename T>
-__global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
-                                                                     const __grid_constant__ LogitsGradParams g, int parts) {
-  extern __shared__ __align__(16) uint4 tile[];
+// A row's maximum and sum over the CTA's threads and its cluster's CTAs, on warp 0. The caller waits for the cluster's barrier
+// before it leaves: its part may be read until then.
+__device__ __forceinline__ void join_rows(float& top, float& sum, int parts) {
   constexpr int kWarps = kPartThreads / 32;
   __shared__ float tops[kWarps];
   __shared__ float sums[kWarps];
   __shared__ float part_top, part_sum;
-  __shared__ float shared_slope;
-  __shared__ float2 shared_lse;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const TokenLossParams& r = p.rows;
-  const int tid = threadIdx.x, rank = static_cast<int>(cluster_rank());
-  const int64_t t = blockIdx.x / static_cast<unsigned>(parts), target = load_index(r.targets, t, r.target64);
-  const T* x = static_cast<const T*>(r.logits) + t * r.row;
-  T* grad = static_cast<T*>(g.grad) + t * g.grad_row;
-  const Part<T> part(x, r.vocab, rank, parts);
-  const bool counts = target >= 0;
-  if (!counts || target >= r.vocab) {  // the same for the whole cluster
-    const float nan = NAN;
-    if (rank == 0 && tid == 0) r.rows[t] = counts ? NAN : 0.0;
-    put_part<kPartThreads>(grad, part, tile, nan, !counts, Slope(nan, 1.0f, make_float2(0.0f, 0.0f)), -1);
-    if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");  // what follows may count on the kernel before
-    return;
-  }
-  fetch_part<kPartThreads>(x, part, tile);
-  float edge = 0.0f, own = 0.0f;
-  if (part.edge >= 0) edge = widen(x[part.edge]);
-  Token token;
-  if (tid == 0) {
-    own = widen(x[target]);
-    token = Token(p, t);
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  float top = kNone.top, sum = 0.0f;
-  if (part.edge >= 0) take<1>(&edge, top, sum);
-  int i = tid;
-  for (; i + 3 * kPartThreads < part.vectors; i += 4 * kPartThreads) {
-    uint4 raw[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) raw[k] = tile[i + k * kPartThreads];
-    take_raw<T>(raw, top, sum);
-  }
-  for (; i < part.vectors; i += kPartThreads) {
-    const uint4 raw[1] = {tile[i]};
-    take_raw<T>(raw, top, sum);
-  }
+  const int tid = threadIdx.x;
   lanes_join_f32<32>(top, sum);
   if ((tid & 31) == 0) {
     tops[tid >> 5] = top;
@@ -432,25 +471,136 @@ __global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __gr
     }
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // its peers' parts are read
   }
+}
+
+// The rows' log-probabilities and log-sums: a CTA per counted row, or a cluster that splits the vocabulary.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads, 5) row_sums_kernel(const __grid_constant__ AnswerRows r, int parts) {
+  constexpr int kLoads = 4;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int tid = threadIdx.x, rank = static_cast<int>(cluster_rank());
+  const int64_t t = blockIdx.x / static_cast<unsigned>(parts), target = load_index(r.targets, t, r.target64);
+  if (target < 0 || target >= r.vocab) {  // the same for the whole cluster
+    if (rank == 0 && tid == 0) r.logp[t] = make_float2(target < 0 ? 0.0f : NAN, 0.0f), r.lse[t] = make_float2(0.0f, 0.0f);
+    return;
+  }
+  const T* x = static_cast<const T*>(r.logits) + t * r.row;
+  const Part<T> part(x, r.vocab, rank, parts);
+  float own = 0.0f, edge = 0.0f, top = kNone.top, sum = 0.0f;
+  if (rank == 0 && tid == 0) own = widen(x[target]);
+  if (part.edge >= 0) edge = widen(x[part.edge]);
+  const uint4* v = reinterpret_cast<const uint4*>(x + part.first);
+  constexpr uint32_t kNothing = sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
+  for (int i = tid; i < part.vectors; i += kLoads * kPartThreads) {
+    uint4 raw[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      raw[k] = make_uint4(kNothing, kNothing, kNothing, kNothing);
+      if (i + k * kPartThreads < part.vectors) raw[k] = __ldg(v + i + k * kPartThreads);
+    }
+    take_raw<T>(raw, top, sum);
+  }
+  if (part.edge >= 0) take<1>(&edge, top, sum);
+  join_rows(top, sum, parts);
+  if (rank == 0 && tid == 0) {
+    const Pair rest = log_pair(sum), logp = logp_of(own, top, rest);
+    r.logp[t] = make_float2(logp.high, logp.low);
+    r.lse[t] = make_float2(top, rest.high);
+  }
+  if (parts > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// The same for vocabularies of at most 4096: a warp per row.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads) row_sums_warp_kernel(const __grid_constant__ AnswerRows r) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kPartThreads / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (t >= r.tokens) return;
+  const int64_t target = load_index(r.targets, t, r.target64);
+  if (target < 0 || target >= r.vocab) {
+    if (lane == 0) r.logp[t] = make_float2(target < 0 ? 0.0f : NAN, 0.0f), r.lse[t] = make_float2(0.0f, 0.0f);
+    return;
+  }
+  const T* x = static_cast<const T*>(r.logits) + t * r.row;
+  float top = kNone.top, sum = 0.0f;
+  row_tail<T, 32>(x, static_cast<int>(r.vocab), lane, top, sum);
+  lanes_join_f32<32>(top, sum);
+  if (lane == 0) {
+    const Pair rest = log_pair(sum), logp = logp_of(widen(x[target]), top, rest);
+    r.logp[t] = make_float2(logp.high, logp.low);
+    r.lse[t] = make_float2(top, rest.high);
+  }
+}
+
+// A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory.
+template <typename T>
+__global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
+                                                                      const __grid_constant__ LogitsGradParams g, int parts) {
+  extern __shared__ __align__(16) uint4 tile[];
+  __shared__ float shared_slope;
+  __shared__ float2 shared_lse;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const AnswerRows& r = p.rows;
+  const int tid = threadIdx.x, rank = static_cast<int>(cluster_rank());
+  const int64_t t = blockIdx.x / static_cast<unsigned>(parts), target = load_index(r.targets, t, r.target64);
+  const T* x = static_cast<const T*>(r.logits) + t * r.row;
+  T* grad = static_cast<T*>(g.grad) + t * g.grad_row;
+  const Part<T> part(x, r.vocab, rank, parts);
+  const bool counts = target >= 0;
+  if (!counts || target >= r.vocab) {  // the same for the whole cluster
+    const float nan = NAN;
+    if (rank == 0 && tid == 0) r.logp[t] = make_float2(counts ? NAN : 0.0f, 0.0f);
+    put_part(grad, part, tile, nan, !counts, Slope(nan, 1.0f, make_float2(0.0f, 0.0f)), -1);
+    if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");  // what follows may count on the kernel before
+    return;
+  }
+  fetch_part(x, part, tile);
+  float edge = 0.0f, own = 0.0f;
+  if (part.edge >= 0) edge = widen(x[part.edge]);
+  Token token;
   if (tid == 0) {
-    const double rest = log_split(sum), logp = (static_cast<double>(own) - top) - rest;
-    if (rank == 0) r.rows[t] = -logp;
+    own = widen(x[target]);
+    token = Token(p, t);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  float top = kNone.top, sum = 0.0f;
+  if (part.edge >= 0) take<1>(&edge, top, sum);
+  int i = tid;
+  for (; i + 3 * kPartThreads < part.vectors; i += 4 * kPartThreads) {
+    uint4 raw[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) raw[k] = tile[i + k * kPartThreads];
+    take_raw<T>(raw, top, sum);
+  }
+  for (; i < part.vectors; i += kPartThreads) {
+    const uint4 raw[1] = {tile[i]};
+    take_raw<T>(raw, top, sum);
+  }
+  join_rows(top, sum, parts);
+  if (tid == 0) {
+    const Pair rest = log_pair(sum), logp = logp_of(own, top, rest);
+    if (rank == 0) r.logp[t] = make_float2(logp.high, logp.low);
     const Term term = policy_term(p, token, logp);
-    if (p.unit != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");
-    shared_slope = static_cast<float>(token.weight * (p.unit != nullptr ? __ldcg(p.unit) : 1.0) * term.slope);
-    shared_lse = make_float2(top, static_cast<float>(rest));
+    float unit = 1.0f;
+    if (p.unit != nullptr) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      unit = __ldcg(p.unit);
+    }
+    shared_slope = token.weight * unit * term.slope;
+    shared_lse = make_float2(top, rest.high);
   }
   __syncthreads();
   const float slope = shared_slope;
-  put_part<kPartThreads>(grad, part, tile, edge, slope == 0.0f, Slope(slope, g.scale, shared_lse), target);
-  if (parts > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // no CTA leaves before its part is read
+  put_part(grad, part, tile, edge, slope == 0.0f, Slope(slope, g.scale, shared_lse), target);
+  if (parts > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// 1 over the counted tokens' weights.
+// What a mean's weights are multiplied by.
 __global__ void __launch_bounds__(kSumThreads) policy_unit_kernel(const __grid_constant__ PolicyLossParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const double weight = counted_weight(p);
-  if (threadIdx.x == 0) *p.unit = weight != 0.0 ? 1.0 / weight : NAN;
+  const float unit = mean_unit(p);
+  if (threadIdx.x == 0) *p.unit = unit;
 }
 
 template <typename T>
@@ -474,6 +624,34 @@ cudaError_t launch_logits_grad(const LogitsGradParams& p, int dtype, cudaStream_
                       : launch_grad<__half>(p, stream);
 }
 
+cudaLaunchAttribute clusters_of(int parts) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = parts;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  return attr;
+}
+
+template <typename T>
+cudaError_t launch_sums(const AnswerRows& r, int sms, cudaStream_t stream) {
+  if (r.vocab <= kWarpVocab) {
+    constexpr int kRows = kPartThreads / 32;
+    row_sums_warp_kernel<T><<<static_cast<unsigned>((r.tokens + kRows - 1) / kRows), kPartThreads, 0, stream>>>(r);
+    return cudaGetLastError();
+  }
+  // as many parts as the SMs hold at once, none with less than 4096 logits
+  int parts = 1;
+  while (parts < kMaxParts && r.tokens * parts * 2 <= 5 * sms && r.vocab / (parts * 2) >= 4096) parts *= 2;
+  return launch_with(row_sums_kernel<T>, static_cast<unsigned>(r.tokens * parts), kPartThreads, clusters_of(parts), stream, r, parts);
+}
+
+cudaError_t launch_row_sums(const AnswerRows& r, int dtype, int sms, cudaStream_t stream) {
+  if (r.tokens == 0) return cudaSuccess;
+  return dtype == 0   ? launch_sums<float>(r, sms, stream)
+         : dtype == 1 ? launch_sums<__nv_bfloat16>(r, sms, stream)
+                      : launch_sums<__half>(r, sms, stream);
+}
+
 constexpr int64_t kMostPart = 200 * 1024;
 
 // Whether rows of that many bytes are taken at once: beyond the vocabularies that a warp takes, up to what a cluster holds.
@@ -483,7 +661,7 @@ template <typename T>
 cudaError_t launch_rows(const PolicyLossParams& p, const LogitsGradParams& g, int sms, cudaStream_t stream) {
   const int64_t bytes = g.vocab * static_cast<int64_t>(sizeof(T));
   int parts = 1;
-  while (parts < kMaxParts && (bytes / parts > 40 * 1024 || (g.tokens * parts * 2 <= 5 * sms && g.vocab / (parts * 2) >= 4096))) parts *= 2;
+  while (parts < kMaxParts && (bytes / parts > 52 * 1024 || (g.tokens * parts * 2 <= 5 * sms && g.vocab / (parts * 2) >= 4096))) parts *= 2;
   const int tile = static_cast<int>((bytes / parts + 31) / 16 * 16);
   cudaError_t e = cudaFuncSetAttribute(policy_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile);
   if (e != cudaSuccess) return e;
@@ -493,9 +671,7 @@ cudaError_t launch_rows(const PolicyLossParams& p, const LogitsGradParams& g, in
     if (e != cudaSuccess) return e;
   }
   cudaLaunchAttribute attr[2] = {};
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = parts;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[0] = clusters_of(parts);
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t c = {};
@@ -523,13 +699,12 @@ cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams
   if (g != nullptr && g->tokens > 0 && rows_at_once(g->vocab, g->vocab * (dtype == 0 ? 4 : 2))) {
     PolicyLossParams at_once = p;
     at_once.slopes = nullptr;
-    if ((p.rows.flags & 1) == 0) at_once.unit = nullptr;
     cudaError_t e = dtype == 0   ? launch_rows<float>(at_once, *g, sms, stream)
                     : dtype == 1 ? launch_rows<__nv_bfloat16>(at_once, *g, sms, stream)
                                  : launch_rows<__half>(at_once, *g, sms, stream);
     return e != cudaSuccess ? e : launch_sum(policy_sum_kernel, at_once, p.rows.tokens, stream);
   }
-  cudaError_t e = launch_token_rows(p.rows, dtype, sms, stream);
+  cudaError_t e = launch_row_sums(p.rows, dtype, sms, stream);
   if (e == cudaSuccess) e = launch_sum(policy_sum_kernel, p, p.rows.tokens, stream);
   if (e == cudaSuccess && g != nullptr) e = launch_logits_grad(*g, dtype, stream);
   return e;
@@ -537,7 +712,7 @@ cudaError_t launch_policy_loss(const PolicyLossParams& p, const LogitsGradParams
 
 cudaError_t launch_preference_loss(const PreferenceLossParams& p, const LogitsGradParams* g, int dtype, int sms,
                                    cudaStream_t stream) {
-  cudaError_t e = launch_token_rows(p.rows, dtype, sms, stream);
+  cudaError_t e = launch_row_sums(p.rows, dtype, sms, stream);
   if (e == cudaSuccess) e = launch_sum(preference_sum_kernel, p, std::max(p.rows.tokens, 64 * p.pairs), stream);
   if (e == cudaSuccess && g != nullptr) e = launch_logits_grad(*g, dtype, stream);
   return e;

@@ -78,28 +78,38 @@ struct TokenLossParams {
   void* loss;
   float* nll;
   double* rows;  // a token's nll before its rounding
-  float2* lse;   // its logits' maximum, and what their log sum exp is above it, or NULL
 };
 
-// Losses over answers: a row's statistics, from them a coefficient per row, from it the row's gradient.
+// Losses over answers: a row's statistics, from them its slope, from it the row's gradient.
+struct AnswerRows {
+  const void* logits;
+  int64_t row, tokens, vocab;
+  const void* targets;
+  int32_t target64, flags;
+  void* loss;
+  float2* logp;  // a target's log-probability, high and low part; 0 for tokens that do not count
+  float2* lse;   // a row's maximum, and what its log sum exp is above it
+};
+
 struct PolicyLossParams {
-  TokenLossParams rows;  // loss and flags are the loss's; nll is not used
+  AnswerRows rows;
   const float *old_logp, *advantages, *ref_logp, *weights;
   float clip_low, clip_high, kl;
   float* logp;
-  double* unit;   // place for what a mean's weights are multiplied by
+  float* unit;    // place for what a mean's weights are multiplied by; NULL: they are not
   float* slopes;  // of the loss by a token's log-probability; NULL without a gradient
 };
 
 struct PreferenceLossParams {
-  TokenLossParams rows;
+  AnswerRows rows;
   const int32_t* starts;
   int64_t pairs;
   const float* ref_logp;
   float beta, margin, smoothing;
   int32_t by_length;
   float* logp;
-  double* sums;   // [2 pairs] of the sequences' tokens, then of the pairs' losses
+  float2* sums;   // [2 pairs] of the sequences' tokens, high and low part; then the loss's slopes by them
+  float* counts;  // [2 pairs] what a sequence's sum is divided by
   float* slopes;  // of the loss by a token's log-probability, per token; NULL without a gradient
 };
 

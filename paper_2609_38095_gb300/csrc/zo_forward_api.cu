@@ -232,22 +232,21 @@ int check_outputs(const void* logits, int64_t row, const void* grad, int64_t gra
   return over ? ZO_ERR_ARG : ZO_OK;
 }
 
-// A workspace's parts, each on 8 bytes: the rows' nll and lse, the sequences' sums (or a mean's weight), the rows' slopes.
+// A workspace's parts, each on 8 bytes: the rows' log-probabilities and log-sums, the sequences' sums (or a mean's weight) and counts, the
+// rows' slopes.
 struct LossWork {
-  double* nll;
-  float2* lse;
-  double* sums;
-  float* slopes;
+  float2 *logp, *lse, *sums;
+  float *counts, *slopes;
 };
 int64_t loss_work_size(int64_t tokens, int64_t sequences) {
   const int64_t t = tokens > 0 ? tokens : 1;
-  return 16 * t + 8 * sequences + (4 * t + 7) / 8 * 8;
+  return 16 * t + 8 * sequences + (4 * (sequences + t) + 7) / 8 * 8;
 }
 LossWork loss_work(void* p, int64_t tokens, int64_t sequences) {
   char* at = static_cast<char*>(p);
   const int64_t t = tokens > 0 ? tokens : 1;
-  return {reinterpret_cast<double*>(at), reinterpret_cast<float2*>(at + 8 * t), reinterpret_cast<double*>(at + 16 * t),
-          reinterpret_cast<float*>(at + 16 * t + 8 * sequences)};
+  return {reinterpret_cast<float2*>(at), reinterpret_cast<float2*>(at + 8 * t), reinterpret_cast<float2*>(at + 16 * t),
+          reinterpret_cast<float*>(at + 16 * t + 8 * sequences), reinterpret_cast<float*>(at + 16 * t + 12 * sequences)};
 }
 
 int finish(cudaError_t e, const char* what) { return e == cudaSuccess ? ZO_OK : zo::report_cuda_error(e, what); }
@@ -505,13 +504,12 @@ int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t voca
   if (rc != ZO_OK) return rc;
   const LossWork work = loss_work(workspace, tokens, 1);
   zo::PolicyLossParams p = {};
-  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags, loss, nullptr, work.nll,
-            grad != nullptr ? work.lse : nullptr};
+  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags, loss, work.logp, work.lse};
   p.old_logp = old_logp, p.advantages = advantages, p.weights = weights;
   p.ref_logp = kl != 0.0f ? ref_logp : nullptr;
   p.clip_low = clip_low, p.clip_high = clip_high, p.kl = kl;
   p.logp = logp;
-  p.unit = work.sums;
+  p.unit = flags & ZO_LOSS_MEAN ? reinterpret_cast<float*>(work.sums) : nullptr;
   p.slopes = grad != nullptr ? work.slopes : nullptr;
   const zo::LogitsGradParams g = {logits, grad, row, grad_row, tokens, vocab, targets, target_bytes == 8, work.slopes,
                                   work.lse, grad_scale};
@@ -545,15 +543,14 @@ int zo_preference_loss(const void* logits, int64_t row, int64_t tokens, int64_t 
   if (rc != ZO_OK) return rc;
   const LossWork work = loss_work(workspace, tokens, 2 * pairs);
   zo::PreferenceLossParams p = {};
-  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags & ~ZO_LOSS_BY_LENGTH, loss, nullptr, work.nll,
-            grad != nullptr ? work.lse : nullptr};
+  p.rows = {logits, row, tokens, vocab, targets, target_bytes == 8, flags & ~ZO_LOSS_BY_LENGTH, loss, work.logp, work.lse};
   p.starts = starts;
   p.pairs = pairs;
   p.ref_logp = ref_logp;
   p.beta = beta, p.margin = margin, p.smoothing = smoothing;
   p.by_length = (flags & ZO_LOSS_BY_LENGTH) != 0;
   p.logp = logp;
-  p.sums = work.sums;
+  p.sums = work.sums, p.counts = work.counts;
   p.slopes = grad != nullptr ? work.slopes : nullptr;
   const zo::LogitsGradParams g = {logits, grad, row, grad_row, tokens, vocab, targets, target_bytes == 8, work.slopes,
                                   work.lse, grad_scale};

@@ -83,37 +83,6 @@ __device__ __forceinline__ void row_tail(const T* x, int n, int tid, float& top,
   }
 }
 
-// log sum exp as the maximum and what is above it: their sum would lose the latter beside logits of the type's lowest value.
-__device__ __forceinline__ float2 row_lse(Tail t) { return make_float2(t.top, static_cast<float>(log(t.sum))); }
-
-// Two sums over the CTA's threads (at most 1024), in an order of their number alone; the result on thread 0.
-struct Sums {
-  double a, b;
-};
-__device__ __forceinline__ Sums cta_sums(Sums s) {
-  __shared__ double first[32];
-  __shared__ double second[32];
-  const auto warp = [&] {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s.a += __shfl_xor_sync(0xFFFFFFFFu, s.a, o);
-      s.b += __shfl_xor_sync(0xFFFFFFFFu, s.b, o);
-    }
-  };
-  warp();
-  if ((threadIdx.x & 31) == 0) {
-    first[threadIdx.x >> 5] = s.a;
-    second[threadIdx.x >> 5] = s.b;
-  }
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    s.a = threadIdx.x < blockDim.x / 32 ? first[threadIdx.x] : 0.0;
-    s.b = threadIdx.x < blockDim.x / 32 ? second[threadIdx.x] : 0.0;
-    warp();
-  }
-  return s;
-}
-
 // The loss to where the caller wants it (flags: 2 added to what is there, 4 fp32).
 __device__ __forceinline__ void put_loss(void* loss, int flags, double sum) {
   if (flags & 4) {
@@ -124,9 +93,6 @@ __device__ __forceinline__ void put_loss(void* loss, int flags, double sum) {
     *out = flags & 2 ? *out + sum : sum;
   }
 }
-
-// The rows' part of zo_token_loss alone (p.loss and p.flags are not used): p.rows, and p.nll and p.lse where they are given.
-cudaError_t launch_token_rows(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream);
 
 template <typename F, typename... A>
 cudaError_t launch_with(F f, unsigned grid, unsigned threads, cudaLaunchAttribute attr, cudaStream_t stream, A... a) {

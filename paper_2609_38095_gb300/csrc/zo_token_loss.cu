@@ -68,7 +68,6 @@ __global__ void __launch_bounds__(kLossThreads, kLossCtas)
     const double nll = log(mine.sum) + (static_cast<double>(mine.top) - widen(x[target]));
     p.rows[t] = nll;
     if (p.nll != nullptr) p.nll[t] = static_cast<float>(nll);
-    if (p.lse != nullptr) p.lse[t] = row_lse(mine);
   }
 }
 
@@ -96,23 +95,40 @@ __global__ void __launch_bounds__(kLossThreads) token_loss_warp_kernel(const __g
     const double nll = log(all.sum) + (static_cast<double>(all.top) - widen(x[target]));
     p.rows[t] = nll;
     if (p.nll != nullptr) p.nll[t] = static_cast<float>(nll);
-    if (p.lse != nullptr) p.lse[t] = row_lse(all);
   }
 }
 
 // The tokens' sum in one CTA, in an order of their number alone. Launched so
 // that it may be resident before the tokens' kernel has ended.
 __global__ void __launch_bounds__(kSumThreads) token_loss_sum_kernel(const __grid_constant__ TokenLossParams p) {
+  __shared__ double sums[kSumThreads / 32];
+  __shared__ double counts[kSumThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   double sum = 0.0, count = 0.0;
   for (int64_t t = threadIdx.x; t < p.tokens; t += blockDim.x) {
     sum += p.rows[t];
     if (p.flags & 1) count += load_index(p.targets, t, p.target64) >= 0 ? 1.0 : 0.0;
   }
-  const Sums all = cta_sums({sum, count});
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    sums[threadIdx.x >> 5] = sum;
+    counts[threadIdx.x >> 5] = count;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  sum = threadIdx.x < blockDim.x / 32 ? sums[threadIdx.x] : 0.0;
+  count = threadIdx.x < blockDim.x / 32 ? counts[threadIdx.x] : 0.0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+  }
   if (threadIdx.x != 0) return;
-  sum = all.a;
-  if (p.flags & 1) sum = all.b > 0.0 ? sum / all.b : NAN;
+  if (p.flags & 1) sum = count > 0.0 ? sum / count : NAN;
   put_loss(p.loss, p.flags, sum);
 }
 
@@ -137,16 +153,13 @@ cudaError_t launch_rows(const TokenLossParams& p, int sms, cudaStream_t stream) 
 
 }  // namespace
 
-cudaError_t launch_token_rows(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream) {
-  if (p.tokens == 0) return cudaSuccess;
-  return dtype == 0   ? launch_rows<float>(p, sms, stream)
-         : dtype == 1 ? launch_rows<__nv_bfloat16>(p, sms, stream)
-                      : launch_rows<__half>(p, sms, stream);
-}
-
 cudaError_t launch_token_loss(const TokenLossParams& p, int dtype, int sms, cudaStream_t stream) {
-  const cudaError_t e = launch_token_rows(p, dtype, sms, stream);
-  if (e != cudaSuccess) return e;
+  if (p.tokens > 0) {
+    const cudaError_t e = dtype == 0   ? launch_rows<float>(p, sms, stream)
+                          : dtype == 1 ? launch_rows<__nv_bfloat16>(p, sms, stream)
+                                       : launch_rows<__half>(p, sms, stream);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
