@@ -1,6 +1,8 @@
 """1.5-SPSA steps of a small decoder whose losses are its own: the library's step (perturb, losses, precondition,
 update) around the library's forward point (head norms and rotation, attention of packed documents, token loss), then
-an answer of the trained weights, token by token over a paged cache.
+an answer of the trained weights, token by token over a paged cache, or several drafted tokens at once. Judged and
+Preferred are batches of a model's own answers, whose losses are those of learning from them; a step takes them as it takes
+documents.
 
 The model has the shape of the Qwen3 decoder in workloads.py at a small size: untied embedding and head, per layer
 q/k/v/o projections, per-head norms of queries and keys, SwiGLU, two RMSNorms. Its matrix products, root-mean-square
@@ -12,6 +14,7 @@ restore folded into the next probe's +eps, the last restore in the update.
 
     python decoder_step.py                          # a few steps and an answer, JSON lines
     python decoder_step.py --steps 20 --probes 32
+    python decoder_step.py --answers policy         # steps on the model's own answers; or: preference
 """
 import argparse
 import json
@@ -75,26 +78,67 @@ class Decoder:
         return attend
 
 
-class Batch:
-    """Packed documents of the task: tokens, positions, targets (-1: not counted) and spans."""
+class Packed:
+    """Documents packed one after another: tokens, positions, targets and spans. A document's first `given` targets are not
+    counted (-1)."""
+
+    def __init__(self, documents, given):
+        tokens, positions, targets, starts = [], [], [], [0]
+        for doc, skip in zip(documents, given):
+            doc = torch.as_tensor(doc)
+            tokens.append(doc[:-1])
+            targets.append(doc[1:].clone())
+            targets[-1][:skip] = -1
+            positions.append(torch.arange(len(doc) - 1))
+            starts.append(starts[-1] + len(doc) - 1)
+        self.tokens, self.positions, self.targets = (torch.cat(x).cuda() for x in (tokens, positions, targets))
+        self.starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        self.spans = forward.document_spans(self.starts, tokens=starts[-1])
+
+    def logits(self, model):
+        return model.logits(self.tokens, self.positions, model.packed(self.spans))
+
+
+class Batch(Packed):
+    """Documents of the task."""
 
     def __init__(self, lengths, vocab, seed):
         g = torch.Generator().manual_seed(seed)
-        tokens, positions, targets, starts = [], [], [], [0]
+        documents = []
         for n in lengths:
             first, stride = (int(torch.randint(1, 8, (1,), generator=g)) for _ in range(2))
-            doc = (first + stride * torch.arange(n + 1)) % vocab
-            tokens.append(doc[:-1])
-            targets.append(doc[1:].clone())
-            targets[-1][0] = -1                                   # the stride is not known yet
-            positions.append(torch.arange(n))
-            starts.append(starts[-1] + n)
-        self.tokens, self.positions, self.targets = (torch.cat(x).cuda() for x in (tokens, positions, targets))
-        self.spans = forward.document_spans(torch.tensor(starts, dtype=torch.int32, device="cuda"), tokens=starts[-1])
+            documents.append((first + stride * torch.arange(n + 1)) % vocab)
+        super().__init__(documents, [1] * len(documents))     # the stride is not known at the first token
 
     def loss_into(self, model, out):
-        logits = model.logits(self.tokens, self.positions, model.packed(self.spans))
-        forward.token_loss(logits, self.targets, mean=True, out=out)
+        forward.token_loss(self.logits(model), self.targets, mean=True, out=out)
+
+
+class Judged(Packed):
+    """Answers of the model with an advantage each: the clipped policy loss of their tokens, with a term that keeps the policy
+    near the one that gave them."""
+
+    def __init__(self, model, prompts, answers, advantages, kl=0.02):
+        super().__init__([p + a for p, a in zip(prompts, answers)], [len(p) - 1 for p in prompts])
+        each = torch.tensor(advantages, dtype=torch.float32, device="cuda")
+        self.advantages, self.kl = each.repeat_interleave(self.starts.diff().long()), kl
+        self.logp = -forward.token_loss(self.logits(model), self.targets, with_nll=True)[1]
+
+    def loss_into(self, model, out):
+        forward.policy_loss(self.logits(model), self.targets, self.logp, self.advantages, ref_logp=self.logp, kl=self.kl, mean=True,
+                            out=out)
+
+
+class Preferred(Packed):
+    """Pairs of answers to a prompt, the preferred one first: the loss of their log-ratios to the model that gave them."""
+
+    def __init__(self, model, prompts, pairs, beta=0.1):
+        super().__init__([p + a for p, pair in zip(prompts, pairs) for a in pair], [len(p) - 1 for p in prompts for _ in range(2)])
+        self.beta = beta
+        self.ref = forward.preference_loss(self.logits(model), self.targets, self.starts, with_logp=True)[1]
+
+    def loss_into(self, model, out):
+        forward.preference_loss(self.logits(model), self.targets, self.starts, ref_logp=self.ref, beta=self.beta, mean=True, out=out)
 
 
 def step(model, batch, seed, K, eps, lr):
@@ -165,12 +209,100 @@ class Answer:
         self.logits = self.model.logits(tokens, positions, attend)
         return self.logits
 
+    def draft(self, tokens, parents):
+        """Logits (sequences, nodes, vocabulary) after each node of a tree of drafted tokens per sequence: tokens and parents
+        (sequences, nodes), a parent ahead of its children, -1: the sequence's last token, -2: no node. Nothing is appended
+        until accept(); ValueError where a sequence's pages have no room for so many."""
+        batch, nodes = tokens.shape
+        if nodes > self.rows_left:
+            raise ValueError("a sequence's pages have no room for so many drafted tokens")
+        model, masks = self.model, forward.draft_masks(parents)
+        depth = ((masks[:, :, None] >> torch.arange(nodes, device="cuda")) & 1).sum(2) - 1
+        sequence = torch.arange(batch, device="cuda").repeat_interleave(nodes)
+        places = (self.lengths[:, None] + torch.arange(nodes, device="cuda")).flatten()     # node j's keys are row lengths + j
+        slots = torch.where(masks.flatten() != 0, self._slots(sequence, places.long()), -1)
+        positions = (self.lengths[:, None] + depth.clamp(min=0)).flatten().long()
+
+        def attend(i, q, k, v, pos):
+            kc, vc = self.caches[i]
+            q, _, _ = forward.rotate_heads(q, k, v, positions=pos, k_out=kc, v_out=vc, slots=slots, **model.heads_of(i))
+            q = q.view(batch, nodes, model.heads, model.head_dim)
+            return forward.draft_attention(q, kc, vc, self.pages, self.lengths, masks).flatten(0, 1)
+
+        self.drafted = model.logits(tokens.flatten().clamp(min=0), positions, attend).view(batch, nodes, -1)
+        return self.drafted
+
+    def accept(self, paths):
+        """Appends a path of the last draft()'s nodes to each sequence, a list of them from the root on (or none)."""
+        batch = len(paths)
+        sequence = torch.tensor([b for b, path in enumerate(paths) for _ in path], dtype=torch.long, device="cuda")
+        node = torch.tensor([j for path in paths for j in path], dtype=torch.long, device="cuda")
+        place = torch.tensor([i for path in paths for i in range(len(path))], dtype=torch.long, device="cuda")
+        start = self.lengths.long()[sequence]
+        source, target = self._slots(sequence, start + node), self._slots(sequence, start + place)
+        for pair in self.caches:
+            for cache in pair:
+                rows = cache.view(-1, self.model.kv_heads, self.model.head_dim)
+                rows[target] = rows[source]
+        last = torch.tensor([path[-1] if path else 0 for path in paths], device="cuda")
+        some = torch.tensor([bool(path) for path in paths], device="cuda")
+        self.logits = torch.where(some[:, None], self.drafted[torch.arange(batch, device="cuda"), last], self.logits)
+        self.lengths += torch.tensor([len(path) for path in paths], dtype=torch.int32, device="cuda")
+        self.rows_left -= max(len(path) for path in paths)
+
+    def greedy_drafted(self, n, propose):
+        """The tokens of greedy(n) -- up to ties -- in fewer passes: propose(sequences' tokens so far) gives a tree for each,
+        lists of tokens and parents; of each the longest path of tokens that greedy() would give is accepted, and the one that
+        comes behind it is known then."""
+        got = [[t] for t in self.logits.argmax(-1).tolist()]     # the last one is not in the cache yet
+        while min(map(len, got)) < n:
+            trees = [([g[-1]] + list(t), [-1] + [p + 1 for p in up]) for g, (t, up) in zip(got, propose(got))]
+            nodes = max(len(t) for t, _ in trees)
+            if not all(0 <= x < self.model.vocab for t, _ in trees for x in t):
+                raise ValueError("a proposed token is outside the vocabulary")
+            tokens, parents = (torch.tensor([x + [fill] * (nodes - len(x)) for x in xs], dtype=kind, device="cuda")
+                               for xs, fill, kind in (([t for t, _ in trees], 0, torch.long), ([up for _, up in trees], -2, torch.int32)))
+            best, paths = self.draft(tokens, parents).argmax(-1).tolist(), []
+            for b, (t, up) in enumerate(trees):
+                path = [0]
+                while True:
+                    nexts = [j for j in range(len(t)) if up[j] == path[-1] and t[j] == best[b][path[-1]]]
+                    got[b].append(best[b][path[-1]])
+                    if not nexts:
+                        break
+                    path.append(nexts[0])
+                paths.append(path)
+            self.accept(paths)
+        return torch.tensor([g[:n] for g in got], device="cuda")
+
     def greedy(self, n):
         got = []
         for _ in range(n):
             got.append(self.logits.argmax(-1))
             self.next(got[-1])
         return torch.stack(got, 1)
+
+
+def strides(got, vocab, most=4, deep=3):
+    """For each sequence a tree of what may come by the task's rule: up to `most` strides, `deep` tokens of each."""
+    trees = []
+    for g in got:
+        likely = [g[-1] - g[-2]] if len(g) > 1 else []
+        steps = (likely + [s for s in range(1, 8) if s not in likely])[:most]
+        tokens = [(g[-1] + s * (i + 1)) % vocab for s in steps for i in range(deep)]
+        trees.append((tokens, [j - 1 if j % deep else -1 for j in range(len(tokens))]))
+    return trees
+
+
+def answered(model, count, kind):
+    """Answers of the model to prompts of the task, judged by how many of their tokens follow the prompt's stride."""
+    prompts = [[(1 + i % 5) + (1 + i % 7) * j for j in range(4)] for i in range(count)]
+    first = Answer(model, prompts, 8).greedy(8).tolist()
+    right = [[p[-1] + (p[1] - p[0]) * (i + 1) for i in range(8)] for p in prompts]
+    if kind == "preference":
+        return Preferred(model, prompts, list(zip(right, first)))
+    score = torch.tensor([[float(x == y) for x, y in zip(a, r)] for a, r in zip(first + right, right + right)]).mean(1)
+    return Judged(model, prompts + prompts, first + right, (score - score.mean()).tolist())
 
 
 def main():
@@ -180,18 +312,20 @@ def main():
     ap.add_argument("--documents", type=int, default=12)
     ap.add_argument("--eps", type=float, default=1e-3)
     ap.add_argument("--lr", type=float, default=1e-3)
+    ap.add_argument("--answers", choices=["policy", "preference"], help="steps on the model's own answers in place of documents")
     a = ap.parse_args()
     model = Decoder(dtype=torch.float32)      # at eps = 1e-3 a perturbation of bf16 weights of this size is mostly lost
     for s in range(a.steps):
         lengths = [5 + (37 * s + 53 * i) % 251 for i in range(a.documents)]
         torch.cuda.synchronize()
         t = time.perf_counter()
-        table, status = step(model, Batch(lengths, model.vocab, s), STEP_SEED_BASE + s, a.probes, a.eps, a.lr)
+        batch = answered(model, a.documents, a.answers) if a.answers else Batch(lengths, model.vocab, s)
+        table, status = step(model, batch, STEP_SEED_BASE + s, a.probes, a.eps, a.lr)
         loss = float(table[0, 2])
-        print(json.dumps({"step": s, "tokens": sum(lengths), "loss": loss, "status": int(status),
+        print(json.dumps({"step": s, "tokens": len(batch.tokens), "loss": loss, "status": int(status),
                           "ms": 1e3 * (time.perf_counter() - t)}), flush=True)
     prompts = [[3, 5, 7, 9], [1, 2, 3, 4, 5, 6]]
-    print(json.dumps({"answers": Answer(model, prompts, 8).greedy(8).tolist()}))
+    print(json.dumps({"answers": Answer(model, prompts, 24).greedy_drafted(8, lambda got: strides(got, model.vocab)).tolist()}))
 
 
 if __name__ == "__main__":
