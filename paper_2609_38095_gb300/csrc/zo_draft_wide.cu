@@ -466,6 +466,8 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         if constexpr (kColumns == 64) tie32(x[1]);
       }
       const auto score = [&](int e) -> uint32_t& { return x[e / kWidth][e % kWidth]; };
+      const auto two = [&](int e) { return static_cast<uint64_t>(score(e + 1)) << 32 | score(e); };
+      const auto put_two = [&](int e, uint64_t y) { score(e) = static_cast<uint32_t>(y), score(e + 1) = static_cast<uint32_t>(y >> 32); };
       const int key0 = (begin + c) * kKeys + copy * kColumns;  // (the last step's end is below 2^31)
       const bool nodes = key0 + kColumns > w.n;  // keys of the tree, or beyond the last
       if (cap) {
@@ -476,24 +478,21 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         if (__builtin_expect(__all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap), 1)) {
           const uint64_t over2 = pack2(scale2, scale2), caps = pack2(cap2, cap2);
 #pragma unroll
-          for (int e = 0; e < kColumns; e += 2) {
-            const uint64_t y = capped_near(static_cast<uint64_t>(score(e + 1)) << 32 | score(e), over2, caps);
-            score(e) = static_cast<uint32_t>(y), score(e + 1) = static_cast<uint32_t>(y >> 32);
-          }
+          for (int e = 0; e < kColumns; e += 2) put_two(e, capped_near(two(e), over2, caps));
         } else {
 #pragma unroll
           for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(capped(__uint_as_float(score(e)), scale2, cap2));
         }
       } else if (!kPlain) {
 #pragma unroll
-        for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(__uint_as_float(score(e)) * scale2);
+        for (int e = 0; e < kColumns; e += 2) put_two(e, mul2(two(e), pack2(scale2, scale2)));
       }
       if (bias) {
         const float away = static_cast<float>(w.n - key0 + depth);  // exact, and its differences, below 2^24
         if (__builtin_expect(!nodes, 1)) {
 #pragma unroll
-          for (int e = 0; e < kColumns; ++e)
-            score(e) = __float_as_uint(fmaf(-slope2, away - static_cast<float>(e), __uint_as_float(score(e))));
+          for (int e = 0; e < kColumns; e += 2)
+            put_two(e, fma2(pack2(-slope2, -slope2), add2(pack2(away, away), pack2(-static_cast<float>(e), -static_cast<float>(e + 1))), two(e)));
         } else {
 #pragma unroll
           for (int e = 0; e < kColumns; ++e) {
@@ -545,7 +544,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       uint32_t weights[kColumns / 2];
 #pragma unroll
       for (int i = 0; i < kColumns / 2; ++i) {
-        const uint64_t t = fma2(pack2(__uint_as_float(score(2 * i)), __uint_as_float(score(2 * i + 1))), times2, shift2);
+        const uint64_t t = fma2(two(2 * i), times2, shift2);
         const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
         sums[i & 1] = add2(sums[i & 1], pack2(u, v));
         weights[i] = narrow2<T>(u, v);
@@ -689,7 +688,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
 // 32 rows of a block, a lane per row: the pieces of their block, if there is more than one; rows that see nothing, and those of
 // sequences whose pages are none. Warps share the columns, and the rows leave through shared memory.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_constant__ WideParams p) {
+__global__ void __launch_bounds__(256, 4) draft_wide_join_kernel(const __grid_constant__ WideParams p) {
   constexpr int kWarps = 8, kMine = D / 4 / kWarps;  // a warp's vectors of 4 columns
   constexpr int kPitch = D + 8;                      // 16-bit elements of a row
   __shared__ __align__(16) T tile[32 * kPitch];
@@ -726,7 +725,7 @@ __global__ void __launch_bounds__(256) draft_wide_join_kernel(const __grid_const
     whole = from == last;
     if (!whole) {
       const auto place = [&](int64_t i) { return 2 * i + (split && i == from_first); };
-      constexpr int kAtOnce = 4;
+      constexpr int kAtOnce = 2;
       for (int64_t i0 = from; i0 <= last; i0 += kAtOnce) {
         float2 part[kAtOnce];
         float4 y[kAtOnce][kMine];

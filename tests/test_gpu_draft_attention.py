@@ -330,12 +330,16 @@ def test_offsets_beyond_32_bits():
     compare(q, args, [(k[:n + drafts], v[:n + drafts])], [n], masks)
 
 
-@pytest.mark.parametrize("drafts", [5, 64])
-def test_repeatable_stream_and_graph(drafts):
+@pytest.mark.parametrize("drafts,room", [(5, 0), (64, 0), (5, 100_000), (64, 100_000)])
+def test_repeatable_stream_and_graph(drafts, room):
     g = gen(6)
     lengths = [3000, 17]
     masks = padded(trees(7, [drafts, 3]), drafts)
     args, rows = paged(g, lengths, masks, 16, 8, 128, torch.bfloat16)
+    if room:                                            # a page table for long answers
+        table = torch.zeros(2, room // 16, dtype=torch.int32, device="cuda")
+        table[:, :args[2].shape[1]] = args[2]
+        args = (*args[:2], table, *args[3:])
     q = randn(g, 2, drafts, 32, 128, dtype=torch.bfloat16)
     want = F.draft_attention(q, *args)
     for _ in range(3):
@@ -354,9 +358,11 @@ def test_repeatable_stream_and_graph(drafts):
     s.synchronize()
     assert torch.equal(got, want)
     other = torch.cuda.Stream()
-    for graph, stream in zip(graphs, (s, other)):       # side by side
-        with torch.cuda.stream(stream):
-            graph.replay()
+    for _ in range(3):
+        for graph, stream in zip(graphs, (s, other)):   # side by side, and beside a call
+            with torch.cuda.stream(stream):
+                graph.replay()
+        assert torch.equal(F.draft_attention(q, *args), want)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
