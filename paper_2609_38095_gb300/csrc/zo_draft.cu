@@ -80,12 +80,16 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
   struct Place {
     int64_t k, v;
   };
+  // With a bias by distance the tiles in turn from the last to the first: a row's largest scores come first then, and its output
+  // is not rescaled at every tile.
+  const bool backward = p.slopes != nullptr;
+  const auto key_of = [&](int64_t tile) { return (backward ? tiles_in - 1 - tile : tile) * L::kKeys; };
   const auto look = [&](int64_t tile) {
-    const int64_t j = tile * L::kKeys + lane % L::kKeys;
-    return draft_sees(w, j) ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+    const int64_t j = key_of(tile) + lane % L::kKeys;
+    return j >= 0 && draft_sees(w, j) ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
   };
   const auto find = [&](int64_t tile, int id) {
-    const int64_t j = tile * L::kKeys + lane % L::kKeys;
+    const int64_t j = key_of(tile) + lane % L::kKeys;
     const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
     Place at = {-1, -1};
     if (key.x >= 0) {
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
         }
       }
     }
-    const int64_t key0 = tile * L::kKeys;
+    const int64_t key0 = key_of(tile);
     const bool nodes = key0 + L::kKeys > w.n;  // keys of the tree, or beyond the last
     float times = scale2;  // what the scores are in, times
     if (p.softcap > 0.0f) {
