@@ -304,9 +304,9 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     bool alive = true;
     int issued = 0;
     for (int l = 0; l < 2 * n && alive; ++l) {
-      if (l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
+      const bool tiled = whole(step_of(l)), mine = !tiled || half == l % 2;  // by TMA one warp has the keys, the other the values
+      if (mine && l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
       if (!alive) break;
-      const bool tiled = whole(step_of(l));
       if (l % 2 == 0) {
         if (tiled) {
           const uint32_t j = static_cast<uint32_t>(begin + step_of(l)) * kKeys + lane * p.rows_at_once;
@@ -326,14 +326,14 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         }
         if (l + 2 < 2 * n && !whole(step_of(l + 2))) id = look(step_of(l + 2));
       }
-      if (tiled) {  // one of the two warps has the keys, the other the values
+      if (tiled) {
         uint64_t* const full = &sh.full[l % L::kStages];
-        if (lane == 0) {
-          if (half == l % 2) mbar_expect(full, L::kTile);
-          else mbar_arrive(full);
+        if (mine && lane == 0) {
+          mbar_expect(full, L::kTile);
+          mbar_arrive(full);  // for the other
         }
         __syncwarp();
-        if (half == l % 2 && lane < boxes) {
+        if (mine && lane < boxes) {
           uint8_t* const to = stages + l % L::kStages * L::kTile + lane * p.rows_at_once * 128;
 #pragma unroll
           for (int c = 0; c < D / 64; ++c)
