@@ -51,7 +51,12 @@ __device__ __forceinline__ bool not_finite2(uint32_t v) {
 // tiles of 16 or 32 keys, by cp.async into its own shared memory, and shares
 // nothing until its last; but the rows are the products' rows, S = Q K^T and
 // O += P V, so that a step's scores are the next product's left operand as they
-// are. What a row sees of the tree's own keys is a bit of its node's mask.
+// are. What a row sees of the tree's own keys is a bit of its node's mask. For few
+// rows or short sequences, and heads beyond 128: bound by latency, the chain
+// length and masks -> pages -> keys -> products -> joins and the code's own way into
+// the instruction caches (one sequence of 2039 keys, 8 nodes, 32 / 8 heads of 128,
+// bf16: 16.4 us a call, where its bytes take 1.3). Every 32
+// rows read the keys again: zo_draft_wide.cu takes over where that costs more.
 template <typename T, int DP, int MB>
 __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 64 ? 3 : 2)
     draft_mma_kernel(const __grid_constant__ DraftParams p) {

@@ -115,7 +115,8 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
       };
       const uint64_t a = mask(lane), b = mask(lane + 32);
       const DraftKeys k = draft_keys(p, max(n, 0), n >= 0 ? a : 0, n >= 0 ? b : 0);
-      const int count = k.bad ? 0 : static_cast<int>((k.len + kKeys - 1) / kKeys), per_step = units_of_step(min(k.nodes * p.group, p.block));
+      const int count = k.bad ? 0 : static_cast<int>((k.len + kKeys - 1) / kKeys);
+      const int per_step = units_of_step(min(k.nodes * p.group, p.block));
       const int64_t each = count == 0 ? 0 : kStart + count * static_cast<int64_t>(per_step);
       const int blocks = (k.nodes * p.group + p.block - 1) / p.block;
       if (lane == 0) {
@@ -158,6 +159,16 @@ __global__ void __launch_bounds__(1024) draft_wide_plan_kernel(const __grid_cons
 //   the next (two)    the products of slot 0 (1)
 //   the last two      keys and values: by TMA, a lane per page, where a step has no key of the tree and pages and steps begin
 //                     together; else by cp.async, a lane per key
+//
+// 16 sequences of up to 16384 keys, trees of up to 64 nodes, 32 / 8 heads of 128, bf16 (646 MB, 97 us by HBM): 138 us, of which
+// 5 plan and launch, 115 to 120 are the steps and 11 the join. A step takes 0.65 us with up to 64 rows, which is HBM's rate
+// (152 x 32 KB), 0.84 with 256, whose softmax and products take turns as in zo_attention_mma.cu; a piece's start and end cost
+// some 8. On the way: clusters per block of rows joined over distributed shared memory 356 us (an SM had work for two thirds
+// of the time: a cluster of 8 waits for 8 SMs of a GPC, and lengths are unequal); equal runs of steps 281; pages by TMA instead of cp.async 183
+// (two warps cannot issue 32 KB of 16-byte copies and their addresses per 0.7 us); pieces by columns 160 (by rows a warp's store
+// touches 32 lines); shares by what a step and a start were measured at, loads ahead of the queries 149; pages looked up in
+// groups 145. 16 of up to 4001 keys, trees of 26, 32 heads of 64, fp16, capped and biased (49 us by HBM): 92 us, with one copy of
+// the rows 180, two 119; a step is held by the softmax's latency (1000 cycles) and the issue of TMA for pages of 16 rows.
 template <typename T, int D, int kSlots, int kCopies, bool kPlain>
 __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
     draft_wide_kernel(const __grid_constant__ WideParams p, const __grid_constant__ CUtensorMap k_map,
@@ -186,503 +197,515 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
   const int64_t stop = blockIdx.x < runs.ctas ? runs.first(blockIdx.x + 1) : 0;
   bool again = false;
   for (int64_t at_unit = start; at_unit < stop;) {
-  // the last sequence whose steps begin here or before: by 32 places at a time
-  int64_t b = 0;
-  for (int64_t end = p.batch; end - b > 1;) {
-    const int64_t stride = (end - b + 31) / 32, mine = b + lane * stride;
-    const uint32_t before = __ballot_sync(0xFFFFFFFFu, mine < end && p.prefix[mine] <= at_unit);
-    b += (31 - __clz(before)) * stride;
-    end = min(end, b + stride);
-  }
-  const int4 shape = p.shape[b];
-  const int64_t inside = at_unit - p.prefix[b];
-  const int item = static_cast<int>(inside / shape.x), from = static_cast<int>(inside - static_cast<int64_t>(item) * shape.x);
-  const int units = static_cast<int>(min(static_cast<int64_t>(shape.x - from), stop - at_unit));
-  const int begin = steps_before(from, shape.z), n = steps_before(from + static_cast<int64_t>(units), shape.z) - begin;
-  if (n == 0) {
-    at_unit += units;
-    continue;
-  }
-  const int g = item / shape.w;
-  const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.w, sh.rows);
-  const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
-  const int live = w.live;
-  const auto warps_of = [&](int s) { return kCopies > 1 ? kCopies * ((live + 31) / 32) : max(0, min(4, (live - s * kRows + 31) / 32)); };
-
-  if (tid == L::kThreads - 32) {
-    const int slots = (live + kRows - 1) / kRows;
-    const auto barrier = [&](uint64_t* x, int count) {
-      if (again) mbar_inval(x);
-      mbar_init(x, count > 0 ? count : 1);
-    };
-    for (int i = 0; i < L::kStages; ++i) {
-      barrier(&sh.full[i], kLoaders);
-      barrier(&sh.empty[i], slots);
+    // the last sequence whose steps begin here or before: by 32 places at a time
+    int64_t b = 0;
+    for (int64_t end = p.batch; end - b > 1;) {
+      const int64_t stride = (end - b + 31) / 32, mine = b + lane * stride;
+      const uint32_t before = __ballot_sync(0xFFFFFFFFu, mine < end && p.prefix[mine] <= at_unit);
+      b += (31 - __clz(before)) * stride;
+      end = min(end, b + stride);
     }
-    for (int s = 0; s < kSlots; ++s) {
-      for (int b = 0; b < 2; ++b) {
-        barrier(&sh.s_full[s][b], 1);
-        barrier(&sh.p_full[s][b], warps_of(s));
-        barrier(&sh.o_done[s][b], 1);
+    const int4 shape = p.shape[b];
+    const int64_t inside = at_unit - p.prefix[b];
+    const int item = static_cast<int>(inside / shape.x), from = static_cast<int>(inside - static_cast<int64_t>(item) * shape.x);
+    const int units = static_cast<int>(min(static_cast<int64_t>(shape.x - from), stop - at_unit));
+    const int begin = steps_before(from, shape.z), n = steps_before(from + static_cast<int64_t>(units), shape.z) - begin;
+    if (n == 0) {
+      at_unit += units;
+      continue;
+    }
+    const int g = item / shape.w;
+    const DraftPlace w = draft_place<L::kBlock>(p, static_cast<int>(b), g, item - g * shape.w, sh.rows);
+    const DraftRows<T, L::kBlock> rows = {p, w, sh.rows};
+    const int live = w.live;
+    const auto warps_of = [&](int s) {
+      return kCopies > 1 ? kCopies * ((live + 31) / 32) : max(0, min(4, (live - s * kRows + 31) / 32));
+    };
+
+    if (tid == L::kThreads - 32) {
+      const int slots = (live + kRows - 1) / kRows;
+      const auto barrier = [&](uint64_t* x, int count) {
+        if (again) mbar_inval(x);
+        mbar_init(x, count > 0 ? count : 1);
+      };
+      for (int i = 0; i < L::kStages; ++i) {
+        barrier(&sh.full[i], kLoaders);
+        barrier(&sh.empty[i], slots);
       }
-      barrier(&sh.drain[s], 1);
+      for (int s = 0; s < kSlots; ++s) {
+        for (int b = 0; b < 2; ++b) {
+          barrier(&sh.s_full[s][b], 1);
+          barrier(&sh.p_full[s][b], warps_of(s));
+          barrier(&sh.o_done[s][b], 1);
+        }
+        barrier(&sh.drain[s], 1);
+      }
+      sh.any_odd = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    sh.any_odd = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  again = true;
-  // With a bias by distance from the last step to the first: a row's largest scores come first then, and its output is not
-  // rescaled at every step (26 rows of 32 heads of 64: 100 -> 96 us).
-  constexpr bool kBackward = !kPlain;
-  const auto step_of = [&](int l) { return kBackward ? n - 1 - l / 2 : l / 2; };  // of tile l
-  // the warps of the softmax and the products; the loads need not wait for the queries
-  const auto softmax_warps = [] { asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory"); };
-  const auto queries_there = [] { asm volatile("bar.sync 1, %0;" ::"n"((kSoftmaxWarps + kSlots) * 32) : "memory"); };
-  for (int i = tid; i < 64 * 4; i += L::kThreads) (&sh.odd[0][0])[i] = 0;
-  __syncthreads();
+    again = true;
+    // With a bias by distance from the last step to the first: a row's largest scores come first then, and its output is not
+    // rescaled at every step (26 rows of 32 heads of 64: 100 -> 96 us).
+    constexpr bool kBackward = !kPlain;
+    const auto step_of = [&](int l) { return kBackward ? n - 1 - l / 2 : l / 2; };  // of tile l
+    // the warps of the softmax and the products; the loads need not wait for the queries
+    const auto softmax_warps = [] { asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory"); };
+    const auto queries_there = [] { asm volatile("bar.sync 1, %0;" ::"n"((kSoftmaxWarps + kSlots) * 32) : "memory"); };
+    for (int i = tid; i < 64 * 4; i += L::kThreads) (&sh.odd[0][0])[i] = 0;
+    __syncthreads();
 
-  if (warp >= kSoftmaxWarps + kSlots) {
-    // Tile l is a step's keys (even) or values. Each of the two warps has 32 of its keys, a lane one of their places.
-    const int half = warp - kSoftmaxWarps - kSlots;
-    const T* kc = static_cast<const T*>(p.k) + w.g * p.k_head;
-    const T* vc = static_cast<const T*>(p.v) + w.g * p.v_head;
-    const int vector = lane % kVectors;
-    const int bytes = vector * 8 < p.dim ? 16 : 0;  // of a vector; the rest is filled with zeros
-    const char* kl = reinterpret_cast<const char*>(kc + (bytes ? vector * 8 : 0));
-    const char* vl = reinterpret_cast<const char*>(vc + (bytes ? vector * 8 : 0));
-    constexpr int kAtOnce = 32 / kVectors;  // keys of a warp's copy
-    const auto place_of = [&](int l, int i) {  // in a stage: the lane's vector of copy i
-      const int r = half * 32 + i * kAtOnce + lane / kVectors;
-      return stages + l % L::kStages * L::kTile + vector / 8 * L::kTileChunk + r * 128 + ((vector % 8 ^ (r & 7)) << 4);
-    };
-    int bad = 0;
-    const auto key_of = [&](int step) { return static_cast<int64_t>(begin + step) * kKeys + half * 32 + lane; };
-    const auto look = [&](int step) {
-      const int64_t j = key_of(step);
-      return draft_sees(w, j) ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
-    };
-    const auto arrived = [&](int l) {  // tile l's copies are done
-      if (l & 1) {
-        const int64_t key0 = static_cast<int64_t>(begin + step_of(l)) * kKeys;
-        if (key0 + kKeys > w.n) {
-          // Values of the tree's keys that are not finite are noted and taken out: a row that does not see one has the
-          // weight 0 there, and 0 times it is NaN.
+    if (warp >= kSoftmaxWarps + kSlots) {
+      // Tile l is a step's keys (even) or values. Each of the two warps has 32 of its keys, a lane one of their places.
+      const int half = warp - kSoftmaxWarps - kSlots;
+      const T* kc = static_cast<const T*>(p.k) + w.g * p.k_head;
+      const T* vc = static_cast<const T*>(p.v) + w.g * p.v_head;
+      const int vector = lane % kVectors;
+      const int bytes = vector * 8 < p.dim ? 16 : 0;  // of a vector; the rest is filled with zeros
+      const char* kl = reinterpret_cast<const char*>(kc + (bytes ? vector * 8 : 0));
+      const char* vl = reinterpret_cast<const char*>(vc + (bytes ? vector * 8 : 0));
+      constexpr int kAtOnce = 32 / kVectors;  // keys of a warp's copy
+      const auto place_of = [&](int l, int i) {  // in a stage: the lane's vector of copy i
+        const int r = half * 32 + i * kAtOnce + lane / kVectors;
+        return stages + l % L::kStages * L::kTile + vector / 8 * L::kTileChunk + r * 128 + ((vector % 8 ^ (r & 7)) << 4);
+      };
+      int bad = 0;
+      const auto key_of = [&](int step) { return static_cast<int64_t>(begin + step) * kKeys + half * 32 + lane; };
+      const auto look = [&](int step) {
+        const int64_t j = key_of(step);
+        return draft_sees(w, j) ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+      };
+      const auto arrived = [&](int l) {  // tile l's copies are done
+        if (l & 1) {
+          const int64_t key0 = static_cast<int64_t>(begin + step_of(l)) * kKeys;
+          if (key0 + kKeys > w.n) {
+            // Values of the tree's keys that are not finite are noted and taken out: a row that does not see one has the
+            // weight 0 there, and 0 times it is NaN.
 #pragma unroll 4
-          for (int i = 0; i < 32 / kAtOnce; ++i) {
-            const int64_t node = key0 + half * 32 + i * kAtOnce + lane / kVectors - w.n;
-            uint16_t* x = reinterpret_cast<uint16_t*>(place_of(l, i));
-            const uint4 u = *reinterpret_cast<const uint4*>(x);
-            if (node < 0 || node >= 64 || !(odd32<T>(u.x) || odd32<T>(u.y) || odd32<T>(u.z) || odd32<T>(u.w))) continue;
-            for (int e = 0; e < 8; ++e)
-              if (odd16<T>(x[e])) {
-                const int column = vector * 8 + e;
-                atomicOr(&sh.odd[node][column / 32], 1u << column % 32);
-                sh.any_odd = 1;
-                x[e] = 0;
-              }
+            for (int i = 0; i < 32 / kAtOnce; ++i) {
+              const int64_t node = key0 + half * 32 + i * kAtOnce + lane / kVectors - w.n;
+              uint16_t* x = reinterpret_cast<uint16_t*>(place_of(l, i));
+              const uint4 u = *reinterpret_cast<const uint4*>(x);
+              if (node < 0 || node >= 64 || !(odd32<T>(u.x) || odd32<T>(u.y) || odd32<T>(u.z) || odd32<T>(u.w))) continue;
+              for (int e = 0; e < 8; ++e)
+                if (odd16<T>(x[e])) {
+                  const int column = vector * 8 + e;
+                  atomicOr(&sh.odd[node][column / 32], 1u << column % 32);
+                  sh.any_odd = 1;
+                  x[e] = 0;
+                }
+            }
           }
         }
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.full[l % L::kStages]);
-    };
-    // by TMA: a box of rows_at_once keys of a page; lanes hold the pages of as many steps as there is room for, and of the next as
-    // many (a page looked up a step ahead would be waited for: 1.0 us of a step of 64 x 64 elements, which takes 0.7)
-    const int boxes = p.rows_at_once > 0 ? kKeys / p.rows_at_once : 0, held = boxes > 0 ? 32 / boxes : 1;
-    const auto whole = [&](int step) { return boxes > 0 && static_cast<int64_t>(begin + step + 1) * kKeys <= w.n; };
-    const auto look_pages = [&](int l) {  // of the steps from tile l on
-      const int step = boxes == 0 ? -1 : kBackward ? step_of(l) - lane / boxes : step_of(l) + lane / boxes;
-      const int64_t j = static_cast<int64_t>(begin + step) * kKeys + lane % (boxes > 0 ? boxes : 1) * p.rows_at_once;
-      return step >= 0 && step < n && j < w.n ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
-    };
-    int first_tiled = 0;  // backward, the first step may hold the tree's keys, and the second
-    while (kBackward && boxes > 0 && first_tiled < 2 * n && !whole(step_of(first_tiled))) first_tiled += 2;
-    int ids = look_pages(first_tiled), next_ids = look_pages(first_tiled + 2 * held), at_id = 0;
-    int id = whole(step_of(0)) ? 0 : look(step_of(0)), box_page = 0, box_row = 0;
-    int64_t k_at = -1, v_at = -1;
-    bool alive = true;
-    int issued = 0;
-    for (int l = 0; l < 2 * n && alive; ++l) {
-      const bool tiled = whole(step_of(l)), mine = !tiled || half == l % 2;  // by TMA one warp has the keys, the other the values
-      if (mine && l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
-      if (!alive) break;
-      if (l % 2 == 0) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.full[l % L::kStages]);
+      };
+      // by TMA: a box of rows_at_once keys of a page; lanes hold the pages of as many steps as there is room for, and of as many
+      // behind them (a page looked up a step ahead would be waited for: 1.0 us of a step of 64 x 64 elements, which takes 0.7)
+      const int boxes = p.rows_at_once > 0 ? kKeys / p.rows_at_once : 0, held = boxes > 0 ? 32 / boxes : 1;
+      const auto whole = [&](int step) { return boxes > 0 && static_cast<int64_t>(begin + step + 1) * kKeys <= w.n; };
+      const auto look_pages = [&](int l) {  // of the steps from tile l on
+        const int step = boxes == 0 ? -1 : kBackward ? step_of(l) - lane / boxes : step_of(l) + lane / boxes;
+        const int64_t j = static_cast<int64_t>(begin + step) * kKeys + lane % (boxes > 0 ? boxes : 1) * p.rows_at_once;
+        return step >= 0 && step < n && j < w.n ? p.pages[w.b * p.pages_stride + decode_page(p, j)] : 0;
+      };
+      int first_tiled = 0;  // backward, the first step may hold the tree's keys, and the second
+      while (kBackward && boxes > 0 && first_tiled < 2 * n && !whole(step_of(first_tiled))) first_tiled += 2;
+      int ids = look_pages(first_tiled), next_ids = look_pages(first_tiled + 2 * held), at_id = 0;
+      int id = whole(step_of(0)) ? 0 : look(step_of(0)), box_page = 0, box_row = 0;
+      int64_t k_at = -1, v_at = -1;
+      bool alive = true;
+      int issued = 0;
+      for (int l = 0; l < 2 * n && alive; ++l) {
+        const bool tiled = whole(step_of(l)), mine = !tiled || half == l % 2;  // by TMA one warp has the keys, the other the values
+        if (mine && l >= L::kStages) alive = mbar_wait_warp(&sh.empty[l % L::kStages], (l / L::kStages - 1) & 1, dead);
+        if (!alive) break;
+        if (l % 2 == 0) {
+          if (tiled) {
+            const uint32_t j = static_cast<uint32_t>(begin + step_of(l)) * kKeys + lane * p.rows_at_once;
+            box_page = __shfl_sync(0xFFFFFFFFu, ids, (at_id * boxes + lane) & 31);
+            box_row = static_cast<int>(j - decode_page(p, j) * static_cast<uint32_t>(p.page_size));
+            if (lane < boxes && (box_page < 0 || box_page >= p.n_pages)) bad = 1;  // (and zeros come)
+            if (++at_id == held) {
+              at_id = 0;
+              ids = next_ids;
+              next_ids = look_pages(l + 2 + 2 * held);
+            }
+          } else {
+            const int64_t j = key_of(step_of(l));
+            const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
+            k_at = key.x >= 0 ? (key.x * p.k_page + key.y * p.k_token) * 2 : -1;
+            v_at = key.x >= 0 ? (key.x * p.v_page + key.y * p.v_token) * 2 : -1;
+          }
+          if (l + 2 < 2 * n && !whole(step_of(l + 2))) id = look(step_of(l + 2));
+        }
         if (tiled) {
-          const uint32_t j = static_cast<uint32_t>(begin + step_of(l)) * kKeys + lane * p.rows_at_once;
-          box_page = __shfl_sync(0xFFFFFFFFu, ids, (at_id * boxes + lane) & 31);
-          box_row = static_cast<int>(j - decode_page(p, j) * static_cast<uint32_t>(p.page_size));
-          if (lane < boxes && (box_page < 0 || box_page >= p.n_pages)) bad = 1;  // (and zeros come)
-          if (++at_id == held) {
-            at_id = 0;
-            ids = next_ids;
-            next_ids = look_pages(l + 2 + 2 * held);
+          uint64_t* const full = &sh.full[l % L::kStages];
+          if (mine && lane == 0) {
+            mbar_expect(full, L::kTile);
+            mbar_arrive(full);  // for the other
           }
+          __syncwarp();
+          if (mine && lane < boxes) {
+            uint8_t* const to = stages + l % L::kStages * L::kTile + lane * p.rows_at_once * 128;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_4d(to + c * L::kTileChunk, l % 2 == 0 ? &k_map : &v_map, c * 64, w.g, box_row, box_page, full);
+          }
+          __syncwarp();
         } else {
-          const int64_t j = key_of(step_of(l));
-          const int2 key = decode_key(p, w, draft_sees(w, j) ? j : w.len, id, bad);
-          k_at = key.x >= 0 ? (key.x * p.k_page + key.y * p.k_token) * 2 : -1;
-          v_at = key.x >= 0 ? (key.x * p.v_page + key.y * p.v_token) * 2 : -1;
-        }
-        if (l + 2 < 2 * n && !whole(step_of(l + 2))) id = look(step_of(l + 2));
-      }
-      if (tiled) {
-        uint64_t* const full = &sh.full[l % L::kStages];
-        if (mine && lane == 0) {
-          mbar_expect(full, L::kTile);
-          mbar_arrive(full);  // for the other
-        }
-        __syncwarp();
-        if (mine && lane < boxes) {
-          uint8_t* const to = stages + l % L::kStages * L::kTile + lane * p.rows_at_once * 128;
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_4d(to + c * L::kTileChunk, l % 2 == 0 ? &k_map : &v_map, c * 64, w.g, box_row, box_page, full);
+          for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const int64_t at = __shfl_sync(0xFFFFFFFFu, l % 2 == 0 ? k_at : v_at, i * kAtOnce + lane / kVectors);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_address(place_of(l, i))),
+                         "l"((l % 2 == 0 ? kl : vl) + (at >= 0 ? at : 0)), "r"(at >= 0 ? bytes : 0)
+                         : "memory");
+          }
         }
-        __syncwarp();
-      } else {
-#pragma unroll
-        for (int i = 0; i < 32 / kAtOnce; ++i) {
-          const int64_t at = __shfl_sync(0xFFFFFFFFu, l % 2 == 0 ? k_at : v_at, i * kAtOnce + lane / kVectors);
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_address(place_of(l, i))),
-                       "l"((l % 2 == 0 ? kl : vl) + (at >= 0 ? at : 0)), "r"(at >= 0 ? bytes : 0)
-                       : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ++issued;
+        if (l >= L::kAhead) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
+          if (!whole(step_of(l - L::kAhead))) arrived(l - L::kAhead);
         }
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      ++issued;
-      if (l >= L::kAhead) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
-        if (!whole(step_of(l - L::kAhead))) arrived(l - L::kAhead);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (alive)
+        for (int l = max(0, issued - L::kAhead); l < issued; ++l)
+          if (!whole(step_of(l))) arrived(l);
+      if (lane == 0 && *dead) {  // nothing may land in shared memory after the CTA is gone
+        const long long start = clock64();
+        for (int l = max(0, issued - L::kStages); l < issued; ++l)
+          while (whole(step_of(l)) && !mbar_try(&sh.full[l % L::kStages], l / L::kStages & 1) && clock64() - start < kWaitCycles) {}
       }
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    if (alive)
-      for (int l = max(0, issued - L::kAhead); l < issued; ++l)
-        if (!whole(step_of(l))) arrived(l);
-    if (lane == 0 && *dead) {  // nothing may land in shared memory after the CTA is gone
-      const long long start = clock64();
-      for (int l = max(0, issued - L::kStages); l < issued; ++l)
-        while (whole(step_of(l)) && !mbar_try(&sh.full[l % L::kStages], l / L::kStages & 1) && clock64() - start < kWaitCycles) {}
-    }
-    __syncwarp();
-    // the barriers are made anew for the next block: every arrival has come before that
-    for (int l = max(0, 2 * n - L::kStages); l < 2 * n && alive; ++l)
-      alive = mbar_wait_warp(&sh.empty[l % L::kStages], l / L::kStages & 1, dead);
-    if (bad) p.bad[w.b] = 1;
-  } else if (warp >= kSoftmaxWarps) {
-    const int s = warp - kSoftmaxWarps;
-    const uint32_t at = uniform(smem_address(stages));
-    const uint64_t queries = operand_desc(uniform(smem_address(tiles)) + s * L::kQueries, 16, 1024);
-    const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, L::kTileChunk, 1024);
-    constexpr uint32_t kScores = mma_desc(kBf16, kKeys, false), kOutput = mma_desc(kBf16, D, true);
-    const uint32_t scores = tmem + s * 128, out = tmem + L::kOutputs + s * D;
-    const int mine = warps_of(s) > 0 ? n : 0;
-    const auto scores_of = [&](int i) {  // one thread; step i's keys are there
-      const int stage = 2 * i % L::kStages;
-      const uint64_t k = keys + static_cast<uint32_t>(stage) * L::kTile / 16;
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d)
-        mma_ss(scores + (i & 1) * kKeys, queries + (d / 4 * kChunk + d % 4 * 32) / 16,
-               k + (d / 4 * L::kTileChunk + d % 4 * 32) / 16, kScores, d > 0);
-      mma_commit(&sh.s_full[s][i & 1]);
-      mma_commit(&sh.empty[stage]);
-    };
-    const auto there = [&](int l) { return mbar_wait_warp(&sh.full[l % L::kStages], l / L::kStages & 1, dead); };
-    queries_there();
-    bool alive = true;
-    for (int i = 0; i < min(2, mine) && alive; ++i) {
-      alive = there(2 * i);
-      if (alive && elect_one()) scores_of(i);
       __syncwarp();
-    }
-    for (int i = 0; i < mine && alive; ++i) {  // step i's output, and step i + 2's scores in the place of its weights
-      alive = there(2 * i + 1) && mbar_wait_warp(&sh.p_full[s][i & 1], i >> 1 & 1, dead);
-      if (!alive) break;
-      tmem_fence_after();
-      const int stage = (2 * i + 1) % L::kStages;
-      const uint64_t v = values + static_cast<uint32_t>(stage) * L::kTile / 16;
-      if (elect_one()) {
+      // the barriers are made anew for the next block: every arrival has come before that
+      for (int l = max(0, 2 * n - L::kStages); l < 2 * n && alive; ++l)
+        alive = mbar_wait_warp(&sh.empty[l % L::kStages], l / L::kStages & 1, dead);
+      if (bad) p.bad[w.b] = 1;
+    } else if (warp >= kSoftmaxWarps) {
+      const int s = warp - kSoftmaxWarps;
+      const uint32_t at = uniform(smem_address(stages));
+      const uint64_t queries = operand_desc(uniform(smem_address(tiles)) + s * L::kQueries, 16, 1024);
+      const uint64_t keys = operand_desc(at, 16, 1024), values = operand_desc(at, L::kTileChunk, 1024);
+      constexpr uint32_t kScores = mma_desc(kBf16, kKeys, false), kOutput = mma_desc(kBf16, D, true);
+      const uint32_t scores = tmem + s * 128, out = tmem + L::kOutputs + s * D;
+      const int mine = warps_of(s) > 0 ? n : 0;
+      const auto scores_of = [&](int i) {  // one thread; step i's keys are there
+        const int stage = 2 * i % L::kStages;
+        const uint64_t k = keys + static_cast<uint32_t>(stage) * L::kTile / 16;
 #pragma unroll
-        for (int d = 0; d < kKeys / 16; ++d)
-          mma_ts(out, scores + (i & 1) * kKeys + d * 8, v + d * (2048 / 16), kOutput, d > 0 || i > 0);
-        mma_commit(&sh.o_done[s][i & 1]);
+        for (int d = 0; d < D / 16; ++d)
+          mma_ss(scores + (i & 1) * kKeys, queries + (d / 4 * kChunk + d % 4 * 32) / 16,
+                 k + (d / 4 * L::kTileChunk + d % 4 * 32) / 16, kScores, d > 0);
+        mma_commit(&sh.s_full[s][i & 1]);
         mma_commit(&sh.empty[stage]);
-      }
-      __syncwarp();
-      if (i + 2 < mine) {
-        alive = there(2 * (i + 2));
-        if (alive && elect_one()) scores_of(i + 2);
+      };
+      const auto there = [&](int l) { return mbar_wait_warp(&sh.full[l % L::kStages], l / L::kStages & 1, dead); };
+      queries_there();
+      bool alive = true;
+      for (int i = 0; i < min(2, mine) && alive; ++i) {
+        alive = there(2 * i);
+        if (alive && elect_one()) scores_of(i);
         __syncwarp();
       }
-    }
-    if (__any_sync(0xFFFFFFFFu, *dead != 0) && elect_one()) {  // the products that are on their way end first
-      mma_commit(&sh.drain[s]);
-      const long long start = clock64();
-      while (!mbar_try(&sh.drain[s], 0) && clock64() - start < kWaitCycles) {}
-    }
-    __syncwarp();
-  } else {
-    // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
-    // elements, a copy behind another. Rows that are none are zeros.
-    const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
-    for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
-      const int r = i / kVectors, v = i % kVectors;
-      uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (r % kSpan < live && v * 8 < p.dim) {
-        const T* q = rows.query(r % kSpan) + v * 8;
-        if (whole) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
-          continue;
-        } else {
-          const uint16_t* u = reinterpret_cast<const uint16_t*>(q);
-          const auto two = [&](int e) { return u[e] | static_cast<uint32_t>(u[e + 1]) << 16; };
-          x = make_uint4(two(0), two(2), two(4), two(6));
-        }
-      }
-      *reinterpret_cast<uint4*>(to) = x;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    queries_there();
-    const int slot = warp >> 2, r = tid % kSpan, copy = kCopies > 1 ? warp / (4 / kCopies) : 0;  // the thread's row
-    const bool in = r < live, cap = !kPlain && p.softcap > 0.0f, bias = !kPlain && p.slopes != nullptr;
-    const uint64_t mask = in ? rows.mask(r) : 0;
-    const int depth = __popcll(mask) - 1;
-    const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + L::kOutputs + slot * D;
-    const float scale2 = cap ? p.scale / p.softcap : p.scale * kLog2e;
-    const float cap2 = p.softcap * kLog2e, slope2 = bias && in ? p.slopes[rows.head(r)] * kLog2e : 0.0f;
-    const int steps = warp * 32 % kSpan < live ? n : 0;
-    float base = -kInf, total = 0.0f;  // log2 of what the weights are relative to, and their sum
-    bool alive = true;
-    for (int c = 0; c < steps; ++c) {
-      const int b = c & 1;
-      const uint32_t scores = at + slot * 128 + b * kKeys;
-      alive = mbar_wait_warp(&sh.s_full[slot][b], c >> 1 & 1, dead);
-      if (!alive) break;
-      tmem_fence_after();
-      constexpr int kWidth = kColumns < 32 ? kColumns : 32;
-      uint32_t x[kColumns / kWidth][kWidth];
-      if constexpr (kWidth == 16) {
-        tmem_load16_wait(x[0], scores + copy * kColumns);
-      } else {
-        tmem_load32(x[0], scores + copy * kColumns);
-        if constexpr (kColumns == 64) tmem_load32(x[1], scores + 32);
-        tmem_wait_ld(x[0]);
-        if constexpr (kColumns == 64) tie32(x[1]);
-      }
-      const auto score = [&](int e) -> uint32_t& { return x[e / kWidth][e % kWidth]; };
-      const auto two = [&](int e) { return static_cast<uint64_t>(score(e + 1)) << 32 | score(e); };
-      const auto put_two = [&](int e, uint64_t y) { score(e) = static_cast<uint32_t>(y), score(e + 1) = static_cast<uint32_t>(y >> 32); };
-      const int key0 = (begin + step_of(2 * c)) * kKeys + copy * kColumns;  // (the last step's end is below 2^31)
-      const bool nodes = key0 + kColumns > w.n;  // keys of the tree, or beyond the last
-      if (cap) {
-        float fars[4] = {};
-#pragma unroll
-        for (int e = 0; e < kColumns; ++e) fars[e % 4] = fmaxf(fars[e % 4], fabsf(__uint_as_float(score(e))));
-        const float far = fmaxf(fmaxf(fars[0], fars[1]), fmaxf(fars[2], fars[3]));
-        if (__builtin_expect(__all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap), 1)) {
-          const uint64_t over2 = pack2(scale2, scale2), caps = pack2(cap2, cap2);
-#pragma unroll
-          for (int e = 0; e < kColumns; e += 2) put_two(e, capped_near(two(e), over2, caps));
-        } else {
-#pragma unroll
-          for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(capped(__uint_as_float(score(e)), scale2, cap2));
-        }
-      } else if (!kPlain) {
-#pragma unroll
-        for (int e = 0; e < kColumns; e += 2) put_two(e, mul2(two(e), pack2(scale2, scale2)));
-      }
-      if (bias) {
-        const float away = static_cast<float>(w.n - key0 + depth);  // exact, and its differences, below 2^24
-        if (__builtin_expect(!nodes, 1)) {
-#pragma unroll
-          for (int e = 0; e < kColumns; e += 2)
-            put_two(e, fma2(pack2(-slope2, -slope2), add2(pack2(away, away), pack2(-static_cast<float>(e), -static_cast<float>(e + 1))), two(e)));
-        } else {
-#pragma unroll
-          for (int e = 0; e < kColumns; ++e) {
-            const int node = key0 - w.n + e;
-            const float far = node < 0 ? away - e : node < 64 ? fabsf(static_cast<float>(depth + 1 - __popcll(sh.rows.masks[node]))) : 0.0f;
-            score(e) = __float_as_uint(fmaf(-slope2, far, __uint_as_float(score(e))));
-          }
-        }
-      }
-      if (__builtin_expect(nodes || __any_sync(0xFFFFFFFFu, mask == 0), 0)) {
-        const int ahead = w.n - key0;  // the columns' first keys that are not the tree's
-        uint64_t seen = mask == 0 || ahead <= 0 ? 0 : ahead >= 64 ? ~UINT64_C(0) : (UINT64_C(1) << ahead) - 1;
-        if (ahead < 64 && ahead > -64) seen |= ahead >= 0 ? mask << ahead : mask >> -ahead;
-#pragma unroll
-        for (int h = 0; h < kColumns / kWidth; ++h) {
-          const uint32_t bits = static_cast<uint32_t>(seen >> 32 * h);
-#pragma unroll
-          for (int e = 0; e < kWidth; ++e)
-            if (!(bits >> e & 1)) x[h][e] = __float_as_uint(-kInf);
-        }
-      }
-      float most[4];
-#pragma unroll
-      for (int e = 0; e < kColumns; ++e) most[e % 4] = e < 4 ? __uint_as_float(score(e)) : fmaxf(most[e % 4], __uint_as_float(score(e)));
-      float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-      if (kPlain) top *= scale2;
-      top -= kLift<T>;
-      const bool moved = base > -kInf && top > base + kSlack;
-      if (__builtin_expect(__any_sync(0xFFFFFFFFu, moved), 0)) {
-        const float back = moved ? exp2_approx(base - top) : 1.0f;
-        total *= back;
-        alive = mbar_wait_warp(&sh.o_done[slot][b ^ 1], (c - 1) >> 1 & 1, dead);  // the step before is in the output
+      for (int i = 0; i < mine && alive; ++i) {  // step i's output, and step i + 2's scores in the place of its weights
+        alive = there(2 * i + 1) && mbar_wait_warp(&sh.p_full[s][i & 1], i >> 1 & 1, dead);
         if (!alive) break;
         tmem_fence_after();
+        const int stage = (2 * i + 1) % L::kStages;
+        const uint64_t v = values + static_cast<uint32_t>(stage) * L::kTile / 16;
+        if (elect_one()) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          uint32_t o[16];
-          tmem_load16_wait(o, out + d * 16);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
-          tmem_store16(out + d * 16, o);
+          for (int d = 0; d < kKeys / 16; ++d)
+            mma_ts(out, scores + (i & 1) * kKeys + d * 8, v + d * (2048 / 16), kOutput, d > 0 || i > 0);
+          mma_commit(&sh.o_done[s][i & 1]);
+          mma_commit(&sh.empty[stage]);
+        }
+        __syncwarp();
+        if (i + 2 < mine) {
+          alive = there(2 * (i + 2));
+          if (alive && elect_one()) scores_of(i + 2);
+          __syncwarp();
         }
       }
-      if (moved || base == -kInf) base = top;
-      const float shift = base == -kInf ? 0.0f : -base;
-      const float times = kPlain ? scale2 : 1.0f;
-      const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
-      uint64_t sums[2] = {0, 0};
-      uint32_t weights[kColumns / 2];
-#pragma unroll
-      for (int i = 0; i < kColumns / 2; ++i) {
-        const uint64_t t = fma2(two(2 * i), times2, shift2);
-        const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
-        sums[i & 1] = add2(sums[i & 1], pack2(u, v));
-        weights[i] = narrow2<T>(u, v);
+      if (__any_sync(0xFFFFFFFFu, *dead != 0) && elect_one()) {  // the products that are on their way end first
+        mma_commit(&sh.drain[s]);
+        const long long start = clock64();
+        while (!mbar_try(&sh.drain[s], 0) && clock64() - start < kWaitCycles) {}
       }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {  // the other copies' keys weigh nothing here
-        uint32_t all[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          constexpr int kMine = kColumns / 2;
-          all[i] = kCopies == 1 || (half * 16 + i) / kMine == copy ? weights[(half * 16 + i) % kMine] : 0;
-        }
-        tmem_store16(scores + half * 16, all);
-      }
-      const uint64_t sum = add2(sums[0], sums[1]);
-      total += low2(sum) + high2(sum);
-      tmem_wait_st();
-      tmem_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.p_full[slot][b]);
-    }
-    for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
-    tmem_fence_after();
-    float scale = 1.0f;  // of a copy's outputs
-    float* const gathered = reinterpret_cast<float*>(stages);  // the copies' behind the first, in place of keys and values
-    constexpr int kPitch = D + 4;
-    if constexpr (kCopies > 1) {  // the copies' statistics, then their outputs, as one
-      sh.part[tid] = make_float2(base, total);
-      softmax_warps();
-      float most = -kInf, all = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kCopies; ++k) most = fmaxf(most, sh.part[k * kSpan + r].x);
-#pragma unroll
-      for (int k = 0; k < kCopies; ++k) {
-        const float2 part = sh.part[k * kSpan + r];
-        all += part.y != part.y ? part.y : part.x == -kInf ? 0.0f : part.y * exp2_approx(part.x - most);
+    } else {
+      // The queries, swizzled as a product's operand is: 16-byte vector v of a row goes to place v ^ (row mod 8) of its 64
+      // elements, a copy behind another. Rows that are none are zeros.
+      const bool whole = aligned_to(p.q, 16) && p.q_token % 8 == 0 && p.q_node % 8 == 0 && p.q_head % 8 == 0;
+      for (int i = tid; i < L::kBlock * kVectors; i += kSoftmaxWarps * 32) {
+        const int r = i / kVectors, v = i % kVectors;
+        uint8_t* to = tiles + r / kRows * L::kQueries + v / 8 * kChunk + r % kRows * 128 + ((v % 8 ^ (r & 7)) << 4);
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r % kSpan < live && v * 8 < p.dim) {
+          const T* q = rows.query(r % kSpan) + v * 8;
+          if (whole) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_address(to)), "l"(q) : "memory");
+            continue;
+          } else {
+            const uint16_t* u = reinterpret_cast<const uint16_t*>(q);
+            const auto two = [&](int e) { return u[e] | static_cast<uint32_t>(u[e + 1]) << 16; };
+            x = make_uint4(two(0), two(2), two(4), two(6));
+          }
+        }
+        *reinterpret_cast<uint4*>(to) = x;
       }
-      scale = base == -kInf ? 0.0f : exp2_approx(base - most);
-      base = most, total = all;
-      if (copy > 0 && steps > 0 && alive) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      queries_there();
+      const int slot = warp >> 2, r = tid % kSpan, copy = kCopies > 1 ? warp / (4 / kCopies) : 0;  // the thread's row
+      const bool in = r < live, cap = !kPlain && p.softcap > 0.0f, bias = !kPlain && p.slopes != nullptr;
+      const uint64_t mask = in ? rows.mask(r) : 0;
+      const int depth = __popcll(mask) - 1;
+      const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), out = at + L::kOutputs + slot * D;
+      const float scale2 = cap ? p.scale / p.softcap : p.scale * kLog2e;
+      const float cap2 = p.softcap * kLog2e, slope2 = bias && in ? p.slopes[rows.head(r)] * kLog2e : 0.0f;
+      const int steps = warp * 32 % kSpan < live ? n : 0;
+      float base = -kInf, total = 0.0f;  // log2 of what the weights are relative to, and their sum
+      bool alive = true;
+      for (int c = 0; c < steps; ++c) {
+        const int b = c & 1;
+        const uint32_t scores = at + slot * 128 + b * kKeys;
+        alive = mbar_wait_warp(&sh.s_full[slot][b], c >> 1 & 1, dead);
+        if (!alive) break;
+        tmem_fence_after();
+        constexpr int kWidth = kColumns < 32 ? kColumns : 32;
+        uint32_t x[kColumns / kWidth][kWidth];
+        if constexpr (kWidth == 16) {
+          tmem_load16_wait(x[0], scores + copy * kColumns);
+        } else {
+          tmem_load32(x[0], scores + copy * kColumns);
+          if constexpr (kColumns == 64) tmem_load32(x[1], scores + 32);
+          tmem_wait_ld(x[0]);
+          if constexpr (kColumns == 64) tie32(x[1]);
+        }
+        const auto score = [&](int e) -> uint32_t& { return x[e / kWidth][e % kWidth]; };
+        const auto two = [&](int e) { return static_cast<uint64_t>(score(e + 1)) << 32 | score(e); };
+        const auto put_two = [&](int e, uint64_t y) {
+          score(e) = static_cast<uint32_t>(y), score(e + 1) = static_cast<uint32_t>(y >> 32);
+        };
+        const int key0 = (begin + step_of(2 * c)) * kKeys + copy * kColumns;  // (the last step's end is below 2^31)
+        const bool nodes = key0 + kColumns > w.n;  // keys of the tree, or beyond the last
+        if (cap) {
+          float fars[4] = {};
+#pragma unroll
+          for (int e = 0; e < kColumns; ++e) fars[e % 4] = fmaxf(fars[e % 4], fabsf(__uint_as_float(score(e))));
+          const float far = fmaxf(fmaxf(fars[0], fars[1]), fmaxf(fars[2], fars[3]));
+          if (__builtin_expect(__all_sync(0xFFFFFFFFu, far * fabsf(scale2) < kNearCap), 1)) {
+            const uint64_t over2 = pack2(scale2, scale2), caps = pack2(cap2, cap2);
+#pragma unroll
+            for (int e = 0; e < kColumns; e += 2) put_two(e, capped_near(two(e), over2, caps));
+          } else {
+#pragma unroll
+            for (int e = 0; e < kColumns; ++e) score(e) = __float_as_uint(capped(__uint_as_float(score(e)), scale2, cap2));
+          }
+        } else if (!kPlain) {
+#pragma unroll
+          for (int e = 0; e < kColumns; e += 2) put_two(e, mul2(two(e), pack2(scale2, scale2)));
+        }
+        if (bias) {
+          const float away = static_cast<float>(w.n - key0 + depth);  // exact, and its differences, below 2^24
+          if (__builtin_expect(!nodes, 1)) {
+#pragma unroll
+            for (int e = 0; e < kColumns; e += 2)
+              put_two(e, fma2(pack2(-slope2, -slope2),
+                              add2(pack2(away, away), pack2(-static_cast<float>(e), -static_cast<float>(e + 1))), two(e)));
+          } else {
+#pragma unroll
+            for (int e = 0; e < kColumns; ++e) {
+              const int node = key0 - w.n + e;
+              const int place = node >= 0 && node < 64 ? __popcll(sh.rows.masks[node]) - 1 : depth;
+              const float far = node < 0 ? away - e : fabsf(static_cast<float>(depth - place));
+              score(e) = __float_as_uint(fmaf(-slope2, far, __uint_as_float(score(e))));
+            }
+          }
+        }
+        if (__builtin_expect(nodes || __any_sync(0xFFFFFFFFu, mask == 0), 0)) {
+          const int ahead = w.n - key0;  // the columns' first keys that are not the tree's
+          uint64_t seen = mask == 0 || ahead <= 0 ? 0 : ahead >= 64 ? ~UINT64_C(0) : (UINT64_C(1) << ahead) - 1;
+          if (ahead < 64 && ahead > -64) seen |= ahead >= 0 ? mask << ahead : mask >> -ahead;
+#pragma unroll
+          for (int h = 0; h < kColumns / kWidth; ++h) {
+            const uint32_t bits = static_cast<uint32_t>(seen >> 32 * h);
+#pragma unroll
+            for (int e = 0; e < kWidth; ++e)
+              if (!(bits >> e & 1)) x[h][e] = __float_as_uint(-kInf);
+          }
+        }
+        float most[4];
+#pragma unroll
+        for (int e = 0; e < kColumns; ++e) {
+          const float y = __uint_as_float(score(e));
+          most[e % 4] = e < 4 ? y : fmaxf(most[e % 4], y);
+        }
+        float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+        if (kPlain) top *= scale2;
+        top -= kLift<T>;
+        const bool moved = base > -kInf && top > base + kSlack;
+        if (__builtin_expect(__any_sync(0xFFFFFFFFu, moved), 0)) {
+          const float back = moved ? exp2_approx(base - top) : 1.0f;
+          total *= back;
+          alive = mbar_wait_warp(&sh.o_done[slot][b ^ 1], (c - 1) >> 1 & 1, dead);  // the step before is in the output
+          if (!alive) break;
+          tmem_fence_after();
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) {
+            uint32_t o[16];
+            tmem_load16_wait(o, out + d * 16);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
+            tmem_store16(out + d * 16, o);
+          }
+        }
+        if (moved || base == -kInf) base = top;
+        const float shift = base == -kInf ? 0.0f : -base;
+        const float times = kPlain ? scale2 : 1.0f;
+        const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
+        uint64_t sums[2] = {0, 0};
+        uint32_t weights[kColumns / 2];
+#pragma unroll
+        for (int i = 0; i < kColumns / 2; ++i) {
+          const uint64_t t = fma2(two(2 * i), times2, shift2);
+          const float u = exp2_approx(low2(t)), v = exp2_approx(high2(t));
+          sums[i & 1] = add2(sums[i & 1], pack2(u, v));
+          weights[i] = narrow2<T>(u, v);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {  // the other copies' keys weigh nothing here
+          uint32_t all[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            constexpr int kMine = kColumns / 2;
+            all[i] = kCopies == 1 || (half * 16 + i) / kMine == copy ? weights[(half * 16 + i) % kMine] : 0;
+          }
+          tmem_store16(scores + half * 16, all);
+        }
+        const uint64_t sum = add2(sums[0], sums[1]);
+        total += low2(sum) + high2(sum);
+        tmem_wait_st();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full[slot][b]);
+      }
+      for (int c = max(0, steps - 2); c < steps && alive; ++c) alive = mbar_wait_warp(&sh.o_done[slot][c & 1], c >> 1 & 1, dead);
+      tmem_fence_after();
+      float scale = 1.0f;  // of a copy's outputs
+      float* const gathered = reinterpret_cast<float*>(stages);  // the copies' behind the first, in place of keys and values
+      constexpr int kPitch = D + 4;
+      if constexpr (kCopies > 1) {  // the copies' statistics, then their outputs, as one
+        sh.part[tid] = make_float2(base, total);
+        softmax_warps();
+        float most = -kInf, all = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k) most = fmaxf(most, sh.part[k * kSpan + r].x);
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k) {
+          const float2 part = sh.part[k * kSpan + r];
+          all += part.y != part.y ? part.y : part.x == -kInf ? 0.0f : part.y * exp2_approx(part.x - most);
+        }
+        scale = base == -kInf ? 0.0f : exp2_approx(base - most);
+        base = most, total = all;
+        if (copy > 0 && steps > 0 && alive) {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_load32(o, out + c * 32);
+            tmem_wait_ld(o);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(gathered + ((copy - 1) * kSpan + r) * kPitch + c * 32 + e) =
+                  make_float4(times_scale(o[e], scale), times_scale(o[e + 1], scale), times_scale(o[e + 2], scale),
+                              times_scale(o[e + 3], scale));
+          }
+          tmem_fence_before();
+        }
+        softmax_warps();
+      }
+      if (steps > 0 && alive && copy == 0) {
+        const bool whole = n == shape.y, seen = total != 0.0f;
+        const float over = seen ? 1.0f / total : 0.0f;
+        const int64_t place_of_cta = 2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start);
+        T* const to = rows.row(r);
+        const bool vectors = reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
           tmem_load32(o, out + c * 32);
           tmem_wait_ld(o);
+          if constexpr (kCopies > 1) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<float4*>(gathered + ((copy - 1) * kSpan + r) * kPitch + c * 32 + e) =
-                make_float4(times_scale(o[e], scale), times_scale(o[e + 1], scale), times_scale(o[e + 2], scale), times_scale(o[e + 3], scale));
+            for (int e = 0; e < 32; e += 4) {
+              float y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = times_scale(o[e + i], scale);
+#pragma unroll
+              for (int k = 0; k < kCopies - 1; ++k) {
+                const float4 z = *reinterpret_cast<const float4*>(gathered + (k * kSpan + r) * kPitch + c * 32 + e);
+                y[0] += z.x, y[1] += z.y, y[2] += z.z, y[3] += z.w;
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[e + i] = __float_as_uint(y[i]);
+            }
+          }
+          if (sh.any_odd) {
+            uint32_t odd = 0;
+            for (int j = 0; j < 64; ++j)
+              if (mask >> j & 1) odd |= sh.odd[j][c];
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (odd >> e & 1) o[e] = 0x7FC00000u;
+          }
+          if (!in) continue;
+          if (whole) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              float f[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) f[i] = seen ? __uint_as_float(o[e + i]) * over : 0.0f;
+              const uint4 u = Vec<T>::narrow_all(f);
+              if (c * 32 + e >= p.dim) continue;
+              if (vectors) {
+                *reinterpret_cast<uint4*>(to + c * 32 + e) = u;
+              } else {
+                const uint32_t two[4] = {u.x, u.y, u.z, u.w};
+                uint16_t* one = reinterpret_cast<uint16_t*>(to + c * 32 + e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) one[i] = static_cast<uint16_t>(two[i / 2] >> 16 * (i & 1));
+              }
+            }
+          } else {
+            float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + tid;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              part[e / 4 * L::kBlock] = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
+                                                    __uint_as_float(o[e + 3]));
+          }
+        }
+        if (in && whole) {
+          if (p.lse != nullptr) *rows.sum(r) = seen ? (base + log2f(total)) * kLn2 : -kInf;
+        } else if (in) {
+          p.stats[place_of_cta * L::kBlock + tid] = make_float2(base, total);
         }
         tmem_fence_before();
       }
-      softmax_warps();
+      if constexpr (kCopies > 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // TMA's turn
     }
-    if (steps > 0 && alive && copy == 0) {
-      const bool whole = n == shape.y, seen = total != 0.0f;
-      const float over = seen ? 1.0f / total : 0.0f;
-      const int64_t place_of_cta = 2 * static_cast<int64_t>(blockIdx.x) + (at_unit > start);
-      T* const to = rows.row(r);
-      const bool vectors = reinterpret_cast<uintptr_t>(to) % 16 == 0;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_load32(o, out + c * 32);
-        tmem_wait_ld(o);
-        if constexpr (kCopies > 1) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float y[4] = {times_scale(o[e], scale), times_scale(o[e + 1], scale), times_scale(o[e + 2], scale), times_scale(o[e + 3], scale)};
-#pragma unroll
-            for (int k = 0; k < kCopies - 1; ++k) {
-              const float4 z = *reinterpret_cast<const float4*>(gathered + (k * kSpan + r) * kPitch + c * 32 + e);
-              y[0] += z.x, y[1] += z.y, y[2] += z.z, y[3] += z.w;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[e + i] = __float_as_uint(y[i]);
-          }
-        }
-        if (sh.any_odd) {
-          uint32_t odd = 0;
-          for (int j = 0; j < 64; ++j)
-            if (mask >> j & 1) odd |= sh.odd[j][c];
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (odd >> e & 1) o[e] = 0x7FC00000u;
-        }
-        if (!in) continue;
-        if (whole) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = seen ? __uint_as_float(o[e + i]) * over : 0.0f;
-            const uint4 u = Vec<T>::narrow_all(f);
-            if (c * 32 + e >= p.dim) continue;
-            if (vectors) {
-              *reinterpret_cast<uint4*>(to + c * 32 + e) = u;
-            } else {
-              const uint32_t two[4] = {u.x, u.y, u.z, u.w};
-              uint16_t* one = reinterpret_cast<uint16_t*>(to + c * 32 + e);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) one[i] = static_cast<uint16_t>(two[i / 2] >> 16 * (i & 1));
-            }
-          }
-        } else {
-          float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + tid;
-#pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            part[e / 4 * L::kBlock] = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
-                                                  __uint_as_float(o[e + 3]));
-        }
-      }
-      if (in && whole) {
-        if (p.lse != nullptr) *rows.sum(r) = seen ? (base + log2f(total)) * kLn2 : -kInf;
-      } else if (in) {
-        p.stats[place_of_cta * L::kBlock + tid] = make_float2(base, total);
-      }
-      tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    if (sh.dead != 0) {  // what is left of the run is not formed
+      if (tid == 0) p.bad[w.b] = 1;
+      at_unit += units;
+      for (b += 1; b < p.batch && p.prefix[b] < stop; ++b)
+        if (tid == 0) p.bad[b] = 1;
+      break;
     }
-    if constexpr (kCopies > 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // TMA's turn
-  }
-  __syncthreads();
-  tmem_fence_after();
-  if (sh.dead != 0) {  // what is left of the run is not formed
-    if (tid == 0) p.bad[w.b] = 1;
     at_unit += units;
-    for (b += 1; b < p.batch && p.prefix[b] < stop; ++b)
-      if (tid == 0) p.bad[b] = 1;
-    break;
-  }
-  at_unit += units;
   }
   tmem_fence_before();
   __syncthreads();
