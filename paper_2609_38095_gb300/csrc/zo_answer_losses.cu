@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_co
     unit = shared_unit;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the gradient's kernel: the rows' CTAs are gone
   Pair sum = {0.0f, 0.0f};
   for (int64_t first = threadIdx.x; first < r.tokens; first += kAtOnce * static_cast<int64_t>(blockDim.x)) {
     if (first != threadIdx.x) read(first);
@@ -193,6 +194,7 @@ __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __gri
   __syncthreads();
   const bool bad = unsorted != 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the gradient's kernel: the rows' CTAs are gone
   for (int64_t first = 0; first < sequences && !bad; first += at_once) {
     const int64_t j = first + mine;
     Pair sum = {0.0f, 0.0f};
@@ -345,23 +347,23 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
 // another's arithmetic. Bound by HBM: rows read and written once (2598 rows of 151936, 2228 of them counted, bf16: 197 us =
 // 7.0 TB/s). The rows go from the last to the first, since the last ones read for their sums may still be in L2 (310 us for
 // the whole call; from the first on 312; with the last 80 MB kept there by hints 305, but the sums' pass alone 2 % slower).
-// Rows of slope 0 are not read.
+// Launched while the sums' kernel runs: what its first CTAs read of the logits is on its way before the slopes are there.
 template <typename T>
 __global__ void __launch_bounds__(kPartThreads) logits_grad_kernel(const __grid_constant__ LogitsGradParams p, int parts) {
   extern __shared__ __align__(16) uint4 tile[];
   const int64_t t = p.tokens - 1 - blockIdx.x / parts;
   const T* x = static_cast<const T*>(p.logits) + t * p.row;
   const Part<T> part(x, p.vocab, blockIdx.x % parts, parts);
-  const float slope = p.slopes[t];
   const int64_t target = load_index(p.targets, t, p.target64);
-  const bool zero = slope == 0.0f || target < 0;
-  float2 lse = make_float2(0.0f, 0.0f);
   float edge = 0.0f;
-  if (!zero) {
+  if (target >= 0) {
     fetch_part(x, part, tile);
-    lse = p.lse[t];
     if (part.edge >= 0) edge = widen(x[part.edge]);
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const float slope = p.slopes[t];
+  const float2 lse = p.lse[t];
+  const bool zero = slope == 0.0f || target < 0;
   asm volatile("cp.async.wait_all;" ::: "memory");
   put_part(static_cast<T*>(p.grad) + t * p.grad_row, part, tile, edge, zero, Slope(slope, p.scale, lse), target);
 }
@@ -373,10 +375,11 @@ __global__ void __launch_bounds__(kPartThreads) logits_grad_warp_kernel(const __
   if (t >= p.tokens) return;
   const T* x = static_cast<const T*>(p.logits) + t * p.row;
   T* g = static_cast<T*>(p.grad) + t * p.grad_row;
-  const float slope = p.slopes[t];
   const int64_t target = load_index(p.targets, t, p.target64);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const float slope = p.slopes[t];
   const bool zero = slope == 0.0f || target < 0;
-  const Slope s(slope, p.scale, zero ? make_float2(0.0f, 0.0f) : p.lse[t]);
+  const Slope s(slope, p.scale, p.lse[t]);
   for (int64_t i = threadIdx.x & 31; i < p.vocab; i += 32) {
     const float v = zero ? 0.0f : widen(x[i]);
     g[i] = narrow<T>(zero ? 0.0f : i == target ? s.target(v) : s.other(v));
@@ -543,7 +546,7 @@ __global__ void __launch_bounds__(kPartThreads) row_sums_warp_kernel(const __gri
 // KB each, four or five per SM. A thread fetches by cp.async what it alone reads, so that a part has no barrier but the joins';
 // the slope's chain (joins, logarithm, exponential, a mean's weight) is on one thread of each CTA while the others' loads are on
 // their way. Bound by HBM, with the instructions at 64 % of their slots (4091 tokens of 151936, 3068 of them counted, bf16: 357
-// us = 6.1 TB/s of the 2.18 GB that have to move; the rows' sums and then the gradient 480; CTAs that take several rows and fetch
+// us = 6.1 TB/s of the 2.18 GB that have to move; the rows' sums and then the gradient 466; CTAs that take several rows and fetch
 // the next row into places as they come free 430, by the instructions that this takes).
 template <typename T>
 __global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __grid_constant__ PolicyLossParams p,
@@ -616,16 +619,24 @@ __global__ void __launch_bounds__(kSumThreads) policy_unit_kernel(const __grid_c
 
 template <typename T>
 cudaError_t launch_grad(const LogitsGradParams& p, cudaStream_t stream) {
-  if (p.vocab <= kWarpVocab) {
-    constexpr int kRows = kPartThreads / 32;
-    logits_grad_warp_kernel<T><<<static_cast<unsigned>((p.tokens + kRows - 1) / kRows), kPartThreads, 0, stream>>>(p);
-    return cudaGetLastError();
-  }
-  constexpr int kMost = 24 * 1024;
+  constexpr int kRows = kPartThreads / 32, kMost = 24 * 1024;
   const int64_t bytes = p.vocab * static_cast<int64_t>(sizeof(T));
   const int parts = static_cast<int>((bytes + kMost - 1) / kMost);
-  logits_grad_kernel<T><<<static_cast<unsigned>(p.tokens * parts), kPartThreads, (bytes / parts + 31) / 16 * 16, stream>>>(p, parts);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.blockDim = dim3(kPartThreads);
+  c.stream = stream;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  if (p.vocab <= kWarpVocab) {
+    c.gridDim = dim3(static_cast<unsigned>((p.tokens + kRows - 1) / kRows));
+    return cudaLaunchKernelEx(&c, logits_grad_warp_kernel<T>, p);
+  }
+  c.gridDim = dim3(static_cast<unsigned>(p.tokens * parts));
+  c.dynamicSmemBytes = static_cast<size_t>((bytes / parts + 31) / 16 * 16);
+  return cudaLaunchKernelEx(&c, logits_grad_kernel<T>, p, parts);
 }
 
 cudaError_t launch_logits_grad(const LogitsGradParams& p, int dtype, cudaStream_t stream) {
