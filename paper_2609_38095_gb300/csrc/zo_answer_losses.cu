@@ -346,7 +346,7 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
 // A row's gradient from its slope and log-sum: parts of a row of up to 24 KB, eight CTAs per SM, so that one's loads cover
 // another's arithmetic. Bound by HBM: rows read and written once (2598 rows of 151936, 2228 of them counted, bf16: 197 us =
 // 7.0 TB/s). The rows go from the last to the first, since the last ones read for their sums may still be in L2 (310 us for
-// the whole call; from the first on 312; with the last 80 MB kept there by hints 305, but the sums' pass alone 2 % slower).
+// the whole call, 308 since; from the first on 312; with the last 80 MB kept there by hints 305, but the sums' pass 2 % slower).
 // Launched while the sums' kernel runs: what its first CTAs read of the logits is on its way before the slopes are there.
 template <typename T>
 __global__ void __launch_bounds__(kPartThreads) logits_grad_kernel(const __grid_constant__ LogitsGradParams p, int parts) {

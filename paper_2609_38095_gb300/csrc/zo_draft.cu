@@ -57,7 +57,7 @@ __device__ __forceinline__ bool not_finite2(uint32_t v) {
 // the instruction caches (one sequence of 2039 keys, 8 nodes, 32 / 8 heads of 128,
 // bf16: 16.4 us a call, where its bytes take 1.3). Every 32
 // rows read the keys again: zo_draft_wide.cu takes over where that costs more.
-template <typename T, int DP, int MB>
+template <typename T, int DP, int MB, bool kPlain>
 __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 64 ? 3 : 2)
     draft_mma_kernel(const __grid_constant__ DraftParams p) {
   using L = Tiles<DP, MB>;
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
   };
   // With a bias by distance the tiles in turn from the last to the first: a row's largest scores come first then, and its output
   // is not rescaled at every tile.
-  const bool backward = p.slopes != nullptr;
+  const bool cap = !kPlain && p.softcap > 0.0f, bias = !kPlain && p.slopes != nullptr, backward = bias;
   const auto key_of = [&](int64_t tile) { return (backward ? tiles_in - 1 - tile : tile) * L::kKeys; };
   const auto look = [&](int64_t tile) {
     const int64_t j = key_of(tile) + lane % L::kKeys;
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
     for (int r = 0; r < 2; ++r) {
       const int h = 16 * m + 8 * r + lane / 4;
       const T* q = rows.query(h);
-      slope2[m][r] = p.slopes != nullptr ? p.slopes[rows.head(h)] * kLog2e : 0.0f;
+      slope2[m][r] = bias ? p.slopes[rows.head(h)] * kLog2e : 0.0f;
       depth[m][r] = static_cast<float>(__popcll(rows.mask(h)) - 1);
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s)
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
           }
         }
     }
-  const float scale2 = p.softcap > 0.0f ? p.scale / p.softcap : p.scale * kLog2e, cap2 = p.softcap * kLog2e;
+  const float scale2 = cap ? p.scale / p.softcap : p.scale * kLog2e, cap2 = p.softcap * kLog2e;
   float base[MB][2], total[MB][2], acc[MB][DP / 8][4];
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
     const int64_t key0 = key_of(tile);
     const bool nodes = key0 + L::kKeys > w.n;  // keys of the tree, or beyond the last
     float times = scale2;  // what the scores are in, times
-    if (p.softcap > 0.0f) {
+    if (cap) {
       times = 1.0f;
       float far = 0.0f;
 #pragma unroll
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
               y[0] = capped(y[0], scale2, cap2), y[1] = capped(y[1], scale2, cap2);
             }
           }
-    } else if (p.slopes != nullptr || nodes || p.scale <= 0.0f) {
+    } else if (bias || nodes || p.scale <= 0.0f) {
       times = 1.0f;
 #pragma unroll
       for (int m = 0; m < MB; ++m)
@@ -254,11 +254,11 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               float& y = s[m][n][2 * r + c];
-              if (p.slopes != nullptr) y -= slope2[m][r] * fabsf(depth[m][r] - place);
+              if (bias) y -= slope2[m][r] * fabsf(depth[m][r] - place);
               if (node >= 0 && !(tree && (rows.mask(16 * m + 8 * r + lane / 4) >> node & 1))) y = -kInf;
             }
         }
-    } else if (p.slopes != nullptr) {
+    } else if (bias) {
       const float from = static_cast<float>(static_cast<int>(w.n - key0) - lane % 4 * 2);  // exact, and its sums, below 2^24
 #pragma unroll
       for (int m = 0; m < MB; ++m)
@@ -425,13 +425,21 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
   rows_join<T, DP, DP, kWarps * 32>(p, w, rows, outs, top, sum, &bad_here);
 }
 
-template <typename T, int DP, int MB>
-cudaError_t launch_size(DraftParams p, int64_t batch, int sms, cudaStream_t stream) {
+template <typename T, int DP, int MB, bool kPlain>
+cudaError_t launch_kind(DraftParams p, int64_t batch, int sms, cudaStream_t stream) {
   using L = Tiles<DP, MB>;
   p.head_blocks = (p.drafts * p.group + L::kRows - 1) / L::kRows;
   const int64_t items = batch * p.kv_heads * p.head_blocks;
   const int c = decode_cluster(items, p.max_pages * p.page_size, sms, MB == 1 ? 6 : 4);
-  return launch_decode(draft_mma_kernel<T, DP, MB>, p, items, c, kWarps * 32, L::kBytes, stream);
+  return launch_decode(draft_mma_kernel<T, DP, MB, kPlain>, p, items, c, kWarps * 32, L::kBytes, stream);
+}
+
+// Without caps and biases in a kernel of its own: less code to come to the SMs (one sequence of 2000
+// keys, 8 nodes, 32 / 8 heads of 128: 20.0 -> 19.0 us with cold caches; 8 of up to 1000, 32 heads: 34.4 -> 32.3).
+template <typename T, int DP, int MB>
+cudaError_t launch_size(const DraftParams& p, int64_t batch, int sms, cudaStream_t stream) {
+  return p.softcap > 0.0f || p.slopes != nullptr ? launch_kind<T, DP, MB, false>(p, batch, sms, stream)
+                                                 : launch_kind<T, DP, MB, true>(p, batch, sms, stream);
 }
 
 template <typename T>
