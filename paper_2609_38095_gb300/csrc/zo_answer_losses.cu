@@ -344,7 +344,7 @@ __device__ __forceinline__ void put_part(T* g, const Part<T>& part, const uint4*
 }
 
 // A row's gradient from its slope and log-sum: parts of a row of up to 24 KB, eight CTAs per SM, so that one's loads cover
-// another's arithmetic. Bound by HBM: rows read and written once (2598 rows of 151936, 2228 of them counted, bf16: 197 us =
+// another's arithmetic. Bound by HBM: rows read and written once (2598 rows of 151936, 1950 of them counted, bf16: 197 us =
 // 7.0 TB/s). The rows go from the last to the first, since the last ones read for their sums may still be in L2 (310 us for
 // the whole call, 308 since; from the first on 312; with the last 80 MB kept there by hints 305, but the sums' pass 2 % slower).
 // Launched while the sums' kernel runs: what its first CTAs read of the logits is on its way before the slopes are there.
@@ -481,7 +481,7 @@ __device__ __forceinline__ void join_rows(float& top, float& sum, int parts) {
 }
 
 // The rows' log-probabilities and log-sums: a CTA per counted row, or a cluster that splits the vocabulary where rows are few.
-// Bound by HBM: each counted row is read once (3068 rows of 151936, bf16: 147 us a call = 6.3 TB/s; six loads a thread in flight and
+// Bound by HBM: each counted row is read once (3069 rows of 151936, bf16: 147 us a call = 6.3 TB/s; six loads a thread in flight and
 // four CTAs per SM instead of four and five: the same, and 16 rows in 11.3 us instead of 10.5).
 template <typename T>
 __global__ void __launch_bounds__(kPartThreads, 5) row_sums_kernel(const __grid_constant__ AnswerRows r, int parts) {
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kPartThreads) row_sums_warp_kernel(const __gri
 // A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory, up to 52
 // KB each, four or five per SM. A thread fetches by cp.async what it alone reads, so that a part has no barrier but the joins';
 // the slope's chain (joins, logarithm, exponential, a mean's weight) is on one thread of each CTA while the others' loads are on
-// their way. Bound by HBM, with the instructions at 64 % of their slots (4091 tokens of 151936, 3068 of them counted, bf16: 357
+// their way. Bound by HBM, with the instructions at 64 % of their slots (4091 tokens of 151936, 3069 of them counted, bf16: 357
 // us = 6.1 TB/s of the 2.18 GB that have to move; the rows' sums and then the gradient 466; CTAs that take several rows and fetch
 // the next row into places as they come free 430, by the instructions that this takes).
 template <typename T>
