@@ -91,27 +91,48 @@ struct DraftShared {
   uint16_t node[HB], head[HB];  // of the rows here
 };
 
-// A warp with each lane's two masks of a sequence (0 where there is no node): which nodes are seen, how many there are up to the
-// last that sees anything, the keys, and whether there are more than the page table or 32 bits hold, a last tile's end among them.
+// Which keys a tree has: `last` nodes up to the last that is seen, `nodes` up to the last that sees anything; and whether there
+// are more than the page table or 32 bits hold, a last tile's end among them.
 struct DraftKeys {
   uint64_t any;
   int64_t len;
   int nodes, bad;
 };
-__device__ __forceinline__ DraftKeys draft_keys(const DraftParams& p, int n, uint64_t a, uint64_t b) {
-  const uint64_t both = a | b;
+__host__ __device__ __forceinline__ DraftKeys draft_reach(const DecodeParams& p, int n, uint64_t any, int last, int nodes) {
   DraftKeys k;
-  k.any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
-          __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
-  const uint32_t high = __ballot_sync(0xFFFFFFFFu, b != 0), low = __ballot_sync(0xFFFFFFFFu, a != 0);
-  k.nodes = 64 - __clzll(static_cast<uint64_t>(high) << 32 | low);
-  k.len = k.any == 0 ? 0 : static_cast<int64_t>(n) + 64 - __clzll(k.any);
+  k.any = any;
+  k.nodes = nodes;
+  k.len = last == 0 ? 0 : static_cast<int64_t>(n) + last;
   k.bad = k.len > p.max_pages * p.page_size || (k.len > 0 && p.n_pages == 0) || k.len > 0x7FFFFFFF - 64;
   return k;
 }
+// A warp with each lane's two masks of a sequence, 0 where there is no node.
+__device__ __forceinline__ DraftKeys draft_keys(const DraftParams& p, int n, uint64_t a, uint64_t b) {
+  const uint64_t both = a | b;
+  const uint64_t any = static_cast<uint64_t>(__reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both >> 32))) << 32 |
+                       __reduce_or_sync(0xFFFFFFFFu, static_cast<uint32_t>(both));
+  const uint32_t high = __ballot_sync(0xFFFFFFFFu, b != 0), low = __ballot_sync(0xFFFFFFFFu, a != 0);
+  return draft_reach(p, n, any, 64 - __clzll(any), 64 - __clzll(static_cast<uint64_t>(high) << 32 | low));
+}
 
-// Every thread of the CTA: sequence b, key-value head g and the block'th HB rows. One behind the last row that sees anything
-// has no keys.
+// What a block of rows has of them. One behind the last row that sees anything, or of a sequence whose keys are more than
+// the page table holds, has none: draft_sees() is what pages are looked up by, so that neither length is left.
+__host__ __device__ __forceinline__ void draft_take(DraftPlace& w, const DecodeParams& p, const DraftKeys& k, int n) {
+  const int live = k.nodes * p.group - w.head0;
+  w.live = live < 0 ? 0 : live < w.heads ? live : w.heads;
+  w.n = n;
+  w.any = k.any;
+  w.len = k.len;
+  w.bad = k.bad;
+  if (w.bad || w.live == 0) w.n = 0, w.len = 0, w.live = 0;
+}
+
+// Whether key j is one that the tree sees.
+__host__ __device__ __forceinline__ bool draft_sees(const DraftPlace& w, int64_t j) {
+  return j < w.n || (j < w.len && (w.any >> (j - w.n) & 1) != 0);
+}
+
+// Every thread of the CTA: sequence b, key-value head g and the block'th HB rows.
 template <int HB>
 __device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, int b, int g, int block, DraftShared<HB>& sh) {
   const uint32_t lane = threadIdx.x & 31;
@@ -130,13 +151,7 @@ __device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, int b, i
     sh.head[h] = static_cast<uint16_t>(w.g * p.group + r - node * p.group);
   }
   __syncthreads();
-  const DraftKeys k = draft_keys(p, max(n, 0), sh.masks[lane], sh.masks[lane + 32]);
-  w.n = max(n, 0);
-  w.any = k.any;
-  w.len = k.len;
-  w.bad = k.bad;
-  w.live = max(0, min(w.heads, k.nodes * p.group - w.head0));
-  if (w.bad || w.live == 0) w.len = w.live = 0;
+  draft_take(w, p, draft_keys(p, max(n, 0), sh.masks[lane], sh.masks[lane + 32]), max(n, 0));
   return w;
 }
 template <int HB>
@@ -144,11 +159,6 @@ __device__ __forceinline__ DraftPlace draft_place(const DraftParams& p, uint32_t
   const uint32_t blocks = p.head_blocks, b = cluster / (p.kv_heads * blocks), rest = cluster - b * (p.kv_heads * blocks);
   const uint32_t g = rest / blocks;
   return draft_place<HB>(p, b, g, rest - g * blocks, sh);
-}
-
-// Whether key j is one that the tree sees.
-__device__ __forceinline__ bool draft_sees(const DraftPlace& w, int64_t j) {
-  return j < w.n || (j < w.len && (w.any >> (j - w.n) & 1) != 0);
 }
 
 // The tree's rows: see DecodeRows. (A row that is none is the last.)
