@@ -687,7 +687,8 @@ cudaError_t launch_rows(const PolicyLossParams& p, const LogitsGradParams& g, in
          (bytes / parts > 52 * 1024 || (g.tokens * parts * 2 <= 5 * sms && g.vocab / (parts * 2) >= 4096)))
     parts *= 2;
   const int tile = static_cast<int>((bytes / parts + 31) / 16 * 16);
-  cudaError_t e = cudaFuncSetAttribute(policy_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile);
+  // the most that a call takes, not this one's: host threads share what is set here
+  cudaError_t e = cudaFuncSetAttribute(policy_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostPart));
   if (e != cudaSuccess) return e;
   if (p.unit != nullptr) {
     policy_unit_kernel<<<1, kSumThreads, 0, stream>>>(p);
