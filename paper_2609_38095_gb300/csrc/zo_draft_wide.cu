@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
       queries_there();
       const int slot = warp >> 2, r = tid % kSpan, copy = kCopies > 1 ? warp / (4 / kCopies) : 0;  // the thread's row
       const bool in = r < live, cap = !kPlain && p.softcap > 0.0f, bias = !kPlain && p.slopes != nullptr;
@@ -636,6 +637,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
+          __syncwarp();  // the load is the whole warp's; the stores of the columns before split it by rows and alignment
           tmem_load32(o, out + c * 32);
           tmem_wait_ld(o);
           if constexpr (kCopies > 1) {
@@ -661,8 +663,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
             for (int e = 0; e < 32; ++e)
               if (odd >> e & 1) o[e] = 0x7FC00000u;
           }
-          if (!in) continue;
-          if (whole) {
+          if (in && whole) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
               float f[8];
@@ -679,7 +680,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
                 for (int i = 0; i < 8; ++i) one[i] = static_cast<uint16_t>(two[i / 2] >> 16 * (i & 1));
               }
             }
-          } else {
+          } else if (in) {
             float4* part = p.outs + (place_of_cta * (D / 4) + c * 8) * L::kBlock + tid;
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
@@ -692,6 +693,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         } else if (in) {
           p.stats[place_of_cta * L::kBlock + tid] = make_float2(base, total);
         }
+        __syncwarp();
         tmem_fence_before();
       }
       if constexpr (kCopies > 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // TMA's turn
