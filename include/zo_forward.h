@@ -286,7 +286,9 @@ int zo_policy_loss(const void* logits, int64_t row, int64_t tokens, int64_t voca
  * number (if any). With e = smoothing, softplus(x) = log(1 + exp(x)):
  *   m_i = beta ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)) - margin
  *   loss = sum_i (1 - e) softplus(-m_i) + e softplus(m_i)
- * and, where grad is given, grad_tv = grad_scale dloss/dx_tv; 0 for rows in no
+ * where a factor of 0 (1 - e, e, beta) leaves out what is infinite behind it: a
+ * rejected answer of probability 0 has the loss 0 without smoothing.
+ * And, where grad is given, grad_tv = grad_scale dloss/dx_tv; 0 for rows in no
  * sequence (whose targets do not count) and tokens that do not count. Starts
  * that descend or lie outside 0 .. tokens make the loss, every logp and the
  * counted rows' gradient NaN.

@@ -35,6 +35,7 @@ __device__ __forceinline__ Pair operator+(Pair a, Pair b) {
 __device__ __forceinline__ Pair operator-(Pair a) { return {-a.high, -a.low}; }
 __device__ __forceinline__ Pair over(Pair a, float n) {
   const float q = __fdiv_rn(a.high, n);
+  if (!(fabsf(q) < kInf)) return {q, 0.0f};
   return two_sum(q, __fdiv_rn(__fadd_rn(fmaf(-q, n, a.high), a.low), n));
 }
 __device__ __forceinline__ double wide(Pair a) { return static_cast<double>(a.high) + a.low; }
@@ -70,6 +71,9 @@ __device__ __forceinline__ Pair logp_of(float x, float top, Pair rest) { return 
 struct Term {
   float value, slope;
 };
+
+// What a factor is multiplied with: where it is 0 and that is infinite, or beyond fp32, nothing (0 times it is NaN). A NaN stays one.
+__device__ __forceinline__ float with_factor(float factor, float x) { return factor == 0.0f && fabsf(x) == kInf ? 0.0f : x; }
 
 // expm1(d) - d: by its series where the difference would lose what is left of it.
 __device__ __forceinline__ float expm1_less(float d) {
@@ -227,17 +231,19 @@ __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __gri
     const Pair chosen = bad ? Pair{NAN, 0.0f} : pair_of(p.sums[2 * i]), rejected = bad ? Pair{NAN, 0.0f} : pair_of(p.sums[2 * i + 1]);
     Pair away = chosen + -rejected;
     if (p.ref_logp != nullptr) away = away + two_sum(p.ref_logp[2 * i + 1], -p.ref_logp[2 * i]);
-    const float m = p.beta * away.high - p.margin;
+    const float m = p.beta * with_factor(p.beta, away.high) - p.margin;
     // softplus(x) = max(x, 0) + log1p(exp(-|x|)), and its derivative
     const float e = expf(-fabsf(m)), tail = log1pf(e), small = e / (1.0f + e), large = 1.0f / (1.0f + e);
     const float up = m > 0.0f ? large : m <= 0.0f ? small : NAN, down = m > 0.0f ? small : m <= 0.0f ? large : NAN;
-    loss = loss + Pair{(1.0f - p.smoothing) * (fmaxf(-m, 0.0f) + tail), p.smoothing * (fmaxf(m, 0.0f) + tail)};
+    // an answer that cannot be given makes one of the two infinite, which without smoothing has the factor 0
+    const float right = 1.0f - p.smoothing, turned = p.smoothing;
+    loss = loss + Pair{right * with_factor(right, fmaxf(-m, 0.0f) + tail), turned * with_factor(turned, fmaxf(m, 0.0f) + tail)};
     if (p.logp != nullptr) {
       p.logp[2 * i] = chosen.high;
       p.logp[2 * i + 1] = rejected.high;
     }
     if (p.slopes != nullptr) {
-      const float slope = per_pair * p.beta * (p.smoothing * up - (1.0f - p.smoothing) * down);
+      const float slope = per_pair * p.beta * (turned * up - right * down);
       p.sums[2 * i] = make_float2(slope, 0.0f);
       p.sums[2 * i + 1] = make_float2(-slope, 0.0f);
     }
