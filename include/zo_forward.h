@@ -256,8 +256,9 @@ int zo_attention_draft(const zo_pages* q, const zo_pages* k, const zo_pages* v, 
  *   grad_tv = grad_scale dloss/dx_tv = grad_scale w_t c_t (1[v = target_t] - p_tv)
  *   c_t = -r_t A_t, or 0 where the clamp is the smaller, + kl (1 - exp(d_t))
  * (0 for tokens that do not count). The second form of the ratio's KL divergence
- * is never negative and has the right mean. The order in which tokens are added
- * depends on `tokens` alone.
+ * is never negative and has the right mean. A factor of 0 (A_t, w_t) leaves out
+ * what is infinite behind it, or beyond fp32: a ratio of exp(89). The order in
+ * which tokens are added depends on `tokens` alone.
  *   old_logp, advantages  fp32 [tokens]
  *   ref_logp     fp32 [tokens]; NULL (with kl = 0): no such term
  *   weights      fp32 [tokens], or NULL: 1

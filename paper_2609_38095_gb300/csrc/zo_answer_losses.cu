@@ -98,7 +98,7 @@ struct Token {  // what stands beside its logits
 __device__ __forceinline__ Term policy_term(const PolicyLossParams& p, const Token& t, Pair logp) {
   const float a = t.advantage, r = expf((logp.high - t.old_logp) + logp.low);
   const float lo = 1.0f - p.clip_low, hi = 1.0f + p.clip_high;
-  const float whole = r * a, cut = (r < lo ? lo : r > hi ? hi : r) * a;
+  const float whole = with_factor(a, r) * a, cut = (r < lo ? lo : r > hi ? hi : r) * a;
   Term term = {whole > cut ? -cut : -whole, whole > cut ? 0.0f : -whole};
   if (p.ref_logp != nullptr) {
     const float d = (t.ref_logp - logp.high) - logp.low;
@@ -106,6 +106,10 @@ __device__ __forceinline__ Term policy_term(const PolicyLossParams& p, const Tok
     term.slope -= p.kl * expm1f(d);
   }
   return term;
+}
+
+__device__ __forceinline__ float token_slope(const Token& t, float unit, const Term& term) {
+  return t.weight * unit * with_factor(t.weight, term.slope);
 }
 
 // 1 over the counted tokens' weights, on thread 0.
@@ -166,11 +170,11 @@ __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const __grid_co
       Term term = {0.0f, 0.0f};
       if (counts[k]) {
         term = policy_term(p, token[k], logp[k]);
-        const float part = token[k].weight * term.value;
-        sum = sum + Pair{part, fmaf(token[k].weight, term.value, -part)};
+        const float w = token[k].weight, value = with_factor(w, term.value), part = w * value;
+        sum = sum + Pair{part, fabsf(part) < kInf ? fmaf(w, value, -part) : 0.0f};
       }
       if (p.logp != nullptr) p.logp[t] = logp[k].high;
-      if (p.slopes != nullptr) p.slopes[t] = counts[k] ? token[k].weight * unit * term.slope : 0.0f;
+      if (p.slopes != nullptr) p.slopes[t] = counts[k] ? token_slope(token[k], unit, term) : 0.0f;
     }
   }
   sum = cta_sum(sum);
@@ -607,7 +611,7 @@ __global__ void __launch_bounds__(kPartThreads, 5) policy_rows_kernel(const __gr
       asm volatile("griddepcontrol.wait;" ::: "memory");
       unit = __ldcg(p.unit);
     }
-    shared_slope = token.weight * unit * term.slope;
+    shared_slope = token_slope(token, unit, term);
     shared_lse = make_float2(top, rest.high);
   }
   __syncthreads();
