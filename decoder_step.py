@@ -168,7 +168,7 @@ class Answer:
         self.caches = [tuple(torch.empty(shape, dtype=model.dtype, device="cuda") for _ in range(2)) for _ in range(model.layers)]
         order = torch.randperm(sum(need), generator=torch.Generator().manual_seed(1)).tolist()
         self.pages = torch.full((len(prompts), max(need)), -1, dtype=torch.int32)   # -1: no page
-        self.rows_left = min(n * page_size - m for n, m in zip(need, lengths))
+        self.rows_left = [n * page_size - m for n, m in zip(need, lengths)]
         for b, n in enumerate(need):
             self.pages[b, :n] = torch.tensor(order[:n])
             del order[:n]
@@ -194,9 +194,9 @@ class Answer:
 
     def next(self, tokens):
         """Appends one token to each sequence; returns the logits after it. ValueError when a sequence's pages are full."""
-        if self.rows_left == 0:
+        if min(self.rows_left) == 0:
             raise ValueError("a sequence's pages are full: there is no room for another token")
-        self.rows_left -= 1
+        self.rows_left = [n - 1 for n in self.rows_left]
         positions = self.lengths.long()
         slots = self._slots(torch.arange(len(positions), device="cuda"), positions)
         self.lengths += 1
@@ -209,19 +209,26 @@ class Answer:
         self.logits = self.model.logits(tokens, positions, attend)
         return self.logits
 
-    def draft(self, tokens, parents):
+    def draft(self, tokens, parents, sizes=None):
         """Logits (sequences, nodes, vocabulary) after each node of a tree of drafted tokens per sequence: tokens and parents
-        (sequences, nodes), a parent ahead of its children, -1: the sequence's last token, -2: no node. Nothing is appended
-        until accept(); ValueError where a sequence's pages have no room for so many."""
+        (sequences, nodes), a parent ahead of its children, -1: the sequence's last token, -2: no node. sizes: each tree's
+        number of nodes, where they differ; what is behind is no node. Nothing is appended until accept(); ValueError where a
+        sequence's pages have no room for its tree."""
         batch, nodes = tokens.shape
-        if nodes > self.rows_left:
+        if sizes is not None and (len(sizes) != batch or not all(0 <= n <= nodes for n in sizes)):
+            raise ValueError("a tree has a size between none and all of its nodes")
+        if any(n > left for n, left in zip(sizes if sizes is not None else [nodes] * batch, self.rows_left)):
             raise ValueError("a sequence's pages have no room for so many drafted tokens")
+        if sizes is not None:
+            ends = torch.tensor(sizes, device="cuda")[:, None]
+            parents = torch.where(torch.arange(nodes, device="cuda") < ends, parents, torch.full_like(parents, -2))
         model, masks = self.model, forward.draft_masks(parents)
         depth = ((masks[:, :, None] >> torch.arange(nodes, device="cuda")) & 1).sum(2) - 1
         sequence = torch.arange(batch, device="cuda").repeat_interleave(nodes)
+        some = masks.flatten() != 0
         places = (self.lengths[:, None] + torch.arange(nodes, device="cuda")).flatten()     # node j's keys are row lengths + j
-        slots = torch.where(masks.flatten() != 0, self._slots(sequence, places.long()), -1)
-        positions = (self.lengths[:, None] + depth.clamp(min=0)).flatten().long()
+        slots = torch.where(some, self._slots(sequence, torch.where(some, places.long(), 0)), -1)
+        positions = torch.where(some, (self.lengths[:, None] + depth).flatten().long(), 0)
 
         def attend(i, q, k, v, pos):
             kc, vc = self.caches[i]
@@ -248,29 +255,31 @@ class Answer:
         some = torch.tensor([bool(path) for path in paths], device="cuda")
         self.logits = torch.where(some[:, None], self.drafted[torch.arange(batch, device="cuda"), last], self.logits)
         self.lengths += torch.tensor([len(path) for path in paths], dtype=torch.int32, device="cuda")
-        self.rows_left -= max(len(path) for path in paths)
+        self.rows_left = [left - len(path) for left, path in zip(self.rows_left, paths)]
 
     def greedy_drafted(self, n, propose):
         """The tokens of greedy(n) -- up to ties -- in fewer passes: propose(sequences' tokens so far) gives a tree for each,
         lists of tokens and parents; of each the longest path of tokens that greedy() would give is accepted, and the one that
-        comes behind it is known then."""
+        comes behind it is known then. A sequence goes no further than its n tokens, and its tree no further than its pages."""
         got = [[t] for t in self.logits.argmax(-1).tolist()]     # the last one is not in the cache yet
         while min(map(len, got)) < n:
             trees = [([g[-1]] + list(t), [-1] + [p + 1 for p in up]) for g, (t, up) in zip(got, propose(got))]
-            nodes = max(len(t) for t, _ in trees)
             if not all(0 <= x < self.model.vocab for t, _ in trees for x in t):
                 raise ValueError("a proposed token is outside the vocabulary")
-            tokens, parents = (torch.tensor([x + [fill] * (nodes - len(x)) for x in xs], dtype=kind, device="cuda")
+            for b, left in enumerate(self.rows_left):            # none for a sequence with its n tokens; what there is room for
+                if len(got[b]) < n and left == 0:
+                    raise ValueError("a sequence's pages are full: there is no room for another token")
+                trees[b] = [x[:left if len(got[b]) < n else 0] for x in trees[b]]
+            sizes = [len(t) for t, _ in trees]
+            tokens, parents = (torch.tensor([x + [fill] * (max(sizes) - len(x)) for x in xs], dtype=kind, device="cuda")
                                for xs, fill, kind in (([t for t, _ in trees], 0, torch.long), ([up for _, up in trees], -2, torch.int32)))
-            best, paths = self.draft(tokens, parents).argmax(-1).tolist(), []
+            best, paths = self.draft(tokens, parents, sizes).argmax(-1).tolist(), []
             for b, (t, up) in enumerate(trees):
-                path = [0]
-                while True:
-                    nexts = [j for j in range(len(t)) if up[j] == path[-1] and t[j] == best[b][path[-1]]]
-                    got[b].append(best[b][path[-1]])
-                    if not nexts:
-                        break
+                path, nexts = [], [0] if t else []
+                while nexts and len(got[b]) < n:
                     path.append(nexts[0])
+                    got[b].append(best[b][path[-1]])
+                    nexts = [j for j in range(len(t)) if up[j] == path[-1] and t[j] == got[b][-1]]
                 paths.append(path)
             self.accept(paths)
         return torch.tensor([g[:n] for g in got], device="cuda")
