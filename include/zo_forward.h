@@ -32,10 +32,14 @@
  * given ranges.
  *
  * Arithmetic. Values are read as fp32; norms, scores, softmax statistics and
- * sums are fp32 (fp64 across tokens) and each output is rounded once. One
- * exception, in zo_attention and zo_attention_decode on 16-bit types: the
- * softmax's weights are rounded to that type for the tensor cores (in fp16 one
- * below 2^-21 of its row's largest loses bits, and one below 2^-32 is lost).
+ * sums are fp32 and each output is rounded once. Across tokens zo_token_loss
+ * adds in fp64; the losses over answers add in pairs of fp32 (48 bits), but
+ * what they add is fp32: a row's sum of exponentials, a token's term, a pair's,
+ * the weights' mean in zo_policy_loss. Their fp64 results have fp32's error of
+ * each term. One exception, in zo_attention, zo_attention_decode and
+ * zo_attention_draft on 16-bit types: the softmax's weights are rounded to that
+ * type for the tensor cores (in fp16 one below 2^-21 of its row's largest loses
+ * bits, and one below 2^-32 is lost).
  *
  * Strides are in elements; the elements of one head are contiguous. An output
  * over an input or another output, or with rows or heads over one another, is
@@ -227,7 +231,9 @@ int zo_draft_masks(const int32_t* parents, int64_t batch, int32_t drafts, int64_
  * = -inf. The place of a key j < lengths[b], for the bias by distance, is j; a
  * node's is lengths[b] + (bits of its mask) - 1.
  * A node's key that no node sees is not looked up, nor is its page; what lies
- * at one does not reach the result of a row that does not see it. A page
+ * at one does not reach the result of a row that does not see it; whether a
+ * row that sees a value that is not finite has NaN or an infinity in its column
+ * is left open, as in zo_attention. A page
  * outside the cache, or more keys than the page table or 31 bits hold, give
  * NaN in all rows of the sequence that see anything.
  *   q, out  node i of sequence b, head h at ptr[b * page + i * token + h * head];

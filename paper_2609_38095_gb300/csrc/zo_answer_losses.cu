@@ -57,7 +57,9 @@ __device__ __forceinline__ Pair cta_sum(Pair s) {
   return s;
 }
 
-// log of a sum: the mantissa's, at most 0.35, and the exponent's times log 2 = 355 / 512 - 2.1219444e-4, the first exactly.
+// log of a sum: the mantissa's, at most 0.35, and the exponent's times log 2 = 355 / 512 - 2.1219444e-4, the first exactly (Cody
+// and Waite, Software Manual for the Elementary Functions, 1980: the logarithm's argument reduction). The sum is fp32, and so is
+// its logarithm's accuracy; the second part is there so that sums of many rows lose no more.
 __device__ __forceinline__ Pair log_pair(float sum) {
   int e;
   float m = frexpf(sum, &e);
@@ -271,8 +273,8 @@ __global__ void __launch_bounds__(kSumThreads) preference_sum_kernel(const __gri
 }
 
 // The gradient of a row's logits in place of the logits: grad_v = slope scale (1[v = target] - exp(x_v - lse)). x - lse is formed
-// from the row's maximum first, then from the rest in the product's rounding. The target's own element is -expm1(x - lse),
-// which 1 - p would lose where p is near 1.
+// from the row's maximum first, then from the rest in the product's rounding. The target's own element is -expm1(x - lse), 1 - p
+// without the rounding of p. (Where all other logits together weigh less than 2^-24 of it the row's sum is 1 in fp32, and it is 0.)
 struct Slope {
   float times, top, rest, low;  // slope scale; of lse; -rest log2(e)
   __device__ __forceinline__ Slope(float slope, float scale, float2 lse)
@@ -553,7 +555,8 @@ __global__ void __launch_bounds__(kPartThreads) row_sums_warp_kernel(const __gri
 }
 
 // A row's sum, its token's term and its gradient with the row read once: a cluster of CTAs holds it in shared memory, up to 52
-// KB each, four or five per SM. A thread fetches by cp.async what it alone reads, so that a part has no barrier but the joins';
+// KB each, four or five per SM, as long as eight of them hold it (rows of up to 416 KB); beyond, up to 200 KB each and fewer per
+// SM (151936 logits in fp32: 76 KB, two). A thread fetches by cp.async what it alone reads, so that a part has no barrier but the joins';
 // the slope's chain (joins, logarithm, exponential, a mean's weight) is on one thread of each CTA while the others' loads are on
 // their way. Bound by HBM, with the instructions at 64 % of their slots (4091 tokens of 151936, 3069 of them counted, bf16: 357
 // us = 6.1 TB/s of the 2.18 GB that have to move; the rows' sums and then the gradient 466; CTAs that take several rows and fetch

@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP > 128 ? 1 : MB == 1 || DP == 6
 #pragma unroll
     for (int b = 0; b < kDeep; ++b) {
       const int row = b * 16 + (lane & 15);
-      uint32_t weight[MB][4];
+      uint32_t weight[MB][4];  // rounded to 16 bits for the tensor cores: off by half a step of each, their sum is of the fp32 ones
 #pragma unroll
       for (int m = 0; m < MB; ++m)
 #pragma unroll

@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(Plan<D, kSlots>::kThreads, 3 - kSlots)
         const float times = kPlain ? scale2 : 1.0f;
         const uint64_t times2 = pack2(times, times), shift2 = pack2(shift, shift);
         uint64_t sums[2] = {0, 0};
-        uint32_t weights[kColumns / 2];
+        uint32_t weights[kColumns / 2];  // rounded to 16 bits for the tensor cores, as in zo_draft.cu
 #pragma unroll
         for (int i = 0; i < kColumns / 2; ++i) {
           const uint64_t t = fma2(two(2 * i), times2, shift2);
